@@ -304,6 +304,85 @@ int32_t he_hrot_batch_levels(he_ctx *ctx, const he_evk *const *rots, const int32
 int32_t he_rotate_sum_batch(he_ctx *ctx, const he_evk *const *rots, int32_t n_rot, uint64_t *d_ct, int32_t level,
                             int32_t count, void *d_ws, size_t ws_bytes, void *stream);
 
+/* ---- device: from token states to embeddings ---------------------------------------------------- */
+
+/* The data owner's half of the paper's pipeline (Section 2.1): what turns the states of a sentence's tokens into the embedding that is
+ * encoded and encrypted, and the gradients of it, for fitting an encoder in the clear.  These functions work on floating-point rows, use
+ * nothing of a context but its device, run on it whatever device is current, and keep the conventions above: caller-owned buffers, work
+ * enqueued on `stream` alone, no allocation, no synchronisation.  Inputs are not written; outputs must not overlap inputs or one another.
+ * Sums, statistics and softmax are in 32 bits; a result is rounded to its type once.  No sequences (count 0): nothing is written. */
+#define HE_F32 0
+#define HE_F16 1
+#define HE_BF16 2
+
+/* Rows of `width` elements of one type, `stride` elements from row to row (stride >= width). */
+typedef struct {
+    void *d;
+    int64_t stride;
+} he_rows;
+/* [rows][heads][dim], the last dimension dense: element (r, h, c) is at r * row + h * head + c.  Base and strides are multiples of 16
+ * bytes; strides of an output are at least dim (inputs may repeat: 0). */
+typedef struct {
+    void *d;
+    int64_t row, head;
+} he_heads;
+/* `count` sequences in a token axis of `rows` rows: sequence i is the rows [d_begin[i], d_end[i]), 0 <= begin <= end <= rows, in ascending
+ * order and apart (d_end[i] <= d_begin[i + 1]).  Empty sequences are allowed; rows between and behind sequences belong to none.  The numbers are on
+ * the device and are not checked: ones that break the rule give results without meaning (no access outside the buffers). */
+typedef struct {
+    const int32_t *d_begin, *d_end; /* [count] */
+    int32_t count;
+    int64_t rows; /* at most 2^31 - 65536 */
+} he_spans;
+
+/* Layer norm over the last dimension: s = x + residual, rounded to the type (no residual: s = x); m and v its mean and variance over the width;
+ * rstd = (v + eps)^-1/2; y = (s - m) rstd w + b.  Weights have the rows' type or HE_F32.  HE_EINVAL: width above 16384, eps negative. */
+typedef struct {
+    int32_t type, weight_type;
+    int64_t rows;
+    int32_t width;
+    double eps;
+} he_norm;
+/* sum: where s is written, with a residual (else not looked at).  d_mean, d_rstd [rows]: for the backward pass. */
+int32_t he_layer_norm(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const void *d_b,
+                      const he_rows *y, const he_rows *sum, float *d_mean, float *d_rstd, void *stream);
+/* With g = dy w, xh = (s - m) rstd: ds = rstd (g - mean(g) - xh mean(g xh)) + add (the gradient of s from elsewhere; may be NULL),
+ * the gradient of x and of the residual both; dw = sum over rows of dy xh, db = sum over rows of dy, of the weights' type.  The order of the sums is
+ * fixed: runs repeat bit for bit. */
+int32_t he_layer_norm_workspace_bytes(const he_ctx *ctx, const he_norm *n, size_t *out);
+int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, const he_rows *s, const void *d_w, const float *d_mean,
+                           const float *d_rstd, const he_rows *add, const he_rows *ds, void *d_dw, void *d_db, void *d_ws, size_t ws_bytes,
+                           void *stream);
+
+/* Mean over the rows of each sequence, d_e [count][width] in 32 bits, zeros for an empty one; and its gradient, dx = de / length on the rows of
+ * each sequence.  fill: rows of no sequence are set to zero, else left as they are.  width at most 2^20. */
+int32_t he_pool_workspace_bytes(const he_ctx *ctx, const he_spans *s, int32_t width, size_t *out);
+int32_t he_pool(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, const he_rows *x, float *d_e, void *d_ws, size_t ws_bytes,
+                void *stream);
+int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, const float *d_de, const he_rows *dx, int32_t fill, void *stream);
+
+/* Attention of the queries of each sequence over the keys of the same sequence (both directions, no other mask):
+ *   t = scale q . k;  u = cap tanh(t / cap) (cap 0: u = t);  s = u - slope_h |position of q - position of k|
+ *   lse = log sum exp(s);  o = sum exp(s - lse) v;  a row whose sequence has no keys: o = 0, lse = -inf
+ * Query head h reads key head h / (heads / kv_heads).  The last query stands at the last key's position (where both have the same rows:
+ * row i of each at the same one).  d_lse [heads][q.rows].  dim: a multiple of 8 up to 128.  fill: query rows of no sequence get o = 0,
+ * lse = -inf (backward: gradient rows of no sequence zeros), else they are left as they are. */
+typedef struct {
+    int32_t type, heads, kv_heads, dim;
+    he_spans q, k;         /* the same count */
+    double scale, cap;     /* scale > 0, cap >= 0, both finite in 32 bits */
+    const float *d_slopes; /* [heads]; NULL: no bias */
+    int32_t fill;
+} he_attn;
+int32_t he_attention_workspace_bytes(const he_ctx *ctx, const he_attn *s, int32_t backward, size_t *out);
+int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q, const he_heads *k, const he_heads *v, const he_heads *o, float *d_lse,
+                     void *d_ws, size_t ws_bytes, void *stream);
+/* Gradients from do, with o and lse as the forward pass left them.  Heads that share a key head add up in dk and dv.  The slopes have no gradient.
+ * No atomics: runs repeat bit for bit. */
+int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_heads *go, const he_heads *q, const he_heads *k, const he_heads *v,
+                          const he_heads *o, const float *d_lse, const he_heads *dq, const he_heads *dk, const he_heads *dv, void *d_ws,
+                          size_t ws_bytes, void *stream);
+
 /* ---- measurement ------------------------------------------------------------------------- */
 
 /* Per-kernel timing for benchmarks: between start and stop every kernel the library launches is

@@ -22,6 +22,8 @@ ERRORS = {
     -5: "HE_EHIP", -6: "HE_ENODEV", -7: "HE_ENOMEM", -8: "HE_ESCRATCH",
 }
 
+_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}  # HE_F32, HE_F16, HE_BF16
+
 # every symbol include/he.h declares
 SYMBOLS = [
     "he_ctx_create", "he_ctx_destroy", "he_strerror", "he_last_hip_error", "he_ctx_modulus",
@@ -35,6 +37,8 @@ SYMBOLS = [
     "he_add_batch", "he_sub_batch", "he_pmult_batch", "he_cmult_batch", "he_add_const_batch", "he_moddrop_batch",
     "he_hmult_relin_batch", "he_hmult_relin_rescale_batch", "he_rescale_batch", "he_hrot_batch", "he_hrot_batch_keys", "he_hrot_batch_levels", "he_rotate_sum_batch",
     "he_hrot_noalloc",
+    "he_layer_norm", "he_layer_norm_workspace_bytes", "he_layer_norm_grad", "he_pool", "he_pool_workspace_bytes", "he_pool_grad",
+    "he_attention", "he_attention_workspace_bytes", "he_attention_grad",
     "he_profile_start", "he_profile_stop",
 ]
 
@@ -50,6 +54,29 @@ class he_kernel_stat(ctypes.Structure):
         ("name", ctypes.c_char * 48), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
         ("bytes", ctypes.c_double),
     ]
+
+
+class he_rows(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class he_heads(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class he_spans(ctypes.Structure):
+    _fields_ = [("begin", ctypes.c_void_p), ("end", ctypes.c_void_p), ("count", ctypes.c_int32), ("rows", ctypes.c_int64)]
+
+
+class he_norm(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("eps", ctypes.c_double)]
+
+
+class he_attn(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("q", he_spans), ("k", he_spans), ("scale", ctypes.c_double), ("cap", ctypes.c_double), ("slopes", ctypes.c_void_p),
+                ("fill", ctypes.c_int32)]
 
 
 class he_params(ctypes.Structure):
@@ -142,6 +169,15 @@ def load_library() -> ctypes.CDLL:
             "he_hrot_batch_keys": [vp, vp, vp, vp, i32, i32, vp, sz, vp],
             "he_hrot_batch_levels": [vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "he_rotate_sum_batch": [vp, vp, i32, vp, i32, i32, vp, sz, vp],
+            "he_layer_norm": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp],
+            "he_layer_norm_workspace_bytes": [vp, vp, ctypes.POINTER(sz)],
+            "he_layer_norm_grad": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            "he_pool": [vp, i32, vp, i32, vp, vp, vp, sz, vp],
+            "he_pool_workspace_bytes": [vp, vp, i32, ctypes.POINTER(sz)],
+            "he_pool_grad": [vp, i32, vp, i32, vp, vp, i32, vp],
+            "he_attention": [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            "he_attention_workspace_bytes": [vp, vp, i32, ctypes.POINTER(sz)],
+            "he_attention_grad": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
             "he_profile_start": [vp],
             "he_profile_stop": [vp, vp, i32, ctypes.POINTER(i32)],
         }
@@ -705,14 +741,230 @@ class HE:
                   "he_rotate_sum_batch")
         return cts
 
+    # ---- device: from token states to embeddings ------------------------------------------------------------------
+    # Floating-point rows on this context's device.  Sequences: an int32 tensor [count + 1] of offsets (sequence i is the rows
+    # offsets[i] .. offsets[i + 1]), or a pair (begin, end) of int32 tensors [count] where rows between them belong to none (a
+    # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.
+    def _rows(self, t, what: str, width=None, dtype=None):
+        """[rows][width], dense along the width: he_rows."""
+        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (width is not None and t.shape[1] != width):
+            raise ValueError(f"{what}: want [rows][width] with dense rows" + (f" of {width}" if width is not None else ""))
+        self._placed(t, what, dtype)
+        return he_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+    def _placed(self, t, what: str, dtype=None):
+        if t.device.type != "cuda" or t.device.index != self.device:
+            raise ValueError(f"{what}: on {t.device}, the context is on device {self.device}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{what}: {t.dtype}, want {dtype}")
+
+    @staticmethod
+    def _type(dtype) -> int:
+        name = str(dtype)
+        if name not in _TYPES:
+            raise ValueError(f"{name}: rows are float32, float16 or bfloat16")
+        return _TYPES[name]
+
+    def _vector(self, t, what: str, n: int, dtype=None):
+        if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+            raise ValueError(f"{what}: want a dense vector of {n}")
+        self._placed(t, what, dtype)
+        return t.data_ptr()
+
+    def _spans(self, offsets, rows: int, what: str = "offsets"):
+        import torch
+
+        if isinstance(offsets, (tuple, list)):
+            begin, end = offsets
+            if begin.dim() != 1 or end.shape != begin.shape:
+                raise ValueError(f"{what}: begin and end are vectors of one length")
+            count = begin.shape[0]
+            return he_spans(self._vector(begin, what, count, torch.int32), self._vector(end, what, count, torch.int32), count, rows)
+        if offsets.dim() != 1 or offsets.shape[0] < 1:
+            raise ValueError(f"{what}: want a vector of count + 1 offsets, or a pair of vectors (begin, end)")
+        p, count = self._vector(offsets, what, offsets.shape[0], torch.int32), offsets.shape[0] - 1
+        return he_spans(p, p + 4, count, rows)
+
+    def _scratch(self, need: int):
+        """A workspace of this call's own, from torch's allocator: calls on other streams and captured graphs have theirs."""
+        import torch
+
+        return torch.empty(need, dtype=torch.uint8, device=self._dev) if need else None
+
+    @property
+    def _dev(self):
+        return f"cuda:{self.device}"
+
+    def layer_norm(self, x, weight, bias, residual=None, eps: float = 1e-5, out=None):
+        """(x - mean) rstd weight + bias over the last dimension of x [rows][width], of s = x + residual with one (rounded to the type).
+        Returns (y, s, mean, rstd); s is x itself without a residual.  Keep s, mean and rstd for layer_norm_backward."""
+        import torch
+
+        rows, width = x.shape if x.dim() == 2 else (0, -1)
+        xr = self._rows(x, "x")
+        n = he_norm(self._type(x.dtype), self._type(weight.dtype), rows, width, eps)
+        w, b = self._vector(weight, "weight", width), self._vector(bias, "bias", width, weight.dtype)
+        rr = sr = None
+        s = x
+        if residual is not None:
+            rr = self._rows(residual, "residual", width, x.dtype)
+            if residual.shape != x.shape:
+                raise ValueError("residual: another shape than x")
+            s = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+            sr = self._rows(s, "sum")
+        y = torch.empty((rows, width), dtype=x.dtype, device=x.device) if out is None else out
+        if y.shape != x.shape:
+            raise ValueError("out: another shape than x")
+        yr = self._rows(y, "out", width, x.dtype)
+        stat = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+        ref = ctypes.byref
+        self._chk(self.lib.he_layer_norm(self.ctx, ref(n), ref(xr), ref(rr) if rr else None, w, b, ref(yr), ref(sr) if sr else None,
+                                         stat.data_ptr(), stat.data_ptr() + 4 * rows, self._stream()), "he_layer_norm")
+        return y, s, stat[0], stat[1]
+
+    def layer_norm_backward(self, dy, s, weight, mean, rstd, ds=None):
+        """(dx, dweight, dbias) from the gradient of y; ds: a gradient that reaches s from elsewhere, added to dx.  dx is the gradient of x and
+        of the residual both."""
+        import torch
+
+        rows, width = s.shape if s.dim() == 2 else (0, -1)
+        sr = self._rows(s, "s")
+        n = he_norm(self._type(s.dtype), self._type(weight.dtype), rows, width, 0.0)
+        if dy.shape != s.shape or (ds is not None and ds.shape != s.shape):
+            raise ValueError("dy, ds: another shape than s")
+        dyr, ar = self._rows(dy, "dy", width, s.dtype), None if ds is None else self._rows(ds, "ds", width, s.dtype)
+        w, m, r = self._vector(weight, "weight", width), self._vector(mean, "mean", rows, torch.float32), self._vector(rstd, "rstd", rows, torch.float32)
+        dx = torch.empty((rows, width), dtype=s.dtype, device=s.device)
+        dw = torch.empty((2, width), dtype=weight.dtype, device=s.device)
+        need, ref = ctypes.c_size_t(), ctypes.byref
+        self._chk(self.lib.he_layer_norm_workspace_bytes(self.ctx, ref(n), ref(need)), "he_layer_norm_workspace_bytes")
+        ws = self._scratch(need.value)
+        dxr = self._rows(dx, "dx")
+        self._chk(self.lib.he_layer_norm_grad(self.ctx, ref(n), ref(dyr), ref(sr), w, m, r, ref(ar) if ar else None, ref(dxr),
+                                              dw.data_ptr(), dw.data_ptr() + width * dw.element_size(), ws.data_ptr() if ws is not None else None,
+                                              need.value, self._stream()), "he_layer_norm_grad")
+        return dx, dw[0], dw[1]
+
+    def pool_mean(self, x, offsets, out=None):
+        """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence."""
+        import torch
+
+        xr = self._rows(x, "x")
+        rows, width = x.shape
+        sp, ref, need = self._spans(offsets, rows), ctypes.byref, ctypes.c_size_t()
+        self._chk(self.lib.he_pool_workspace_bytes(self.ctx, ref(sp), width, ref(need)), "he_pool_workspace_bytes")
+        e = torch.empty((sp.count, width), dtype=torch.float32, device=x.device) if out is None else out
+        if tuple(e.shape) != (sp.count, width) or not e.is_contiguous():
+            raise ValueError(f"out: want a dense [{sp.count}][{width}]")
+        self._placed(e, "out", torch.float32)
+        ws = self._scratch(need.value)
+        self._chk(self.lib.he_pool(self.ctx, self._type(x.dtype), ref(sp), width, ref(xr), e.data_ptr(), ws.data_ptr() if ws is not None else None,
+                                   need.value, self._stream()), "he_pool")
+        return e
+
+    def pool_mean_backward(self, de, offsets, rows: int, dtype, out=None):
+        """Gradient of pool_mean's x [rows][width], of type dtype, from de [count][width]."""
+        import torch
+
+        width = de.shape[1] if de.dim() == 2 else -1
+        sp = self._spans(offsets, rows)
+        if tuple(de.shape) != (sp.count, width) or not de.is_contiguous():
+            raise ValueError(f"de: want a dense [{sp.count}][width]")
+        self._placed(de, "de", torch.float32)
+        make = torch.empty if sp.count else torch.zeros
+        dx = make((rows, width), dtype=dtype, device=de.device) if out is None else out
+        if tuple(dx.shape) != (rows, width):
+            raise ValueError(f"out: want [{rows}][{width}]")
+        xr = self._rows(dx, "out", width, dtype)
+        self._chk(self.lib.he_pool_grad(self.ctx, self._type(dtype), ctypes.byref(sp), width, de.data_ptr(), ctypes.byref(xr), out is None,
+                                        self._stream()), "he_pool_grad")
+        return dx
+
+    def _heads(self, t, what: str, shape=None, dtype=None):
+        """[rows][heads][dim] with a dense last dimension: he_heads."""
+        if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{what}: want [rows][heads][dim]" + (f" = {tuple(shape)}" if shape is not None else ""))
+        if t.shape[2] > 1 and t.stride(2) != 1:
+            raise ValueError(f"{what}: the last dimension is not dense")
+        self._placed(t, what, dtype)
+        bad = [n for n, a, b in (("address", t.data_ptr(), 1), ("row stride", t.stride(0), t.element_size()), ("head stride", t.stride(1), t.element_size()))
+               if a * b % 16 and t.numel()]
+        if bad:
+            raise ValueError(f"{what}: {', '.join(bad)} not a multiple of 16 bytes")
+        return he_heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _attn(self, q, k, v, offsets, offsets_k, scale, cap, slopes, fill):
+        import torch
+
+        qh = self._heads(q, "q")
+        (rows, heads, dim), (rows_k, kv, _) = q.shape, k.shape if k.dim() == 3 else (0, 0, 0)
+        kh, vh = self._heads(k, "k", (rows_k, kv, dim), q.dtype), self._heads(v, "v", (rows_k, kv, dim), q.dtype)
+        if kv == 0 or heads % kv:
+            raise ValueError(f"{heads} query heads on {kv} key heads")
+        sq = self._spans(offsets, rows)
+        if offsets_k is None and rows_k != rows:
+            raise ValueError("keys of another length than the queries need offsets_k")
+        sk = sq if offsets_k is None else self._spans(offsets_k, rows_k, "offsets_k")
+        if sk.count != sq.count:
+            raise ValueError("offsets and offsets_k: another number of sequences")
+        sl = None if slopes is None else self._vector(slopes, "slopes", heads, torch.float32)
+        s = he_attn(self._type(q.dtype), heads, kv, dim, sq, sk, 1.0 / dim**0.5 if scale is None else scale, cap, sl, fill)
+        return s, qh, kh, vh
+
+    def _attn_scratch(self, s, backward: bool):
+        need = ctypes.c_size_t()
+        self._chk(self.lib.he_attention_workspace_bytes(self.ctx, ctypes.byref(s), backward, ctypes.byref(need)), "he_attention_workspace_bytes")
+        ws = self._scratch(need.value)
+        return ws, (ws.data_ptr() if ws is not None else None), need.value
+
+    def attention(self, q, k, v, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None):
+        """Attention inside each sequence: q [rows][heads][dim], k and v [rows_k][kv_heads][dim] (strided views of a joint projection are fine;
+        query head h reads key head h // (heads / kv_heads)).  offsets_k: the sequences of the keys, where they are not the queries'.
+        scale: of the products, 1 / sqrt(dim) by default; cap > 0: cap tanh(score / cap); slopes [heads] float32: minus slope times distance.
+        Returns (o, lse): o like q, lse [heads][rows] float32."""
+        import torch
+
+        s, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None)
+        make = torch.empty if s.q.count else torch.zeros
+        o = make(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        oh = self._heads(o, "out", q.shape, q.dtype)
+        lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
+        if out is not None or not s.q.count:
+            lse.fill_(float("-inf"))
+        ws, p, n = self._attn_scratch(s, False)
+        ref = ctypes.byref
+        self._chk(self.lib.he_attention(self.ctx, ref(s), ref(qh), ref(kh), ref(vh), ref(oh), lse.data_ptr(), p, n, self._stream()), "he_attention")
+        return o, lse
+
+    def attention_backward(self, do, q, k, v, o, lse, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None,
+                           fill=None):
+        """(dq, dk, dv) from the gradient of o, with o and lse of the forward call and its other arguments.  out: three tensors (strided views are
+        fine) to write them to; fill: whether their rows of no sequence become zeros (by default where they are made here).  Slopes are constants:
+        they have no gradient."""
+        import torch
+
+        s, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None if fill is None else fill)
+        gh, oh = self._heads(do, "do", q.shape, q.dtype), self._heads(o, "o", q.shape, q.dtype)
+        if tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+            raise ValueError("lse: want a dense [heads][rows]")
+        self._placed(lse, "lse", torch.float32)
+        make = torch.empty if s.q.count else torch.zeros
+        dq, dk, dv = [make(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)] if out is None else out
+        grads = self._heads(dq, "dq", q.shape, q.dtype), self._heads(dk, "dk", k.shape, q.dtype), self._heads(dv, "dv", k.shape, q.dtype)
+        ws, p, n = self._attn_scratch(s, True)
+        ref = ctypes.byref
+        self._chk(self.lib.he_attention_grad(self.ctx, ref(s), ref(gh), ref(qh), ref(kh), ref(vh), ref(oh), lse.data_ptr(), *[ref(g) for g in grads],
+                                             p, n, self._stream()), "he_attention_grad")
+        return dq, dk, dv
+
     # ---- measurement -------------------------------------------------------------------------------------------------
     def profile_start(self):
         self._chk(self.lib.he_profile_start(self.ctx), "he_profile_start")
 
     def profile_stop(self):
         """Per-kernel {name: (launches, total_ms, bytes)} since profile_start."""
-        buf = (he_kernel_stat * 32)()
+        buf = (he_kernel_stat * 64)()
         n = ctypes.c_int32()
-        self._chk(self.lib.he_profile_stop(self.ctx, buf, 32, ctypes.byref(n)), "he_profile_stop")
+        self._chk(self.lib.he_profile_stop(self.ctx, buf, 64, ctypes.byref(n)), "he_profile_stop")
         return {buf[i].name.decode(): (int(buf[i].launches), float(buf[i].total_ms), float(buf[i].bytes))
                 for i in range(n.value)}

@@ -67,6 +67,15 @@ class EncryptedInference:
         return [he.to_device(he.plain_to_ntt(he.encode(d, self.pt_scale), self.level))
                 for d in weight_diagonals(W, he.n)]
 
+    def encrypt_sentences(self, sk, encoder, states, offsets, scale: float, seed: int):
+        """The data owner's side: token states -> embeddings (embedding.SentenceEncoder) -> packed slots -> ciphertexts for run(), n / 1024
+        sentences each."""
+        from .embedding import pack_embeddings
+
+        he = self.he
+        return [he.to_device(he.encrypt_coeffs(sk, he.encode(z, scale), self.level, seed + i))
+                for i, z in enumerate(pack_embeddings(encoder(states, offsets), he.n))]
+
     def run(self, ct, pts, keys):
         """ct: device ciphertext at self.level, scale s; returns a level-1 lower ciphertext at scale s."""
         he = self.he

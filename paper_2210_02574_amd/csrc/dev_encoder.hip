@@ -1,0 +1,382 @@
+// Entry points of the operators on token states: attention inside sequences, layer norm, mean over sequences.
+#include <cmath>
+#include <cstring>
+
+#include "enc_launch.h"
+#include "kernels_attn.h"
+#include "kernels_norm.h"
+#include "kernels_pool.h"
+
+namespace {
+
+// The context's device is the current one while kernels are launched, and the caller's is afterwards.
+struct DeviceGuard {
+    int before = -1, rc = HE_OK;
+    explicit DeviceGuard(he_ctx *c)
+    {
+        hipError_t e = hipGetDevice(&before);
+        if (e == hipSuccess && before != c->device) e = hipSetDevice(c->device);
+        else before = -1;
+        if (e != hipSuccess) {
+            c->hip_err = std::string("hipSetDevice: ") + hipGetErrorString(e);
+            rc = HE_EHIP;
+        }
+    }
+    ~DeviceGuard()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+// The arguments are checked ahead of the device, so that a context without one refuses the same ones.
+#define NEEDS_DEVICE(c)                                                                                              \
+    if ((c)->device < 0) return HE_ENODEV
+
+int32_t launched(he_ctx *c)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return HE_OK;
+    c->hip_err = std::string("kernel launch: ") + hipGetErrorString(e);
+    return HE_EHIP;
+}
+
+constexpr int64_t MAX_ROWS = ((int64_t)1 << 31) - 65536; // row numbers and a tile more fit 32 bits
+
+bool type_ok(int32_t t) { return t == HE_F32 || t == HE_F16 || t == HE_BF16; }
+size_t type_size(int32_t t) { return t == HE_F32 ? 4 : 2; }
+bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+const RowsLaunch &rows_launch(int32_t t)
+{
+    static const RowsLaunch tables[3] = {
+        [] { RowsLaunch x{}; rows_launch_0(x); return x; }(),
+        [] { RowsLaunch x{}; rows_launch_1(x); return x; }(),
+        [] { RowsLaunch x{}; rows_launch_2(x); return x; }(),
+    };
+    return tables[t];
+}
+const AttnLaunch &attn_launch(int32_t t, int dim)
+{
+#define ROW(t)                                                                                                        \
+    {                                                                                                                \
+        [] { AttnLaunch x{}; attn_launch_##t##_32(x); return x; }(), [] { AttnLaunch x{}; attn_launch_##t##_64(x); return x; }(),            \
+            [] { AttnLaunch x{}; attn_launch_##t##_96(x); return x; }(), [] { AttnLaunch x{}; attn_launch_##t##_128(x); return x; }(),     \
+    }
+    static const AttnLaunch tables[3][4] = {ROW(0), ROW(1), ROW(2)};
+#undef ROW
+    return tables[t][(dim - 1) / 32];
+}
+
+// ---- layer norm ------------------------------------------------------------------------------------------------------
+
+int32_t norm_check(const he_norm *n)
+{
+    if (!n || !type_ok(n->type) || (n->weight_type != n->type && n->weight_type != HE_F32)) return HE_EINVAL;
+    if (n->rows < 0 || n->rows > MAX_ROWS || n->width < 1 || n->width > NORM_MAX_WIDTH) return HE_EINVAL;
+    return HE_OK;
+}
+bool rows_ok(const he_rows *r, int64_t width) { return r && r->d && r->stride >= width; }
+// whether 16-byte accesses reach every row
+bool wide(const he_rows *r, int32_t type) { return !r || (aligned(r->d, 16) && (r->stride * type_size(type)) % 16 == 0); }
+
+// Work-groups of the backward pass: each writes a partial row of dw and db, so a few for each of the 256 CUs and no more than rows.
+int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
+
+// ---- mean ----------------------------------------------------------------------------------------------------------------
+
+int32_t spans_check(const he_spans *s)
+{
+    if (!s || s->count < 0 || s->rows < 0 || s->rows > MAX_ROWS || s->count > (1 << 24)) return HE_EINVAL;
+    if (s->count > 0 && (!s->d_begin || !s->d_end)) return HE_EINVAL;
+    return HE_OK;
+}
+Spans spans_of(const he_spans *s) { return Spans{s->d_begin, s->d_end, s->count, (int32_t)s->rows}; }
+
+// Sequences are cut where there are too few of them to fill the card: about 512 work-groups, of at least 256 rows on average.
+int pool_splits(const he_spans *s)
+{
+    if (s->count == 0) return 1;
+    const int64_t mean = s->rows / s->count, most = std::max<int64_t>(1, mean / 256);
+    return (int)std::min<int64_t>(std::min<int64_t>(most, (512 + s->count - 1) / s->count), 512);
+}
+
+// ---- attention -------------------------------------------------------------------------------------------------------------
+
+int32_t attn_check(const he_attn *s)
+{
+    if (!s || !type_ok(s->type) || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads || s->heads > 65535) return HE_EINVAL;
+    if (s->dim < 8 || s->dim > 128 || s->dim % 8) return HE_EINVAL;
+    if (spans_check(&s->q) != HE_OK || spans_check(&s->k) != HE_OK || s->q.count != s->k.count) return HE_EINVAL;
+    if (!(s->scale > 0.0) || !std::isfinite((float)s->scale) || !((float)s->scale > 0.f)) return HE_EINVAL;
+    if (!(s->cap >= 0.0) || !std::isfinite((float)s->cap) || (s->cap > 0.0 && !((float)s->cap > 0.f))) return HE_EINVAL;
+    return HE_OK;
+}
+bool heads_ok(const he_heads *h, int32_t type)
+{
+    const int64_t size = (int64_t)type_size(type);
+    return h && h->d && aligned(h->d, 16) && h->row >= 0 && h->head >= 0 && (h->row * size) % 16 == 0 && (h->head * size) % 16 == 0;
+}
+// Buffers that are written: elements of different rows or heads have different addresses if the strides hold a row of a head each.
+bool out_ok(const he_heads *h, const he_attn *s, int64_t rows, int heads)
+{
+    return heads_ok(h, s->type) && (rows <= 1 || h->row >= s->dim) && (heads <= 1 || h->head >= s->dim);
+}
+
+struct AttnPlan {
+    int nwq, splits;
+    int64_t slots;
+};
+AttnPlan attn_plan(const he_attn *s)
+{
+    AttnPlan p;
+    const int64_t mean_q = s->q.count ? s->q.rows / s->q.count : 0, mean_k = s->q.count ? s->k.rows / s->q.count : 0;
+    p.nwq = mean_q <= 32 ? 1 : mean_q <= 64 ? 2 : 4;
+    p.slots = tile_slots(s->q.rows, s->q.count, 32 * p.nwq);
+    const int64_t groups = p.slots * s->heads;
+    p.splits = groups > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, mean_k / 256, 64})) : 1;
+    return p;
+}
+size_t attn_bytes(const he_attn *s, bool backward)
+{
+    const size_t rows = (size_t)s->q.rows * s->heads;
+    if (backward) return rows * 4;
+    const AttnPlan p = attn_plan(s);
+    return p.splits > 1 ? rows * p.splits * (s->dim + 1) * 4 : 0;
+}
+AttnArgs attn_args(const he_attn *s)
+{
+    AttnArgs a;
+    memset(&a, 0, sizeof(a));
+    a.sq = spans_of(&s->q);
+    a.sk = spans_of(&s->k);
+    a.heads = s->heads;
+    a.group = s->heads / s->kv_heads;
+    a.dim = s->dim;
+    a.scale = (float)s->scale;
+    a.cap = (float)s->cap;
+    a.slope = s->d_slopes;
+    a.splits = 1;
+    a.fill = s->fill;
+    return a;
+}
+// work-groups, a multiple of eight for the eight dies; false: more than a launch holds
+bool attn_grid(AttnArgs &a, int64_t slots, int64_t per_slot, unsigned &grid)
+{
+    const int64_t w = slots * per_slot;
+    if (w >= ((int64_t)1 << 31) / ATTN_THREADS) return false;
+    a.slots = (int)slots;
+    a.work = (unsigned)w;
+    grid = (unsigned)((w + 7) / 8 * 8);
+    return true;
+}
+#define SET(dst, h) a.dst##_row = (h)->row, a.dst##_head = (h)->head
+
+} // namespace
+
+extern "C" int32_t he_layer_norm(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const void *d_b,
+                                 const he_rows *y, const he_rows *sum, float *d_mean, float *d_rstd, void *stream)
+{
+    if (!ctx || norm_check(n) != HE_OK || !(n->eps >= 0.0) || !std::isfinite((float)n->eps)) return HE_EINVAL;
+    if (n->rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!rows_ok(x, n->width) || !rows_ok(y, n->width) || !d_w || !d_b || !d_mean || !d_rstd) return HE_EINVAL;
+    if (residual && (!rows_ok(residual, n->width) || !rows_ok(sum, n->width))) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    if (!residual) sum = nullptr;
+    NormArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = x->d, a.x_row = x->stride, a.y = y->d, a.y_row = y->stride;
+    if (residual) a.r = residual->d, a.r_row = residual->stride, a.s = sum->d, a.s_row = sum->stride;
+    a.w = d_w, a.b = d_b, a.mean = d_mean, a.rstd = d_rstd;
+    a.rows = (int)n->rows, a.width = n->width, a.eps = (float)n->eps;
+    const bool vec = wide(x, n->type) && wide(residual, n->type) && wide(y, n->type) && wide(sum, n->type) && aligned(d_w, 16) && aligned(d_b, 16) &&
+                     (n->width * type_size(n->type)) % 16 == 0;
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const double row = (double)n->width * type_size(n->type);
+    rows_launch(n->type).norm(ctx, (hipStream_t)stream, n->rows * (row * (residual ? 4 : 2) + 8) + 2.0 * n->width * type_size(n->weight_type), vec,
+                              n->weight_type == HE_F32, a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_layer_norm_workspace_bytes(const he_ctx *ctx, const he_norm *n, size_t *out)
+{
+    if (!ctx || !out || norm_check(n) != HE_OK) return HE_EINVAL;
+    *out = n->rows ? (size_t)norm_parts(n->rows) * 2 * n->width * sizeof(float) : 0;
+    return HE_OK;
+}
+
+extern "C" int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, const he_rows *s, const void *d_w, const float *d_mean,
+                                      const float *d_rstd, const he_rows *add, const he_rows *ds, void *d_dw, void *d_db, void *d_ws, size_t ws_bytes,
+                                      void *stream)
+{
+    if (!ctx || norm_check(n) != HE_OK || !d_w || !d_dw || !d_db) return HE_EINVAL;
+    NormGradArgs a;
+    memset(&a, 0, sizeof(a));
+    a.rows = (int)n->rows, a.width = n->width;
+    const int parts = n->rows ? norm_parts(n->rows) : 0;
+    if (n->rows) {
+        if (!rows_ok(dy, n->width) || !rows_ok(s, n->width) || !rows_ok(ds, n->width) || !d_mean || !d_rstd) return HE_EINVAL;
+        if (add && !rows_ok(add, n->width)) return HE_EINVAL;
+        if (!d_ws || ws_bytes < (size_t)parts * 2 * n->width * sizeof(float)) return HE_EWORKSPACE;
+        if (!aligned(d_ws, 4)) return HE_EINVAL;
+        a.dy = dy->d, a.dy_row = dy->stride, a.s = s->d, a.s_row = s->stride, a.ds = ds->d, a.ds_row = ds->stride;
+        if (add) a.add = add->d, a.add_row = add->stride;
+        a.w = d_w, a.mean = d_mean, a.rstd = d_rstd, a.part = (float *)d_ws;
+    }
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const RowsLaunch &l = rows_launch(n->type);
+    const bool ww = n->weight_type == HE_F32;
+    const double row = (double)n->width * type_size(n->type), part = (double)parts * 2 * n->width * 4;
+    if (n->rows) {
+        const bool vec = wide(dy, n->type) && wide(s, n->type) && wide(ds, n->type) && wide(add, n->type) && aligned(d_w, 16) &&
+                         (n->width * type_size(n->type)) % 16 == 0;
+        l.norm_grad(ctx, (hipStream_t)stream, n->rows * (row * (add ? 4 : 3) + 8) + part, vec, ww, parts, a);
+    }
+    l.weight_grad(ctx, (hipStream_t)stream, part + 2.0 * n->width * type_size(n->weight_type), ww, (const float *)d_ws, parts, n->width, d_dw, d_db);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_pool_workspace_bytes(const he_ctx *ctx, const he_spans *s, int32_t width, size_t *out)
+{
+    if (!ctx || !out || spans_check(s) != HE_OK || width < 1 || width > (1 << 20)) return HE_EINVAL;
+    const int splits = pool_splits(s);
+    *out = splits > 1 ? (size_t)s->count * splits * width * sizeof(float) : 0;
+    return HE_OK;
+}
+
+extern "C" int32_t he_pool(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, const he_rows *x, float *d_e, void *d_ws, size_t ws_bytes,
+                           void *stream)
+{
+    if (!ctx || spans_check(s) != HE_OK || !type_ok(type) || width < 1 || width > (1 << 20)) return HE_EINVAL;
+    if (s->count == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!d_e || (s->rows > 0 && !rows_ok(x, width))) return HE_EINVAL;
+    PoolArgs a;
+    memset(&a, 0, sizeof(a));
+    if (s->rows > 0) a.x = x->d, a.x_row = x->stride;
+    a.e = d_e, a.s = spans_of(s), a.width = width, a.splits = pool_splits(s), a.part = (float *)d_ws;
+    if (a.splits > 1 && (!d_ws || ws_bytes < (size_t)s->count * a.splits * width * sizeof(float))) return HE_EWORKSPACE;
+    if (a.splits > 1 && !aligned(d_ws, 4)) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    const bool vec = (s->rows == 0 || wide(x, type)) && (width * type_size(type)) % 16 == 0;
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    rows_launch(type).pool(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width, vec, a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, const float *d_de, const he_rows *dx, int32_t fill,
+                                void *stream)
+{
+    if (!ctx || spans_check(s) != HE_OK || !type_ok(type) || width < 1 || width > (1 << 20)) return HE_EINVAL;
+    if (s->count == 0 || s->rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!d_de || !rows_ok(dx, width)) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    PoolGradArgs a;
+    memset(&a, 0, sizeof(a));
+    a.de = d_de, a.dx = dx->d, a.dx_row = dx->stride, a.s = spans_of(s), a.width = width, a.fill = fill;
+    const bool vec = wide(dx, type) && (width * type_size(type)) % 16 == 0;
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    rows_launch(type).pool_grad(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width, vec,
+                                (unsigned)tile_slots(s->rows, s->count, POOL_TILE), a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_attention_workspace_bytes(const he_ctx *ctx, const he_attn *s, int32_t backward, size_t *out)
+{
+    if (!ctx || !out || attn_check(s) != HE_OK) return HE_EINVAL;
+    *out = attn_bytes(s, backward != 0);
+    return HE_OK;
+}
+
+extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q, const he_heads *k, const he_heads *v, const he_heads *o,
+                                float *d_lse, void *d_ws, size_t ws_bytes, void *stream)
+{
+    if (!ctx || attn_check(s) != HE_OK) return HE_EINVAL;
+    if (s->q.rows == 0 || s->q.count == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!heads_ok(q, s->type) || !out_ok(o, s, s->q.rows, s->heads) || !d_lse) return HE_EINVAL;
+    if (s->k.rows > 0 && (!heads_ok(k, s->type) || !heads_ok(v, s->type))) return HE_EINVAL;
+    const size_t need = attn_bytes(s, false);
+    if (need && (!d_ws || ws_bytes < need)) return HE_EWORKSPACE;
+    if (need && !aligned(d_ws, 16)) return HE_EINVAL;
+    const AttnPlan p = attn_plan(s);
+    AttnArgs a = attn_args(s);
+    a.q = q->d, a.o = o->d, a.lse = d_lse, a.splits = p.splits;
+    SET(q, q), SET(o, o);
+    if (s->k.rows > 0) {
+        a.k = k->d, a.v = v->d;
+        SET(k, k), SET(v, v);
+    }
+    a.part_o = (float *)d_ws;
+    a.part_lse = a.part_o + (size_t)p.splits * s->heads * s->q.rows * s->dim;
+    unsigned grid;
+    if (!attn_grid(a, p.slots, (int64_t)s->heads * p.splits, grid)) return HE_EINVAL;
+    const int64_t rows = s->q.rows * s->heads;
+    if (p.splits > 1 && rows >= (int64_t)4 << 23) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const AttnLaunch &l = attn_launch(s->type, s->dim);
+    const double size = (double)type_size(s->type) * s->dim, kv = 2.0 * s->k.rows * s->kv_heads * size;
+    l.fwd(ctx, (hipStream_t)stream, rows * (2 * size + 4) + kv, p.nwq, s->cap > 0.0 || s->d_slopes, grid, a);
+    if (p.splits > 1)
+        l.join(ctx, (hipStream_t)stream, rows * (size + 4 + 4.0 * p.splits * (s->dim + 1)), (unsigned)((rows + 3) / 4), a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_heads *go, const he_heads *q, const he_heads *k, const he_heads *v,
+                                     const he_heads *o, const float *d_lse, const he_heads *dq, const he_heads *dk, const he_heads *dv, void *d_ws,
+                                     size_t ws_bytes, void *stream)
+{
+    if (!ctx || attn_check(s) != HE_OK) return HE_EINVAL;
+    if (s->q.count == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    const bool some_q = s->q.rows > 0, some_k = s->k.rows > 0;
+    if (some_q && (!heads_ok(q, s->type) || !heads_ok(o, s->type) || !heads_ok(go, s->type) || !out_ok(dq, s, s->q.rows, s->heads) || !d_lse)) return HE_EINVAL;
+    if (some_k && (!heads_ok(k, s->type) || !heads_ok(v, s->type) || !out_ok(dk, s, s->k.rows, s->kv_heads) ||
+                   !out_ok(dv, s, s->k.rows, s->kv_heads)))
+        return HE_EINVAL;
+    const size_t need = attn_bytes(s, true);
+    if (need && (!d_ws || ws_bytes < need)) return HE_EWORKSPACE;
+    if (need && !aligned(d_ws, 16)) return HE_EINVAL;
+    AttnArgs a = attn_args(s);
+    if (some_q) {
+        a.q = q->d, a.o_in = o->d, a.go = go->d, a.dq = dq->d;
+        SET(q, q), SET(oi, o), SET(go, go), SET(dq, dq);
+    }
+    if (some_k) {
+        a.k = k->d, a.v = v->d, a.dk = dk->d, a.dv = dv->d;
+        SET(k, k), SET(v, v), SET(dk, dk), SET(dv, dv);
+    }
+    a.lse = const_cast<float *>(d_lse);
+    a.delta = (float *)d_ws;
+    AttnArgs b = a;
+    unsigned grid_q = 0, grid_kv = 0;
+    if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, 128), s->heads, grid_q)) return HE_EINVAL;
+    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, 128), s->kv_heads, grid_kv)) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const AttnLaunch &l = attn_launch(s->type, s->dim);
+    const bool mods = s->cap > 0.0 || s->d_slopes;
+    const double size = (double)type_size(s->type) * s->dim, qb = s->q.rows * s->heads * size, kb = s->k.rows * s->kv_heads * size;
+    if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, mods, grid_q, a);
+    if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, mods, grid_kv, b);
+    return launched(ctx);
+}

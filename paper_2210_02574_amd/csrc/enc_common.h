@@ -1,0 +1,77 @@
+// What the kernels on token states share: element types, vectors of them, sums over lanes, the sequence of a tile of rows.
+//
+// Sequences are rows [begin[i], end[i]) of one token axis, in ascending order and apart from one another.  The numbers are device
+// data that the host never sees, so every kernel clamps them to the buffer: numbers that break the rule give results
+// without meaning, never an access outside the buffers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+template <class T, int N> struct VecOf {
+    typedef T type __attribute__((ext_vector_type(N)));
+};
+template <class T> struct VecOf<T, 1> {
+    struct type {
+        T v;
+        __device__ T &operator[](int) { return v; }
+        __device__ T operator[](int) const { return v; }
+    };
+};
+template <class T, int N> using Vec = typename VecOf<T, N>::type;
+typedef Vec<float, 4> f32x4;
+typedef Vec<float, 16> f32x16;
+
+// Sum over the LANES lanes of an aligned group, the same in each of them.
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int s = LANES / 2; s > 0; s >>= 1) v += __shfl_xor(v, s, 64);
+    return v;
+}
+
+struct Spans {
+    const int32_t *begin, *end;
+    int32_t count; // sequences
+    int32_t rows;  // of the token axis
+};
+__device__ __forceinline__ int span_begin(const Spans &s, int i) { return min(max(s.begin[i], 0), s.rows); }
+__device__ __forceinline__ int span_end(const Spans &s, int i) { return min(max(s.end[i], 0), s.rows); }
+
+// Tiles of `tile` rows never span two sequences: a neighbour's infinities and NaN stay away from a product with zero weights.
+// Sequence i is given the rows from its begin up to the next one's begin (the first one from row 0, the last one to the last row: so
+// the rows between and behind sequences have a tile too), cover_i = [c_i, c_{i+1}), and the slots f_i .. f_{i+1} - 1 with
+// f_i = floor(c_i / tile) + i, which are at least ceil((c_{i+1} - c_i) / tile): no sums over the lengths are needed, and floor(rows / tile) + count
+// slots hold them all.  A slot behind the last row of its sequence's cover is empty.
+struct TileRows {
+    int seq;        // the sequence
+    int first, top; // the tile's rows, [first, top); empty: first >= top
+    int begin, end; // of the sequence: rows of the tile outside belong to none
+};
+__device__ __forceinline__ TileRows tile_rows(const Spans &s, int slot, int tile)
+{
+    // the last i with f_i <= slot, sought by 64 lanes at a time
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = s.count; // i is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lo + lane * step;
+        const bool ok = lane * step < n && (i == 0 || span_begin(s, i) / tile + i <= slot);
+        const unsigned long long m = __ballot(ok);
+        const int k = m ? 63 - __clzll(m) : 0;
+        n = min(step, n - k * step);
+        lo += k * step;
+    }
+    TileRows t;
+    t.seq = __builtin_amdgcn_readfirstlane(lo);
+    t.begin = __builtin_amdgcn_readfirstlane(span_begin(s, t.seq));
+    t.end = __builtin_amdgcn_readfirstlane(span_end(s, t.seq));
+    const int c = t.seq ? t.begin : 0;
+    const int top = t.seq + 1 < s.count ? __builtin_amdgcn_readfirstlane(span_begin(s, t.seq + 1)) : s.rows;
+    const long long first = c + (long long)(slot - (c / tile + t.seq)) * tile;
+    t.first = first < c ? top : (int)(first < top ? first : top);
+    t.top = min(t.first + tile, top);
+    return t;
+}
+static inline int64_t tile_slots(int64_t rows, int64_t count, int tile) { return rows / tile + count; }

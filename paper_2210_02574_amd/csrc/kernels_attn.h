@@ -1,0 +1,578 @@
+// Attention inside each sequence of a batch, forward and backward, by matrix instructions.
+//
+//   t_ij = scale q_i . k_j, u_ij = cap tanh(t_ij / cap) (no cap: t_ij), s_ij = u_ij - slope_h |pos_i - pos_j|
+//   lse_i = log sum_j exp(s_ij), p_ij = exp(s_ij - lse_i), o_i = sum_j p_ij v_j; no keys: o_i = 0, lse_i = -inf
+//   delta_i = do_i . o_i, dp_ij = do_i . v_j, ds_ij = p_ij (dp_ij - delta_i), dt_ij = ds_ij (1 - (u_ij / cap)^2) scale
+//   dv_j = sum_i p_ij do_i, dk_j = sum_i dt_ij q_i, dq_i = sum_j dt_ij k_j (dv, dk: over the query heads that share the key head too)
+//
+// One layout carries all three kernels.  A 32 x 32 product C = A B leaves lane l with column l mod 32 and the rows 8 (r / 4) + 4 (l / 32) + r mod 4,
+// r < 16.  The rows of a work-group's own tile (queries in the forward pass and for dq, keys for dk and dv) are the columns n, the rows that
+// stream by are the rows m.  So a softmax statistic belongs to one lane and its partner 32 further on; and eight of a lane's values of C, rounded, are
+// its operand B of the next product over those rows, whose order inside a block of 16 does not matter as long as A has the same one:
+// slot (l / 32, e) holds row 4 (l / 32) + e for e < 4 and 8 + 4 (l / 32) + e - 4 above.  Nothing moves between lanes on the way.
+// The operand A of that product is a transposed tile: 16-bit types read it from LDS with the transposing read, 32-bit ones word by word.
+//
+// Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
+// everything else, sums and statistics included, is in 32 bits.  fp16 holds dt down to 6e-8: gradients as small as that need a
+// scaled loss, as everywhere in fp16.
+#pragma once
+#include "enc_common.h"
+
+struct AttnArgs {
+    const void *q, *k, *v, *o_in, *go; // o_in, go: the forward pass's o and the gradient that reaches it (backward)
+    void *o, *dq, *dk, *dv;
+    float *lse;         // [heads][rows_q], natural logarithm
+    float *delta;       // [heads][rows_q]
+    float *part_o;      // [splits][heads][rows_q][dim]
+    float *part_lse;    // [splits][heads][rows_q]
+    const float *slope; // [heads] or null
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, oi_row, oi_head, go_row, go_head; // strides, in elements
+    int64_t dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+    Spans sq, sk;
+    int heads, group, dim; // group: query heads that share a key head
+    float scale, cap;
+    int slots, splits, fill;
+    unsigned work; // work-groups that have something to do
+};
+
+template <class T> struct AttnType;
+template <> struct AttnType<f16> {
+    static __device__ __forceinline__ f32x16 mma(Vec<f16, 8> a, Vec<f16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct AttnType<bf16> {
+    static __device__ __forceinline__ f32x16 mma(Vec<bf16, 8> a, Vec<bf16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct AttnType<float> {
+    // slot (l / 32, e): eight products over two rows each
+    static __device__ __forceinline__ f32x16 mma(Vec<float, 8> a, Vec<float, 8> b, f32x16 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+#define ATTN_THREADS 256
+#define LOG2E 1.44269504088896340736f
+#define LN2 0.69314718055994530942f
+
+// The value of the other lane of the pair (l, l + 32), joined.
+__device__ __forceinline__ float pair_max(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float pair_sum(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// tanh by the exponential where values have 16 bits (absolute error 2^-23), the library's for 32.
+template <class T> __device__ __forceinline__ float tanh_of(float x)
+{
+    if constexpr (sizeof(T) == 4) return tanhf(x);
+    return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * LOG2E)));
+}
+
+// Tiles in LDS: rows of DP elements and 16 bytes more, which spreads the 16-byte reads of eight rows over all banks.
+template <class T, int DP> struct AttnTile {
+    static constexpr int ROW = DP + 16 / (int)sizeof(T); // elements
+    static constexpr int VEC = 16 / (int)sizeof(T);      // of a 16-byte access
+    static constexpr int CHUNKS = DP / VEC;
+    typedef Vec<T, VEC> Chunk;
+
+    // 16-byte chunks of ROWS rows by `NT` threads: from memory to registers, zeros outside the rows [.., end) and the columns below dim ..
+    template <int ROWS, int NT> static constexpr int per() { return (ROWS * CHUNKS + NT - 1) / NT; }
+    template <int ROWS, int NT>
+    static __device__ __forceinline__ void load(Chunk (&c)[per<ROWS, NT>()], const T *base, int64_t stride, int first, int end, int dim, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < per<ROWS, NT>(); i++) {
+            const int at = i * NT + tid, row = first + at / CHUNKS, col = (at % CHUNKS) * VEC;
+            Chunk x = {};
+            if (at < ROWS * CHUNKS && row < end && col < dim) x = *(const Chunk *)(base + row * stride + col);
+            c[i] = x;
+        }
+    }
+    // .. and from registers to LDS
+    template <int ROWS, int NT> static __device__ __forceinline__ void store(const Chunk (&c)[per<ROWS, NT>()], T *lds, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < per<ROWS, NT>(); i++) {
+            const int at = i * NT + tid;
+            if (at < ROWS * CHUNKS) *(Chunk *)(lds + (at / CHUNKS) * ROW + (at % CHUNKS) * VEC) = c[i];
+        }
+    }
+    // operand A or B: lane's row `row0 + l mod 32`, columns 16 kk + 8 (l / 32) ..
+    static __device__ __forceinline__ Vec<T, 8> rows(const T *lds, int row0, int kk, int lane)
+    {
+        const T *p = lds + (row0 + (lane & 31)) * ROW + 16 * kk + 8 * (lane >> 5);
+        return eight(p);
+    }
+    static __device__ __forceinline__ Vec<T, 8> eight(const T *p)
+    {
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+            return Vec<T, 8>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        } else
+            return *(const Vec<T, 8> *)p;
+    }
+    // operand A of a transposed tile: lane's column 32 db + l mod 32, the rows row0 + .. in slot order
+    static __device__ __forceinline__ Vec<T, 8> cols(const T *lds, int row0, int db, int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (sizeof(T) == 4) {
+            const T *p = lds + (row0 + 4 * h) * ROW + 32 * db + (lane & 31);
+            Vec<T, 8> x;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                x[e] = p[e * ROW];
+                x[4 + e] = p[(8 + e) * ROW];
+            }
+            return x;
+        } else {
+            // 16 lanes read four rows of 16 elements, four lanes to a row; lane j of them gets element j of each row
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef short s8 __attribute__((ext_vector_type(8)));
+            typedef __attribute__((address_space(3))) s4 *Ptr;
+            const int j = lane & 15;
+            const T *p = lds + (row0 + 4 * h + (j >> 2)) * ROW + 32 * db + (lane & 16) + (j & 3) * 4;
+            const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + 8 * ROW));
+            const s8 x = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            return __builtin_bit_cast(Vec<T, 8>, x);
+        }
+    }
+    // the operand from memory: row `row` of base, or zeros
+    static __device__ __forceinline__ Vec<T, 8> own(const T *base, int64_t stride, int row, bool in, int kk, int dim, int lane)
+    {
+        const int col = 16 * kk + 8 * (lane >> 5);
+        Vec<T, 8> x = {};
+        if (in && col < dim) x = eight(base + row * stride + col);
+        return x;
+    }
+};
+
+// eight of a lane's values of C as operand B
+template <class T> __device__ __forceinline__ Vec<T, 8> round8(const f32x16 &c, int half)
+{
+    Vec<T, 8> x;
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = (T)c[8 * half + e];
+    return x;
+}
+
+// a lane's column of C^T blocks, times f, as a row of memory
+template <class T, int DB> __device__ __forceinline__ void store_row(const f32x16 (&c)[DB], float f, T *row, int dim, int lane)
+{
+    const int h = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < DB; db++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int col = 32 * db + 2 * r + 4 * h;
+            Vec<T, 4> x;
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = (T)(c[db][r + e] * f);
+            if (col < dim) *(Vec<T, 4> *)(row + col) = x;
+        }
+}
+
+// Work-group -> (head, slot, split), neighbours on one of the eight dies' caches: work-groups go to the dies in turn, so die d is given
+// the d-th eighth of the work, in which tiles of one head, which read the same keys, come one after the other.
+__device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, int &head, int &slot, int &split)
+{
+    const unsigned w = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (w >= a.work) return false;
+    head = w / per_head;
+    const unsigned r = w % per_head;
+    split = r % a.splits;
+    slot = r / a.splits;
+    return true;
+}
+
+// Scores of one 32 x 32 block from the products: x = log2(e) s.  pos: position of the lane's own row minus the one of row 0 of the block, so that the
+// distance of row m is |pos - m| (symmetric: it serves keys as columns too).
+template <class T> __device__ __forceinline__ void scores(f32x16 &c, f32x16 *th, const AttnArgs &a, float slope, float pos, int h)
+{
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        float x = c[r] * a.scale;
+        if (a.cap > 0.f) {
+            const float t = tanh_of<T>(x / a.cap);
+            if (th) (*th)[r] = t;
+            x = a.cap * t;
+        }
+        x -= slope * fabsf(pos - (float)(8 * (r >> 2) + 4 * h + (r & 3)));
+        c[r] = x * LOG2E;
+    }
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------------------
+//
+// Four waves: NWQ of them along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: few queries then still
+// keep four waves busy.  KB blocks of 32 keys per wave and step.  MODS: there is a cap or a distance bias.
+template <class T, int DP, int NWQ> struct AttnFwd {
+    static constexpr int NWK = 4 / NWQ, KB = NWK > 1 || sizeof(T) == 4 ? 1 : 2, BM = 32 * NWQ, BN = 32 * KB * NWK;
+    static constexpr int TILE = BN * AttnTile<T, DP>::ROW;                    // elements of a tile
+    static constexpr int JOIN = NWK > 1 ? (NWK - 1) * NWQ * 64 * (DP / 2 + 2) : 0; // floats
+    static constexpr int LDS = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
+};
+
+template <class T, int DP, int NWQ, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
+{
+    typedef AttnFwd<T, DP, NWQ> F;
+    typedef AttnTile<T, DP> L;
+    constexpr int NWK = F::NWK, KB = F::KB, BN = F::BN, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) char lds[F::LDS];
+    T *const lk = (T *)lds, *const lv = lk + F::TILE;
+
+    int head, slot, split;
+    if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
+    const TileRows t = tile_rows(a.sq, slot, F::BM);
+    if (t.first >= t.top) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wq = wave % NWQ, wk = wave / NWQ;
+    const int row = t.first + 32 * wq + (lane & 31);
+    const bool in = row < t.top && row >= t.begin && row < t.end; // a row of the sequence
+
+    int kb = span_begin(a.sk, t.seq), ke = span_end(a.sk, t.seq);
+    ke = max(ke, kb);
+    const int pos0 = row - t.begin + (ke - kb) - (t.end - t.begin); // the row's position among the keys, the first at 0
+    if (t.first >= t.end || t.top <= t.begin) ke = kb; // a tile between sequences: nothing to sum
+    const int tiles = (ke - kb + BN - 1) / BN, per = (tiles + a.splits - 1) / a.splits;
+    const int lo = kb + min(split * per, tiles) * BN, hi = min(ke, kb + min((split + 1) * per, tiles) * BN);
+
+    const T *const q = (const T *)a.q + head * a.q_head;
+    const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    Vec<T, 8> fq[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) fq[kk] = L::own(q, a.q_row, row, in, kk, a.dim, lane);
+
+    const float slope = MODS && a.slope ? a.slope[head] : 0.f;
+    const float c2 = MODS ? 1.f : a.scale * LOG2E; // scores are kept times this below
+    float top = -INFINITY, sum = 0.f;              // running maximum (in units of log2) and the lane's own sum
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) o[db] = f32x16{};
+
+    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
+    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, lo, hi, a.dim, tid);
+    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, lo, hi, a.dim, tid);
+    for (int j0 = lo; j0 < hi; j0 += BN) {
+        __syncthreads();
+        L::template store<BN, ATTN_THREADS>(ck, lk, tid);
+        L::template store<BN, ATTN_THREADS>(cv, lv, tid);
+        __syncthreads();
+        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, hi, a.dim, tid); // the next tile is under way meanwhile
+        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, hi, a.dim, tid);
+        const int w0 = wk * KB * 32; // the wave's keys of the tile
+        if (j0 + w0 >= hi) continue;
+        f32x16 s[KB];
+#pragma unroll
+        for (int b = 0; b < KB; b++) {
+            s[b] = f32x16{};
+#pragma unroll
+            for (int kk = 0; kk < KK; kk++) s[b] = AttnType<T>::mma(L::rows(lk, w0 + 32 * b, kk, lane), fq[kk], s[b]);
+        }
+        if constexpr (MODS)
+#pragma unroll
+            for (int b = 0; b < KB; b++) scores<T>(s[b], nullptr, a, slope, (float)(pos0 - (j0 + w0 + 32 * b - kb)), h);
+        if (j0 + w0 + 32 * KB > hi)
+#pragma unroll
+            for (int b = 0; b < KB; b++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    if (j0 + w0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3) >= hi) s[b][r] = -INFINITY;
+        float m = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) m = fmaxf(m, s[b][r]);
+        m = pair_max(m) * c2;
+        // The maximum that the sums refer to moves only when it is left 8 behind (2^8 fits every type): most steps skip the rescaling.
+        if (__any(m > top + 8.f)) {
+            const float now = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
+            top = now;
+            sum *= f;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) o[db][r] *= f;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c2, -ref));
+                sum += s[b][r];
+            }
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                const Vec<T, 8> p = round8<T>(s[b], half);
+#pragma unroll
+                for (int db = 0; db < DB; db++) o[db] = AttnType<T>::mma(L::cols(lv, w0 + 32 * b + 16 * half, db, lane), p, o[db]);
+            }
+    }
+    sum = pair_sum(sum);
+
+    if constexpr (NWK > 1) { // join the waves along the keys: word i of all lanes side by side
+        float *const join = (float *)lds;
+        __syncthreads();
+        if (wk > 0) {
+            float *p = join + ((wk - 1) * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
+            p[0] = top;
+            p[64] = sum;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) p[(2 + db * 16 + r) * 64] = o[db][r];
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int w = 0; w < NWK - 1; w++) {
+            const float *p = join + (w * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
+            const float m = fmaxf(top, p[0]), ref = m == -INFINITY ? 0.f : m;
+            const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(p[0] - ref);
+            top = m;
+            sum = sum * f + p[64] * g;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) o[db][r] = o[db][r] * f + p[(2 + db * 16 + r) * 64] * g;
+        }
+    }
+    if (row >= t.top || (!in && !a.fill)) return;
+    // a row without keys, and a row of no sequence: zeros
+    const bool some = in && hi > lo;
+    const float f = some ? 1.f / sum : 0.f, lse = some ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    const int64_t at = (int64_t)head * a.sq.rows + row;
+    if (a.splits > 1) {
+        const int64_t part = (int64_t)split * a.heads * a.sq.rows + at;
+        if (h == 0) a.part_lse[part] = lse;
+        if (some) store_row<float, DB>(o, f, a.part_o + part * a.dim, a.dim, lane);
+        return;
+    }
+    if (h == 0) a.lse[at] = lse;
+    if (!some) // not 0 * o: the row may hold what a zero does not clear
+#pragma unroll
+        for (int db = 0; db < DB; db++) o[db] = f32x16{};
+    store_row<T, DB>(o, f, (T *)a.o + head * a.o_head + row * a.o_row, a.dim, lane);
+}
+
+// The splits of a row: weights exp(lse_s - lse).  A wave per row and head, blockIdx.x * 4 + wave over [heads][rows].
+template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
+{
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.heads * a.sq.rows;
+    if (at >= all) return;
+    const int lane = threadIdx.x & 63, head = at / a.sq.rows, row = at % a.sq.rows;
+    // the splits of a row that no tile wrote hold nothing: find out whether the row belongs to a sequence
+    int lo = 0, n = a.sq.count;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lo + lane * step;
+        const unsigned long long m = __ballot(lane * step < n && span_begin(a.sq, i) <= row);
+        const int k = m ? 63 - __clzll(m) : 0;
+        n = min(step, n - k * step);
+        lo += k * step;
+    }
+    const bool in = row >= span_begin(a.sq, lo) && row < span_end(a.sq, lo);
+    if (!in && !a.fill) return;
+    float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
+    if (in)
+        for (int s = 0; s < a.splits; s++) {
+            const float l = a.part_lse[s * all + at];
+            if (l == -INFINITY) continue;
+            const float m = fmaxf(top, l), f = expf(top - m), g = expf(l - m);
+            const float *p = a.part_o + (s * all + at) * a.dim;
+            top = m;
+            sum = sum * f + g;
+            o0 = o0 * f + (lane < a.dim ? p[lane] * g : 0.f);
+            o1 = o1 * f + (lane + 64 < a.dim ? p[lane + 64] * g : 0.f);
+        }
+    const float f = sum > 0.f ? 1.f / sum : sum; // NaN stays
+    if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : top + logf(sum);
+    T *o = (T *)a.o + head * a.o_head + row * a.o_row;
+    if (lane < a.dim) o[lane] = (T)(o0 * f);
+    if (lane + 64 < a.dim) o[lane + 64] = (T)(o1 * f);
+}
+
+// ---- backward: dq -----------------------------------------------------------------------------------------------------
+//
+// Queries as columns, keys stream by.  Also leaves delta for the kernel of dk and dv, which runs after it.
+template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_q(AttnArgs a)
+{
+    typedef AttnTile<T, DP> L;
+    constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lk[BN * L::ROW], lv[BN * L::ROW];
+
+    int head, slot, split;
+    if (!attn_work(a, a.slots, head, slot, split)) return;
+    const TileRows t = tile_rows(a.sq, slot, 128);
+    if (t.first >= t.top) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = t.first + 32 * wave + (lane & 31);
+    const bool in = row < t.top && row >= t.begin && row < t.end;
+    int kb = span_begin(a.sk, t.seq), ke = span_end(a.sk, t.seq);
+    ke = max(ke, kb);
+    const int pos0 = row - t.begin + (ke - kb) - (t.end - t.begin);
+    if (t.first >= t.end || t.top <= t.begin) ke = kb;
+
+    const T *const q = (const T *)a.q + head * a.q_head, *const go = (const T *)a.go + head * a.go_head;
+    const T *const oi = (const T *)a.o_in + head * a.oi_head;
+    const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    Vec<T, 8> fq[KK], fg[KK];
+    float delta = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) {
+        fq[kk] = L::own(q, a.q_row, row, in, kk, a.dim, lane);
+        fg[kk] = L::own(go, a.go_row, row, in, kk, a.dim, lane);
+        const Vec<T, 8> x = L::own(oi, a.oi_row, row, in, kk, a.dim, lane);
+#pragma unroll
+        for (int e = 0; e < 8; e++) delta += (float)x[e] * (float)fg[kk][e];
+    }
+    delta = pair_sum(delta);
+    const int64_t at = (int64_t)head * a.sq.rows + row;
+    if (in && h == 0) a.delta[at] = delta;
+    const float lse = in ? a.lse[at] * LOG2E : INFINITY; // rows of no sequence: p = 0
+    const float slope = MODS && a.slope ? a.slope[head] : 0.f, c2 = MODS ? 1.f : a.scale * LOG2E;
+    f32x16 dq[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) dq[db] = f32x16{};
+
+    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
+    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, kb, ke, a.dim, tid);
+    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, kb, ke, a.dim, tid);
+    for (int j0 = kb; j0 < ke; j0 += BN) {
+        __syncthreads();
+        L::template store<BN, ATTN_THREADS>(ck, lk, tid);
+        L::template store<BN, ATTN_THREADS>(cv, lv, tid);
+        __syncthreads();
+        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, ke, a.dim, tid);
+        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, ke, a.dim, tid);
+        f32x16 s = {}, dp = {}, th;
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            s = AttnType<T>::mma(L::rows(lk, 0, kk, lane), fq[kk], s);
+            dp = AttnType<T>::mma(L::rows(lv, 0, kk, lane), fg[kk], dp);
+        }
+        if constexpr (MODS) scores<T>(s, &th, a, slope, (float)(pos0 - (j0 - kb)), h);
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -lse));
+            if (j0 + BN > ke && j0 + 8 * (r >> 2) + 4 * h + (r & 3) >= ke) p = 0.f; // exp of a missing key's score may be anything
+            float d = p * (dp[r] - delta);
+            if (MODS && a.cap > 0.f) d *= 1.f - th[r] * th[r];
+            s[r] = d * a.scale;
+        }
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            const Vec<T, 8> d = round8<T>(s, half);
+#pragma unroll
+            for (int db = 0; db < DB; db++) dq[db] = AttnType<T>::mma(L::cols(lk, 16 * half, db, lane), d, dq[db]);
+        }
+    }
+    if (row >= t.top || (!in && !a.fill)) return;
+    if (!in || ke == kb)
+#pragma unroll
+        for (int db = 0; db < DB; db++) dq[db] = f32x16{};
+    store_row<T, DB>(dq, 1.f, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
+}
+
+// ---- backward: dk, dv ---------------------------------------------------------------------------------------------------
+//
+// Keys as columns, the queries of all heads that share the key head stream by.
+template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_kv(AttnArgs a)
+{
+    typedef AttnTile<T, DP> L;
+    constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lq[BN * L::ROW], lg[BN * L::ROW];
+    __shared__ __attribute__((aligned(16))) float stat[2][BN];
+
+    int kh, slot, split;
+    if (!attn_work(a, a.slots, kh, slot, split)) return;
+    const TileRows t = tile_rows(a.sk, slot, 128);
+    if (t.first >= t.top) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = t.first + 32 * wave + (lane & 31);
+    const bool in = row < t.top && row >= t.begin && row < t.end;
+    int qb = span_begin(a.sq, t.seq), qe = span_end(a.sq, t.seq);
+    qe = max(qe, qb);
+    const int pos0 = row - t.begin - (t.end - t.begin) + (qe - qb); // the row's position among the queries, the first at 0
+    if (t.first >= t.end || t.top <= t.begin) qe = qb;
+
+    const T *const k = (const T *)a.k + kh * a.k_head, *const v = (const T *)a.v + kh * a.v_head;
+    Vec<T, 8> fk[KK], fv[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) {
+        fk[kk] = L::own(k, a.k_row, row, in, kk, a.dim, lane);
+        fv[kk] = L::own(v, a.v_row, row, in, kk, a.dim, lane);
+    }
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
+    const float c2 = MODS ? 1.f : a.scale * LOG2E;
+
+    for (int g = 0; g < a.group; g++) {
+        const int head = kh * a.group + g;
+        const T *const q = (const T *)a.q + head * a.q_head, *const go = (const T *)a.go + head * a.go_head;
+        const float *const lse = a.lse + (int64_t)head * a.sq.rows, *const delta = a.delta + (int64_t)head * a.sq.rows;
+        const float slope = MODS && a.slope ? a.slope[head] : 0.f;
+        typename L::Chunk cq[L::template per<BN, ATTN_THREADS>()], cg[L::template per<BN, ATTN_THREADS>()];
+        float cs = 0.f;
+        const auto load = [&](int i0) {
+            L::template load<BN, ATTN_THREADS>(cq, q, a.q_row, i0, qe, a.dim, tid);
+            L::template load<BN, ATTN_THREADS>(cg, go, a.go_row, i0, qe, a.dim, tid);
+            const int i = i0 + (tid & 31);
+            if (tid < 32) cs = i < qe ? lse[i] * LOG2E : INFINITY; // a missing query: p = 0
+            else if (tid < 64) cs = i < qe ? delta[i] : 0.f;
+        };
+        load(qb);
+        for (int i0 = qb; i0 < qe; i0 += BN) {
+            __syncthreads();
+            L::template store<BN, ATTN_THREADS>(cq, lq, tid);
+            L::template store<BN, ATTN_THREADS>(cg, lg, tid);
+            if (tid < 64) stat[tid >> 5][tid & 31] = cs;
+            __syncthreads();
+            load(i0 + BN);
+            f32x16 s = {}, dp = {}, th;
+#pragma unroll
+            for (int kk = 0; kk < KK; kk++) {
+                s = AttnType<T>::mma(L::rows(lq, 0, kk, lane), fk[kk], s);
+                dp = AttnType<T>::mma(L::rows(lg, 0, kk, lane), fv[kk], dp);
+            }
+            if constexpr (MODS) scores<T>(s, &th, a, slope, (float)(pos0 - (i0 - qb)), h);
+#pragma unroll
+            for (int r4 = 0; r4 < 4; r4++) {
+                const f32x4 l4 = *(const f32x4 *)&stat[0][8 * r4 + 4 * h], d4 = *(const f32x4 *)&stat[1][8 * r4 + 4 * h];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int r = 4 * r4 + e;
+                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -l4[e]));
+                    float d = s[r] * (dp[r] - d4[e]);
+                    if (MODS && a.cap > 0.f) d *= 1.f - th[r] * th[r];
+                    dp[r] = d * a.scale;
+                }
+            }
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                const Vec<T, 8> p = round8<T>(s, half), d = round8<T>(dp, half);
+#pragma unroll
+                for (int db = 0; db < DB; db++) {
+                    dv[db] = AttnType<T>::mma(L::cols(lg, 16 * half, db, lane), p, dv[db]);
+                    dk[db] = AttnType<T>::mma(L::cols(lq, 16 * half, db, lane), d, dk[db]);
+                }
+            }
+        }
+    }
+    if (row >= t.top || (!in && !a.fill)) return;
+    if (!in || qe == qb)
+#pragma unroll
+        for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
+    store_row<T, DB>(dk, 1.f, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
+    store_row<T, DB>(dv, 1.f, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
+}
