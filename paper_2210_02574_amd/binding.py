@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Sequence
 
 import numpy as np
@@ -21,8 +22,6 @@ ERRORS = {
     -1: "HE_EINVAL", -2: "HE_ELEVEL", -3: "HE_ENOKEY", -4: "HE_EWORKSPACE",
     -5: "HE_EHIP", -6: "HE_ENODEV", -7: "HE_ENOMEM", -8: "HE_ESCRATCH",
 }
-
-_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}  # HE_F32, HE_F16, HE_BF16
 
 # every symbol include/he.h declares
 SYMBOLS = [
@@ -56,27 +55,12 @@ class he_kernel_stat(ctypes.Structure):
     ]
 
 
-class he_rows(ctypes.Structure):
-    _fields_ = [("d", ctypes.c_void_p), ("stride", ctypes.c_int64)]
-
-
-class he_heads(ctypes.Structure):
-    _fields_ = [("d", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
-
-
-class he_spans(ctypes.Structure):
-    _fields_ = [("begin", ctypes.c_void_p), ("end", ctypes.c_void_p), ("count", ctypes.c_int32), ("rows", ctypes.c_int64)]
-
-
-class he_norm(ctypes.Structure):
-    _fields_ = [("type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int32),
-                ("eps", ctypes.c_double)]
-
-
-class he_attn(ctypes.Structure):
-    _fields_ = [("type", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
-                ("q", he_spans), ("k", he_spans), ("scale", ctypes.c_double), ("cap", ctypes.c_double), ("slopes", ctypes.c_void_p),
-                ("fill", ctypes.c_int32)]
+# descriptors of the operators on token states, laid out as C does
+_ROWS = struct.Struct("@Pq")               # he_rows: d, stride
+_HEADS = struct.Struct("@Pqq")             # he_heads: d, row, head
+_SPANS = struct.Struct("@PPiq")            # he_spans: d_begin, d_end, count, rows
+_NORM = struct.Struct("@iiqid")            # he_norm: type, weight_type, rows, width, eps
+_ATTN = struct.Struct("@4iPPiqPPiqddPi4x") # he_attn: type, heads, kv_heads, dim, q, k, scale, cap, d_slopes, fill
 
 
 class he_params(ctypes.Structure):
@@ -111,6 +95,7 @@ def load_library() -> ctypes.CDLL:
 
         lib = ctypes.CDLL(LIB_PATH)
         vp, i32, u64, sz, dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_double
+        ds = ctypes.c_char_p
         sig = {
             "he_ctx_create": [ctypes.POINTER(he_params), i32, ctypes.POINTER(vp)],
             "he_ctx_destroy": [vp],
@@ -169,15 +154,16 @@ def load_library() -> ctypes.CDLL:
             "he_hrot_batch_keys": [vp, vp, vp, vp, i32, i32, vp, sz, vp],
             "he_hrot_batch_levels": [vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "he_rotate_sum_batch": [vp, vp, i32, vp, i32, i32, vp, sz, vp],
-            "he_layer_norm": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp],
-            "he_layer_norm_workspace_bytes": [vp, vp, ctypes.POINTER(sz)],
-            "he_layer_norm_grad": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
-            "he_pool": [vp, i32, vp, i32, vp, vp, vp, sz, vp],
-            "he_pool_workspace_bytes": [vp, vp, i32, ctypes.POINTER(sz)],
-            "he_pool_grad": [vp, i32, vp, i32, vp, vp, i32, vp],
-            "he_attention": [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
-            "he_attention_workspace_bytes": [vp, vp, i32, ctypes.POINTER(sz)],
-            "he_attention_grad": [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            # descriptors go as bytes (ds)
+            "he_layer_norm": [vp, ds, ds, ds, vp, vp, ds, ds, vp, vp, vp],
+            "he_layer_norm_workspace_bytes": [vp, ds, ctypes.POINTER(sz)],
+            "he_layer_norm_grad": [vp, ds, ds, ds, vp, vp, vp, ds, ds, vp, vp, vp, sz, vp],
+            "he_pool": [vp, i32, ds, i32, ds, vp, vp, sz, vp],
+            "he_pool_workspace_bytes": [vp, ds, i32, ctypes.POINTER(sz)],
+            "he_pool_grad": [vp, i32, ds, i32, vp, ds, i32, vp],
+            "he_attention": [vp, ds, ds, ds, ds, ds, vp, vp, sz, vp],
+            "he_attention_workspace_bytes": [vp, ds, i32, ctypes.POINTER(sz)],
+            "he_attention_grad": [vp, ds, ds, ds, ds, ds, ds, vp, ds, ds, ds, vp, sz, vp],
             "he_profile_start": [vp],
             "he_profile_stop": [vp, vp, i32, ctypes.POINTER(i32)],
         }
@@ -253,6 +239,7 @@ class HE:
             raise HeError(rc, "he_ctx_create")
         self.ctx = h
         self._ws = None
+        self._type_of = None
 
     @classmethod
     def from_params(cls, params, device: int = -1):
@@ -745,195 +732,226 @@ class HE:
     # Floating-point rows on this context's device.  Sequences: an int32 tensor [count + 1] of offsets (sequence i is the rows
     # offsets[i] .. offsets[i + 1]), or a pair (begin, end) of int32 tensors [count] where rows between them belong to none (a
     # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.
-    def _rows(self, t, what: str, width=None, dtype=None):
-        """[rows][width], dense along the width: he_rows."""
-        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (width is not None and t.shape[1] != width):
-            raise ValueError(f"{what}: want [rows][width] with dense rows" + (f" of {width}" if width is not None else ""))
-        self._placed(t, what, dtype)
-        return he_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    # Calls on short sentences last as long as this code does, so descriptors are packed as bytes (a ctypes structure takes
+    # several times as long to fill) and tensors are asked for each number once.
+    def _types(self):
+        import torch
+
+        self._t32, self._i32 = torch.float32, torch.int32
+        self._type_of = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # HE_F32, HE_F16, HE_BF16
+        self._raw_stream = torch._C._cuda_getCurrentRawStream  # of torch.cuda.current_stream, without an object around it
+        return self._type_of
+
+    def _type(self, dtype) -> int:
+        code = (self._type_of or self._types()).get(dtype)
+        if code is None:
+            raise ValueError(f"{dtype}: rows are float32, float16 or bfloat16")
+        return code
 
     def _placed(self, t, what: str, dtype=None):
-        if t.device.type != "cuda" or t.device.index != self.device:
+        if t.get_device() != self.device or self.device < 0:
             raise ValueError(f"{what}: on {t.device}, the context is on device {self.device}")
         if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{what}: {t.dtype}, want {dtype}")
 
-    @staticmethod
-    def _type(dtype) -> int:
-        name = str(dtype)
-        if name not in _TYPES:
-            raise ValueError(f"{name}: rows are float32, float16 or bfloat16")
-        return _TYPES[name]
+    def _rows(self, t, what: str, shape, dtype=None) -> bytes:
+        """[rows][width], dense along the width: he_rows."""
+        if t.shape != shape or t.dim() != 2:
+            raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][width]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
+        rows, width = shape
+        stride, dense = t.stride()
+        if dense != 1 and width > 1:
+            raise ValueError(f"{what}: want rows that are dense along the width")
+        self._placed(t, what, dtype)
+        return _ROWS.pack(t.data_ptr(), stride if rows > 1 else width)
 
-    def _vector(self, t, what: str, n: int, dtype=None):
+    def _vector(self, t, what: str, n: int, dtype) -> int:
         if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
             raise ValueError(f"{what}: want a dense vector of {n}")
         self._placed(t, what, dtype)
         return t.data_ptr()
 
     def _spans(self, offsets, rows: int, what: str = "offsets"):
-        import torch
-
+        """The fields of he_spans."""
+        if self._type_of is None:
+            self._types()
         if isinstance(offsets, (tuple, list)):
             begin, end = offsets
             if begin.dim() != 1 or end.shape != begin.shape:
                 raise ValueError(f"{what}: begin and end are vectors of one length")
             count = begin.shape[0]
-            return he_spans(self._vector(begin, what, count, torch.int32), self._vector(end, what, count, torch.int32), count, rows)
+            return self._vector(begin, what, count, self._i32), self._vector(end, what, count, self._i32), count, rows
         if offsets.dim() != 1 or offsets.shape[0] < 1:
             raise ValueError(f"{what}: want a vector of count + 1 offsets, or a pair of vectors (begin, end)")
-        p, count = self._vector(offsets, what, offsets.shape[0], torch.int32), offsets.shape[0] - 1
-        return he_spans(p, p + 4, count, rows)
+        n = offsets.shape[0]
+        p = self._vector(offsets, what, n, self._i32)
+        return p, p + 4, n - 1, rows
 
-    def _scratch(self, need: int):
+    def _scratch(self, like, need: int):
         """A workspace of this call's own, from torch's allocator: calls on other streams and captured graphs have theirs."""
-        import torch
-
-        return torch.empty(need, dtype=torch.uint8, device=self._dev) if need else None
-
-    @property
-    def _dev(self):
-        return f"cuda:{self.device}"
+        return like.new_empty((need + 3) // 4, dtype=self._t32) if need else None
 
     def layer_norm(self, x, weight, bias, residual=None, eps: float = 1e-5, out=None):
         """(x - mean) rstd weight + bias over the last dimension of x [rows][width], of s = x + residual with one (rounded to the type).
         Returns (y, s, mean, rstd); s is x itself without a residual.  Keep s, mean and rstd for layer_norm_backward."""
-        import torch
-
-        rows, width = x.shape if x.dim() == 2 else (0, -1)
-        xr = self._rows(x, "x")
-        n = he_norm(self._type(x.dtype), self._type(weight.dtype), rows, width, eps)
-        w, b = self._vector(weight, "weight", width), self._vector(bias, "bias", width, weight.dtype)
+        dtype, shape = x.dtype, x.shape
+        code = self._type(dtype)
+        xr = self._rows(x, "x", shape)
+        rows, width = shape
+        wd = weight.dtype
+        w, b = self._vector(weight, "weight", width, None), self._vector(bias, "bias", width, wd)
         rr = sr = None
         s = x
         if residual is not None:
-            rr = self._rows(residual, "residual", width, x.dtype)
-            if residual.shape != x.shape:
-                raise ValueError("residual: another shape than x")
-            s = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-            sr = self._rows(s, "sum")
-        y = torch.empty((rows, width), dtype=x.dtype, device=x.device) if out is None else out
-        if y.shape != x.shape:
-            raise ValueError("out: another shape than x")
-        yr = self._rows(y, "out", width, x.dtype)
-        stat = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        ref = ctypes.byref
-        self._chk(self.lib.he_layer_norm(self.ctx, ref(n), ref(xr), ref(rr) if rr else None, w, b, ref(yr), ref(sr) if sr else None,
-                                         stat.data_ptr(), stat.data_ptr() + 4 * rows, self._stream()), "he_layer_norm")
-        return y, s, stat[0], stat[1]
+            rr = self._rows(residual, "residual", shape, dtype)
+            s = x.new_empty(shape)
+            sr = _ROWS.pack(s.data_ptr(), width)
+        if out is None:
+            y = x.new_empty(shape)
+            yr = _ROWS.pack(y.data_ptr(), width)
+        else:
+            y, yr = out, self._rows(out, "out", shape, dtype)
+        mean, rstd = x.new_empty((2, rows), dtype=self._t32).unbind(0)
+        rc = self.lib.he_layer_norm(self.ctx, _NORM.pack(code, self._type(wd), rows, width, eps), xr, rr, w, b, yr, sr, mean.data_ptr(), rstd.data_ptr(),
+                                    self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_layer_norm")
+        return y, s, mean, rstd
 
     def layer_norm_backward(self, dy, s, weight, mean, rstd, ds=None):
         """(dx, dweight, dbias) from the gradient of y; ds: a gradient that reaches s from elsewhere, added to dx.  dx is the gradient of x and
         of the residual both."""
-        import torch
-
-        rows, width = s.shape if s.dim() == 2 else (0, -1)
-        sr = self._rows(s, "s")
-        n = he_norm(self._type(s.dtype), self._type(weight.dtype), rows, width, 0.0)
-        if dy.shape != s.shape or (ds is not None and ds.shape != s.shape):
-            raise ValueError("dy, ds: another shape than s")
-        dyr, ar = self._rows(dy, "dy", width, s.dtype), None if ds is None else self._rows(ds, "ds", width, s.dtype)
-        w, m, r = self._vector(weight, "weight", width), self._vector(mean, "mean", rows, torch.float32), self._vector(rstd, "rstd", rows, torch.float32)
-        dx = torch.empty((rows, width), dtype=s.dtype, device=s.device)
-        dw = torch.empty((2, width), dtype=weight.dtype, device=s.device)
-        need, ref = ctypes.c_size_t(), ctypes.byref
-        self._chk(self.lib.he_layer_norm_workspace_bytes(self.ctx, ref(n), ref(need)), "he_layer_norm_workspace_bytes")
-        ws = self._scratch(need.value)
-        dxr = self._rows(dx, "dx")
-        self._chk(self.lib.he_layer_norm_grad(self.ctx, ref(n), ref(dyr), ref(sr), w, m, r, ref(ar) if ar else None, ref(dxr),
-                                              dw.data_ptr(), dw.data_ptr() + width * dw.element_size(), ws.data_ptr() if ws is not None else None,
-                                              need.value, self._stream()), "he_layer_norm_grad")
-        return dx, dw[0], dw[1]
+        dtype, shape = s.dtype, s.shape
+        code = self._type(dtype)
+        sr = self._rows(s, "s", shape)
+        rows, width = shape
+        dyr, ar = self._rows(dy, "dy", shape, dtype), None if ds is None else self._rows(ds, "ds", shape, dtype)
+        w, m, r = self._vector(weight, "weight", width, None), self._vector(mean, "mean", rows, self._t32), self._vector(rstd, "rstd", rows, self._t32)
+        n = _NORM.pack(code, self._type(weight.dtype), rows, width, 0.0)
+        need = ctypes.c_size_t()
+        rc = self.lib.he_layer_norm_workspace_bytes(self.ctx, n, need)
+        if rc:
+            self._chk(rc, "he_layer_norm_workspace_bytes")
+        dx = s.new_empty(shape)
+        dw, db = weight.new_empty((2, width)).unbind(0)
+        ws = self._scratch(s, need.value)
+        rc = self.lib.he_layer_norm_grad(self.ctx, n, dyr, sr, w, m, r, ar, _ROWS.pack(dx.data_ptr(), width), dw.data_ptr(), db.data_ptr(),
+                                         ws.data_ptr() if ws is not None else None, need.value, self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_layer_norm_grad")
+        return dx, dw, db
 
     def pool_mean(self, x, offsets, out=None):
         """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence."""
-        import torch
-
-        xr = self._rows(x, "x")
-        rows, width = x.shape
-        sp, ref, need = self._spans(offsets, rows), ctypes.byref, ctypes.c_size_t()
-        self._chk(self.lib.he_pool_workspace_bytes(self.ctx, ref(sp), width, ref(need)), "he_pool_workspace_bytes")
-        e = torch.empty((sp.count, width), dtype=torch.float32, device=x.device) if out is None else out
-        if tuple(e.shape) != (sp.count, width) or not e.is_contiguous():
-            raise ValueError(f"out: want a dense [{sp.count}][{width}]")
-        self._placed(e, "out", torch.float32)
-        ws = self._scratch(need.value)
-        self._chk(self.lib.he_pool(self.ctx, self._type(x.dtype), ref(sp), width, ref(xr), e.data_ptr(), ws.data_ptr() if ws is not None else None,
-                                   need.value, self._stream()), "he_pool")
+        code, shape = self._type(x.dtype), x.shape
+        xr = self._rows(x, "x", shape)
+        rows, width = shape
+        span = self._spans(offsets, rows)
+        count, sp = span[2], _SPANS.pack(*span)
+        need = ctypes.c_size_t()
+        rc = self.lib.he_pool_workspace_bytes(self.ctx, sp, width, need)
+        if rc:
+            self._chk(rc, "he_pool_workspace_bytes")
+        if out is None:
+            e = x.new_empty((count, width), dtype=self._t32)
+        else:
+            e = out
+            if e.shape != (count, width) or not e.is_contiguous():
+                raise ValueError(f"out: want a dense [{count}][{width}]")
+            self._placed(e, "out", self._t32)
+        ws = self._scratch(x, need.value)
+        rc = self.lib.he_pool(self.ctx, code, sp, width, xr, e.data_ptr(), ws.data_ptr() if ws is not None else None, need.value,
+                              self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_pool")
         return e
 
     def pool_mean_backward(self, de, offsets, rows: int, dtype, out=None):
         """Gradient of pool_mean's x [rows][width], of type dtype, from de [count][width]."""
-        import torch
-
-        width = de.shape[1] if de.dim() == 2 else -1
-        sp = self._spans(offsets, rows)
-        if tuple(de.shape) != (sp.count, width) or not de.is_contiguous():
-            raise ValueError(f"de: want a dense [{sp.count}][width]")
-        self._placed(de, "de", torch.float32)
-        make = torch.empty if sp.count else torch.zeros
-        dx = make((rows, width), dtype=dtype, device=de.device) if out is None else out
-        if tuple(dx.shape) != (rows, width):
-            raise ValueError(f"out: want [{rows}][{width}]")
-        xr = self._rows(dx, "out", width, dtype)
-        self._chk(self.lib.he_pool_grad(self.ctx, self._type(dtype), ctypes.byref(sp), width, de.data_ptr(), ctypes.byref(xr), out is None,
-                                        self._stream()), "he_pool_grad")
+        code, span = self._type(dtype), self._spans(offsets, rows)
+        count = span[2]
+        if de.dim() != 2 or de.shape[0] != count or not de.is_contiguous():
+            raise ValueError(f"de: want a dense [{count}][width]")
+        width = de.shape[1]
+        self._placed(de, "de", self._t32)
+        if out is None:
+            dx = de.new_empty((rows, width), dtype=dtype) if count else de.new_zeros((rows, width), dtype=dtype)
+            xr = _ROWS.pack(dx.data_ptr(), width)
+        else:
+            dx = out
+            if tuple(dx.shape) != (rows, width):
+                raise ValueError(f"out: want [{rows}][{width}]")
+            xr = self._rows(dx, "out", dx.shape, dtype)
+        rc = self.lib.he_pool_grad(self.ctx, code, _SPANS.pack(*span), width, de.data_ptr(), xr, out is None, self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_pool_grad")
         return dx
 
-    def _heads(self, t, what: str, shape=None, dtype=None):
+    def _heads(self, t, what: str, shape, dtype=None) -> bytes:
         """[rows][heads][dim] with a dense last dimension: he_heads."""
-        if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-            raise ValueError(f"{what}: want [rows][heads][dim]" + (f" = {tuple(shape)}" if shape is not None else ""))
-        if t.shape[2] > 1 and t.stride(2) != 1:
+        if t.shape != shape or t.dim() != 3:
+            raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][heads][dim]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
+        row, head, dense = t.stride()
+        p = t.data_ptr()
+        if dense != 1 and shape[2] > 1:
             raise ValueError(f"{what}: the last dimension is not dense")
         self._placed(t, what, dtype)
-        bad = [n for n, a, b in (("address", t.data_ptr(), 1), ("row stride", t.stride(0), t.element_size()), ("head stride", t.stride(1), t.element_size()))
-               if a * b % 16 and t.numel()]
-        if bad:
-            raise ValueError(f"{what}: {', '.join(bad)} not a multiple of 16 bytes")
-        return he_heads(t.data_ptr(), t.stride(0), t.stride(1))
+        if (p | (row | head) * t.element_size()) & 15 and t.numel():
+            raise ValueError(f"{what}: address {p:#x} or strides {t.stride()} not in multiples of 16 bytes")
+        return _HEADS.pack(p, row, head)
 
     def _attn(self, q, k, v, offsets, offsets_k, scale, cap, slopes, fill):
-        import torch
-
-        qh = self._heads(q, "q")
-        (rows, heads, dim), (rows_k, kv, _) = q.shape, k.shape if k.dim() == 3 else (0, 0, 0)
-        kh, vh = self._heads(k, "k", (rows_k, kv, dim), q.dtype), self._heads(v, "v", (rows_k, kv, dim), q.dtype)
+        """(he_attn, count of sequences, he_heads of q, k, v)"""
+        dtype, shape = q.dtype, q.shape
+        code, qh = self._type(dtype), self._heads(q, "q", shape)
+        rows, heads, dim = shape
+        kshape = k.shape
+        if len(kshape) != 3 or kshape[2] != dim:
+            raise ValueError(f"k: {tuple(kshape)}, want [rows][heads][{dim}]")
+        rows_k, kv, _ = kshape
+        kh, vh = self._heads(k, "k", kshape, dtype), self._heads(v, "v", kshape, dtype)
         if kv == 0 or heads % kv:
             raise ValueError(f"{heads} query heads on {kv} key heads")
-        sq = self._spans(offsets, rows)
-        if offsets_k is None and rows_k != rows:
+        sq = sk = self._spans(offsets, rows)
+        if offsets_k is not None and (offsets_k is not offsets or rows_k != rows):
+            sk = self._spans(offsets_k, rows_k, "offsets_k")
+            if sk[2] != sq[2]:
+                raise ValueError("offsets and offsets_k: another number of sequences")
+        elif rows_k != rows:
             raise ValueError("keys of another length than the queries need offsets_k")
-        sk = sq if offsets_k is None else self._spans(offsets_k, rows_k, "offsets_k")
-        if sk.count != sq.count:
-            raise ValueError("offsets and offsets_k: another number of sequences")
-        sl = None if slopes is None else self._vector(slopes, "slopes", heads, torch.float32)
-        s = he_attn(self._type(q.dtype), heads, kv, dim, sq, sk, 1.0 / dim**0.5 if scale is None else scale, cap, sl, fill)
-        return s, qh, kh, vh
+        sl = 0 if slopes is None else self._vector(slopes, "slopes", heads, self._t32)
+        return _ATTN.pack(code, heads, kv, dim, *sq, *sk, dim**-0.5 if scale is None else scale, cap, sl, fill), sq[2], qh, kh, vh
 
-    def _attn_scratch(self, s, backward: bool):
+    def _attn_scratch(self, s, like, backward: bool):
         need = ctypes.c_size_t()
-        self._chk(self.lib.he_attention_workspace_bytes(self.ctx, ctypes.byref(s), backward, ctypes.byref(need)), "he_attention_workspace_bytes")
-        ws = self._scratch(need.value)
-        return ws, (ws.data_ptr() if ws is not None else None), need.value
+        rc = self.lib.he_attention_workspace_bytes(self.ctx, s, backward, need)
+        if rc:
+            self._chk(rc, "he_attention_workspace_bytes")
+        n = need.value
+        if not n:
+            return None, None, 0
+        ws = self._scratch(like, n)
+        return ws, ws.data_ptr(), n
 
     def attention(self, q, k, v, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None):
         """Attention inside each sequence: q [rows][heads][dim], k and v [rows_k][kv_heads][dim] (strided views of a joint projection are fine;
         query head h reads key head h // (heads / kv_heads)).  offsets_k: the sequences of the keys, where they are not the queries'.
         scale: of the products, 1 / sqrt(dim) by default; cap > 0: cap tanh(score / cap); slopes [heads] float32: minus slope times distance.
         Returns (o, lse): o like q, lse [heads][rows] float32."""
-        import torch
-
-        s, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None)
-        make = torch.empty if s.q.count else torch.zeros
-        o = make(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        oh = self._heads(o, "out", q.shape, q.dtype)
-        lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
-        if out is not None or not s.q.count:
+        s, count, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None)
+        shape = q.shape
+        lse = q.new_empty((shape[1], shape[0]), dtype=self._t32)
+        if out is None:
+            o = q.new_empty(shape) if count else q.new_zeros(shape)
+            oh = _HEADS.pack(o.data_ptr(), shape[1] * shape[2], shape[2])
+        else:
+            o, oh = out, self._heads(out, "out", shape, q.dtype)
+        if out is not None or not count:
             lse.fill_(float("-inf"))
-        ws, p, n = self._attn_scratch(s, False)
-        ref = ctypes.byref
-        self._chk(self.lib.he_attention(self.ctx, ref(s), ref(qh), ref(kh), ref(vh), ref(oh), lse.data_ptr(), p, n, self._stream()), "he_attention")
+        ws, p, n = self._attn_scratch(s, q, False)
+        rc = self.lib.he_attention(self.ctx, s, qh, kh, vh, oh, lse.data_ptr(), p, n, self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_attention")
         return o, lse
 
     def attention_backward(self, do, q, k, v, o, lse, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None,
@@ -941,20 +959,23 @@ class HE:
         """(dq, dk, dv) from the gradient of o, with o and lse of the forward call and its other arguments.  out: three tensors (strided views are
         fine) to write them to; fill: whether their rows of no sequence become zeros (by default where they are made here).  Slopes are constants:
         they have no gradient."""
-        import torch
-
-        s, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None if fill is None else fill)
-        gh, oh = self._heads(do, "do", q.shape, q.dtype), self._heads(o, "o", q.shape, q.dtype)
-        if tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+        s, count, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None if fill is None else bool(fill))
+        dtype, shape = q.dtype, q.shape
+        gh, oh = self._heads(do, "do", shape, dtype), self._heads(o, "o", shape, dtype)
+        if lse.shape != (shape[1], shape[0]) or not lse.is_contiguous():
             raise ValueError("lse: want a dense [heads][rows]")
-        self._placed(lse, "lse", torch.float32)
-        make = torch.empty if s.q.count else torch.zeros
-        dq, dk, dv = [make(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)] if out is None else out
-        grads = self._heads(dq, "dq", q.shape, q.dtype), self._heads(dk, "dk", k.shape, q.dtype), self._heads(dv, "dv", k.shape, q.dtype)
-        ws, p, n = self._attn_scratch(s, True)
-        ref = ctypes.byref
-        self._chk(self.lib.he_attention_grad(self.ctx, ref(s), ref(gh), ref(qh), ref(kh), ref(vh), ref(oh), lse.data_ptr(), *[ref(g) for g in grads],
-                                             p, n, self._stream()), "he_attention_grad")
+        self._placed(lse, "lse", self._t32)
+        if out is None:
+            dq, dk, dv = [q.new_empty(t.shape) if count else q.new_zeros(t.shape) for t in (q, k, v)]
+            kv = k.shape[1] * shape[2]
+            gq, gk, gv = (_HEADS.pack(t.data_ptr(), n, shape[2]) for t, n in ((dq, shape[1] * shape[2]), (dk, kv), (dv, kv)))
+        else:
+            dq, dk, dv = out
+            gq, gk, gv = self._heads(dq, "dq", shape, dtype), self._heads(dk, "dk", k.shape, dtype), self._heads(dv, "dv", k.shape, dtype)
+        ws, p, n = self._attn_scratch(s, q, True)
+        rc = self.lib.he_attention_grad(self.ctx, s, gh, qh, kh, vh, oh, lse.data_ptr(), gq, gk, gv, p, n, self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, "he_attention_grad")
         return dq, dk, dv
 
     # ---- measurement -------------------------------------------------------------------------------------------------

@@ -10,40 +10,42 @@ typedef f16 T;
 typedef bf16 T;
 #endif
 
-template <int NWQ> static void fwd(he_ctx *c, hipStream_t st, double bytes, bool mods, unsigned grid, const AttnArgs &a)
+// F with the variant of cap and distance bias
+template <class F> static void by_mode(const AttnArgs &a, F f)
 {
-    if (mods)
-        KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, NWQ, true>), grid, ATTN_THREADS, a);
+    const int mode = (a.cap > 0.f ? MODE_CAP : 0) | (a.slope ? MODE_SLOPE : 0);
+    if (mode == 0)
+        f(std::integral_constant<int, 0>{});
+    else if (mode == MODE_CAP)
+        f(std::integral_constant<int, MODE_CAP>{});
+    else if (mode == MODE_SLOPE)
+        f(std::integral_constant<int, MODE_SLOPE>{});
     else
-        KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, NWQ, false>), grid, ATTN_THREADS, a);
+        f(std::integral_constant<int, MODE_CAP | MODE_SLOPE>{});
 }
 
-static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int nwq, bool mods, unsigned grid, const AttnArgs &a)
+static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int nwq, unsigned grid, const AttnArgs &a)
 {
-    if (nwq == 1)
-        fwd<1>(c, st, bytes, mods, grid, a);
-    else if (nwq == 2)
-        fwd<2>(c, st, bytes, mods, grid, a);
-    else
-        fwd<4>(c, st, bytes, mods, grid, a);
+    by_mode(a, [&](auto mode) {
+        if (nwq == 1)
+            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 1, mode>), grid, ATTN_THREADS, a);
+        else if (nwq == 2)
+            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
+        else
+            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 4, mode>), grid, ATTN_THREADS, a);
+    });
 }
 static void attn_join(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
 {
     KLAUNCH(c, st, KID_ATTN_JOIN, bytes, (k_attn_join<T>), grid, a);
 }
-static void attn_grad_q(he_ctx *c, hipStream_t st, double bytes, bool mods, unsigned grid, const AttnArgs &a)
+static void attn_grad_q(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
 {
-    if (mods)
-        KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, true>), grid, ATTN_THREADS, a);
-    else
-        KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, false>), grid, ATTN_THREADS, a);
+    by_mode(a, [&](auto mode) { KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, mode>), grid, ATTN_THREADS, a); });
 }
-static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, bool mods, unsigned grid, const AttnArgs &a)
+static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
 {
-    if (mods)
-        KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, true>), grid, ATTN_THREADS, a);
-    else
-        KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, false>), grid, ATTN_THREADS, a);
+    by_mode(a, [&](auto mode) { KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, mode>), grid, ATTN_THREADS, a); });
 }
 
 #define NAME_(t, d) attn_launch_##t##_##d

@@ -332,7 +332,7 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
     if (dg.rc != HE_OK) return dg.rc;
     const AttnLaunch &l = attn_launch(s->type, s->dim);
     const double size = (double)type_size(s->type) * s->dim, kv = 2.0 * s->k.rows * s->kv_heads * size;
-    l.fwd(ctx, (hipStream_t)stream, rows * (2 * size + 4) + kv, p.nwq, s->cap > 0.0 || s->d_slopes, grid, a);
+    l.fwd(ctx, (hipStream_t)stream, rows * (2 * size + 4) + kv, p.nwq, grid, a);
     if (p.splits > 1)
         l.join(ctx, (hipStream_t)stream, rows * (size + 4 + 4.0 * p.splits * (s->dim + 1)), (unsigned)((rows + 3) / 4), a);
     return launched(ctx);
@@ -374,9 +374,8 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
     const AttnLaunch &l = attn_launch(s->type, s->dim);
-    const bool mods = s->cap > 0.0 || s->d_slopes;
     const double size = (double)type_size(s->type) * s->dim, qb = s->q.rows * s->heads * size, kb = s->k.rows * s->kv_heads * size;
-    if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, mods, grid_q, a);
-    if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, mods, grid_kv, b);
+    if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, grid_q, a);
+    if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, grid_kv, b);
     return launched(ctx);
 }

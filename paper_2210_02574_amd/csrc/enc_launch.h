@@ -10,11 +10,11 @@ struct PoolArgs;
 struct PoolGradArgs;
 
 struct AttnLaunch {
-    // nwq: waves along the queries, 1, 2 or 4 (tiles of 32 nwq queries); mods: a cap or a distance bias
-    void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int nwq, bool mods, unsigned grid, const AttnArgs &a);
+    // nwq: waves along the queries, 1, 2 or 4 (tiles of 32 nwq queries)
+    void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int nwq, unsigned grid, const AttnArgs &a);
     void (*join)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
-    void (*grad_q)(he_ctx *c, hipStream_t st, double bytes, bool mods, unsigned grid, const AttnArgs &a);
-    void (*grad_kv)(he_ctx *c, hipStream_t st, double bytes, bool mods, unsigned grid, const AttnArgs &a);
+    void (*grad_q)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
+    void (*grad_kv)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
 };
 #define HE_DECL_ATTN(t)                                                                                              \
     void attn_launch_##t##_32(AttnLaunch &t_);                                                                       \

@@ -13,7 +13,7 @@
 // The operand A of that product is a transposed tile: 16-bit types read it from LDS with the transposing read, 32-bit ones word by word.
 //
 // Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
-// everything else, sums and statistics included, is in 32 bits.  fp16 holds dt down to 6e-8: gradients as small as that need a
+// everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  fp16 holds it down to 6e-8: gradients as small as that need a
 // scaled loss, as everywhere in fp16.
 #pragma once
 #include "enc_common.h"
@@ -66,13 +66,6 @@ __device__ __forceinline__ float pair_sum(float v)
 {
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
-}
-
-// tanh by the exponential where values have 16 bits (absolute error 2^-23), the library's for 32.
-template <class T> __device__ __forceinline__ float tanh_of(float x)
-{
-    if constexpr (sizeof(T) == 4) return tanhf(x);
-    return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * LOG2E)));
 }
 
 // Tiles in LDS: rows of DP elements and 16 bytes more, which spreads the 16-byte reads of eight rows over all banks.
@@ -191,27 +184,54 @@ __device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, 
     return true;
 }
 
-// Scores of one 32 x 32 block from the products: x = log2(e) s.  pos: position of the lane's own row minus the one of row 0 of the block, so that the
-// distance of row m is |pos - m| (symmetric: it serves keys as columns too).
-template <class T> __device__ __forceinline__ void scores(f32x16 &c, f32x16 *th, const AttnArgs &a, float slope, float pos, int h)
-{
-#pragma unroll
-    for (int r = 0; r < 16; r++) {
-        float x = c[r] * a.scale;
-        if (a.cap > 0.f) {
-            const float t = tanh_of<T>(x / a.cap);
-            if (th) (*th)[r] = t;
-            x = a.cap * t;
+// Scores of 32 x 32 blocks, x = log2(e) s, from products c = q . k.  MODE: MODE_CAP, MODE_SLOPE, both or neither.  16-bit types take tanh(y) =
+// 1 - 2 / (1 + e^2y) by the hardware's exponential and reciprocal (off by 2^-22 at most, absolutely: cap times that in a score), 32 bits the library's.
+enum { MODE_CAP = 1, MODE_SLOPE = 2 };
+template <class T, int MODE> struct Scores {
+    float in, out, slope; // of c before tanh, of tanh (or of c), of the distance
+
+    __device__ __forceinline__ Scores(const AttnArgs &a, int head)
+    {
+        out = a.scale * LOG2E;
+        if (MODE & MODE_CAP) {
+            out = a.cap * LOG2E;
+            in = sizeof(T) == 4 ? a.scale / a.cap : a.scale / a.cap * (2.f * LOG2E);
         }
-        x -= slope * fabsf(pos - (float)(8 * (r >> 2) + 4 * h + (r & 3)));
-        c[r] = x * LOG2E;
+        if (MODE & MODE_SLOPE) slope = a.slope[head] * LOG2E;
     }
-}
+    // what is left to multiply scores with: without a cap or a bias the exponential's fma does it
+    __device__ __forceinline__ float rest() const { return MODE ? 1.f : out; }
+    // pos: position of the lane's own row minus the one of row 0 of the block: the distance of row m is |pos - m|.  th: the tanh, for the backward pass
+    __device__ __forceinline__ void operator()(f32x16 &c, float pos, int h, f32x16 *th = nullptr) const
+    {
+        if constexpr (MODE != 0) {
+            const float p = pos - (float)(4 * h);
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                float x;
+                if constexpr (MODE & MODE_CAP) {
+                    if constexpr (sizeof(T) == 4) {
+                        x = tanhf(c[r] * in);
+                        if (th) (*th)[r] = x;
+                        x *= out;
+                    } else {
+                        const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c[r] * in));
+                        if (th) (*th)[r] = fmaf(-2.f, g, 1.f);
+                        x = fmaf(-2.f * out, g, out);
+                    }
+                } else
+                    x = c[r] * out;
+                if constexpr (MODE & MODE_SLOPE) x = fmaf(-slope, fabsf(p - (float)(8 * (r >> 2) + (r & 3))), x);
+                c[r] = x;
+            }
+        }
+    }
+};
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
 //
 // Four waves: NWQ of them along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: few queries then still
-// keep four waves busy.  KB blocks of 32 keys per wave and step.  MODS: there is a cap or a distance bias.
+// keep four waves busy.  KB blocks of 32 keys per wave and step.
 template <class T, int DP, int NWQ> struct AttnFwd {
     static constexpr int NWK = 4 / NWQ, KB = NWK > 1 || sizeof(T) == 4 ? 1 : 2, BM = 32 * NWQ, BN = 32 * KB * NWK;
     static constexpr int TILE = BN * AttnTile<T, DP>::ROW;                    // elements of a tile
@@ -219,7 +239,7 @@ template <class T, int DP, int NWQ> struct AttnFwd {
     static constexpr int LDS = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
 };
 
-template <class T, int DP, int NWQ, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
+template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
 {
     typedef AttnFwd<T, DP, NWQ> F;
     typedef AttnTile<T, DP> L;
@@ -249,8 +269,8 @@ template <class T, int DP, int NWQ, bool MODS> __global__ __launch_bounds__(ATTN
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) fq[kk] = L::own(q, a.q_row, row, in, kk, a.dim, lane);
 
-    const float slope = MODS && a.slope ? a.slope[head] : 0.f;
-    const float c2 = MODS ? 1.f : a.scale * LOG2E; // scores are kept times this below
+    const Scores<T, MODE> scores(a, head);
+    const float c2 = scores.rest();
     float top = -INFINITY, sum = 0.f;              // running maximum (in units of log2) and the lane's own sum
     f32x16 o[DB];
 #pragma unroll
@@ -275,9 +295,8 @@ template <class T, int DP, int NWQ, bool MODS> __global__ __launch_bounds__(ATTN
 #pragma unroll
             for (int kk = 0; kk < KK; kk++) s[b] = AttnType<T>::mma(L::rows(lk, w0 + 32 * b, kk, lane), fq[kk], s[b]);
         }
-        if constexpr (MODS)
 #pragma unroll
-            for (int b = 0; b < KB; b++) scores<T>(s[b], nullptr, a, slope, (float)(pos0 - (j0 + w0 + 32 * b - kb)), h);
+        for (int b = 0; b < KB; b++) scores(s[b], (float)(pos0 - (j0 + w0 + 32 * b - kb)), h);
         if (j0 + w0 + 32 * KB > hi)
 #pragma unroll
             for (int b = 0; b < KB; b++)
@@ -404,7 +423,7 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
 // ---- backward: dq -----------------------------------------------------------------------------------------------------
 //
 // Queries as columns, keys stream by.  Also leaves delta for the kernel of dk and dv, which runs after it.
-template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_q(AttnArgs a)
+template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_q(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
     constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
@@ -439,7 +458,8 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
     const int64_t at = (int64_t)head * a.sq.rows + row;
     if (in && h == 0) a.delta[at] = delta;
     const float lse = in ? a.lse[at] * LOG2E : INFINITY; // rows of no sequence: p = 0
-    const float slope = MODS && a.slope ? a.slope[head] : 0.f, c2 = MODS ? 1.f : a.scale * LOG2E;
+    const Scores<T, MODE> scores(a, head);
+    const float c2 = scores.rest();
     f32x16 dq[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dq[db] = f32x16{};
@@ -460,14 +480,14 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
             s = AttnType<T>::mma(L::rows(lk, 0, kk, lane), fq[kk], s);
             dp = AttnType<T>::mma(L::rows(lv, 0, kk, lane), fg[kk], dp);
         }
-        if constexpr (MODS) scores<T>(s, &th, a, slope, (float)(pos0 - (j0 - kb)), h);
+        scores(s, (float)(pos0 - (j0 - kb)), h, &th);
 #pragma unroll
         for (int r = 0; r < 16; r++) {
             float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -lse));
             if (j0 + BN > ke && j0 + 8 * (r >> 2) + 4 * h + (r & 3) >= ke) p = 0.f; // exp of a missing key's score may be anything
             float d = p * (dp[r] - delta);
-            if (MODS && a.cap > 0.f) d *= 1.f - th[r] * th[r];
-            s[r] = d * a.scale;
+            if (MODE & MODE_CAP) d *= 1.f - th[r] * th[r];
+            s[r] = d; // the scale is put on at the end
         }
 #pragma unroll
         for (int half = 0; half < 2; half++) {
@@ -480,13 +500,13 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
     if (!in || ke == kb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dq[db] = f32x16{};
-    store_row<T, DB>(dq, 1.f, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
+    store_row<T, DB>(dq, a.scale, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
 }
 
 // ---- backward: dk, dv ---------------------------------------------------------------------------------------------------
 //
 // Keys as columns, the queries of all heads that share the key head stream by.
-template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_kv(AttnArgs a)
+template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_kv(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
     constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
@@ -515,13 +535,13 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
-    const float c2 = MODS ? 1.f : a.scale * LOG2E;
 
     for (int g = 0; g < a.group; g++) {
         const int head = kh * a.group + g;
         const T *const q = (const T *)a.q + head * a.q_head, *const go = (const T *)a.go + head * a.go_head;
         const float *const lse = a.lse + (int64_t)head * a.sq.rows, *const delta = a.delta + (int64_t)head * a.sq.rows;
-        const float slope = MODS && a.slope ? a.slope[head] : 0.f;
+        const Scores<T, MODE> scores(a, head);
+        const float c2 = scores.rest();
         typename L::Chunk cq[L::template per<BN, ATTN_THREADS>()], cg[L::template per<BN, ATTN_THREADS>()];
         float cs = 0.f;
         const auto load = [&](int i0) {
@@ -545,7 +565,7 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
                 s = AttnType<T>::mma(L::rows(lq, 0, kk, lane), fk[kk], s);
                 dp = AttnType<T>::mma(L::rows(lg, 0, kk, lane), fv[kk], dp);
             }
-            if constexpr (MODS) scores<T>(s, &th, a, slope, (float)(pos0 - (i0 - qb)), h);
+            scores(s, (float)(pos0 - (i0 - qb)), h, &th);
 #pragma unroll
             for (int r4 = 0; r4 < 4; r4++) {
                 const f32x4 l4 = *(const f32x4 *)&stat[0][8 * r4 + 4 * h], d4 = *(const f32x4 *)&stat[1][8 * r4 + 4 * h];
@@ -554,8 +574,8 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
                     const int r = 4 * r4 + e;
                     s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -l4[e]));
                     float d = s[r] * (dp[r] - d4[e]);
-                    if (MODS && a.cap > 0.f) d *= 1.f - th[r] * th[r];
-                    dp[r] = d * a.scale;
+                    if (MODE & MODE_CAP) d *= 1.f - th[r] * th[r];
+                    dp[r] = d;
                 }
             }
 #pragma unroll
@@ -573,6 +593,6 @@ template <class T, int DP, bool MODS> __global__ __launch_bounds__(ATTN_THREADS)
     if (!in || qe == qb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
-    store_row<T, DB>(dk, 1.f, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
+    store_row<T, DB>(dk, a.scale, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
     store_row<T, DB>(dv, 1.f, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
 }

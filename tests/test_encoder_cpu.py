@@ -21,39 +21,45 @@ def he():
     return pkg.HE.from_params(wl.C1B)
 
 
+class _C:
+    """Descriptors as bytes."""
+
+    he_rows, he_heads, he_spans, he_norm = bd._ROWS.pack, bd._HEADS.pack, bd._SPANS.pack, bd._NORM.pack
+
+
 def _ref(x):
-    return None if x is None else ctypes.byref(x)
+    return ctypes.byref(x) if isinstance(x, ctypes.c_size_t) else x
 
 
 def _norm(he, n=None, x=(P, 64), residual=None, w=P, b=P, y=(P, 64), sum_=None, mean=P, rstd=P):
-    r = [None if t is None else bd.he_rows(*t) for t in (x, residual, y, sum_)]
-    n = n or bd.he_norm(2, 0, 5, 64, 1e-5)
+    r = [None if t is None else _C.he_rows(*t) for t in (x, residual, y, sum_)]
+    n = n or _C.he_norm(2, 0, 5, 64, 1e-5)
     return he.lib.he_layer_norm(he.ctx, _ref(n), _ref(r[0]), _ref(r[1]), w, b, _ref(r[2]), _ref(r[3]), mean, rstd, None)
 
 
 def test_layer_norm_refusals(he):
     assert _norm(he) == ENODEV  # nothing wrong but the device
-    for bad in (bd.he_norm(3, 0, 5, 64, 1e-5), bd.he_norm(-1, 0, 5, 64, 1e-5), bd.he_norm(2, 1, 5, 64, 1e-5), bd.he_norm(0, 2, 5, 64, 1e-5),
-                bd.he_norm(2, 0, -1, 64, 1e-5), bd.he_norm(2, 0, 1 << 31, 64, 1e-5), bd.he_norm(2, 0, 5, 0, 1e-5),
-                bd.he_norm(2, 0, 5, 16385, 1e-5), bd.he_norm(2, 0, 5, 64, -1.0), bd.he_norm(2, 0, 5, 64, float("nan")),
-                bd.he_norm(2, 0, 5, 64, float("inf")), bd.he_norm(2, 0, 5, 64, 1e300)):
+    for bad in (_C.he_norm(3, 0, 5, 64, 1e-5), _C.he_norm(-1, 0, 5, 64, 1e-5), _C.he_norm(2, 1, 5, 64, 1e-5), _C.he_norm(0, 2, 5, 64, 1e-5),
+                _C.he_norm(2, 0, -1, 64, 1e-5), _C.he_norm(2, 0, 1 << 31, 64, 1e-5), _C.he_norm(2, 0, 5, 0, 1e-5),
+                _C.he_norm(2, 0, 5, 16385, 1e-5), _C.he_norm(2, 0, 5, 64, -1.0), _C.he_norm(2, 0, 5, 64, float("nan")),
+                _C.he_norm(2, 0, 5, 64, float("inf")), _C.he_norm(2, 0, 5, 64, 1e300)):
         assert _norm(he, bad) == EINVAL
     for kw in ({"x": None}, {"x": (0, 64)}, {"x": (P, 63)}, {"y": None}, {"y": (P, 63)}, {"w": None}, {"b": None}, {"mean": None},
                {"rstd": None}, {"residual": (P, 64)}, {"residual": (P, 63), "sum_": (P, 64)}, {"residual": (P, 64), "sum_": (P, 63)}):
         assert _norm(he, **kw) == EINVAL, kw
     assert he.lib.he_layer_norm(None, *[None] * 10) == EINVAL
-    assert _norm(he, bd.he_norm(2, 0, 0, 64, 1e-5), x=None, y=None) == ENODEV  # no rows: buffers are not looked at
+    assert _norm(he, _C.he_norm(2, 0, 0, 64, 1e-5), x=None, y=None) == ENODEV  # no rows: buffers are not looked at
 
 
 def test_layer_norm_grad_refusals(he):
     need = ctypes.c_size_t()
-    n = bd.he_norm(2, 0, 5, 64, 0.0)
+    n = _C.he_norm(2, 0, 5, 64, 0.0)
     assert he.lib.he_layer_norm_workspace_bytes(he.ctx, _ref(n), _ref(need)) == 0 and need.value >= 2 * 64 * 4
-    assert he.lib.he_layer_norm_workspace_bytes(he.ctx, _ref(bd.he_norm(2, 0, 5, 0, 0.0)), _ref(need)) == EINVAL
+    assert he.lib.he_layer_norm_workspace_bytes(he.ctx, _ref(_C.he_norm(2, 0, 5, 0, 0.0)), _ref(need)) == EINVAL
     assert he.lib.he_layer_norm_workspace_bytes(he.ctx, _ref(n), None) == EINVAL
 
     def call(dy=(P, 64), s=(P, 64), w=P, mean=P, rstd=P, add=None, ds=(P, 64), dw=P, db=P, ws=P, size=1 << 20, n=n):
-        r = [None if t is None else bd.he_rows(*t) for t in (dy, s, add, ds)]
+        r = [None if t is None else _C.he_rows(*t) for t in (dy, s, add, ds)]
         return he.lib.he_layer_norm_grad(he.ctx, _ref(n), _ref(r[0]), _ref(r[1]), w, mean, rstd, _ref(r[2]), _ref(r[3]), dw, db, ws, size, None)
 
     assert call() == ENODEV
@@ -63,15 +69,19 @@ def test_layer_norm_grad_refusals(he):
     assert call(ws=None) == EWORKSPACE and call(size=need.value - 1) == EWORKSPACE
 
 
-def _spans(count=3, rows=40, begin=P, end=P):
-    return bd.he_spans(begin, end, count, rows)
+def _span(count=3, rows=40, begin=P, end=P):
+    return begin or 0, end or 0, count, rows
+
+
+def _spans(*args, **kw):
+    return _C.he_spans(*_span(*args, **kw))
 
 
 def test_pool_refusals(he):
     need = ctypes.c_size_t()
     long = _spans(1, 100000)
     assert he.lib.he_pool_workspace_bytes(he.ctx, _ref(long), 64, _ref(need)) == 0 and need.value >= 2 * 64 * 4
-    x = bd.he_rows(P, 64)
+    x = _C.he_rows(P, 64)
     pool = lambda s, width=64, x=x, e=P, ws=P, size=1 << 30, type=0: he.lib.he_pool(  # noqa: E731
         he.ctx, type, _ref(s), width, _ref(x), e, ws, size, None)
     grad = lambda s, width=64, x=x, e=P, type=0: he.lib.he_pool_grad(he.ctx, type, _ref(s), width, e, _ref(x), 1, None)  # noqa: E731
@@ -80,17 +90,17 @@ def test_pool_refusals(he):
     for s in (None, _spans(-1), _spans((1 << 24) + 1), _spans(3, -1), _spans(3, 1 << 31), _spans(begin=None), _spans(end=None)):
         assert pool(s) == EINVAL and grad(s) == EINVAL
         assert he.lib.he_pool_workspace_bytes(he.ctx, _ref(s), 64, _ref(need)) == EINVAL
-    for kw in ({"width": 0}, {"width": (1 << 20) + 1}, {"x": None}, {"x": bd.he_rows(P, 63)}, {"e": None}, {"type": 3}):
+    for kw in ({"width": 0}, {"width": (1 << 20) + 1}, {"x": None}, {"x": _C.he_rows(P, 63)}, {"e": None}, {"type": 3}):
         assert pool(_spans(), **kw) == EINVAL and grad(_spans(), **kw) == EINVAL, kw
     assert pool(long, ws=None) == EWORKSPACE and pool(long, size=64) == EWORKSPACE and pool(long, ws=P + 2) == EINVAL
 
 
 def _attn(type=2, heads=4, kv=2, dim=64, q=None, k=None, scale=0.125, cap=0.0):
-    return bd.he_attn(type, heads, kv, dim, q or _spans(), k or _spans(), scale, cap, None, 1)
+    return bd._ATTN.pack(type, heads, kv, dim, *(q or _span()), *(k or _span()), scale, cap, 0, 1)
 
 
 def test_attention_refusals(he):
-    h = bd.he_heads(P, 512, 64)
+    h = _C.he_heads(P, 512, 64)
 
     def fwd(s, q=h, k=h, v=h, o=h, lse=P, ws=P, size=1 << 40):
         return he.lib.he_attention(he.ctx, _ref(s), _ref(q), _ref(k), _ref(v), _ref(o), lse, ws, size, None)
@@ -99,28 +109,28 @@ def test_attention_refusals(he):
         return he.lib.he_attention_grad(he.ctx, _ref(s), *[_ref(t) for t in (go, q, k, v, o)], lse, _ref(dq), _ref(dk), _ref(dv), ws, size, None)
 
     assert fwd(_attn()) == ENODEV and bwd(_attn()) == ENODEV
-    assert fwd(_attn(q=_spans(0, 5), k=_spans(0, 5))) == ENODEV and bwd(_attn(q=_spans(0, 5), k=_spans(0, 5))) == ENODEV
+    assert fwd(_attn(q=_span(0, 5), k=_span(0, 5))) == ENODEV and bwd(_attn(q=_span(0, 5), k=_span(0, 5))) == ENODEV
     need = ctypes.c_size_t()
     inf, nan = float("inf"), float("nan")
     for s in (None, _attn(type=3), _attn(heads=0), _attn(kv=0), _attn(heads=5), _attn(heads=65536, kv=1), _attn(dim=0), _attn(dim=12),
               _attn(dim=136), _attn(scale=0.0), _attn(scale=-1.0), _attn(scale=nan), _attn(scale=inf), _attn(scale=1e-60), _attn(scale=1e60), _attn(cap=-1.0),
-              _attn(cap=nan), _attn(cap=inf), _attn(cap=1e-60), _attn(q=_spans(2)), _attn(q=_spans(-1), k=_spans(-1)), _attn(q=_spans(3, -1)),
-              _attn(q=_spans(3, 1 << 31)), _attn(q=_spans(begin=None)), _attn(k=_spans(end=None))):
+              _attn(cap=nan), _attn(cap=inf), _attn(cap=1e-60), _attn(q=_span(2)), _attn(q=_span(-1), k=_span(-1)), _attn(q=_span(3, -1)),
+              _attn(q=_span(3, 1 << 31)), _attn(q=_span(begin=None)), _attn(k=_span(end=None))):
         assert fwd(s) == EINVAL and bwd(s) == EINVAL
         assert he.lib.he_attention_workspace_bytes(he.ctx, _ref(s), 0, _ref(need)) == EINVAL
-    for bad in (None, bd.he_heads(0, 512, 64), bd.he_heads(P + 8, 512, 64), bd.he_heads(P, 508, 64), bd.he_heads(P, 512, 60), bd.he_heads(P, -512, 64)):
+    for bad in (None, _C.he_heads(0, 512, 64), _C.he_heads(P + 8, 512, 64), _C.he_heads(P, 508, 64), _C.he_heads(P, 512, 60), _C.he_heads(P, -512, 64)):
         for name in ("q", "k", "v", "o"):
             assert fwd(_attn(), **{name: bad}) == EINVAL, (name, bad)
         for name in ("go", "q", "k", "v", "o", "dq", "dk", "dv"):
             assert bwd(_attn(), **{name: bad}) == EINVAL, (name, bad)
     assert fwd(_attn(), lse=None) == EINVAL and bwd(_attn(), lse=None) == EINVAL
     assert bwd(_attn(), ws=None) == EWORKSPACE and bwd(_attn(), size=40 * 4 * 4 - 1) == EWORKSPACE and bwd(_attn(), ws=P + 4) == EINVAL
-    long = _attn(q=_spans(1, 1), k=_spans(1, 1 << 20))  # one query of many keys: cut along the keys
+    long = _attn(q=_span(1, 1), k=_span(1, 1 << 20))  # one query of many keys: cut along the keys
     assert he.lib.he_attention_workspace_bytes(he.ctx, _ref(long), 0, _ref(need)) == 0 and need.value >= 2 * 4 * 65 * 4
     assert fwd(long) == ENODEV and fwd(long, ws=None) == EWORKSPACE and fwd(long, size=need.value - 1) == EWORKSPACE and fwd(long, ws=P + 4) == EINVAL
-    huge = _attn(heads=4096, kv=4096, q=_spans(1, 1 << 30), k=_spans(1, 1 << 30))  # more work-groups than a launch holds
+    huge = _attn(heads=4096, kv=4096, q=_span(1, 1 << 30), k=_span(1, 1 << 30))  # more work-groups than a launch holds
     assert fwd(huge, size=1 << 62) == EINVAL and bwd(huge, size=1 << 62) == EINVAL
-    for bad in (bd.he_heads(P, 32, 64), bd.he_heads(P, 512, 32), bd.he_heads(P, 0, 64), bd.he_heads(P, 512, 0)):  # outputs that overlap themselves
+    for bad in (_C.he_heads(P, 32, 64), _C.he_heads(P, 512, 32), _C.he_heads(P, 0, 64), _C.he_heads(P, 512, 0)):  # outputs that overlap themselves
         assert fwd(_attn(), o=bad) == EINVAL
         for name in ("dq", "dk", "dv"):
             assert bwd(_attn(), **{name: bad}) == EINVAL, name
@@ -135,7 +145,7 @@ def test_binding_refusals(he):
         with pytest.raises(ValueError, match="device|want"):
             f()  # CPU tensors: there is no fallback
     for f in (lambda: he.layer_norm(x[0], w, w), lambda: he.layer_norm(x.t(), w, w), lambda: he.pool_mean(x.view(2, 2, 8), off), lambda: he.attention(x, x, x, off),
-              lambda: he._spans(off.view(1, 2), 4), lambda: he._spans((off, off[:1]), 4), lambda: he._heads(x.view(4, 1, 8).transpose(0, 2), "q")):
+              lambda: he._spans(off.view(1, 2), 4), lambda: he._spans((off, off[:1]), 4), lambda: he._heads(x.view(4, 1, 8).transpose(0, 2), "q", (8, 1, 4))):
         with pytest.raises(ValueError):
             f()
     with pytest.raises(ValueError, match="float32, float16 or bfloat16"):

@@ -186,8 +186,8 @@ def test_attention_cuts_long_keys(he):
 
     sq, sk = he._spans(i32(0, 1), 1), he._spans(i32(0, 4000), 4000)
     need = ctypes.c_size_t()
-    s = bd.he_attn(2, 4, 2, 64, sq, sk, 0.125, 0.0, None, 1)
-    assert he.lib.he_attention_workspace_bytes(he.ctx, ctypes.byref(s), 0, ctypes.byref(need)) == 0 and need.value > 0
+    s = bd._ATTN.pack(2, 4, 2, 64, *sq, *sk, 0.125, 0.0, 0, 1)
+    assert he.lib.he_attention_workspace_bytes(he.ctx, s, 0, ctypes.byref(need)) == 0 and need.value > 0
 
 
 def test_attention_scores_far_from_zero(he):
