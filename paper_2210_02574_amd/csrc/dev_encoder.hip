@@ -76,8 +76,6 @@ int32_t norm_check(const he_norm *n)
     return HE_OK;
 }
 bool rows_ok(const he_rows *r, int64_t width) { return r && r->d && r->stride >= width; }
-// whether 16-byte accesses reach every row
-bool wide(const he_rows *r, int32_t type) { return !r || (aligned(r->d, 16) && (r->stride * type_size(type)) % 16 == 0); }
 
 // Work-groups of the backward pass: each writes a partial row of dw and db, so a few for each of the 256 CUs and no more than rows.
 int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
@@ -92,12 +90,17 @@ int32_t spans_check(const he_spans *s)
 }
 Spans spans_of(const he_spans *s) { return Spans{s->d_begin, s->d_end, s->count, (int32_t)s->rows}; }
 
-// Sequences are cut where there are too few of them to fill the card: about 512 work-groups, of at least 256 rows on average.
-int pool_splits(const he_spans *s)
+// A work-group per sequence while their rows are few; else tiles of equal length, about 2048 of them, whatever the lengths are, and a second launch that joins
+// them.
+int pool_tile(const he_spans *s)
 {
-    if (s->count == 0) return 1;
-    const int64_t mean = s->rows / s->count, most = std::max<int64_t>(1, mean / 256);
-    return (int)std::min<int64_t>(std::min<int64_t>(most, (512 + s->count - 1) / s->count), 512);
+    if (s->count == 0 || (s->rows <= 8192 && s->rows / s->count <= 256)) return 0;
+    return (int)std::max<int64_t>(64, (s->rows / 2048 + 15) / 16 * 16);
+}
+size_t pool_bytes(const he_spans *s, int32_t width)
+{
+    const int tile = pool_tile(s);
+    return tile ? (size_t)tile_slots(s->rows, s->count, tile) * width * sizeof(float) : 0;
 }
 
 // ---- attention -------------------------------------------------------------------------------------------------------------
@@ -191,12 +194,10 @@ extern "C" int32_t he_layer_norm(he_ctx *ctx, const he_norm *n, const he_rows *x
     if (residual) a.r = residual->d, a.r_row = residual->stride, a.s = sum->d, a.s_row = sum->stride;
     a.w = d_w, a.b = d_b, a.mean = d_mean, a.rstd = d_rstd;
     a.rows = (int)n->rows, a.width = n->width, a.eps = (float)n->eps;
-    const bool vec = wide(x, n->type) && wide(residual, n->type) && wide(y, n->type) && wide(sum, n->type) && aligned(d_w, 16) && aligned(d_b, 16) &&
-                     (n->width * type_size(n->type)) % 16 == 0;
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
     const double row = (double)n->width * type_size(n->type);
-    rows_launch(n->type).norm(ctx, (hipStream_t)stream, n->rows * (row * (residual ? 4 : 2) + 8) + 2.0 * n->width * type_size(n->weight_type), vec,
+    rows_launch(n->type).norm(ctx, (hipStream_t)stream, n->rows * (row * (residual ? 4 : 2) + 8) + 2.0 * n->width * type_size(n->weight_type),
                               n->weight_type == HE_F32, a);
     return launched(ctx);
 }
@@ -232,11 +233,7 @@ extern "C" int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_ro
     const RowsLaunch &l = rows_launch(n->type);
     const bool ww = n->weight_type == HE_F32;
     const double row = (double)n->width * type_size(n->type), part = (double)parts * 2 * n->width * 4;
-    if (n->rows) {
-        const bool vec = wide(dy, n->type) && wide(s, n->type) && wide(ds, n->type) && wide(add, n->type) && aligned(d_w, 16) &&
-                         (n->width * type_size(n->type)) % 16 == 0;
-        l.norm_grad(ctx, (hipStream_t)stream, n->rows * (row * (add ? 4 : 3) + 8) + part, vec, ww, parts, a);
-    }
+    if (n->rows) l.norm_grad(ctx, (hipStream_t)stream, n->rows * (row * (add ? 4 : 3) + 8) + part, ww, parts, a);
     l.weight_grad(ctx, (hipStream_t)stream, part + 2.0 * n->width * type_size(n->weight_type), ww, (const float *)d_ws, parts, n->width, d_dw, d_db);
     return launched(ctx);
 }
@@ -244,8 +241,7 @@ extern "C" int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_ro
 extern "C" int32_t he_pool_workspace_bytes(const he_ctx *ctx, const he_spans *s, int32_t width, size_t *out)
 {
     if (!ctx || !out || spans_check(s) != HE_OK || width < 1 || width > (1 << 20)) return HE_EINVAL;
-    const int splits = pool_splits(s);
-    *out = splits > 1 ? (size_t)s->count * splits * width * sizeof(float) : 0;
+    *out = pool_bytes(s, width);
     return HE_OK;
 }
 
@@ -261,14 +257,15 @@ extern "C" int32_t he_pool(he_ctx *ctx, int32_t type, const he_spans *s, int32_t
     PoolArgs a;
     memset(&a, 0, sizeof(a));
     if (s->rows > 0) a.x = x->d, a.x_row = x->stride;
-    a.e = d_e, a.s = spans_of(s), a.width = width, a.splits = pool_splits(s), a.part = (float *)d_ws;
-    if (a.splits > 1 && (!d_ws || ws_bytes < (size_t)s->count * a.splits * width * sizeof(float))) return HE_EWORKSPACE;
-    if (a.splits > 1 && !aligned(d_ws, 4)) return HE_EINVAL;
+    a.e = d_e, a.s = spans_of(s), a.width = width, a.tile = pool_tile(s), a.part = (float *)d_ws;
+    const size_t need = pool_bytes(s, width);
+    if (need && (!d_ws || ws_bytes < need)) return HE_EWORKSPACE;
+    if (need && !aligned(d_ws, 4)) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
-    const bool vec = (s->rows == 0 || wide(x, type)) && (width * type_size(type)) % 16 == 0;
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
-    rows_launch(type).pool(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width, vec, a);
+    rows_launch(type).pool(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width,
+                           a.tile ? (unsigned)tile_slots(s->rows, s->count, a.tile) : 0, a);
     return launched(ctx);
 }
 
@@ -285,10 +282,9 @@ extern "C" int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, in
     PoolGradArgs a;
     memset(&a, 0, sizeof(a));
     a.de = d_de, a.dx = dx->d, a.dx_row = dx->stride, a.s = spans_of(s), a.width = width, a.fill = fill;
-    const bool vec = wide(dx, type) && (width * type_size(type)) % 16 == 0;
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
-    rows_launch(type).pool_grad(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width, vec,
+    rows_launch(type).pool_grad(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width,
                                 (unsigned)tile_slots(s->rows, s->count, POOL_TILE), a);
     return launched(ctx);
 }

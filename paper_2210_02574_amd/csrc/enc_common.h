@@ -13,16 +13,35 @@ typedef __bf16 bf16;
 template <class T, int N> struct VecOf {
     typedef T type __attribute__((ext_vector_type(N)));
 };
-template <class T> struct VecOf<T, 1> {
-    struct type {
-        T v;
-        __device__ T &operator[](int) { return v; }
-        __device__ T operator[](int) const { return v; }
-    };
-};
 template <class T, int N> using Vec = typename VecOf<T, N>::type;
 typedef Vec<float, 4> f32x4;
 typedef Vec<float, 16> f32x16;
+
+// The elements col .. col + VEC - 1 of a row of `width` elements, zeros behind its end.  Rows may begin anywhere: global memory takes 16-byte accesses at every
+// address, so rows of any width and stride go by whole vectors, and only a vector across a row's end by elements.
+template <class T, int VEC> struct UnalignedVec {
+    typedef T type __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+};
+template <class T, int VEC> __device__ __forceinline__ Vec<T, VEC> load_vec(const T *row, int col, int width)
+{
+    Vec<T, VEC> x = {};
+    if (col + VEC <= width)
+        x = *(const typename UnalignedVec<T, VEC>::type *)(row + col);
+    else
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            if (col + e < width) x[e] = row[col + e];
+    return x;
+}
+template <class T, int VEC> __device__ __forceinline__ void store_vec(Vec<T, VEC> x, T *row, int col, int width)
+{
+    if (col + VEC <= width)
+        *(typename UnalignedVec<T, VEC>::type *)(row + col) = x;
+    else
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            if (col + e < width) row[col + e] = x[e];
+}
 
 // Sum over the LANES lanes of an aligned group, the same in each of them.
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v)

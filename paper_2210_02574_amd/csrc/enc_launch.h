@@ -27,12 +27,12 @@ HE_DECL_ATTN(2)
 #undef HE_DECL_ATTN
 
 struct RowsLaunch {
-    // vec: vectors of 16 bytes (else single elements); wide_w: weights in 32 bits whatever the rows' type
-    void (*norm)(he_ctx *c, hipStream_t st, double bytes, bool vec, bool wide_w, const NormArgs &a);
-    void (*norm_grad)(he_ctx *c, hipStream_t st, double bytes, bool vec, bool wide_w, int parts, const NormGradArgs &a);
+    // wide_w: weights in 32 bits whatever the rows' type
+    void (*norm)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const NormArgs &a);
+    void (*norm_grad)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, int parts, const NormGradArgs &a);
     void (*weight_grad)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const float *part, int parts, int width, void *dw, void *db);
-    void (*pool)(he_ctx *c, hipStream_t st, double bytes, bool vec, const PoolArgs &a);
-    void (*pool_grad)(he_ctx *c, hipStream_t st, double bytes, bool vec, unsigned slots, const PoolGradArgs &a);
+    void (*pool)(he_ctx *c, hipStream_t st, double bytes, unsigned slots, const PoolArgs &a);
+    void (*pool_grad)(he_ctx *c, hipStream_t st, double bytes, unsigned slots, const PoolGradArgs &a);
 };
 void rows_launch_0(RowsLaunch &t);
 void rows_launch_1(RowsLaunch &t);

@@ -53,20 +53,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
 #pragma unroll
     for (int c = 0; c < NC; c++) {
         const int col = (c * TPR + t) * VEC;
-        Vec<T, VEC> x, r;
-        const bool in = live && col < a.width;
-        if (in) {
-            x = *(const Vec<T, VEC> *)((const T *)a.x + row * a.x_row + col);
+        Vec<T, VEC> x = {};
+        if (live && col < a.width) {
+            x = load_vec<T, VEC>((const T *)a.x + row * a.x_row, col, a.width);
             if (a.r) {
-                r = *(const Vec<T, VEC> *)((const T *)a.r + row * a.r_row + col);
+                const Vec<T, VEC> r = load_vec<T, VEC>((const T *)a.r + row * a.r_row, col, a.width);
 #pragma unroll
                 for (int e = 0; e < VEC; e++) x[e] = (T)((float)x[e] + (float)r[e]);
-                *(Vec<T, VEC> *)((T *)a.s + row * a.s_row + col) = x;
+                store_vec<T, VEC>(x, (T *)a.s + row * a.s_row, col, a.width);
             }
         }
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-            v[c][e] = in ? (float)x[e] : 0.f;
+            v[c][e] = (float)x[e];
             sum += v[c][e];
         }
     }
@@ -75,10 +74,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const bool in = (c * TPR + t) * VEC < a.width;
+        const int col = (c * TPR + t) * VEC;
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-            const float d = in ? v[c][e] - mean : 0.f;
+            const float d = col + e < a.width ? v[c][e] - mean : 0.f;
             sq += d * d;
         }
     }
@@ -92,11 +91,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
     for (int c = 0; c < NC; c++) {
         const int col = (c * TPR + t) * VEC;
         if (col >= a.width) continue;
-        const Vec<TW, VEC> w = *(const Vec<TW, VEC> *)((const TW *)a.w + col), b = *(const Vec<TW, VEC> *)((const TW *)a.b + col);
+        const Vec<TW, VEC> w = load_vec<TW, VEC>((const TW *)a.w, col, a.width), b = load_vec<TW, VEC>((const TW *)a.b, col, a.width);
         Vec<T, VEC> y;
 #pragma unroll
         for (int e = 0; e < VEC; e++) y[e] = (T)((v[c][e] - mean) * rstd * (float)w[e] + (float)b[e]);
-        *(Vec<T, VEC> *)((T *)a.y + row * a.y_row + col) = y;
+        store_vec<T, VEC>(y, (T *)a.y + row * a.y_row, col, a.width);
     }
 }
 
@@ -113,11 +112,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
 #pragma unroll
     for (int c = 0; c < NC; c++) {
         const int col = (c * TPR + t) * VEC;
-        Vec<TW, VEC> u;
-        if (col < a.width) u = *(const Vec<TW, VEC> *)((const TW *)a.w + col);
+        const Vec<TW, VEC> u = load_vec<TW, VEC>((const TW *)a.w, col, a.width);
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-            w[c][e] = col < a.width ? (float)u[e] : 0.f;
+            w[c][e] = (float)u[e];
             dw[c][e] = db[c][e] = 0.f;
         }
     }
@@ -131,16 +129,15 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
 #pragma unroll
         for (int c = 0; c < NC; c++) {
             const int col = (c * TPR + t) * VEC;
-            const bool in = live && col < a.width;
-            Vec<T, VEC> d, s;
-            if (in) {
-                d = *(const Vec<T, VEC> *)((const T *)a.dy + row * a.dy_row + col);
-                s = *(const Vec<T, VEC> *)((const T *)a.s + row * a.s_row + col);
+            Vec<T, VEC> d = {}, s = {};
+            if (live && col < a.width) {
+                d = load_vec<T, VEC>((const T *)a.dy + row * a.dy_row, col, a.width);
+                s = load_vec<T, VEC>((const T *)a.s + row * a.s_row, col, a.width);
             }
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                const float dy = in ? (float)d[e] : 0.f;
-                xh[c][e] = in ? ((float)s[e] - mean) * rstd : 0.f;
+                const float dy = (float)d[e];
+                xh[c][e] = col + e < a.width ? ((float)s[e] - mean) * rstd : 0.f;
                 g[c][e] = dy * w[c][e];
                 c1 += g[c][e];
                 c2 += g[c][e] * xh[c][e];
@@ -155,15 +152,15 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
         for (int c = 0; c < NC; c++) {
             const int col = (c * TPR + t) * VEC;
             if (col >= a.width) continue;
-            Vec<T, VEC> o, add;
-            if (a.add) add = *(const Vec<T, VEC> *)((const T *)a.add + row * a.add_row + col);
+            Vec<T, VEC> o, add = {};
+            if (a.add) add = load_vec<T, VEC>((const T *)a.add + row * a.add_row, col, a.width);
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
                 float v = rstd * (g[c][e] - c1 - xh[c][e] * c2);
                 if (a.add) v += (float)add[e];
                 o[e] = (T)v;
             }
-            *(Vec<T, VEC> *)((T *)a.ds + row * a.ds_row + col) = o;
+            store_vec<T, VEC>(o, (T *)a.ds + row * a.ds_row, col, a.width);
         }
     }
     float *part = a.part + (size_t)blockIdx.x * 2 * a.width;
@@ -180,9 +177,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
                 }
             __syncthreads();
         }
-        if (sub == 0 && col < a.width)
+        if (sub == 0)
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
+                if (col + e >= a.width) break;
                 float u = dw[c][e], v = db[c][e];
                 if constexpr (RPW > 1)
 #pragma unroll
@@ -204,6 +202,7 @@ template <class TW> __global__ __launch_bounds__(256) void k_norm_weight_grad(co
     const float *p = part + (size_t)blockIdx.y * width + col;
     float s = 0.f;
     if (col < width)
+#pragma unroll 8
         for (int k = k0; k < parts; k += 16) s += p[(size_t)k * 2 * width];
     red[threadIdx.x] = s;
     __syncthreads();

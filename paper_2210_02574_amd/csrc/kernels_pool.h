@@ -6,10 +6,11 @@
 struct PoolArgs {
     const void *x;
     float *e;
-    float *part; // [count][splits][width] sums, where a sequence is cut
+    float *part; // [slots][width]: the sums of the tiles
     int64_t x_row;
     Spans s;
-    int width, splits;
+    int width;
+    int tile; // rows of a tile, or 0: a work-group per sequence
 };
 struct PoolGradArgs {
     const float *de;
@@ -19,58 +20,69 @@ struct PoolGradArgs {
     int width, fill;
 };
 
-// grid (sequences, column blocks, splits).  A thread has one vector of columns and every RG-th row; CL = threads along the columns.
-#define POOL_THREADS 1024
-template <class T, int VEC> __global__ __launch_bounds__(POOL_THREADS) void k_pool(PoolArgs a, int CL)
+// grid (sequences or tile slots, column blocks).  A thread has one vector of columns and every RG-th row; CL = threads along the columns.
+template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) void k_pool(PoolArgs a, int CL)
 {
-    __shared__ float join[POOL_THREADS * VEC];
-    const int RG = POOL_THREADS / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
-    const int col = (blockIdx.y * CL + cl) * VEC, i = blockIdx.x;
-    const int begin = span_begin(a.s, i), end = span_end(a.s, i), n = max(end - begin, 0);
-    const int per = (n + a.splits - 1) / a.splits, lo = begin + min(n, (int)blockIdx.z * per), hi = min(lo + per, begin + n);
+    __shared__ float join[THREADS * VEC];
+    const int RG = THREADS / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
+    const int col = (blockIdx.y * CL + cl) * VEC;
+    int lo, hi, n;
+    if (a.tile) {
+        const TileRows t = tile_rows(a.s, blockIdx.x, a.tile);
+        lo = max(t.first, t.begin), hi = min(t.top, t.end), n = 1;
+        if (lo >= hi) return; // k_pool_join does not ask for it
+    } else {
+        lo = span_begin(a.s, blockIdx.x), hi = span_end(a.s, blockIdx.x), n = max(hi - lo, 1);
+    }
     float s[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; e++) s[e] = 0.f;
     if (rg < RG && col < a.width) {
-        const T *x = (const T *)a.x + col;
+        const T *x = (const T *)a.x;
         int j = lo + rg;
         for (; j + 3 * RG < hi; j += 4 * RG) { // four rows in flight
             Vec<T, VEC> v[4];
 #pragma unroll
-            for (int u = 0; u < 4; u++) v[u] = *(const Vec<T, VEC> *)(x + (j + u * RG) * a.x_row);
+            for (int u = 0; u < 4; u++) v[u] = load_vec<T, VEC>(x + (j + u * RG) * a.x_row, col, a.width);
 #pragma unroll
             for (int u = 0; u < 4; u++)
 #pragma unroll
                 for (int e = 0; e < VEC; e++) s[e] += (float)v[u][e];
         }
         for (; j < hi; j += RG) {
-            const Vec<T, VEC> v = *(const Vec<T, VEC> *)(x + j * a.x_row);
+            const Vec<T, VEC> v = load_vec<T, VEC>(x + j * a.x_row, col, a.width);
 #pragma unroll
             for (int e = 0; e < VEC; e++) s[e] += (float)v[e];
         }
     }
 #pragma unroll
-    for (int e = 0; e < VEC; e++) join[e * POOL_THREADS + threadIdx.x] = s[e];
+    for (int e = 0; e < VEC; e++) join[e * THREADS + threadIdx.x] = s[e];
     __syncthreads();
-    if (rg != 0 || col >= a.width) return;
-    const float f = a.splits > 1 ? 1.f : n > 0 ? 1.f / (float)n : 0.f;
-    float *out = a.splits > 1 ? a.part + ((size_t)i * a.splits + blockIdx.z) * a.width : a.e + (size_t)i * a.width;
+    if (rg != 0) return;
+    float *out = (a.tile ? a.part : a.e) + (size_t)blockIdx.x * a.width;
+    const float f = 1.f / (float)n;
 #pragma unroll
     for (int e = 0; e < VEC; e++) {
-        for (int k = 1; k < RG; k++) s[e] += join[e * POOL_THREADS + k * CL + cl];
-        out[col + e] = s[e] * f;
+        for (int k = 1; k < RG; k++) s[e] += join[e * THREADS + k * CL + cl];
+        if (col + e < a.width) out[col + e] = s[e] * f;
     }
 }
 
-// grid (sequences, columns / 256)
+// grid (sequences, columns / 256): the tiles of a sequence are those of the slots c / tile + i .. that reach into it.
 static __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 {
     const int col = blockIdx.y * 256 + threadIdx.x, i = blockIdx.x;
     if (col >= a.width) return;
-    const int n = span_end(a.s, i) - span_begin(a.s, i);
+    const int begin = span_begin(a.s, i), end = span_end(a.s, i), c = i ? begin : 0, top = i + 1 < a.s.count ? span_begin(a.s, i + 1) : a.s.rows;
+    const int stop = min(end, top); // a tile ends at the next sequence's begin
+    const int64_t slot = c / a.tile + i;
     float s = 0.f;
-    for (int k = 0; k < a.splits; k++) s += a.part[((size_t)i * a.splits + k) * a.width + col];
-    a.e[(size_t)i * a.width + col] = n > 0 ? s / (float)n : 0.f;
+    if (stop > begin) {
+        const int first = (begin - c) / a.tile, last = (stop - 1 - c) / a.tile;
+#pragma unroll 4
+        for (int k = first; k <= last; k++) s += a.part[(size_t)(slot + k) * a.width + col];
+    }
+    a.e[(size_t)i * a.width + col] = end > begin ? s / (float)(end - begin) : 0.f;
 }
 
 // grid (tile slots, column blocks): the rows of one tile get the sequence's row, rows of no sequence zeros if `fill`.
@@ -82,15 +94,13 @@ template <class T, int VEC> __global__ __launch_bounds__(256) void k_pool_grad(P
     const int RG = 256 / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
     const int col = (blockIdx.y * CL + cl) * VEC, n = t.end - t.begin;
     if (rg >= RG || col >= a.width) return;
-    Vec<T, VEC> v, zero;
     const float nf = (float)max(n, 1);
+    const Vec<float, VEC> de = load_vec<float, VEC>(a.de + (size_t)t.seq * a.width, col, a.width);
+    Vec<T, VEC> v, zero = {};
 #pragma unroll
-    for (int e = 0; e < VEC; e++) {
-        v[e] = (T)(a.de[(size_t)t.seq * a.width + col + e] / nf);
-        zero[e] = (T)0.f;
-    }
+    for (int e = 0; e < VEC; e++) v[e] = (T)(de[e] / nf);
     for (int j = t.first + rg; j < t.top; j += RG) {
         const bool in = j >= t.begin && j < t.end;
-        if (in || a.fill) *(Vec<T, VEC> *)((T *)a.dx + j * a.dx_row + col) = in ? v : zero;
+        if (in || a.fill) store_vec<T, VEC>(in ? v : zero, (T *)a.dx + j * a.dx_row, col, a.width);
     }
 }
