@@ -77,7 +77,7 @@ int32_t norm_check(const he_norm *n)
 }
 bool rows_ok(const he_rows *r, int64_t width) { return r && r->d && r->stride >= width; }
 
-// Work-groups of the backward pass: each writes a partial row of dw and db, so a few for each of the 256 CUs and no more than rows.
+// Work-groups of the backward pass: each writes a partial row of dw and db, so two for each of the 256 CUs and no more than rows need.
 int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
 
 // ---- mean ----------------------------------------------------------------------------------------------------------------

@@ -14,10 +14,15 @@ static constexpr int VEC = 16 / sizeof(T);
 
 // Threads per row and vectors per thread by the width: the fewest threads that hold a row in few registers, since a sum over a wave or less costs no
 // barrier.
+template <int N> using Int = std::integral_constant<int, N>;
 template <class F> static void row_shape(int width, F f)
 {
+    if (width < VEC) return f(Int<32>{}, Int<1>{}, Int<WIDTH_SMALL>{});
 #define SHAPE(tpr, nc)                                                                                               \
-    if (width <= VEC * (tpr) * (nc)) return f(std::integral_constant<int, tpr>{}, std::integral_constant<int, nc>{});
+    if (width <= VEC * (tpr) * (nc)) {                                                                               \
+        if (width % VEC) return f(Int<tpr>{}, Int<nc>{}, Int<WIDTH_ODD>{});                                          \
+        return f(Int<tpr>{}, Int<nc>{}, Int<WIDTH_EVEN>{});                                                          \
+    }
     SHAPE(32, 1) SHAPE(32, 2) SHAPE(32, 3) SHAPE(32, 4)
     SHAPE(64, 3) SHAPE(64, 4)
     SHAPE(256, 2) SHAPE(256, 3) SHAPE(256, 4)
@@ -27,23 +32,23 @@ template <class F> static void row_shape(int width, F f)
 
 static void norm(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const NormArgs &a)
 {
-    row_shape(a.width, [&](auto tpr, auto nc) {
+    row_shape(a.width, [&](auto tpr, auto nc, auto kind) {
         constexpr int threads = tpr > 256 ? tpr : 256, rpw = threads / tpr;
         const unsigned grid = (unsigned)((a.rows + rpw - 1) / rpw);
         if (wide_w)
-            KLAUNCH_T(c, st, KID_NORM, bytes, (k_layer_norm<T, float, VEC, tpr, nc>), grid, threads, a);
+            KLAUNCH_T(c, st, KID_NORM, bytes, (k_layer_norm<T, float, VEC, tpr, nc, kind>), grid, threads, a);
         else
-            KLAUNCH_T(c, st, KID_NORM, bytes, (k_layer_norm<T, T, VEC, tpr, nc>), grid, threads, a);
+            KLAUNCH_T(c, st, KID_NORM, bytes, (k_layer_norm<T, T, VEC, tpr, nc, kind>), grid, threads, a);
     });
 }
 static void norm_grad(he_ctx *c, hipStream_t st, double bytes, bool wide_w, int parts, const NormGradArgs &a)
 {
-    row_shape(a.width, [&](auto tpr, auto nc) {
+    row_shape(a.width, [&](auto tpr, auto nc, auto kind) {
         constexpr int threads = tpr > 256 ? tpr : 256;
         if (wide_w)
-            KLAUNCH_T(c, st, KID_NORM_GRAD, bytes, (k_layer_norm_grad<T, float, VEC, tpr, nc>), (unsigned)parts, threads, a);
+            KLAUNCH_T(c, st, KID_NORM_GRAD, bytes, (k_layer_norm_grad<T, float, VEC, tpr, nc, kind>), (unsigned)parts, threads, a);
         else
-            KLAUNCH_T(c, st, KID_NORM_GRAD, bytes, (k_layer_norm_grad<T, T, VEC, tpr, nc>), (unsigned)parts, threads, a);
+            KLAUNCH_T(c, st, KID_NORM_GRAD, bytes, (k_layer_norm_grad<T, T, VEC, tpr, nc, kind>), (unsigned)parts, threads, a);
     });
 }
 static void weight_grad(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const float *part, int parts, int width, void *dw, void *db)

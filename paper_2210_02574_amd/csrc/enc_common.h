@@ -43,6 +43,12 @@ template <class T, int VEC> __device__ __forceinline__ void store_vec(Vec<T, VEC
             if (col + e < width) row[col + e] = x[e];
 }
 
+// A whole vector, whose lines are not kept: rows that one kernel reads once and no other soon.
+template <class T, int VEC> __device__ __forceinline__ Vec<T, VEC> load_once(const T *p)
+{
+    return __builtin_nontemporal_load((const typename UnalignedVec<T, VEC>::type *)p);
+}
+
 // Sum over the LANES lanes of an aligned group, the same in each of them.
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
 {

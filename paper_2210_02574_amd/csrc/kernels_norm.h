@@ -41,32 +41,63 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *red)
     return t;
 }
 
-template <class T, class TW, int VEC, int TPR, int NC>
+// The vector c of a thread.  Every load is a whole vector and none is behind a branch, so that all loads of a row are under way together: a vector that
+// would reach over the row's end (ODD: widths that VEC does not divide) begins earlier and repeats elements of its neighbour, which it does
+// not count (count(e) false) and stores with the same values; a thread behind the row's end reads the last vector and counts nothing.
+// A width below VEC (SMALL) is one thread's, element by element.
+enum { WIDTH_EVEN, WIDTH_ODD, WIDTH_SMALL };
+template <int VEC, int WIDTH> struct Cols {
+    int at, first, width;
+    bool in;
+    __device__ __forceinline__ Cols(int col, int width) : at(WIDTH == WIDTH_SMALL ? col : min(col, width - VEC)), first(col - at), width(width), in(col < width) {}
+    __device__ __forceinline__ bool count(int e) const
+    {
+        return in && (WIDTH == WIDTH_EVEN || (WIDTH == WIDTH_ODD ? e >= first : at + e < width));
+    }
+    template <class T> __device__ __forceinline__ Vec<T, VEC> load(const T *row) const
+    {
+        if constexpr (WIDTH == WIDTH_SMALL) return load_vec<T, VEC>(row, at, width);
+        return *(const typename UnalignedVec<T, VEC>::type *)(row + at);
+    }
+    template <class T> __device__ __forceinline__ void store(Vec<T, VEC> x, T *row) const
+    {
+        if constexpr (WIDTH == WIDTH_SMALL)
+            store_vec<T, VEC>(x, row, at, width);
+        else if (in)
+            *(typename UnalignedVec<T, VEC>::type *)(row + at) = x;
+    }
+};
+
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
     __shared__ float red[THREADS / 64];
     const int t = threadIdx.x % TPR, row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
-    const bool live = row < a.rows; // a row's lanes are live or not together; all of them take part in the sums
+    const bool live = row < a.rows; // a row's lanes are live or not together; all of them take part in the sums, on the last row
+    const int64_t r = min(row, a.rows - 1);
+    Vec<T, VEC> x[NC], res[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        x[c] = k.load((const T *)a.x + r * a.x_row);
+        if (a.r) res[c] = k.load((const T *)a.r + r * a.r_row);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     float v[NC][VEC];
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const int col = (c * TPR + t) * VEC;
-        Vec<T, VEC> x = {};
-        if (live && col < a.width) {
-            x = load_vec<T, VEC>((const T *)a.x + row * a.x_row, col, a.width);
-            if (a.r) {
-                const Vec<T, VEC> r = load_vec<T, VEC>((const T *)a.r + row * a.r_row, col, a.width);
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        if (a.r) {
 #pragma unroll
-                for (int e = 0; e < VEC; e++) x[e] = (T)((float)x[e] + (float)r[e]);
-                store_vec<T, VEC>(x, (T *)a.s + row * a.s_row, col, a.width);
-            }
+            for (int e = 0; e < VEC; e++) x[c][e] = (T)((float)x[c][e] + (float)res[c][e]);
+            if (live) k.store(x[c], (T *)a.s + r * a.s_row);
         }
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-            v[c][e] = (float)x[e];
-            sum += v[c][e];
+            v[c][e] = (float)x[c][e];
+            sum += k.count(e) ? v[c][e] : 0.f;
         }
     }
     const float inv_w = 1.f / (float)a.width;
@@ -74,10 +105,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const int col = (c * TPR + t) * VEC;
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-            const float d = col + e < a.width ? v[c][e] - mean : 0.f;
+            const float d = k.count(e) ? v[c][e] - mean : 0.f;
             sq += d * d;
         }
     }
@@ -89,59 +120,60 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
     }
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const int col = (c * TPR + t) * VEC;
-        if (col >= a.width) continue;
-        const Vec<TW, VEC> w = load_vec<TW, VEC>((const TW *)a.w, col, a.width), b = load_vec<TW, VEC>((const TW *)a.b, col, a.width);
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        const Vec<TW, VEC> w = k.load((const TW *)a.w), b = k.load((const TW *)a.b);
         Vec<T, VEC> y;
 #pragma unroll
         for (int e = 0; e < VEC; e++) y[e] = (T)((v[c][e] - mean) * rstd * (float)w[e] + (float)b[e]);
-        store_vec<T, VEC>(y, (T *)a.y + row * a.y_row, col, a.width);
+        k.store(y, (T *)a.y + r * a.y_row);
     }
 }
 
+// 2 work-groups per CU: their partial rows cost little to sum and their registers (about 180 for 768 columns) leave room for no third (16384 x 768 bf16: 18 us;
+// 256 work-groups 22, 768 of them 22; asking for the next row ahead of this one's sums changed nothing).
 // Work-group g takes the rows g, g + gridDim.x, .. (times the rows of a work-group), keeps its columns' shares of dw and db in registers, joins those of its
 // rows in LDS and writes one partial row each; k_norm_weight_grad sums the partial rows.  No atomics: a run repeats bit for bit.
-template <class T, class TW, int VEC, int TPR, int NC>
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormGradArgs a)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256, RPW = THREADS / TPR;
     __shared__ float red[THREADS / 64];
     __shared__ float join[RPW > 1 ? (RPW - 1) * TPR * VEC * 2 : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    float w[NC][VEC], dw[NC][VEC], db[NC][VEC];
+    float dw[NC][VEC], db[NC][VEC];
+    Vec<TW, VEC> w[NC];
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const int col = (c * TPR + t) * VEC;
-        const Vec<TW, VEC> u = load_vec<TW, VEC>((const TW *)a.w, col, a.width);
+        w[c] = Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).load((const TW *)a.w);
 #pragma unroll
-        for (int e = 0; e < VEC; e++) {
-            w[c][e] = (float)u[e];
-            dw[c][e] = db[c][e] = 0.f;
-        }
+        for (int e = 0; e < VEC; e++) dw[c][e] = db[c][e] = 0.f;
     }
     const float inv_w = 1.f / (float)a.width;
     for (int row0 = blockIdx.x * RPW; row0 < a.rows; row0 += gridDim.x * RPW) {
+        Vec<T, VEC> d[NC], s[NC], add[NC];
+        const int64_t r = min(row0 + sub, a.rows - 1);
+        const float mean = a.mean[r], rstd = a.rstd[r];
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+            d[c] = k.load((const T *)a.dy + r * a.dy_row);
+            s[c] = k.load((const T *)a.s + r * a.s_row);
+            if (a.add) add[c] = k.load((const T *)a.add + r * a.add_row);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const int row = row0 + sub;
         const bool live = row < a.rows;
-        const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-        float g[NC][VEC], xh[NC][VEC];
         float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; c++) {
-            const int col = (c * TPR + t) * VEC;
-            Vec<T, VEC> d = {}, s = {};
-            if (live && col < a.width) {
-                d = load_vec<T, VEC>((const T *)a.dy + row * a.dy_row, col, a.width);
-                s = load_vec<T, VEC>((const T *)a.s + row * a.s_row, col, a.width);
-            }
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                const float dy = (float)d[e];
-                xh[c][e] = col + e < a.width ? ((float)s[e] - mean) * rstd : 0.f;
-                g[c][e] = dy * w[c][e];
-                c1 += g[c][e];
-                c2 += g[c][e] * xh[c][e];
-                dw[c][e] += dy * xh[c][e];
+                const float dy = live && k.count(e) ? (float)d[c][e] : 0.f, g = dy * (float)w[c][e], xh = ((float)s[c][e] - mean) * rstd;
+                c1 += g;
+                if (!live || !k.count(e)) continue; // (a product with an infinity of no account would not be zero)
+                c2 += g * xh;
+                dw[c][e] += dy * xh;
                 db[c][e] += dy;
             }
         }
@@ -150,23 +182,21 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
         if (!live) continue; // rows of one wave or more: all of its threads; the barriers are behind
 #pragma unroll
         for (int c = 0; c < NC; c++) {
-            const int col = (c * TPR + t) * VEC;
-            if (col >= a.width) continue;
-            Vec<T, VEC> o, add = {};
-            if (a.add) add = load_vec<T, VEC>((const T *)a.add + row * a.add_row, col, a.width);
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+            Vec<T, VEC> o;
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                float v = rstd * (g[c][e] - c1 - xh[c][e] * c2);
-                if (a.add) v += (float)add[e];
-                o[e] = (T)v;
+                float u = rstd * ((float)d[c][e] * (float)w[c][e] - c1 - ((float)s[c][e] - mean) * rstd * c2);
+                if (a.add) u += (float)add[c][e];
+                o[e] = (T)u;
             }
-            store_vec<T, VEC>(o, (T *)a.ds + row * a.ds_row, col, a.width);
+            k.store(o, (T *)a.ds + row * a.ds_row);
         }
     }
     float *part = a.part + (size_t)blockIdx.x * 2 * a.width;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
-        const int col = (c * TPR + t) * VEC;
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
         if constexpr (RPW > 1) {
             __syncthreads();
             if (sub > 0)
@@ -180,16 +210,16 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
         if (sub == 0)
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                if (col + e >= a.width) break;
+                if (!k.count(e)) continue;
                 float u = dw[c][e], v = db[c][e];
                 if constexpr (RPW > 1)
 #pragma unroll
-                    for (int k = 0; k < RPW - 1; k++) {
-                        u += join[(k * 2 * VEC + e) * TPR + t];
-                        v += join[(k * 2 * VEC + VEC + e) * TPR + t];
+                    for (int i = 0; i < RPW - 1; i++) {
+                        u += join[(i * 2 * VEC + e) * TPR + t];
+                        v += join[(i * 2 * VEC + VEC + e) * TPR + t];
                     }
-                part[col + e] = u;
-                part[a.width + col + e] = v;
+                part[k.at + e] = u;
+                part[a.width + k.at + e] = v;
             }
     }
 }

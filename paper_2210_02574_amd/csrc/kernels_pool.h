@@ -38,19 +38,22 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
 #pragma unroll
     for (int e = 0; e < VEC; e++) s[e] = 0.f;
     if (rg < RG && col < a.width) {
-        const T *x = (const T *)a.x;
-        int j = lo + rg;
-        for (; j + 3 * RG < hi; j += 4 * RG) { // four rows in flight
-            Vec<T, VEC> v[4];
+        const T *x = (const T *)a.x + (lo + rg) * a.x_row;
+        const int64_t step = RG * a.x_row;
+        int left = (hi - lo - rg + RG - 1) / RG; // rows of this thread
+        if (col + VEC <= a.width)
+            for (; left >= 8; left -= 8) {
+                Vec<T, VEC> v[8];
 #pragma unroll
-            for (int u = 0; u < 4; u++) v[u] = load_vec<T, VEC>(x + (j + u * RG) * a.x_row, col, a.width);
+                for (int u = 0; u < 8; u++, x += step) v[u] = load_once<T, VEC>(x + col);
+                __builtin_amdgcn_sched_barrier(0); // eight rows are under way before the first one is waited for
 #pragma unroll
-            for (int u = 0; u < 4; u++)
+                for (int u = 0; u < 8; u++)
 #pragma unroll
-                for (int e = 0; e < VEC; e++) s[e] += (float)v[u][e];
-        }
-        for (; j < hi; j += RG) {
-            const Vec<T, VEC> v = load_vec<T, VEC>(x + j * a.x_row, col, a.width);
+                    for (int e = 0; e < VEC; e++) s[e] += (float)v[u][e];
+            }
+        for (; left > 0; left--, x += step) {
+            const Vec<T, VEC> v = load_vec<T, VEC>(x, col, a.width);
 #pragma unroll
             for (int e = 0; e < VEC; e++) s[e] += (float)v[e];
         }
