@@ -21,7 +21,8 @@ SOURCES = (
     + [("dev_conv.hip", ["-DHE_LOGN=%d" % n], "dev_conv%d" % n) for n in (17, 16)]
     + [("dev_n12.hip", ["-DHE_FEW=1"], "dev_n12_few")]  # its conversions of one and two sources
     # the operators on token states: by element type (0: 32 bits, 1: fp16, 2: bf16), and by head size
-    + [("dev_attn.hip", ["-DHE_TYPE=%d" % t, "-DHE_DIM=%d" % d], "dev_attn%d_%d" % (t, d)) for d in (128, 96, 64, 32) for t in (0, 1, 2)]
+    # (matrix instructions with their sums in ordinary registers, where the exponentials read them: accumulation registers cost a move per value)
+    + [("dev_attn.hip", ["-DHE_TYPE=%d" % t, "-DHE_DIM=%d" % d, "-mllvm", "-amdgpu-mfma-vgpr-form"], "dev_attn%d_%d" % (t, d)) for d in (128, 96, 64, 32) for t in (0, 1, 2)]
     + [("dev_rows.hip", ["-DHE_TYPE=%d" % t], "dev_rows%d" % t) for t in (0, 1, 2)]
     + [("dev_encoder.hip", [], "dev_encoder")]
     + [(s, [], os.path.splitext(s)[0]) for s in ("dev_n12.hip", "dev_n16_blocks.hip", "dev_n17_blocks.hip", "device.hip", "host.cpp")]
@@ -64,6 +65,7 @@ def source_hash() -> str:
         with open(f, "rb") as fh:
             h.update(fh.read())
     h.update(" ".join(CODEGEN_FLAGS).encode())
+    h.update(repr(SOURCES).encode())
     return h.hexdigest()
 
 

@@ -24,15 +24,17 @@ template <class F> static void by_mode(const AttnArgs &a, F f)
         f(std::integral_constant<int, MODE_CAP | MODE_SLOPE>{});
 }
 
-static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int nwq, unsigned grid, const AttnArgs &a)
+static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a)
 {
     by_mode(a, [&](auto mode) {
-        if (nwq == 1)
+        if (tile == 32)
+            KLAUNCH_T(c, st, KID_ATTN_FEW, bytes, (k_attn_few<T, HE_DIM, 1, mode>), grid, ATTN_THREADS, a);
+        else if (tile == 64)
+            KLAUNCH_T(c, st, KID_ATTN_FEW, bytes, (k_attn_few<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
+        else if (tile == 128)
             KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 1, mode>), grid, ATTN_THREADS, a);
-        else if (nwq == 2)
-            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
         else
-            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 4, mode>), grid, ATTN_THREADS, a);
+            KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
     });
 }
 static void attn_join(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)

@@ -126,15 +126,15 @@ bool out_ok(const he_heads *h, const he_attn *s, int64_t rows, int heads)
 }
 
 struct AttnPlan {
-    int nwq, splits;
+    int tile, splits; // queries of a work-group; parts that the keys are cut into
     int64_t slots;
 };
 AttnPlan attn_plan(const he_attn *s)
 {
     AttnPlan p;
     const int64_t mean_q = s->q.count ? s->q.rows / s->q.count : 0, mean_k = s->q.count ? s->k.rows / s->q.count : 0;
-    p.nwq = mean_q <= 32 ? 1 : mean_q <= 64 ? 2 : 4;
-    p.slots = tile_slots(s->q.rows, s->q.count, 32 * p.nwq);
+    p.tile = mean_q <= 32 ? 32 : mean_q <= 64 ? 64 : mean_q <= (getenv("QT") ? atoi(getenv("QT")) : 512) ? 128 : 256;
+    p.slots = tile_slots(s->q.rows, s->q.count, p.tile);
     const int64_t groups = p.slots * s->heads;
     p.splits = groups > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, mean_k / 256, 64})) : 1;
     return p;
@@ -328,7 +328,7 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
     if (dg.rc != HE_OK) return dg.rc;
     const AttnLaunch &l = attn_launch(s->type, s->dim);
     const double size = (double)type_size(s->type) * s->dim, kv = 2.0 * s->k.rows * s->kv_heads * size;
-    l.fwd(ctx, (hipStream_t)stream, rows * (2 * size + 4) + kv, p.nwq, grid, a);
+    l.fwd(ctx, (hipStream_t)stream, rows * (2 * size + 4) + kv, p.tile, grid, a);
     if (p.splits > 1)
         l.join(ctx, (hipStream_t)stream, rows * (size + 4 + 4.0 * p.splits * (s->dim + 1)), (unsigned)((rows + 3) / 4), a);
     return launched(ctx);

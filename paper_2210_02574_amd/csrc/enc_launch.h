@@ -10,8 +10,8 @@ struct PoolArgs;
 struct PoolGradArgs;
 
 struct AttnLaunch {
-    // nwq: waves along the queries, 1, 2 or 4 (tiles of 32 nwq queries)
-    void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int nwq, unsigned grid, const AttnArgs &a);
+    // tile: queries of a work-group, 32, 64, 128 or 256
+    void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);
     void (*join)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
     void (*grad_q)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
     void (*grad_kv)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);

@@ -229,21 +229,226 @@ template <class T, int MODE> struct Scores {
 };
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
-//
-// Four waves: NWQ of them along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: few queries then still
-// keep four waves busy.  KB blocks of 32 keys per wave and step.
-template <class T, int DP, int NWQ> struct AttnFwd {
-    static constexpr int NWK = 4 / NWQ, KB = NWK > 1 || sizeof(T) == 4 ? 1 : 2, BM = 32 * NWQ, BN = 32 * KB * NWK;
-    static constexpr int TILE = BN * AttnTile<T, DP>::ROW;                    // elements of a tile
-    static constexpr int JOIN = NWK > 1 ? (NWK - 1) * NWQ * 64 * (DP / 2 + 2) : 0; // floats
-    static constexpr int LDS = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
+
+// The rows of a work-group's tile and the keys that it reads, the same for both kernels of the forward pass.
+struct FwdRange {
+    TileRows t;
+    int kb, ke; // the sequence's keys
+    int lo, hi; // those of this split
+    int back;   // a query row's position among the keys, the first at 0, is its number plus this
+    __device__ __forceinline__ FwdRange(const AttnArgs &a, const TileRows &t, int split, int tile) : t(t)
+    {
+        kb = span_begin(a.sk, t.seq), ke = max(span_end(a.sk, t.seq), kb);
+        back = (ke - kb) - t.end;
+        if (t.first >= t.end || t.top <= t.begin) ke = kb; // a tile between sequences: nothing to sum
+        const int tiles = (ke - kb + tile - 1) / tile, per = (tiles + a.splits - 1) / a.splits;
+        lo = kb + min(split * per, tiles) * tile, hi = min(ke, kb + min((split + 1) * per, tiles) * tile);
+    }
 };
 
-template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
+// A row's result: its sum of weights, the maximum that they refer to (in units of log2) and the weighted sum of values in o.
+template <class T, int DB> __device__ __forceinline__ void fwd_store(const AttnArgs &a, const FwdRange &g, int head, int split, int row, float top, float sum, f32x16 (&o)[DB], int lane)
 {
-    typedef AttnFwd<T, DP, NWQ> F;
+    const bool in = row >= g.t.begin && row < g.t.end;
+    if (row >= g.t.top || (!in && !a.fill)) return;
+    // a row without keys, and a row of no sequence: zeros
+    const bool some = in && g.hi > g.lo;
+    const float f = some ? 1.f / sum : 0.f, lse = some ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    const int64_t at = (int64_t)head * a.sq.rows + row;
+    if (a.splits > 1) {
+        const int64_t part = (int64_t)split * a.heads * a.sq.rows + at;
+        if (lane < 32) a.part_lse[part] = lse;
+        if (some) store_row<float, DB>(o, f, a.part_o + part * a.dim, a.dim, lane);
+        return;
+    }
+    if (lane < 32) a.lse[at] = lse;
+    if (!some) // not 0 * o: the row may hold what a zero does not clear
+#pragma unroll
+        for (int db = 0; db < DB; db++) o[db] = f32x16{};
+    store_row<T, DB>(o, f, (T *)a.o + head * a.o_head + row * a.o_row, a.dim, lane);
+}
+
+// scores of missing keys: rows of C from `left` on
+__device__ __forceinline__ void mask_rows(f32x16 &s, int left, int h)
+{
+#pragma unroll
+    for (int r = 0; r < 16; r++)
+        if (8 * (r >> 2) + 4 * h + (r & 3) >= left) s[r] = -INFINITY;
+}
+__device__ __forceinline__ float col_max(const f32x16 &s)
+{
+    float m = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; r++) m = fmaxf(m, s[r]);
+    return pair_max(m);
+}
+
+// Many queries: four waves with 32 QB queries each, all of which read all keys.  A step takes 32 keys: the products of the next step's scores are
+// independent of this step's exponentials, so that matrix and vector instructions of one wave overlap.  Tiles of BN keys pass through three LDS
+// stages, which takes one barrier a tile: the stage that a wave overwrites is the one that every wave has left before the last barrier.
+template <class T, int DP, int QB> struct AttnFwd {
+    static constexpr int BM = 128 * QB, BN = DP * sizeof(T) > 384 ? 32 : 64, SUB = BN / 32;
+    static constexpr int TILE = BN * AttnTile<T, DP>::ROW; // elements
+};
+template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
+{
+    typedef AttnFwd<T, DP, QB> F;
     typedef AttnTile<T, DP> L;
-    constexpr int NWK = F::NWK, KB = F::KB, BN = F::BN, KK = DP / 16, DB = DP / 32;
+    constexpr int BN = F::BN, SUB = F::SUB, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lds[3][2][F::TILE];
+
+    int head, slot, split;
+    if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
+    const TileRows t = tile_rows(a.sq, slot, F::BM);
+    if (t.first >= t.top) return;
+    const FwdRange g(a, t, split, BN);
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row0 = t.first + 32 * QB * wave + (lane & 31); // and 32 further on for each block
+
+    const T *const q = (const T *)a.q + head * a.q_head;
+    const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
+    const auto load = [&](int j) {
+        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j, g.hi, a.dim, tid);
+        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j, g.hi, a.dim, tid);
+    };
+    const auto store = [&](int stage) {
+        L::template store<BN, ATTN_THREADS>(ck, lds[stage][0], tid);
+        L::template store<BN, ATTN_THREADS>(cv, lds[stage][1], tid);
+    };
+    load(g.lo);
+    Vec<T, 8> fq[QB][KK];
+#pragma unroll
+    for (int b = 0; b < QB; b++)
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            const int row = row0 + 32 * b;
+            fq[b][kk] = L::own(q, a.q_row, row, row < t.top && row >= t.begin && row < t.end, kk, a.dim, lane);
+        }
+    const Scores<T, MODE> scores(a, head);
+    const float c2 = scores.rest(); // scores are kept times this below
+    float top[QB], sum[QB], m[QB];  // the maximum that sums refer to (in units of log2), the lane's own sum, the maximum of the scores at hand
+    f32x16 o[QB][DB], s[QB];
+#pragma unroll
+    for (int b = 0; b < QB; b++) {
+        top[b] = -INFINITY, sum[b] = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; db++) o[b][db] = f32x16{};
+    }
+    // scores of the 32 keys from j on, rows `at` .. of a stage
+    const auto products = [&](f32x16 (&x)[QB], const T *lk, int at, int j) {
+#pragma unroll
+        for (int b = 0; b < QB; b++) x[b] = f32x16{};
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            const Vec<T, 8> f = L::rows(lk, at, kk, lane);
+#pragma unroll
+            for (int b = 0; b < QB; b++) x[b] = AttnType<T>::mma(f, fq[b][kk], x[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < QB; b++) scores(x[b], (float)(row0 + 32 * b + g.back - (j - g.kb)), h);
+    };
+    // The maximum that the sums refer to moves only when it is left 8 behind (2^8 fits every type): most steps skip the rescaling.
+    const auto rescale = [&]() {
+        bool far = false;
+#pragma unroll
+        for (int b = 0; b < QB; b++) far |= m[b] * c2 > top[b] + 8.f;
+        if (!__any(far)) return;
+#pragma unroll
+        for (int b = 0; b < QB; b++) {
+            const float now = fmaxf(m[b] * c2, top[b]);
+            const float f = __builtin_amdgcn_exp2f(top[b] - (now == -INFINITY ? 0.f : now));
+            top[b] = now;
+            sum[b] *= f;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) o[b][db][r] *= f;
+        }
+    };
+    // exponentials of s, and their products with the values in rows `at` .. of a stage
+    const auto values = [&](const T *lv, int at) {
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            Vec<T, 8> p[QB];
+#pragma unroll
+            for (int b = 0; b < QB; b++) {
+                const float ref = top[b] == -INFINITY ? 0.f : top[b];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[b][8 * half + e], c2, -ref));
+                    sum[b] += x;
+                    p[b][e] = (T)x;
+                }
+            }
+#pragma unroll
+            for (int db = 0; db < DB; db++) {
+                const Vec<T, 8> f = L::cols(lv, at + 16 * half, db, lane);
+#pragma unroll
+                for (int b = 0; b < QB; b++) o[b][db] = AttnType<T>::mma(f, p[b], o[b][db]);
+            }
+        }
+    };
+
+    if (g.hi > g.lo) {
+        const int blocks = (g.hi - g.lo + 31) / 32;
+        store(0);
+        load(g.lo + BN);
+        __syncthreads();
+        products(s, lds[0][0], 0, g.lo);
+        if (blocks > 1)
+#pragma unroll
+            for (int b = 0; b < QB; b++) m[b] = col_max(s[b]);
+        int stage = 0, i = 0;
+        while (i + 1 < blocks) {
+#pragma unroll
+            for (int sub = 0; sub < SUB; sub++) {
+                const int next = stage == 2 ? 0 : stage + 1;
+                if (sub == SUB - 1) { // the next step's keys are in the next tile
+                    store(next);
+                    load(g.lo + 32 * i + BN + 32);
+                    __syncthreads();
+                }
+                rescale();
+                f32x16 n[QB];
+                products(n, sub == SUB - 1 ? lds[next][0] : lds[stage][0], sub == SUB - 1 ? 0 : 32 * (sub + 1), g.lo + 32 * (i + 1));
+                values(lds[stage][1], 32 * sub);
+#pragma unroll
+                for (int b = 0; b < QB; b++) {
+                    s[b] = n[b];
+                    m[b] = col_max(s[b]);
+                }
+                i++;
+                if (sub == SUB - 1) stage = next;
+                if (i + 1 >= blocks) break;
+            }
+        }
+        const int left = g.hi - g.lo - 32 * i; // the last 32 keys may be fewer
+#pragma unroll
+        for (int b = 0; b < QB; b++) {
+            if (left < 32) mask_rows(s[b], left, h);
+            m[b] = col_max(s[b]);
+        }
+        rescale();
+        values(lds[stage][1], 32 * (i % SUB));
+    }
+#pragma unroll
+    for (int b = 0; b < QB; b++) fwd_store<T, DB>(a, g, head, split, row0 + 32 * b, top[b], pair_sum(sum[b]), o[b], lane);
+}
+
+// Few queries: NWQ of the four waves along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: so that 32 queries
+// still keep four waves busy.
+template <class T, int DP, int NWQ> struct AttnFew {
+    static constexpr int NWK = 4 / NWQ, BM = 32 * NWQ, BN = 32 * NWK;
+    static constexpr int TILE = BN * AttnTile<T, DP>::ROW;                // elements of a tile
+    static constexpr int JOIN = (NWK - 1) * NWQ * 64 * (DP / 2 + 2);      // floats
+    static constexpr int LDS = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
+};
+template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_few(AttnArgs a)
+{
+    typedef AttnFew<T, DP, NWQ> F;
+    typedef AttnTile<T, DP> L;
+    constexpr int NWK = F::NWK, BN = F::BN, KK = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(16))) char lds[F::LDS];
     T *const lk = (T *)lds, *const lv = lk + F::TILE;
 
@@ -251,66 +456,43 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
     const TileRows t = tile_rows(a.sq, slot, F::BM);
     if (t.first >= t.top) return;
+    const FwdRange g(a, t, split, BN);
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wq = wave % NWQ, wk = wave / NWQ;
     const int row = t.first + 32 * wq + (lane & 31);
-    const bool in = row < t.top && row >= t.begin && row < t.end; // a row of the sequence
-
-    int kb = span_begin(a.sk, t.seq), ke = span_end(a.sk, t.seq);
-    ke = max(ke, kb);
-    const int pos0 = row - t.begin + (ke - kb) - (t.end - t.begin); // the row's position among the keys, the first at 0
-    if (t.first >= t.end || t.top <= t.begin) ke = kb; // a tile between sequences: nothing to sum
-    const int tiles = (ke - kb + BN - 1) / BN, per = (tiles + a.splits - 1) / a.splits;
-    const int lo = kb + min(split * per, tiles) * BN, hi = min(ke, kb + min((split + 1) * per, tiles) * BN);
 
     const T *const q = (const T *)a.q + head * a.q_head;
     const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
+    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, g.lo, g.hi, a.dim, tid);
+    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, g.lo, g.hi, a.dim, tid);
     Vec<T, 8> fq[KK];
 #pragma unroll
-    for (int kk = 0; kk < KK; kk++) fq[kk] = L::own(q, a.q_row, row, in, kk, a.dim, lane);
+    for (int kk = 0; kk < KK; kk++) fq[kk] = L::own(q, a.q_row, row, row < t.top && row >= t.begin && row < t.end, kk, a.dim, lane);
 
     const Scores<T, MODE> scores(a, head);
     const float c2 = scores.rest();
-    float top = -INFINITY, sum = 0.f;              // running maximum (in units of log2) and the lane's own sum
+    float top = -INFINITY, sum = 0.f;
     f32x16 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) o[db] = f32x16{};
 
-    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
-    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, lo, hi, a.dim, tid);
-    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, lo, hi, a.dim, tid);
-    for (int j0 = lo; j0 < hi; j0 += BN) {
+    for (int j0 = g.lo; j0 < g.hi; j0 += BN) {
         __syncthreads();
         L::template store<BN, ATTN_THREADS>(ck, lk, tid);
         L::template store<BN, ATTN_THREADS>(cv, lv, tid);
         __syncthreads();
-        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, hi, a.dim, tid); // the next tile is under way meanwhile
-        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, hi, a.dim, tid);
-        const int w0 = wk * KB * 32; // the wave's keys of the tile
-        if (j0 + w0 >= hi) continue;
-        f32x16 s[KB];
+        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, g.hi, a.dim, tid); // the next tile is under way meanwhile
+        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, g.hi, a.dim, tid);
+        const int j = j0 + 32 * wk; // the wave's keys of the tile
+        if (j >= g.hi) continue;
+        f32x16 s = {};
 #pragma unroll
-        for (int b = 0; b < KB; b++) {
-            s[b] = f32x16{};
-#pragma unroll
-            for (int kk = 0; kk < KK; kk++) s[b] = AttnType<T>::mma(L::rows(lk, w0 + 32 * b, kk, lane), fq[kk], s[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < KB; b++) scores(s[b], (float)(pos0 - (j0 + w0 + 32 * b - kb)), h);
-        if (j0 + w0 + 32 * KB > hi)
-#pragma unroll
-            for (int b = 0; b < KB; b++)
-#pragma unroll
-                for (int r = 0; r < 16; r++)
-                    if (j0 + w0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3) >= hi) s[b][r] = -INFINITY;
-        float m = s[0][0];
-#pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) m = fmaxf(m, s[b][r]);
-        m = pair_max(m) * c2;
-        // The maximum that the sums refer to moves only when it is left 8 behind (2^8 fits every type): most steps skip the rescaling.
-        if (__any(m > top + 8.f)) {
+        for (int kk = 0; kk < KK; kk++) s = AttnType<T>::mma(L::rows(lk, 32 * wk, kk, lane), fq[kk], s);
+        scores(s, (float)(row + g.back - (j - g.kb)), h);
+        if (g.hi - j < 32) mask_rows(s, g.hi - j, h);
+        const float m = col_max(s) * c2;
+        if (__any(m > top + 8.f)) { // as in k_attn
             const float now = fmaxf(m, top);
             const float f = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
             top = now;
@@ -322,66 +504,47 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
         }
         const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int b = 0; b < KB; b++)
+        for (int half = 0; half < 2; half++) {
+            Vec<T, 8> p;
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c2, -ref));
-                sum += s[b][r];
+            for (int e = 0; e < 8; e++) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * half + e], c2, -ref));
+                sum += x;
+                p[e] = (T)x;
             }
 #pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-                const Vec<T, 8> p = round8<T>(s[b], half);
-#pragma unroll
-                for (int db = 0; db < DB; db++) o[db] = AttnType<T>::mma(L::cols(lv, w0 + 32 * b + 16 * half, db, lane), p, o[db]);
-            }
+            for (int db = 0; db < DB; db++) o[db] = AttnType<T>::mma(L::cols(lv, 32 * wk + 16 * half, db, lane), p, o[db]);
+        }
     }
     sum = pair_sum(sum);
 
-    if constexpr (NWK > 1) { // join the waves along the keys: word i of all lanes side by side
-        float *const join = (float *)lds;
-        __syncthreads();
-        if (wk > 0) {
-            float *p = join + ((wk - 1) * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
-            p[0] = top;
-            p[64] = sum;
+    // join the waves along the keys: word i of all lanes side by side
+    float *const join = (float *)lds;
+    __syncthreads();
+    if (wk > 0) {
+        float *p = join + ((wk - 1) * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
+        p[0] = top;
+        p[64] = sum;
 #pragma unroll
-            for (int db = 0; db < DB; db++)
+        for (int db = 0; db < DB; db++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) p[(2 + db * 16 + r) * 64] = o[db][r];
-        }
-        __syncthreads();
-        if (wk > 0) return;
-#pragma unroll
-        for (int w = 0; w < NWK - 1; w++) {
-            const float *p = join + (w * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
-            const float m = fmaxf(top, p[0]), ref = m == -INFINITY ? 0.f : m;
-            const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(p[0] - ref);
-            top = m;
-            sum = sum * f + p[64] * g;
-#pragma unroll
-            for (int db = 0; db < DB; db++)
-#pragma unroll
-                for (int r = 0; r < 16; r++) o[db][r] = o[db][r] * f + p[(2 + db * 16 + r) * 64] * g;
-        }
+            for (int r = 0; r < 16; r++) p[(2 + db * 16 + r) * 64] = o[db][r];
     }
-    if (row >= t.top || (!in && !a.fill)) return;
-    // a row without keys, and a row of no sequence: zeros
-    const bool some = in && hi > lo;
-    const float f = some ? 1.f / sum : 0.f, lse = some ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
-    const int64_t at = (int64_t)head * a.sq.rows + row;
-    if (a.splits > 1) {
-        const int64_t part = (int64_t)split * a.heads * a.sq.rows + at;
-        if (h == 0) a.part_lse[part] = lse;
-        if (some) store_row<float, DB>(o, f, a.part_o + part * a.dim, a.dim, lane);
-        return;
-    }
-    if (h == 0) a.lse[at] = lse;
-    if (!some) // not 0 * o: the row may hold what a zero does not clear
+    __syncthreads();
+    if (wk > 0) return;
 #pragma unroll
-        for (int db = 0; db < DB; db++) o[db] = f32x16{};
-    store_row<T, DB>(o, f, (T *)a.o + head * a.o_head + row * a.o_row, a.dim, lane);
+    for (int w = 0; w < NWK - 1; w++) {
+        const float *p = join + (w * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
+        const float m = fmaxf(top, p[0]), ref = m == -INFINITY ? 0.f : m;
+        const float f = __builtin_amdgcn_exp2f(top - ref), x = __builtin_amdgcn_exp2f(p[0] - ref);
+        top = m;
+        sum = sum * f + p[64] * x;
+#pragma unroll
+        for (int db = 0; db < DB; db++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) o[db][r] = o[db][r] * f + p[(2 + db * 16 + r) * 64] * x;
+    }
+    fwd_store<T, DB>(a, g, head, split, row, top, sum, o, lane);
 }
 
 // The splits of a row: weights exp(lse_s - lse).  A wave per row and head, blockIdx.x * 4 + wave over [heads][rows].
