@@ -321,7 +321,7 @@ typedef struct {
     int64_t stride;
 } he_rows;
 /* [rows][heads][dim], the last dimension dense: element (r, h, c) is at r * row + h * head + c.  Base and strides are multiples of 16
- * bytes; strides of an output are at least dim (inputs may repeat: 0). */
+ * bytes; strides of an output are at least dim (inputs may repeat: 0), row strides are below 2^24 bytes. */
 typedef struct {
     void *d;
     int64_t row, head;

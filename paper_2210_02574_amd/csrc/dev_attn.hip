@@ -10,6 +10,8 @@ typedef f16 T;
 typedef bf16 T;
 #endif
 
+static constexpr bool ATTN_WIDE = attn_wide(sizeof(T), HE_DIM);
+
 // F with the variant of cap and distance bias
 template <class F> static void by_mode(const AttnArgs &a, F f)
 {
@@ -33,7 +35,7 @@ static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned
             KLAUNCH_T(c, st, KID_ATTN_FEW, bytes, (k_attn_few<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
         else if (tile == 128)
             KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 1, mode>), grid, ATTN_THREADS, a);
-        else
+        else if constexpr (ATTN_WIDE)
             KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
     });
 }

@@ -117,7 +117,7 @@ int32_t attn_check(const he_attn *s)
 bool heads_ok(const he_heads *h, int32_t type)
 {
     const int64_t size = (int64_t)type_size(type);
-    return h && h->d && aligned(h->d, 16) && h->row >= 0 && h->head >= 0 && (h->row * size) % 16 == 0 && (h->head * size) % 16 == 0;
+    return h && h->d && aligned(h->d, 16) && h->row >= 0 && h->head >= 0 && h->row < (1 << 24) / size && (h->row * size) % 16 == 0 && (h->head * size) % 16 == 0;
 }
 // Buffers that are written: elements of different rows or heads have different addresses if the strides hold a row of a head each.
 bool out_ok(const he_heads *h, const he_attn *s, int64_t rows, int heads)
@@ -133,7 +133,7 @@ AttnPlan attn_plan(const he_attn *s)
 {
     AttnPlan p;
     const int64_t mean_q = s->q.count ? s->q.rows / s->q.count : 0, mean_k = s->q.count ? s->k.rows / s->q.count : 0;
-    p.tile = mean_q <= 32 ? 32 : mean_q <= 64 ? 64 : mean_q <= (getenv("QT") ? atoi(getenv("QT")) : 512) ? 128 : 256;
+    p.tile = mean_q <= 32 ? 32 : mean_q <= 64 ? 64 : mean_q < 1024 || !attn_wide(type_size(s->type), s->dim) ? 128 : 256;
     p.slots = tile_slots(s->q.rows, s->q.count, p.tile);
     const int64_t groups = p.slots * s->heads;
     p.splits = groups > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, mean_k / 256, 64})) : 1;

@@ -9,6 +9,11 @@ struct NormGradArgs;
 struct PoolArgs;
 struct PoolGradArgs;
 
+// Whether there are tiles of 256 queries, two blocks of 32 to a wave: they halve what is read of LDS for a product, and pay where the registers still
+// hold two waves per SIMD.  12 heads of 64 in bf16, tiles of 256 against 128: one sequence of 16384 1013 us, 1086; 16 of 2048 300, 312; 32 of 1024 146, 150;
+// 42 of 768 130, 112.  Heads of 128 (one wave per SIMD): 16384 1771 us, 1822; 4096 1095, 1059; 1024 378, 326.
+constexpr bool attn_wide(size_t type_size, int dim) { return type_size == 2 && dim <= 64; }
+
 struct AttnLaunch {
     // tile: queries of a work-group, 32, 64, 128 or 256
     void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);

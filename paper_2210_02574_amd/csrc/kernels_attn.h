@@ -68,42 +68,66 @@ __device__ __forceinline__ float pair_sum(float v)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
-// Tiles in LDS: rows of DP elements and 16 bytes more, which spreads the 16-byte reads of eight rows over all banks.
+// Tiles in LDS, rows of DP elements in 16-byte chunks.  LDS has 64 banks of 4 bytes, 16 chunks, and takes 16 lanes of a 16-byte read at a time: one
+// chunk of 16 rows; or 32 lanes of a transposing read: four neighbouring chunks of four rows.  Chunk c of row r is stored at c ^ twist(r), which gives
+// both of them 16 different places.
 template <class T, int DP> struct AttnTile {
-    static constexpr int ROW = DP + 16 / (int)sizeof(T); // elements
-    static constexpr int VEC = 16 / (int)sizeof(T);      // of a 16-byte access
+    static constexpr int VEC = 16 / (int)sizeof(T); // elements of a chunk
     static constexpr int CHUNKS = DP / VEC;
     typedef Vec<T, VEC> Chunk;
 
-    // 16-byte chunks of ROWS rows by `NT` threads: from memory to registers, zeros outside the rows [.., end) and the columns below dim ..
-    template <int ROWS, int NT> static constexpr int per() { return (ROWS * CHUNKS + NT - 1) / NT; }
-    template <int ROWS, int NT>
-    static __device__ __forceinline__ void load(Chunk (&c)[per<ROWS, NT>()], const T *base, int64_t stride, int first, int end, int dim, int tid)
+    static __device__ __forceinline__ int twist(int row)
     {
-#pragma unroll
-        for (int i = 0; i < per<ROWS, NT>(); i++) {
-            const int at = i * NT + tid, row = first + at / CHUNKS, col = (at % CHUNKS) * VEC;
-            Chunk x = {};
-            if (at < ROWS * CHUNKS && row < end && col < dim) x = *(const Chunk *)(base + row * stride + col);
-            c[i] = x;
-        }
+        // Four neighbouring rows four chunks apart, as far as the row's length does not do that by itself; rows four apart in the chunks between.
+        if constexpr (CHUNKS % 16 == 0) return (row & 3) << 2 | (row >> 2 & 3); // 256 bytes
+        if constexpr (CHUNKS % 8 == 0) return (row << 1 & 4) | (row >> 1 & 2) | (row >> 3 & 1);
+        return row >> 2 & 3; // 64 or 192
     }
+    static __device__ __forceinline__ int place(int row, int chunk) { return (row * CHUNKS + (chunk ^ twist(row))) * VEC; }
+
+    // ROWS rows by `NT` threads: from memory to registers, zeros for the rows from `end` on and the columns from dim on.  The reads go through a
+    // buffer descriptor whose length is that of the rows that are there: behind it they return zeros, without a comparison or an address in
+    // 64 bits per read (row strides are below 2^24 bytes).
+    template <int ROWS, int NT> static constexpr int per() { return (ROWS * CHUNKS + NT - 1) / NT; }
+    template <int ROWS, int NT> struct Reads {
+        unsigned at[per<ROWS, NT>()]; // bytes from the first row
+        __device__ __forceinline__ Reads(int64_t stride, int dim, int tid)
+        {
+#pragma unroll
+            for (int i = 0; i < per<ROWS, NT>(); i++) {
+                const int n = i * NT + tid, col = (n % CHUNKS) * VEC;
+                at[i] = n < ROWS * CHUNKS && col < dim ? (unsigned)(n / CHUNKS * (int)stride + col) * (unsigned)sizeof(T) : 0xfffffff0u;
+            }
+        }
+        __device__ __forceinline__ void load(Chunk (&c)[per<ROWS, NT>()], const T *base, int64_t stride, int first, int end, int dim) const
+        {
+            const int rows = min(max(end - first, 0), ROWS), bytes = rows ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)(base + first * stride), 0, bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < per<ROWS, NT>(); i++) c[i] = __builtin_bit_cast(Chunk, __builtin_amdgcn_raw_buffer_load_b128(r, at[i], 0, 0));
+        }
+    };
     // .. and from registers to LDS
     template <int ROWS, int NT> static __device__ __forceinline__ void store(const Chunk (&c)[per<ROWS, NT>()], T *lds, int tid)
     {
 #pragma unroll
         for (int i = 0; i < per<ROWS, NT>(); i++) {
             const int at = i * NT + tid;
-            if (at < ROWS * CHUNKS) *(Chunk *)(lds + (at / CHUNKS) * ROW + (at % CHUNKS) * VEC) = c[i];
+            if (at < ROWS * CHUNKS) *(Chunk *)(lds + place(at / CHUNKS, at % CHUNKS)) = c[i];
         }
     }
-    // operand A or B: lane's row `row0 + l mod 32`, columns 16 kk + 8 (l / 32) ..
+    // operand A or B: lane's row `row0 + l mod 32` (row0: a multiple of 32), columns 16 kk + 8 (l / 32) ..
     static __device__ __forceinline__ Vec<T, 8> rows(const T *lds, int row0, int kk, int lane)
     {
-        const T *p = lds + (row0 + (lane & 31)) * ROW + 16 * kk + 8 * (lane >> 5);
-        return eight(p);
+        const int row = lane & 31, col = 16 * kk + 8 * (lane >> 5);
+        const T *p = lds + row0 * DP;
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4 *)(p + place(row, col / VEC)), b = *(const f32x4 *)(p + place(row, col / VEC + 1));
+            return Vec<T, 8>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        } else
+            return *(const Vec<T, 8> *)(p + place(row, col / VEC));
     }
-    static __device__ __forceinline__ Vec<T, 8> eight(const T *p)
+    static __device__ __forceinline__ Vec<T, 8> eight(const T *p) // of memory
     {
         if constexpr (sizeof(T) == 4) {
             const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
@@ -111,27 +135,26 @@ template <class T, int DP> struct AttnTile {
         } else
             return *(const Vec<T, 8> *)p;
     }
-    // operand A of a transposed tile: lane's column 32 db + l mod 32, the rows row0 + .. in slot order
+    // operand A of a transposed tile: lane's column 32 db + l mod 32, the rows row0 + .. (row0: a multiple of 16) in slot order
     static __device__ __forceinline__ Vec<T, 8> cols(const T *lds, int row0, int db, int lane)
     {
         const int h = lane >> 5;
+        const T *p = lds + row0 * DP;
         if constexpr (sizeof(T) == 4) {
-            const T *p = lds + (row0 + 4 * h) * ROW + 32 * db + (lane & 31);
+            const int col = 32 * db + (lane & 31);
             Vec<T, 8> x;
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                x[e] = p[e * ROW];
-                x[4 + e] = p[(8 + e) * ROW];
-            }
+            for (int e = 0; e < 8; e++) x[e] = p[place(4 * h + (e & 3) + 8 * (e >> 2), col / VEC) + col % VEC];
             return x;
         } else {
             // 16 lanes read four rows of 16 elements, four lanes to a row; lane j of them gets element j of each row
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef short s8 __attribute__((ext_vector_type(8)));
             typedef __attribute__((address_space(3))) s4 *Ptr;
-            const int j = lane & 15;
-            const T *p = lds + (row0 + 4 * h + (j >> 2)) * ROW + 32 * db + (lane & 16) + (j & 3) * 4;
-            const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + 8 * ROW));
+            const int j = lane & 15, col = 32 * db + (lane & 16) + (j & 3) * 4;
+            const int row = 4 * h + (j >> 2);
+            const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + place(row, col / VEC) + col % VEC));
+            const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + place(row + 8, col / VEC) + col % VEC));
             const s8 x = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             return __builtin_bit_cast(Vec<T, 8>, x);
         }
@@ -238,7 +261,7 @@ struct FwdRange {
     int back;   // a query row's position among the keys, the first at 0, is its number plus this
     __device__ __forceinline__ FwdRange(const AttnArgs &a, const TileRows &t, int split, int tile) : t(t)
     {
-        kb = span_begin(a.sk, t.seq), ke = max(span_end(a.sk, t.seq), kb);
+        kb = t.other_begin, ke = t.other_end;
         back = (ke - kb) - t.end;
         if (t.first >= t.end || t.top <= t.begin) ke = kb; // a tile between sequences: nothing to sum
         const int tiles = (ke - kb + tile - 1) / tile, per = (tiles + a.splits - 1) / a.splits;
@@ -287,10 +310,13 @@ __device__ __forceinline__ float col_max(const f32x16 &s)
 // independent of this step's exponentials, so that matrix and vector instructions of one wave overlap.  Tiles of BN keys pass through three LDS
 // stages, which takes one barrier a tile: the stage that a wave overwrites is the one that every wave has left before the last barrier.
 template <class T, int DP, int QB> struct AttnFwd {
-    static constexpr int BM = 128 * QB, BN = DP * sizeof(T) > 384 ? 32 : 64, SUB = BN / 32;
-    static constexpr int TILE = BN * AttnTile<T, DP>::ROW; // elements
+    // Two blocks of queries halve what is read of LDS for a product; heads above 64 then take the registers of one wave per SIMD, everything
+    // else leaves room for two or three, and its stages for as many work-groups.
+    static constexpr int BM = 128 * QB, BN = QB == 1 && DP * sizeof(T) > 128 ? 32 : 64, SUB = BN / 32;
+    static constexpr int WAVES = sizeof(T) == 4 || (QB == 2 && DP > 64) ? 1 : 2;
+    static constexpr int TILE = BN * DP; // elements
 };
-template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn(AttnArgs a)
+template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_THREADS, (AttnFwd<T, DP, QB>::WAVES)) void k_attn(AttnArgs a)
 {
     typedef AttnFwd<T, DP, QB> F;
     typedef AttnTile<T, DP> L;
@@ -299,7 +325,7 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 
     int head, slot, split;
     if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
-    const TileRows t = tile_rows(a.sq, slot, F::BM);
+    const TileRows t = tile_rows(a.sq, a.sk, slot, F::BM);
     if (t.first >= t.top) return;
     const FwdRange g(a, t, split, BN);
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -308,9 +334,10 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
     const T *const q = (const T *)a.q + head * a.q_head;
     const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
     typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
+    const typename L::template Reads<BN, ATTN_THREADS> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
     const auto load = [&](int j) {
-        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j, g.hi, a.dim, tid);
-        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j, g.hi, a.dim, tid);
+        reads_k.load(ck, k, a.k_row, j, g.hi, a.dim);
+        reads_v.load(cv, v, a.v_row, j, g.hi, a.dim);
     };
     const auto store = [&](int stage) {
         L::template store<BN, ATTN_THREADS>(ck, lds[stage][0], tid);
@@ -335,16 +362,25 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 #pragma unroll
         for (int db = 0; db < DB; db++) o[b][db] = f32x16{};
     }
-    // scores of the 32 keys from j on, rows `at` .. of a stage
-    const auto products = [&](f32x16 (&x)[QB], const T *lk, int at, int j) {
+    // operands of the 32 keys in rows `at` .. of a stage: keys, and values by halves
+    Vec<T, 8> fk[KK], fv[2][DB];
+    const auto read_keys = [&](const T *lk, int at) {
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) fk[kk] = L::rows(lk, at, kk, lane);
+    };
+    const auto read_values = [&](const T *lv, int at, int half) {
+#pragma unroll
+        for (int db = 0; db < DB; db++) fv[half][db] = L::cols(lv, at + 16 * half, db, lane);
+    };
+    const auto products = [&](f32x16 (&x)[QB]) {
 #pragma unroll
         for (int b = 0; b < QB; b++) x[b] = f32x16{};
 #pragma unroll
-        for (int kk = 0; kk < KK; kk++) {
-            const Vec<T, 8> f = L::rows(lk, at, kk, lane);
+        for (int kk = 0; kk < KK; kk++)
 #pragma unroll
-            for (int b = 0; b < QB; b++) x[b] = AttnType<T>::mma(f, fq[b][kk], x[b]);
-        }
+            for (int b = 0; b < QB; b++) x[b] = AttnType<T>::mma(fk[kk], fq[b][kk], x[b]);
+    };
+    const auto finish = [&](f32x16 (&x)[QB], int j) { // of the keys from j on
 #pragma unroll
         for (int b = 0; b < QB; b++) scores(x[b], (float)(row0 + 32 * b + g.back - (j - g.kb)), h);
     };
@@ -366,28 +402,24 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
                 for (int r = 0; r < 16; r++) o[b][db][r] *= f;
         }
     };
-    // exponentials of s, and their products with the values in rows `at` .. of a stage
-    const auto values = [&](const T *lv, int at) {
+    Vec<T, 8> p[2][QB];
+    const auto exponentials = [&](int half) {
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            Vec<T, 8> p[QB];
+        for (int b = 0; b < QB; b++) {
+            const float ref = top[b] == -INFINITY ? 0.f : top[b];
 #pragma unroll
-            for (int b = 0; b < QB; b++) {
-                const float ref = top[b] == -INFINITY ? 0.f : top[b];
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[b][8 * half + e], c2, -ref));
-                    sum[b] += x;
-                    p[b][e] = (T)x;
-                }
-            }
-#pragma unroll
-            for (int db = 0; db < DB; db++) {
-                const Vec<T, 8> f = L::cols(lv, at + 16 * half, db, lane);
-#pragma unroll
-                for (int b = 0; b < QB; b++) o[b][db] = AttnType<T>::mma(f, p[b], o[b][db]);
+            for (int e = 0; e < 8; e++) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[b][8 * half + e], c2, -ref));
+                sum[b] += x;
+                p[half][b][e] = (T)x;
             }
         }
+    };
+    const auto weigh = [&](int half) {
+#pragma unroll
+        for (int db = 0; db < DB; db++)
+#pragma unroll
+            for (int b = 0; b < QB; b++) o[b][db] = AttnType<T>::mma(fv[half][db], p[half][b], o[b][db]);
     };
 
     if (g.hi > g.lo) {
@@ -395,7 +427,9 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
         store(0);
         load(g.lo + BN);
         __syncthreads();
-        products(s, lds[0][0], 0, g.lo);
+        read_keys(lds[0][0], 0);
+        products(s);
+        finish(s, g.lo);
         if (blocks > 1)
 #pragma unroll
             for (int b = 0; b < QB; b++) m[b] = col_max(s[b]);
@@ -404,33 +438,47 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 #pragma unroll
             for (int sub = 0; sub < SUB; sub++) {
                 const int next = stage == 2 ? 0 : stage + 1;
-                if (sub == SUB - 1) { // the next step's keys are in the next tile
+                const bool last = sub == SUB - 1;
+                if (last) { // the next step's keys are in the next tile
                     store(next);
                     load(g.lo + 32 * i + BN + 32);
                     __syncthreads();
                 }
+                // operands are asked for ahead of the products that take them: a lone wave waits for LDS otherwise
+                read_keys(lds[last ? next : stage][0], last ? 0 : 32 * (sub + 1));
+                read_values(lds[stage][1], 32 * sub, 0);
+                read_values(lds[stage][1], 32 * sub, 1);
                 rescale();
                 f32x16 n[QB];
-                products(n, sub == SUB - 1 ? lds[next][0] : lds[stage][0], sub == SUB - 1 ? 0 : 32 * (sub + 1), g.lo + 32 * (i + 1));
-                values(lds[stage][1], 32 * sub);
+                products(n);
+                exponentials(0);
+                weigh(0);
+                exponentials(1);
+                weigh(1);
+                finish(n, g.lo + 32 * (i + 1));
 #pragma unroll
                 for (int b = 0; b < QB; b++) {
                     s[b] = n[b];
                     m[b] = col_max(s[b]);
                 }
                 i++;
-                if (sub == SUB - 1) stage = next;
+                if (last) stage = next;
                 if (i + 1 >= blocks) break;
             }
         }
         const int left = g.hi - g.lo - 32 * i; // the last 32 keys may be fewer
+        read_values(lds[stage][1], 32 * (i % SUB), 0);
+        read_values(lds[stage][1], 32 * (i % SUB), 1);
 #pragma unroll
         for (int b = 0; b < QB; b++) {
             if (left < 32) mask_rows(s[b], left, h);
             m[b] = col_max(s[b]);
         }
         rescale();
-        values(lds[stage][1], 32 * (i % SUB));
+        exponentials(0);
+        weigh(0);
+        exponentials(1);
+        weigh(1);
     }
 #pragma unroll
     for (int b = 0; b < QB; b++) fwd_store<T, DB>(a, g, head, split, row0 + 32 * b, top[b], pair_sum(sum[b]), o[b], lane);
@@ -440,7 +488,7 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 // still keep four waves busy.
 template <class T, int DP, int NWQ> struct AttnFew {
     static constexpr int NWK = 4 / NWQ, BM = 32 * NWQ, BN = 32 * NWK;
-    static constexpr int TILE = BN * AttnTile<T, DP>::ROW;                // elements of a tile
+    static constexpr int TILE = BN * DP; // elements of a tile
     static constexpr int JOIN = (NWK - 1) * NWQ * 64 * (DP / 2 + 2);      // floats
     static constexpr int LDS = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
 };
@@ -454,7 +502,7 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
 
     int head, slot, split;
     if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
-    const TileRows t = tile_rows(a.sq, slot, F::BM);
+    const TileRows t = tile_rows(a.sq, a.sk, slot, F::BM);
     if (t.first >= t.top) return;
     const FwdRange g(a, t, split, BN);
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -464,8 +512,9 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     const T *const q = (const T *)a.q + head * a.q_head;
     const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
     typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
-    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, g.lo, g.hi, a.dim, tid);
-    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, g.lo, g.hi, a.dim, tid);
+    const typename L::template Reads<BN, ATTN_THREADS> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
+    reads_k.load(ck, k, a.k_row, g.lo, g.hi, a.dim);
+    reads_v.load(cv, v, a.v_row, g.lo, g.hi, a.dim);
     Vec<T, 8> fq[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) fq[kk] = L::own(q, a.q_row, row, row < t.top && row >= t.begin && row < t.end, kk, a.dim, lane);
@@ -482,8 +531,8 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
         L::template store<BN, ATTN_THREADS>(ck, lk, tid);
         L::template store<BN, ATTN_THREADS>(cv, lv, tid);
         __syncthreads();
-        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, g.hi, a.dim, tid); // the next tile is under way meanwhile
-        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, g.hi, a.dim, tid);
+        reads_k.load(ck, k, a.k_row, j0 + BN, g.hi, a.dim); // the next tile is under way meanwhile
+        reads_v.load(cv, v, a.v_row, j0 + BN, g.hi, a.dim);
         const int j = j0 + 32 * wk; // the wave's keys of the tile
         if (j >= g.hi) continue;
         f32x16 s = {};
@@ -590,17 +639,17 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
 {
     typedef AttnTile<T, DP> L;
     constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lk[BN * L::ROW], lv[BN * L::ROW];
+    __shared__ __attribute__((aligned(16))) T lk[BN * DP], lv[BN * DP];
 
     int head, slot, split;
     if (!attn_work(a, a.slots, head, slot, split)) return;
-    const TileRows t = tile_rows(a.sq, slot, 128);
+    const TileRows t = tile_rows(a.sq, a.sk, slot, 128);
     if (t.first >= t.top) return;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = t.first + 32 * wave + (lane & 31);
     const bool in = row < t.top && row >= t.begin && row < t.end;
-    int kb = span_begin(a.sk, t.seq), ke = span_end(a.sk, t.seq);
-    ke = max(ke, kb);
+    const int kb = t.other_begin;
+    int ke = t.other_end;
     const int pos0 = row - t.begin + (ke - kb) - (t.end - t.begin);
     if (t.first >= t.end || t.top <= t.begin) ke = kb;
 
@@ -628,15 +677,16 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
     for (int db = 0; db < DB; db++) dq[db] = f32x16{};
 
     typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
-    L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, kb, ke, a.dim, tid);
-    L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, kb, ke, a.dim, tid);
+    const typename L::template Reads<BN, ATTN_THREADS> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
+    reads_k.load(ck, k, a.k_row, kb, ke, a.dim);
+    reads_v.load(cv, v, a.v_row, kb, ke, a.dim);
     for (int j0 = kb; j0 < ke; j0 += BN) {
         __syncthreads();
         L::template store<BN, ATTN_THREADS>(ck, lk, tid);
         L::template store<BN, ATTN_THREADS>(cv, lv, tid);
         __syncthreads();
-        L::template load<BN, ATTN_THREADS>(ck, k, a.k_row, j0 + BN, ke, a.dim, tid);
-        L::template load<BN, ATTN_THREADS>(cv, v, a.v_row, j0 + BN, ke, a.dim, tid);
+        reads_k.load(ck, k, a.k_row, j0 + BN, ke, a.dim);
+        reads_v.load(cv, v, a.v_row, j0 + BN, ke, a.dim);
         f32x16 s = {}, dp = {}, th;
 #pragma unroll
         for (int kk = 0; kk < KK; kk++) {
@@ -673,18 +723,18 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
 {
     typedef AttnTile<T, DP> L;
     constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lq[BN * L::ROW], lg[BN * L::ROW];
+    __shared__ __attribute__((aligned(16))) T lq[BN * DP], lg[BN * DP];
     __shared__ __attribute__((aligned(16))) float stat[2][BN];
 
     int kh, slot, split;
     if (!attn_work(a, a.slots, kh, slot, split)) return;
-    const TileRows t = tile_rows(a.sk, slot, 128);
+    const TileRows t = tile_rows(a.sk, a.sq, slot, 128);
     if (t.first >= t.top) return;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = t.first + 32 * wave + (lane & 31);
     const bool in = row < t.top && row >= t.begin && row < t.end;
-    int qb = span_begin(a.sq, t.seq), qe = span_end(a.sq, t.seq);
-    qe = max(qe, qb);
+    const int qb = t.other_begin;
+    int qe = t.other_end;
     const int pos0 = row - t.begin - (t.end - t.begin) + (qe - qb); // the row's position among the queries, the first at 0
     if (t.first >= t.end || t.top <= t.begin) qe = qb;
 
@@ -695,6 +745,7 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
         fk[kk] = L::own(k, a.k_row, row, in, kk, a.dim, lane);
         fv[kk] = L::own(v, a.v_row, row, in, kk, a.dim, lane);
     }
+    const typename L::template Reads<BN, ATTN_THREADS> reads_q(a.q_row, a.dim, tid), reads_g(a.go_row, a.dim, tid);
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
@@ -708,8 +759,8 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
         typename L::Chunk cq[L::template per<BN, ATTN_THREADS>()], cg[L::template per<BN, ATTN_THREADS>()];
         float cs = 0.f;
         const auto load = [&](int i0) {
-            L::template load<BN, ATTN_THREADS>(cq, q, a.q_row, i0, qe, a.dim, tid);
-            L::template load<BN, ATTN_THREADS>(cg, go, a.go_row, i0, qe, a.dim, tid);
+            reads_q.load(cq, q, a.q_row, i0, qe, a.dim);
+            reads_g.load(cg, go, a.go_row, i0, qe, a.dim);
             const int i = i0 + (tid & 31);
             if (tid < 32) cs = i < qe ? lse[i] * LOG2E : INFINITY; // a missing query: p = 0
             else if (tid < 64) cs = i < qe ? delta[i] : 0.f;

@@ -28,7 +28,7 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
     const int col = (blockIdx.y * CL + cl) * VEC;
     int lo, hi, n;
     if (a.tile) {
-        const TileRows t = tile_rows(a.s, blockIdx.x, a.tile);
+        const TileRows t = tile_rows(a.s, a.s, blockIdx.x, a.tile);
         lo = max(t.first, t.begin), hi = min(t.top, t.end), n = 1;
         if (lo >= hi) return; // k_pool_join does not ask for it
     } else {
@@ -71,14 +71,14 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
     }
 }
 
-// grid (sequences, columns / 256): the tiles of a sequence are those of the slots c / tile + i .. that reach into it.
+// grid (sequences, columns / 256): the tiles of a sequence are those of the slots tile_slot(c, i) .. that reach into it.
 static __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 {
     const int col = blockIdx.y * 256 + threadIdx.x, i = blockIdx.x;
     if (col >= a.width) return;
     const int begin = span_begin(a.s, i), end = span_end(a.s, i), c = i ? begin : 0, top = i + 1 < a.s.count ? span_begin(a.s, i + 1) : a.s.rows;
     const int stop = min(end, top); // a tile ends at the next sequence's begin
-    const int64_t slot = c / a.tile + i;
+    const int64_t slot = tile_slot(c, i, a.tile);
     float s = 0.f;
     if (stop > begin) {
         const int first = (begin - c) / a.tile, last = (stop - 1 - c) / a.tile;
@@ -92,7 +92,7 @@ static __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 #define POOL_TILE 32
 template <class T, int VEC> __global__ __launch_bounds__(256) void k_pool_grad(PoolGradArgs a, int CL)
 {
-    const TileRows t = tile_rows(a.s, blockIdx.x, POOL_TILE);
+    const TileRows t = tile_rows(a.s, a.s, blockIdx.x, POOL_TILE);
     if (t.first >= t.top) return;
     const int RG = 256 / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
     const int col = (blockIdx.y * CL + cl) * VEC, n = t.end - t.begin;
