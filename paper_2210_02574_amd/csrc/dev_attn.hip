@@ -43,13 +43,23 @@ static void attn_join(he_ctx *c, hipStream_t st, double bytes, unsigned grid, co
 {
     KLAUNCH(c, st, KID_ATTN_JOIN, bytes, (k_attn_join<T>), grid, a);
 }
-static void attn_grad_q(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
+static void attn_grad_q(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a)
 {
-    by_mode(a, [&](auto mode) { KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, mode>), grid, ATTN_THREADS, a); });
+    by_mode(a, [&](auto mode) {
+        if (tile == 64)
+            KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, 2, mode>), grid, 128, a);
+        else
+            KLAUNCH_T(c, st, KID_ATTN_GRAD_Q, bytes, (k_attn_grad_q<T, HE_DIM, 4, mode>), grid, 256, a);
+    });
 }
-static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
+static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a)
 {
-    by_mode(a, [&](auto mode) { KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, mode>), grid, ATTN_THREADS, a); });
+    by_mode(a, [&](auto mode) {
+        if (tile == 32)
+            KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 1, mode>), grid, 64, a);
+        else
+            KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 4, mode>), grid, 256, a);
+    });
 }
 
 #define NAME_(t, d) attn_launch_##t##_##d

@@ -139,6 +139,12 @@ AttnPlan attn_plan(const he_attn *s)
     p.splits = groups > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, mean_k / 256, 64})) : 1;
     return p;
 }
+// Rows of a work-group of the backward pass.  Short sequences leave a part of a tile empty and a work-group little to do between its first loads and its last
+// stores: small ones then waste less and more of them are resident.  12 heads of 64 in bf16, dq with 64 rows against 128: 1000 sequences of 18 rows on average
+// 49 us, 79; 200 of 56 30, 34; 64 of 290 62, 63; 32 of 570 92, 88; one of 8192 415, 366.  dk and dv with 32 against 128: 42 us, 101; 30, 42; 77, 85; 123, 129;
+// with 64 the last one 607, 500.
+int grad_tile_q(const he_spans &s) { return s.rows / s.count < 256 ? 64 : 128; }
+int grad_tile_k(const he_spans &s) { return s.rows / s.count < 512 ? 32 : 128; }
 size_t attn_bytes(const he_attn *s, bool backward)
 {
     const size_t rows = (size_t)s->q.rows * s->heads;
@@ -364,14 +370,15 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     a.delta = (float *)d_ws;
     AttnArgs b = a;
     unsigned grid_q = 0, grid_kv = 0;
-    if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, 128), s->heads, grid_q)) return HE_EINVAL;
-    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, 128), s->kv_heads, grid_kv)) return HE_EINVAL;
+    const int tile_q = grad_tile_q(s->q), tile_k = grad_tile_k(s->k);
+    if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, tile_q), s->heads, grid_q)) return HE_EINVAL;
+    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, tile_k), s->kv_heads, grid_kv)) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
     const AttnLaunch &l = attn_launch(s->type, s->dim);
     const double size = (double)type_size(s->type) * s->dim, qb = s->q.rows * s->heads * size, kb = s->k.rows * s->kv_heads * size;
-    if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, grid_q, a);
-    if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, grid_kv, b);
+    if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, tile_q, grid_q, a);
+    if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, tile_k, grid_kv, b);
     return launched(ctx);
 }

@@ -17,6 +17,7 @@
 // scaled loss, as everywhere in fp16.
 #pragma once
 #include "enc_common.h"
+#include <type_traits>
 
 struct AttnArgs {
     const void *q, *k, *v, *o_in, *go; // o_in, go: the forward pass's o and the gradient that reaches it (backward)
@@ -195,7 +196,8 @@ template <class T, int DB> __device__ __forceinline__ void store_row(const f32x1
 }
 
 // Work-group -> (head, slot, split), neighbours on one of the eight dies' caches: work-groups go to the dies in turn, so die d is given
-// the d-th eighth of the work, in which tiles of one head, which read the same keys, come one after the other.
+// the d-th eighth of the work, in which tiles of one head, which read the same keys, come one after the other.  (All heads of a tile one after the
+// other instead: 2 sequences of 16384 4 % slower, 64 of up to 512 2 to 5 %.)
 __device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, int &head, int &slot, int &split)
 {
     const unsigned w = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
@@ -224,8 +226,8 @@ template <class T, int MODE> struct Scores {
     }
     // what is left to multiply scores with: without a cap or a bias the exponential's fma does it
     __device__ __forceinline__ float rest() const { return MODE ? 1.f : out; }
-    // pos: position of the lane's own row minus the one of row 0 of the block: the distance of row m is |pos - m|.  th: the tanh, for the backward pass
-    __device__ __forceinline__ void operator()(f32x16 &c, float pos, int h, f32x16 *th = nullptr) const
+    // pos: position of the lane's own row minus the one of row 0 of the block: the distance of row m is |pos - m|
+    __device__ __forceinline__ void operator()(f32x16 &c, float pos, int h) const
     {
         if constexpr (MODE != 0) {
             const float p = pos - (float)(4 * h);
@@ -235,11 +237,9 @@ template <class T, int MODE> struct Scores {
                 if constexpr (MODE & MODE_CAP) {
                     if constexpr (sizeof(T) == 4) {
                         x = tanhf(c[r] * in);
-                        if (th) (*th)[r] = x;
                         x *= out;
                     } else {
                         const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c[r] * in));
-                        if (th) (*th)[r] = fmaf(-2.f, g, 1.f);
                         x = fmaf(-2.f * out, g, out);
                     }
                 } else
@@ -632,30 +632,76 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
     if (lane + 64 < a.dim) o[lane + 64] = (T)(o1 * f);
 }
 
-// ---- backward: dq -----------------------------------------------------------------------------------------------------
+// ---- backward ---------------------------------------------------------------------------------------------------------
 //
-// Queries as columns, keys stream by.  Also leaves delta for the kernel of dk and dv, which runs after it.
-template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_q(AttnArgs a)
+// NW waves of 32 rows each (queries for dq, keys for dk and dv); the other axis streams by in blocks of 32 rows through two LDS stages, one barrier a
+// block.  delta is where the sums of do . v begin, lse is part of the exponential's fma: one subtraction less each.  A lone wave hides little, so
+// registers are kept for more of them: three per SIMD for dq and two for dk and dv, with heads up to 64.  (Row operands read a block ahead, at the
+// price of a wave: dq of one sequence of 8192, 12 heads of 64, 484 us instead of 424.)  The next block goes to LDS ahead of the barrier at the block's
+// beginning for dq, in its middle for dk and dv, whose barrier is there too (at the beginning: 578 us instead of 500).
+template <class T, int DP> struct AttnGrad {
+    static constexpr int TILE = 32 * DP;
+    static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : DP > 64 ? 2 : 3, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2; // per SIMD
+};
+// What the backward pass makes of one score: x: the product, rest: what is added in units of log2 (-lse).  Gives p and the factor of ds (1 without a cap;
+// a quarter of 1 - tanh^2 for 16-bit types: 1 / (1 + e^2y) times 1 minus that).
+template <class T, int MODE> struct GradScore {
+    float in, out, slope;
+    __device__ __forceinline__ GradScore(const AttnArgs &a, int head)
+    {
+        const Scores<T, MODE> s(a, head);
+        out = s.out;
+        if (MODE & MODE_CAP) in = s.in;
+        if (MODE & MODE_SLOPE) slope = s.slope;
+    }
+    // what ds lacks at the end
+    static __device__ __forceinline__ float scale(const AttnArgs &a) { return (MODE & MODE_CAP) && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
+    __device__ __forceinline__ float p(float x, float rest, float dist, float &factor) const
+    {
+        if constexpr (MODE & MODE_SLOPE) rest = fmaf(-slope, fabsf(dist), rest);
+        if constexpr (MODE & MODE_CAP) {
+            if constexpr (sizeof(T) == 4) {
+                const float th = tanhf(x * in);
+                factor = fmaf(-th, th, 1.f);
+                return __builtin_amdgcn_exp2f(fmaf(th, out, rest));
+            }
+            const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * in));
+            factor = fmaf(-g, g, g);
+            return __builtin_amdgcn_exp2f(fmaf(-2.f * out, g, rest)); // `rest` has cap in it
+        }
+        return __builtin_amdgcn_exp2f(fmaf(x, out, rest));
+    }
+    // rest from lse
+    __device__ __forceinline__ float rest(float lse) const { return (MODE & MODE_CAP) && sizeof(T) == 2 ? out - lse * LOG2E : -lse * LOG2E; }
+};
+
+// dq: queries as columns.  Also leaves -delta for the kernel of dk and dv, which runs after it.
+template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP>::WAVES_Q)) void k_attn_grad_q(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
-    constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lk[BN * DP], lv[BN * DP];
+    constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP>::TILE];
 
     int head, slot, split;
     if (!attn_work(a, a.slots, head, slot, split)) return;
-    const TileRows t = tile_rows(a.sq, a.sk, slot, 128);
+    const TileRows t = tile_rows(a.sq, a.sk, slot, 32 * NW);
     if (t.first >= t.top) return;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = t.first + 32 * wave + (lane & 31);
     const bool in = row < t.top && row >= t.begin && row < t.end;
-    const int kb = t.other_begin;
-    int ke = t.other_end;
-    const int pos0 = row - t.begin + (ke - kb) - (t.end - t.begin);
-    if (t.first >= t.end || t.top <= t.begin) ke = kb;
+    const int kb = t.other_begin, ke = t.first >= t.end || t.top <= t.begin ? kb : t.other_end;
+    const int pos0 = row - t.end + (t.other_end - kb);
 
     const T *const q = (const T *)a.q + head * a.q_head, *const go = (const T *)a.go + head * a.go_head;
     const T *const oi = (const T *)a.o_in + head * a.oi_head;
     const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    const typename L::template Reads<32, NT> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
+    typename L::Chunk ck[L::template per<32, NT>()], cv[L::template per<32, NT>()];
+    const auto load = [&](int j) {
+        reads_k.load(ck, k, a.k_row, j, ke, a.dim);
+        reads_v.load(cv, v, a.v_row, j, ke, a.dim);
+    };
+    load(kb);
     Vec<T, 8> fq[KK], fg[KK];
     float delta = 0.f;
 #pragma unroll
@@ -664,149 +710,171 @@ template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) 
         fg[kk] = L::own(go, a.go_row, row, in, kk, a.dim, lane);
         const Vec<T, 8> x = L::own(oi, a.oi_row, row, in, kk, a.dim, lane);
 #pragma unroll
-        for (int e = 0; e < 8; e++) delta += (float)x[e] * (float)fg[kk][e];
+        for (int e = 0; e < 8; e++) delta -= (float)x[e] * (float)fg[kk][e];
     }
     delta = pair_sum(delta);
+    const GradScore<T, MODE> score(a, head);
     const int64_t at = (int64_t)head * a.sq.rows + row;
     if (in && h == 0) a.delta[at] = delta;
-    const float lse = in ? a.lse[at] * LOG2E : INFINITY; // rows of no sequence: p = 0
-    const Scores<T, MODE> scores(a, head);
-    const float c2 = scores.rest();
+    const float rest = in ? score.rest(a.lse[at]) : -INFINITY; // rows of no sequence: p = 0
     f32x16 dq[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dq[db] = f32x16{};
 
-    typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
-    const typename L::template Reads<BN, ATTN_THREADS> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
-    reads_k.load(ck, k, a.k_row, kb, ke, a.dim);
-    reads_v.load(cv, v, a.v_row, kb, ke, a.dim);
-    for (int j0 = kb; j0 < ke; j0 += BN) {
+    int stage = 0;
+    const auto block = [&](int j, auto tail) { // the 32 keys from j on
+        L::template store<32, NT>(ck, lds[stage][0], tid);
+        L::template store<32, NT>(cv, lds[stage][1], tid);
         __syncthreads();
-        L::template store<BN, ATTN_THREADS>(ck, lk, tid);
-        L::template store<BN, ATTN_THREADS>(cv, lv, tid);
-        __syncthreads();
-        reads_k.load(ck, k, a.k_row, j0 + BN, ke, a.dim);
-        reads_v.load(cv, v, a.v_row, j0 + BN, ke, a.dim);
-        f32x16 s = {}, dp = {}, th;
+        if (j + 32 < ke) load(j + 32);
+        f32x16 s = {}, dp;
+#pragma unroll
+        for (int r = 0; r < 16; r++) dp[r] = delta;
 #pragma unroll
         for (int kk = 0; kk < KK; kk++) {
-            s = AttnType<T>::mma(L::rows(lk, 0, kk, lane), fq[kk], s);
-            dp = AttnType<T>::mma(L::rows(lv, 0, kk, lane), fg[kk], dp);
+            s = AttnType<T>::mma(L::rows(lds[stage][0], 0, kk, lane), fq[kk], s);
+            dp = AttnType<T>::mma(L::rows(lds[stage][1], 0, kk, lane), fg[kk], dp);
         }
-        scores(s, (float)(pos0 - (j0 - kb)), h, &th);
+        const float pos = (float)(pos0 - (j - kb) - 4 * h);
+        Vec<T, 8> d[2];
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -lse));
-            if (j0 + BN > ke && j0 + 8 * (r >> 2) + 4 * h + (r & 3) >= ke) p = 0.f; // exp of a missing key's score may be anything
-            float d = p * (dp[r] - delta);
-            if (MODE & MODE_CAP) d *= 1.f - th[r] * th[r];
-            s[r] = d; // the scale is put on at the end
+            const int m = 8 * (r >> 2) + (r & 3);
+            float f = 1.f, p = score.p(s[r], rest, pos - (float)m, f);
+            if (tail && m + 4 * h >= ke - j) p = 0.f; // a missing key's score may be anything
+            p *= dp[r];
+            if (MODE & MODE_CAP) p *= f;
+            d[r >> 3][r & 7] = (T)p; // the scale is put on at the end
         }
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const Vec<T, 8> d = round8<T>(s, half);
+        for (int half = 0; half < 2; half++)
 #pragma unroll
-            for (int db = 0; db < DB; db++) dq[db] = AttnType<T>::mma(L::cols(lk, 16 * half, db, lane), d, dq[db]);
-        }
-    }
+            for (int db = 0; db < DB; db++) dq[db] = AttnType<T>::mma(L::cols(lds[stage][0], 16 * half, db, lane), d[half], dq[db]);
+        stage ^= 1;
+    };
+    int j = kb;
+    for (; j + 32 <= ke; j += 32) block(j, std::false_type{});
+    if (j < ke) block(j, std::true_type{});
     if (row >= t.top || (!in && !a.fill)) return;
     if (!in || ke == kb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dq[db] = f32x16{};
-    store_row<T, DB>(dq, a.scale, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
+    store_row<T, DB>(dq, score.scale(a), (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
 }
 
-// ---- backward: dk, dv ---------------------------------------------------------------------------------------------------
-//
-// Keys as columns, the queries of all heads that share the key head stream by.
-template <class T, int DP, int MODE> __global__ __launch_bounds__(ATTN_THREADS) void k_attn_grad_kv(AttnArgs a)
+// dk, dv: keys as columns, the queries of all heads that share the key head stream by.
+template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP>::WAVES_KV)) void k_attn_grad_kv(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
-    constexpr int BN = 32, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lq[BN * DP], lg[BN * DP];
-    __shared__ __attribute__((aligned(16))) float stat[2][BN];
+    constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP>::TILE];
+    __shared__ __attribute__((aligned(16))) float stat[2][2][32]; // what is added to scores, -delta
 
     int kh, slot, split;
     if (!attn_work(a, a.slots, kh, slot, split)) return;
-    const TileRows t = tile_rows(a.sk, a.sq, slot, 128);
+    const TileRows t = tile_rows(a.sk, a.sq, slot, 32 * NW);
     if (t.first >= t.top) return;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = t.first + 32 * wave + (lane & 31);
     const bool in = row < t.top && row >= t.begin && row < t.end;
-    const int qb = t.other_begin;
-    int qe = t.other_end;
-    const int pos0 = row - t.begin - (t.end - t.begin) + (qe - qb); // the row's position among the queries, the first at 0
-    if (t.first >= t.end || t.top <= t.begin) qe = qb;
+    const int qb = t.other_begin, qe = t.first >= t.end || t.top <= t.begin ? qb : t.other_end;
+    const int pos0 = row - t.end + (t.other_end - qb); // the row's position among the queries, the first at 0
 
     const T *const k = (const T *)a.k + kh * a.k_head, *const v = (const T *)a.v + kh * a.v_head;
+    const typename L::template Reads<32, NT> reads_q(a.q_row, a.dim, tid), reads_g(a.go_row, a.dim, tid);
+    typename L::Chunk cq[L::template per<32, NT>()], cg[L::template per<32, NT>()];
+    float cs = 0.f; // lse of 32 queries and -delta of 32, the first 64 threads
+    const auto load = [&](int head, int i) {
+        reads_q.load(cq, (const T *)a.q + head * a.q_head, a.q_row, i, qe, a.dim);
+        reads_g.load(cg, (const T *)a.go + head * a.go_head, a.go_row, i, qe, a.dim);
+        if (tid < 64) cs = (h ? a.delta : a.lse)[(int64_t)head * a.sq.rows + min(i + (lane & 31), qe - 1)];
+    };
+    const auto store = [&](int stage, int head, int i) {
+        L::template store<32, NT>(cq, lds[stage][0], tid);
+        L::template store<32, NT>(cg, lds[stage][1], tid);
+        if (tid < 64) stat[stage][h][lane & 31] = h ? cs : i + lane < qe ? GradScore<T, MODE>(a, head).rest(cs) : -INFINITY; // a missing query: p = 0
+    };
+    if (qb < qe) load(kh * a.group, qb);
     Vec<T, 8> fk[KK], fv[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
         fk[kk] = L::own(k, a.k_row, row, in, kk, a.dim, lane);
         fv[kk] = L::own(v, a.v_row, row, in, kk, a.dim, lane);
     }
-    const typename L::template Reads<BN, ATTN_THREADS> reads_q(a.q_row, a.dim, tid), reads_g(a.go_row, a.dim, tid);
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
 
-    for (int g = 0; g < a.group; g++) {
-        const int head = kh * a.group + g;
-        const T *const q = (const T *)a.q + head * a.q_head, *const go = (const T *)a.go + head * a.go_head;
-        const float *const lse = a.lse + (int64_t)head * a.sq.rows, *const delta = a.delta + (int64_t)head * a.sq.rows;
-        const Scores<T, MODE> scores(a, head);
-        const float c2 = scores.rest();
-        typename L::Chunk cq[L::template per<BN, ATTN_THREADS>()], cg[L::template per<BN, ATTN_THREADS>()];
-        float cs = 0.f;
-        const auto load = [&](int i0) {
-            reads_q.load(cq, q, a.q_row, i0, qe, a.dim);
-            reads_g.load(cg, go, a.go_row, i0, qe, a.dim);
-            const int i = i0 + (tid & 31);
-            if (tid < 32) cs = i < qe ? lse[i] * LOG2E : INFINITY; // a missing query: p = 0
-            else if (tid < 64) cs = i < qe ? delta[i] : 0.f;
-        };
-        load(qb);
-        for (int i0 = qb; i0 < qe; i0 += BN) {
-            __syncthreads();
-            L::template store<BN, ATTN_THREADS>(cq, lq, tid);
-            L::template store<BN, ATTN_THREADS>(cg, lg, tid);
-            if (tid < 64) stat[tid >> 5][tid & 31] = cs;
-            __syncthreads();
-            load(i0 + BN);
-            f32x16 s = {}, dp = {}, th;
+    // blocks of queries, one head after the other: the one in registers or under way
+    int head1 = kh * a.group, i1 = qb;
+    const int heads_end = head1 + a.group;
+    const auto advance = [&]() {
+        i1 += 32;
+        if (i1 >= qe) i1 = qb, head1++;
+        if (head1 < heads_end) load(head1, i1);
+    };
+    if (qb < qe) {
+        store(0, head1, i1);
+        advance();
+        __syncthreads();
+    }
+    int stage = 0;
+    for (int head = kh * a.group; head < heads_end; head++) {
+        const GradScore<T, MODE> score(a, head);
+        for (int i = qb; i < qe; i += 32, stage ^= 1) {
+            const T *const lq = lds[stage][0], *const lg = lds[stage][1];
+            f32x16 s = {}, dp;
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 d = *(const f32x4 *)&stat[stage][1][2 * r + 4 * h];
+#pragma unroll
+                for (int e = 0; e < 4; e++) dp[r + e] = d[e];
+            }
 #pragma unroll
             for (int kk = 0; kk < KK; kk++) {
                 s = AttnType<T>::mma(L::rows(lq, 0, kk, lane), fk[kk], s);
                 dp = AttnType<T>::mma(L::rows(lg, 0, kk, lane), fv[kk], dp);
             }
-            scores(s, (float)(pos0 - (i0 - qb)), h, &th);
+            Vec<T, 8> tq[2][DB], tg[2][DB];
 #pragma unroll
-            for (int r4 = 0; r4 < 4; r4++) {
-                const f32x4 l4 = *(const f32x4 *)&stat[0][8 * r4 + 4 * h], d4 = *(const f32x4 *)&stat[1][8 * r4 + 4 * h];
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int r = 4 * r4 + e;
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -l4[e]));
-                    float d = s[r] * (dp[r] - d4[e]);
-                    if (MODE & MODE_CAP) d *= 1.f - th[r] * th[r];
-                    dp[r] = d;
-                }
-            }
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-                const Vec<T, 8> p = round8<T>(s, half), d = round8<T>(dp, half);
+            for (int half = 0; half < 2; half++)
 #pragma unroll
                 for (int db = 0; db < DB; db++) {
-                    dv[db] = AttnType<T>::mma(L::cols(lg, 16 * half, db, lane), p, dv[db]);
-                    dk[db] = AttnType<T>::mma(L::cols(lq, 16 * half, db, lane), d, dk[db]);
+                    tq[half][db] = L::cols(lq, 16 * half, db, lane);
+                    tg[half][db] = L::cols(lg, 16 * half, db, lane);
                 }
+            f32x4 rest[4];
+#pragma unroll
+            for (int r4 = 0; r4 < 4; r4++) rest[r4] = *(const f32x4 *)&stat[stage][0][8 * r4 + 4 * h];
+            if (head1 < heads_end) {
+                store(stage ^ 1, head1, i1);
+                advance();
             }
+            const float pos = (float)(pos0 - (i - qb) - 4 * h);
+            Vec<T, 8> p[2], d[2];
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                float f = 1.f;
+                const float w = score.p(s[r], rest[r >> 2][r & 3], pos - (float)(8 * (r >> 2) + (r & 3)), f);
+                float x = w * dp[r];
+                if (MODE & MODE_CAP) x *= f;
+                p[r >> 3][r & 7] = (T)w;
+                d[r >> 3][r & 7] = (T)x;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int half = 0; half < 2; half++)
+#pragma unroll
+                for (int db = 0; db < DB; db++) {
+                    dv[db] = AttnType<T>::mma(tg[half][db], p[half], dv[db]);
+                    dk[db] = AttnType<T>::mma(tq[half][db], d[half], dk[db]);
+                }
         }
     }
     if (row >= t.top || (!in && !a.fill)) return;
     if (!in || qe == qb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
-    store_row<T, DB>(dk, a.scale, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
+    store_row<T, DB>(dk, GradScore<T, MODE>::scale(a), (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
     store_row<T, DB>(dv, 1.f, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
 }
