@@ -738,6 +738,7 @@ class HE:
         import torch
 
         self._t32, self._i32 = torch.float32, torch.int32
+        self._empty_like, self._dense = torch.empty_like, torch.contiguous_format
         self._type_of = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # HE_F32, HE_F16, HE_BF16
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # of torch.cuda.current_stream, without an object around it
         return self._type_of
@@ -756,19 +757,22 @@ class HE:
 
     def _rows(self, t, what: str, shape, dtype=None) -> bytes:
         """[rows][width], dense along the width: he_rows."""
-        if t.shape != shape or t.dim() != 2:
+        if t.shape != shape or len(shape) != 2:
             raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][width]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
         rows, width = shape
         stride, dense = t.stride()
         if dense != 1 and width > 1:
             raise ValueError(f"{what}: want rows that are dense along the width")
-        self._placed(t, what, dtype)
+        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
+            self._placed(t, what, dtype)
         return _ROWS.pack(t.data_ptr(), stride if rows > 1 else width)
 
     def _vector(self, t, what: str, n: int, dtype) -> int:
-        if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        shape = t.shape
+        if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
             raise ValueError(f"{what}: want a dense vector of {n}")
-        self._placed(t, what, dtype)
+        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
+            self._placed(t, what, dtype)
         return t.data_ptr()
 
     def _spans(self, offsets, rows: int, what: str = "offsets"):
@@ -781,9 +785,10 @@ class HE:
                 raise ValueError(f"{what}: begin and end are vectors of one length")
             count = begin.shape[0]
             return self._vector(begin, what, count, self._i32), self._vector(end, what, count, self._i32), count, rows
-        if offsets.dim() != 1 or offsets.shape[0] < 1:
+        shape = offsets.shape
+        if len(shape) != 1 or shape[0] < 1:
             raise ValueError(f"{what}: want a vector of count + 1 offsets, or a pair of vectors (begin, end)")
-        n = offsets.shape[0]
+        n = shape[0]
         p = self._vector(offsets, what, n, self._i32)
         return p, p + 4, n - 1, rows
 
@@ -804,10 +809,10 @@ class HE:
         s = x
         if residual is not None:
             rr = self._rows(residual, "residual", shape, dtype)
-            s = x.new_empty(shape)
+            s = self._empty_like(x, memory_format=self._dense)
             sr = _ROWS.pack(s.data_ptr(), width)
         if out is None:
-            y = x.new_empty(shape)
+            y = self._empty_like(x, memory_format=self._dense)
             yr = _ROWS.pack(y.data_ptr(), width)
         else:
             y, yr = out, self._rows(out, "out", shape, dtype)
@@ -832,7 +837,7 @@ class HE:
         rc = self.lib.he_layer_norm_workspace_bytes(self.ctx, n, need)
         if rc:
             self._chk(rc, "he_layer_norm_workspace_bytes")
-        dx = s.new_empty(shape)
+        dx = self._empty_like(s, memory_format=self._dense)
         dw, db = weight.new_empty((2, width)).unbind(0)
         ws = self._scratch(s, need.value)
         rc = self.lib.he_layer_norm_grad(self.ctx, n, dyr, sr, w, m, r, ar, _ROWS.pack(dx.data_ptr(), width), dw.data_ptr(), db.data_ptr(),
@@ -889,13 +894,14 @@ class HE:
 
     def _heads(self, t, what: str, shape, dtype=None) -> bytes:
         """[rows][heads][dim] with a dense last dimension: he_heads."""
-        if t.shape != shape or t.dim() != 3:
+        if t.shape != shape or len(shape) != 3:
             raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][heads][dim]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
         row, head, dense = t.stride()
         p = t.data_ptr()
+        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
+            self._placed(t, what, dtype)
         if dense != 1 and shape[2] > 1:
             raise ValueError(f"{what}: the last dimension is not dense")
-        self._placed(t, what, dtype)
         if (p | (row | head) * t.element_size()) & 15 and t.numel():
             raise ValueError(f"{what}: address {p:#x} or strides {t.stride()} not in multiples of 16 bytes")
         return _HEADS.pack(p, row, head)
@@ -942,7 +948,7 @@ class HE:
         shape = q.shape
         lse = q.new_empty((shape[1], shape[0]), dtype=self._t32)
         if out is None:
-            o = q.new_empty(shape) if count else q.new_zeros(shape)
+            o = self._empty_like(q, memory_format=self._dense) if count else q.new_zeros(shape)
             oh = _HEADS.pack(o.data_ptr(), shape[1] * shape[2], shape[2])
         else:
             o, oh = out, self._heads(out, "out", shape, q.dtype)
@@ -966,7 +972,7 @@ class HE:
             raise ValueError("lse: want a dense [heads][rows]")
         self._placed(lse, "lse", self._t32)
         if out is None:
-            dq, dk, dv = [q.new_empty(t.shape) if count else q.new_zeros(t.shape) for t in (q, k, v)]
+            dq, dk, dv = [self._empty_like(t, memory_format=self._dense) if count else t.new_zeros(t.shape) for t in (q, k, v)]
             kv = k.shape[1] * shape[2]
             gq, gk, gv = (_HEADS.pack(t.data_ptr(), n, shape[2]) for t, n in ((dq, shape[1] * shape[2]), (dk, kv), (dv, kv)))
         else:

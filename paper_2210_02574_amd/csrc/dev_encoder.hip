@@ -129,16 +129,25 @@ struct AttnPlan {
     int tile, splits; // queries of a work-group; parts that the keys are cut into
     int64_t slots;
 };
+// Tiles by the sequences' mean length: 128 queries, 64 for short sequences, 256 where attn_wide() says so, no cap keeps the vector instructions busy
+// anyway (one sequence of 8192, 12 heads of 64, capped: 496 us, with 128 426) and three rounds of them fill the card.  Tiles of 32, whose four waves
+// share the keys, where tiles of 128 would leave half of the CUs without one, or few queries meet many keys.  12 heads of 64 in bf16, tiles of 32,
+// 64, 128: 64 tokens 5.4, 6.0, 5.4 us; 512 tokens 8.2, 8.8, 10; 1024 16, 17, 15; 4 x 512 14, 13, 13; 64 x 64 13, 9.2, 9.5; 256 x 24 24, 18, 21.
+// The keys are cut where even so there are few work-groups: two launches cost 4 to 10 us more than one (512 tokens cut in two: 14 us instead of 8.2).
 AttnPlan attn_plan(const he_attn *s)
 {
-    AttnPlan p;
-    const int64_t mean_q = s->q.count ? s->q.rows / s->q.count : 0, mean_k = s->q.count ? s->k.rows / s->q.count : 0;
-    p.tile = mean_q <= 32 ? 32 : mean_q <= 64 ? 64 : mean_q < 1024 || !attn_wide(type_size(s->type), s->dim) ? 128 : 256;
+    AttnPlan p{128, 1, 0};
+    if (s->q.count == 0) return p;
+    const int64_t mean_q = s->q.rows / s->q.count, mean_k = s->k.rows / s->q.count;
+    const auto groups = [&](int tile) { return tile_slots(s->q.rows, s->q.count, tile) * s->heads; };
+    if (mean_q <= 64) p.tile = 64;
+    if (groups(p.tile) < 128 || (mean_q <= 32 && mean_k > 128)) p.tile = 32;
+    if (mean_q >= 1024 && s->cap == 0.0 && attn_wide(type_size(s->type), s->dim) && groups(256) >= 768) p.tile = 256;
     p.slots = tile_slots(s->q.rows, s->q.count, p.tile);
-    const int64_t groups = p.slots * s->heads;
-    p.splits = groups > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, mean_k / 256, 64})) : 1;
+    if (p.tile == 32 && p.slots > 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / groups(32), mean_k / 512, 64}));
     return p;
 }
+
 // Rows of a work-group of the backward pass.  Short sequences leave a part of a tile empty and a work-group little to do between its first loads and its last
 // stores: small ones then waste less and more of them are resident.  12 heads of 64 in bf16, dq with 64 rows against 128: 1000 sequences of 18 rows on average
 // 49 us, 79; 200 of 56 30, 34; 64 of 290 62, 63; 32 of 570 92, 88; one of 8192 415, 366.  dk and dv with 32 against 128: 42 us, 101; 30, 42; 77, 85; 123, 129;

@@ -567,7 +567,12 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     }
     sum = pair_sum(sum);
 
-    // join the waves along the keys: word i of all lanes side by side
+    // join the waves along the keys that had any: word i of all lanes side by side
+    const int waves = min(NWK, (g.hi - g.lo + 31) >> 5);
+    if (waves <= 1) {
+        if (wk == 0) fwd_store<T, DB>(a, g, head, split, row, top, sum, o, lane);
+        return;
+    }
     float *const join = (float *)lds;
     __syncthreads();
     if (wk > 0) {
@@ -581,8 +586,7 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     }
     __syncthreads();
     if (wk > 0) return;
-#pragma unroll
-    for (int w = 0; w < NWK - 1; w++) {
+    for (int w = 0; w < waves - 1; w++) {
         const float *p = join + (w * NWQ + wq) * 64 * (DP / 2 + 2) + lane;
         const float m = fmaxf(top, p[0]), ref = m == -INFINITY ? 0.f : m;
         const float f = __builtin_amdgcn_exp2f(top - ref), x = __builtin_amdgcn_exp2f(p[0] - ref);

@@ -25,22 +25,23 @@ def spans(offsets):
     return list(zip(o[:-1], o[1:]))
 
 
-def attention(q, k, v, offsets, offsets_k=None, scale=None, cap=0.0, slopes=None, do=None):
-    """{name: (value, bound)} for o, lse and, with do, dq, dk, dv."""
+def attention(q, k, v, offsets, offsets_k=None, scale=None, cap=0.0, slopes=None, do=None, device="cpu"):
+    """{name: (value, bound)} for o, lse and, with do, dq, dk, dv.  device: where the 64-bit arithmetic runs."""
     u = half_step(q.dtype)
     zero = 2.0**-25 if q.dtype == torch.float16 else 0.0
-    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    q, k, v = (t.double().to(device) for t in (q, k, v))
     (tq, h, d), (tk, kv, _) = q.shape, k.shape
     scale = d**-0.5 if scale is None else scale
-    z = lambda *s: torch.zeros(*s, dtype=torch.float64)  # noqa: E731
+    z = lambda *s: torch.zeros(*s, dtype=torch.float64, device=device)  # noqa: E731
     out = {n: [z(*s), z(*s)] for n, s in (("o", q.shape), ("lse", (h, tq)), ("dq", q.shape), ("dk", k.shape), ("dv", k.shape))}
     out["lse"][0] -= math.inf
     if do is not None:
-        do = do.double().cpu()
+        do = do.double().to(device)
     for (qb, qe), (kb, ke) in zip(spans(offsets), spans(offsets if offsets_k is None else offsets_k)):
         if qe <= qb or ke <= kb:
             continue
-        dist = (torch.arange(qe - qb)[:, None] + (ke - kb) - (qe - qb) - torch.arange(ke - kb)[None, :]).abs().double()
+        at = torch.arange(max(qe - qb, ke - kb), device=device)
+        dist = (at[:qe - qb, None] + (ke - kb) - (qe - qb) - at[None, :ke - kb]).abs().double()
         for i in range(h):
             c = i // (h // kv)
             Q, K, V = q[qb:qe, i], k[kb:ke, c], v[kb:ke, c]
@@ -82,7 +83,7 @@ def attention(q, k, v, offsets, offsets_k=None, scale=None, cap=0.0, slopes=None
             out["dv"][1][kb:ke, c] += (rel * p + zero).T @ G.abs()
     for n in ("dq", "dk", "dv"):
         out[n][1] = out[n][1] + u * out[n][0].abs()
-    return {n: (a, b + 1e-30 + (2.0**-24 if u == 2.0**-11 else 0.0)) for n, (a, b) in out.items()}  # fp16: its smallest step
+    return {n: (a.cpu(), (b + 1e-30 + (2.0**-24 if u == 2.0**-11 else 0.0)).cpu()) for n, (a, b) in out.items()}  # fp16: its smallest step
 
 
 def layer_norm(x, w, b, r=None, eps=1e-5, dy=None, ds=None):

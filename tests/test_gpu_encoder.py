@@ -157,6 +157,18 @@ def test_attention(he, lengths, dim, dtype):
     compare(he, q, k, v, off, do)
 
 
+@pytest.mark.parametrize("dtype,heads,kv,dim,cap", [(BF16, 96, 48, 64, 0.0), (F16, 100, 100, 40, 0.0), (BF16, 8, 4, 64, 15.0), (F32, 3, 1, 96, 0.0), (F16, 5, 5, 128, 0.0)])
+def test_attention_of_long_sequences(he, dtype, heads, kv, dim, cap):
+    """Tiles of 256 queries (the first two) and of 128 queries and keys."""
+    off = offsets_of([1100, 2061])
+    q, do = rand(1, 3161, heads, dim, dtype=dtype), rand(2, 3161, heads, dim, dtype=dtype)
+    k, v = rand(3, 3161, kv, dim, dtype=dtype), rand(4, 3161, kv, dim, dtype=dtype)
+    slopes = 0.01 * torch.arange(heads).float().cuda() if cap else None
+    want, got = ref.attention(q, k, v, off, do=do, cap=cap, slopes=slopes, device="cuda"), attend(he, q, k, v, off, do, cap=cap, slopes=slopes)
+    for name in got:
+        ref.check(got[name], want[name], name)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("cap,bias", [(0.0, True), (2.0, False), (30.0, True)])
 @pytest.mark.parametrize("heads,kv", [(4, 4), (6, 2), (5, 1)])
