@@ -61,6 +61,10 @@ static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, int tile, unsi
             KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 4, mode>), grid, 256, a);
     });
 }
+static void attn_grad_join(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
+{
+    KLAUNCH(c, st, KID_ATTN_GRAD_JOIN, bytes, (k_attn_grad_join<T>), grid, a);
+}
 
 #define NAME_(t, d) attn_launch_##t##_##d
 #define NAME(t, d) NAME_(t, d)
@@ -70,4 +74,5 @@ void NAME(HE_TYPE, HE_DIM)(AttnLaunch &t)
     t.join = attn_join;
     t.grad_q = attn_grad_q;
     t.grad_kv = attn_grad_kv;
+    t.grad_join = attn_grad_join;
 }

@@ -154,10 +154,22 @@ AttnPlan attn_plan(const he_attn *s)
 // with 64 the last one 607, 500.
 int grad_tile_q(const he_spans &s) { return s.rows / s.count < 256 ? 64 : 128; }
 int grad_tile_k(const he_spans &s) { return s.rows / s.count < 512 ? 32 : 128; }
+// Parts that the queries of a tile of 128 keys are cut into, where those tiles are few for 256 CUs that hold two each: shared key heads have long work and few
+// tiles (one sequence of 8192, heads of 64 in bf16, 12 on 4: 636 us whole, 472 in two or three; 2 of 2048, heads of 128, 8 on 2: 291, 105; of one of 4096 with
+// heads of their own 148, 150).
+int grad_splits(const he_attn *s)
+{
+    if (s->k.count == 0 || s->k.rows == 0 || grad_tile_k(s->k) != 128) return 1;
+    const int64_t groups = tile_slots(s->k.rows, s->k.count, 128) * s->kv_heads, work = s->q.rows / s->q.count * (s->heads / s->kv_heads);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(640 + groups / 2) / groups, work / 512, 8}));
+}
 size_t attn_bytes(const he_attn *s, bool backward)
 {
     const size_t rows = (size_t)s->q.rows * s->heads;
-    if (backward) return rows * 4;
+    if (backward) {
+        const int splits = grad_splits(s);
+        return (rows + 3) / 4 * 16 + (splits > 1 ? (size_t)splits * 2 * s->kv_heads * s->k.rows * s->dim * 4 : 0);
+    }
     const AttnPlan p = attn_plan(s);
     return p.splits > 1 ? rows * p.splits * (s->dim + 1) * 4 : 0;
 }
@@ -378,10 +390,14 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     a.lse = const_cast<float *>(d_lse);
     a.delta = (float *)d_ws;
     AttnArgs b = a;
+    b.splits = grad_splits(s);
+    b.part_o = a.delta + (s->q.rows * s->heads + 3) / 4 * 4;
     unsigned grid_q = 0, grid_kv = 0;
     const int tile_q = grad_tile_q(s->q), tile_k = grad_tile_k(s->k);
     if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, tile_q), s->heads, grid_q)) return HE_EINVAL;
-    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, tile_k), s->kv_heads, grid_kv)) return HE_EINVAL;
+    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, tile_k), (int64_t)s->kv_heads * b.splits, grid_kv)) return HE_EINVAL;
+    const int64_t rows_kv = s->k.rows * s->kv_heads;
+    if (b.splits > 1 && rows_kv >= (int64_t)4 << 23) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
@@ -389,5 +405,6 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     const double size = (double)type_size(s->type) * s->dim, qb = s->q.rows * s->heads * size, kb = s->k.rows * s->kv_heads * size;
     if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, tile_q, grid_q, a);
     if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, tile_k, grid_kv, b);
+    if (some_k && b.splits > 1) l.grad_join(ctx, (hipStream_t)stream, 2.0 * rows_kv * (size + 4.0 * b.splits * s->dim), (unsigned)((rows_kv + 3) / 4), b);
     return launched(ctx);
 }

@@ -21,6 +21,7 @@ struct AttnLaunch {
     // tile: rows of a work-group, 64 or 128 queries, 32 or 128 keys
     void (*grad_q)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);
     void (*grad_kv)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);
+    void (*grad_join)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
 };
 #define HE_DECL_ATTN(t)                                                                                              \
     void attn_launch_##t##_32(AttnLaunch &t_);                                                                       \

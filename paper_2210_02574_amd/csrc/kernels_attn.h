@@ -24,7 +24,7 @@ struct AttnArgs {
     void *o, *dq, *dk, *dv;
     float *lse;         // [heads][rows_q], natural logarithm
     float *delta;       // [heads][rows_q]
-    float *part_o;      // [splits][heads][rows_q][dim]
+    float *part_o;      // forward: [splits][heads][rows_q][dim]; dk and dv: [splits][2][kv_heads][rows_k][dim]
     float *part_lse;    // [splits][heads][rows_q]
     const float *slope; // [heads] or null
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, oi_row, oi_head, go_row, go_head; // strides, in elements
@@ -600,22 +600,28 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     fwd_store<T, DB>(a, g, head, split, row, top, sum, o, lane);
 }
 
+// Whether a row belongs to a sequence, sought by 64 lanes.
+__device__ __forceinline__ bool row_in(const Spans &s, int row)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = s.count;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lo + lane * step;
+        const unsigned long long m = __ballot(lane * step < n && span_begin(s, i) <= row);
+        const int k = m ? 63 - __clzll(m) : 0;
+        n = min(step, n - k * step);
+        lo += k * step;
+    }
+    return row >= span_begin(s, lo) && row < span_end(s, lo);
+}
+
 // The splits of a row: weights exp(lse_s - lse).  A wave per row and head, blockIdx.x * 4 + wave over [heads][rows].
 template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
 {
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.heads * a.sq.rows;
     if (at >= all) return;
     const int lane = threadIdx.x & 63, head = at / a.sq.rows, row = at % a.sq.rows;
-    // the splits of a row that no tile wrote hold nothing: find out whether the row belongs to a sequence
-    int lo = 0, n = a.sq.count;
-    while (n > 1) {
-        const int step = (n + 63) >> 6, i = lo + lane * step;
-        const unsigned long long m = __ballot(lane * step < n && span_begin(a.sq, i) <= row);
-        const int k = m ? 63 - __clzll(m) : 0;
-        n = min(step, n - k * step);
-        lo += k * step;
-    }
-    const bool in = row >= span_begin(a.sq, lo) && row < span_end(a.sq, lo);
+    const bool in = row_in(a.sq, row); // the splits of other rows hold nothing
     if (!in && !a.fill) return;
     float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
     if (in)
@@ -766,7 +772,8 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     store_row<T, DB>(dq, score.scale(a), (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
 }
 
-// dk, dv: keys as columns, the queries of all heads that share the key head stream by.
+// dk, dv: keys as columns, the queries of all heads that share the key head stream by, one head after the other.  Where that leaves too few work-groups
+// their blocks are cut into a.splits parts, whose sums k_attn_grad_join adds up.
 template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP>::WAVES_KV)) void k_attn_grad_kv(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
@@ -775,7 +782,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     __shared__ __attribute__((aligned(16))) float stat[2][2][32]; // what is added to scores, -delta
 
     int kh, slot, split;
-    if (!attn_work(a, a.slots, kh, slot, split)) return;
+    if (!attn_work(a, a.slots * a.splits, kh, slot, split)) return;
     const TileRows t = tile_rows(a.sk, a.sq, slot, 32 * NW);
     if (t.first >= t.top) return;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -798,7 +805,6 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         L::template store<32, NT>(cg, lds[stage][1], tid);
         if (tid < 64) stat[stage][h][lane & 31] = h ? cs : i + lane < qe ? GradScore<T, MODE>(a, head).rest(cs) : -INFINITY; // a missing query: p = 0
     };
-    if (qb < qe) load(kh * a.group, qb);
     Vec<T, 8> fk[KK], fv[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
@@ -809,23 +815,28 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
 
-    // blocks of queries, one head after the other: the one in registers or under way
-    int head1 = kh * a.group, i1 = qb;
-    const int heads_end = head1 + a.group;
+    // blocks of queries, one head after the other
+    const int per = (qe - qb + 31) >> 5, share = (per * a.group + a.splits - 1) / a.splits;
+    const int first = min(split * share, per * a.group), blocks = min(share, per * a.group - first);
+    int head = kh * a.group, i = qb; // of the block at hand
+    if (blocks > 0) head += first / per, i += first % per * 32;
+    int head1 = head, i1 = i, left1 = blocks; // of the block in registers or under way, and how many there are from it on
     const auto advance = [&]() {
+        left1--;
         i1 += 32;
         if (i1 >= qe) i1 = qb, head1++;
-        if (head1 < heads_end) load(head1, i1);
+        if (left1 > 0) load(head1, i1);
     };
-    if (qb < qe) {
+    if (blocks > 0) {
+        load(head1, i1);
         store(0, head1, i1);
         advance();
         __syncthreads();
     }
     int stage = 0;
-    for (int head = kh * a.group; head < heads_end; head++) {
+    for (int u = 0; u < blocks;) {
         const GradScore<T, MODE> score(a, head);
-        for (int i = qb; i < qe; i += 32, stage ^= 1) {
+        for (; u < blocks && i < qe; u++, i += 32, stage ^= 1) {
             const T *const lq = lds[stage][0], *const lg = lds[stage][1];
             f32x16 s = {}, dp;
 #pragma unroll
@@ -850,7 +861,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
             f32x4 rest[4];
 #pragma unroll
             for (int r4 = 0; r4 < 4; r4++) rest[r4] = *(const f32x4 *)&stat[stage][0][8 * r4 + 4 * h];
-            if (head1 < heads_end) {
+            if (left1 > 0) {
                 store(stage ^ 1, head1, i1);
                 advance();
             }
@@ -874,11 +885,38 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
                     dk[db] = AttnType<T>::mma(tq[half][db], d[half], dk[db]);
                 }
         }
+        head++;
+        i = qb;
     }
-    if (row >= t.top || (!in && !a.fill)) return;
-    if (!in || qe == qb)
+    if (row >= t.top) return;
+    if (!in || blocks <= 0)
 #pragma unroll
         for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
+    if (a.splits > 1) {
+        float *part = a.part_o + (((int64_t)split * 2 * (a.heads / a.group) + kh) * a.sk.rows + row) * a.dim;
+        store_row<float, DB>(dk, GradScore<T, MODE>::scale(a), part, a.dim, lane);
+        store_row<float, DB>(dv, 1.f, part + (int64_t)(a.heads / a.group) * a.sk.rows * a.dim, a.dim, lane);
+        return;
+    }
+    if (!in && !a.fill) return;
     store_row<T, DB>(dk, GradScore<T, MODE>::scale(a), (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
     store_row<T, DB>(dv, 1.f, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
+}
+
+// dk and dv from the parts: a wave per row and key head, blockIdx.x * 4 + wave over [kv_heads][rows].
+template <class T> __global__ __launch_bounds__(256) void k_attn_grad_join(AttnArgs a)
+{
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)(a.heads / a.group) * a.sk.rows;
+    if (at >= all) return;
+    const int lane = threadIdx.x & 63, kh = at / a.sk.rows, row = at % a.sk.rows;
+    if (!a.fill && !row_in(a.sk, row)) return;
+    T *const dk = (T *)a.dk + kh * a.dk_head + row * a.dk_row, *const dv = (T *)a.dv + kh * a.dv_head + row * a.dv_row;
+    for (int c = lane; c < a.dim; c += 64) {
+        float k = 0.f, v = 0.f;
+        for (int s = 0; s < a.splits; s++) {
+            k += a.part_o[(2 * s * all + at) * a.dim + c];
+            v += a.part_o[((2 * s + 1) * all + at) * a.dim + c];
+        }
+        dk[c] = (T)k, dv[c] = (T)v;
+    }
 }

@@ -190,16 +190,20 @@ def test_attention_of_other_keys_and_few_queries(he, queries, keys, dtype):
         compare(he, q, k, v, oq, do, offsets_k=ok, slopes=sl)
 
 
-def test_attention_cuts_long_keys(he):
-    """One query against many keys is cut along the keys and joined: the sizes really reach that path."""
+def test_attention_is_cut_where_it_should_be(he):
+    """Sizes that test_attention_of_other_keys_and_few_queries (one query of many keys) and test_attention_of_long_sequences (few tiles of keys under many
+    queries) run really are cut and joined."""
     import ctypes
 
     from paper_2210_02574_amd import binding as bd
 
-    sq, sk = he._spans(i32(0, 1), 1), he._spans(i32(0, 4000), 4000)
     need = ctypes.c_size_t()
+    sq, sk = he._spans(i32(0, 1), 1), he._spans(i32(0, 4000), 4000)
     s = bd._ATTN.pack(2, 4, 2, 64, *sq, *sk, 0.125, 0.0, 0, 1)
     assert he.lib.he_attention_workspace_bytes(he.ctx, s, 0, ctypes.byref(need)) == 0 and need.value > 0
+    both = he._spans(i32(0, 1100, 3161), 3161)
+    s = bd._ATTN.pack(2, 8, 4, 64, *both, *both, 0.125, 15.0, 0, 1)
+    assert he.lib.he_attention_workspace_bytes(he.ctx, s, 1, ctypes.byref(need)) == 0 and need.value > 2 * 2 * 4 * 3161 * 64 * 4
 
 
 def test_attention_scores_far_from_zero(he):
