@@ -653,9 +653,12 @@ template <class T, int DP> struct AttnGrad {
     static constexpr int TILE = 32 * DP;
     static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : DP > 64 ? 2 : 3, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2; // per SIMD
 };
-// What the backward pass makes of one score: x: the product, rest: what is added in units of log2 (-lse).  Gives p and the factor of ds (1 without a cap;
-// a quarter of 1 - tanh^2 for 16-bit types: 1 / (1 + e^2y) times 1 minus that).
+// What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p and the factor of ds, 1 - tanh^2 under
+// a cap.  16-bit types have tanh as 1 - 2 g, g = 1 / (1 + e^2y), and 1 - tanh^2 as 4 g (1 - g): the 4 is in p there (LIFT), so that ds keeps the size that fp16
+// was chosen for, and dv is divided by it.
 template <class T, int MODE> struct GradScore {
+    static constexpr bool FAST = (MODE & MODE_CAP) && sizeof(T) == 2;
+    static constexpr float LIFT = FAST ? 4.f : 1.f;
     float in, out, slope;
     __device__ __forceinline__ GradScore(const AttnArgs &a, int head)
     {
@@ -664,25 +667,21 @@ template <class T, int MODE> struct GradScore {
         if (MODE & MODE_CAP) in = s.in;
         if (MODE & MODE_SLOPE) slope = s.slope;
     }
-    // what ds lacks at the end
-    static __device__ __forceinline__ float scale(const AttnArgs &a) { return (MODE & MODE_CAP) && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
     __device__ __forceinline__ float p(float x, float rest, float dist, float &factor) const
     {
         if constexpr (MODE & MODE_SLOPE) rest = fmaf(-slope, fabsf(dist), rest);
-        if constexpr (MODE & MODE_CAP) {
-            if constexpr (sizeof(T) == 4) {
-                const float th = tanhf(x * in);
-                factor = fmaf(-th, th, 1.f);
-                return __builtin_amdgcn_exp2f(fmaf(th, out, rest));
-            }
+        if constexpr (FAST) {
             const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * in));
             factor = fmaf(-g, g, g);
-            return __builtin_amdgcn_exp2f(fmaf(-2.f * out, g, rest)); // `rest` has cap in it
+            return __builtin_amdgcn_exp2f(fmaf(-2.f * out, g, rest)); // `rest` has the cap in it
+        } else if constexpr (MODE & MODE_CAP) {
+            const float th = tanhf(x * in);
+            factor = fmaf(-th, th, 1.f);
+            return __builtin_amdgcn_exp2f(fmaf(th, out, rest));
         }
         return __builtin_amdgcn_exp2f(fmaf(x, out, rest));
     }
-    // rest from lse
-    __device__ __forceinline__ float rest(float lse) const { return (MODE & MODE_CAP) && sizeof(T) == 2 ? out - lse * LOG2E : -lse * LOG2E; }
+    __device__ __forceinline__ float rest(float lse) const { return FAST ? out + 2.f - lse * LOG2E : -lse * LOG2E; }
 };
 
 // dq: queries as columns.  Also leaves -delta for the kernel of dk and dv, which runs after it.
@@ -769,7 +768,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     if (!in || ke == kb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dq[db] = f32x16{};
-    store_row<T, DB>(dq, score.scale(a), (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
+    store_row<T, DB>(dq, a.scale, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
 }
 
 // dk, dv: keys as columns, the queries of all heads that share the key head stream by, one head after the other.  Where that leaves too few work-groups
@@ -894,13 +893,13 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
     if (a.splits > 1) {
         float *part = a.part_o + (((int64_t)split * 2 * (a.heads / a.group) + kh) * a.sk.rows + row) * a.dim;
-        store_row<float, DB>(dk, GradScore<T, MODE>::scale(a), part, a.dim, lane);
-        store_row<float, DB>(dv, 1.f, part + (int64_t)(a.heads / a.group) * a.sk.rows * a.dim, a.dim, lane);
+        store_row<float, DB>(dk, a.scale, part, a.dim, lane);
+        store_row<float, DB>(dv, 1.f / GradScore<T, MODE>::LIFT, part + (int64_t)(a.heads / a.group) * a.sk.rows * a.dim, a.dim, lane);
         return;
     }
     if (!in && !a.fill) return;
-    store_row<T, DB>(dk, GradScore<T, MODE>::scale(a), (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
-    store_row<T, DB>(dv, 1.f, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
+    store_row<T, DB>(dk, a.scale, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
+    store_row<T, DB>(dv, 1.f / GradScore<T, MODE>::LIFT, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
 }
 
 // dk and dv from the parts: a wave per row and key head, blockIdx.x * 4 + wave over [kv_heads][rows].
