@@ -18,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhe_gfx950.so")
 
 HE_OK = 0
+HE_EWORKSPACE = -4
 ERRORS = {
     -1: "HE_EINVAL", -2: "HE_ELEVEL", -3: "HE_ENOKEY", -4: "HE_EWORKSPACE",
     -5: "HE_EHIP", -6: "HE_ENODEV", -7: "HE_ENOMEM", -8: "HE_ESCRATCH",
@@ -853,10 +854,6 @@ class HE:
         rows, width = shape
         span = self._spans(offsets, rows)
         count, sp = span[2], _SPANS.pack(*span)
-        need = ctypes.c_size_t()
-        rc = self.lib.he_pool_workspace_bytes(self.ctx, sp, width, need)
-        if rc:
-            self._chk(rc, "he_pool_workspace_bytes")
         if out is None:
             e = x.new_empty((count, width), dtype=self._t32)
         else:
@@ -864,11 +861,13 @@ class HE:
             if e.shape != (count, width) or not e.is_contiguous():
                 raise ValueError(f"out: want a dense [{count}][{width}]")
             self._placed(e, "out", self._t32)
-        ws = self._scratch(x, need.value)
-        rc = self.lib.he_pool(self.ctx, code, sp, width, xr, e.data_ptr(), ws.data_ptr() if ws is not None else None, need.value,
-                              self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_pool")
+
+        def sizes():
+            need = ctypes.c_size_t()
+            self._chk(self.lib.he_pool_workspace_bytes(self.ctx, sp, width, need), "he_pool_workspace_bytes")
+            return need.value
+
+        self._with_scratch(self.lib.he_pool, sizes, "he_pool", x, code, sp, width, xr, e.data_ptr())
         return e
 
     def pool_mean_backward(self, de, offsets, rows: int, dtype, out=None):
@@ -908,10 +907,9 @@ class HE:
 
     def _attn(self, q, k, v, offsets, offsets_k, scale, cap, slopes, fill):
         """(he_attn, count of sequences, he_heads of q, k, v)"""
-        dtype, shape = q.dtype, q.shape
+        dtype, shape, kshape = q.dtype, q.shape, k.shape
         code, qh = self._type(dtype), self._heads(q, "q", shape)
         rows, heads, dim = shape
-        kshape = k.shape
         if len(kshape) != 3 or kshape[2] != dim:
             raise ValueError(f"k: {tuple(kshape)}, want [rows][heads][{dim}]")
         rows_k, kv, _ = kshape
@@ -928,16 +926,23 @@ class HE:
         sl = 0 if slopes is None else self._vector(slopes, "slopes", heads, self._t32)
         return _ATTN.pack(code, heads, kv, dim, *sq, *sk, dim**-0.5 if scale is None else scale, cap, sl, fill), sq[2], qh, kh, vh
 
-    def _attn_scratch(self, s, like, backward: bool):
+    def _with_scratch(self, fn, sizes, where: str, like, *args):
+        """fn(ctx, *args, workspace, bytes, stream), first without a workspace: most calls take none, and one that does says so before it enqueues
+        anything.  sizes() gives the bytes then."""
+        rc = fn(self.ctx, *args, None, 0, self._raw_stream(self.device))
+        if rc == HE_EWORKSPACE:
+            need = sizes()
+            ws = self._scratch(like, need)
+            rc = fn(self.ctx, *args, ws.data_ptr(), need, self._raw_stream(self.device))
+        if rc:
+            self._chk(rc, where)
+
+    def _attn_bytes(self, s, backward: bool) -> int:
         need = ctypes.c_size_t()
         rc = self.lib.he_attention_workspace_bytes(self.ctx, s, backward, need)
         if rc:
             self._chk(rc, "he_attention_workspace_bytes")
-        n = need.value
-        if not n:
-            return None, None, 0
-        ws = self._scratch(like, n)
-        return ws, ws.data_ptr(), n
+        return need.value
 
     def attention(self, q, k, v, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None):
         """Attention inside each sequence: q [rows][heads][dim], k and v [rows_k][kv_heads][dim] (strided views of a joint projection are fine;
@@ -954,10 +959,7 @@ class HE:
             o, oh = out, self._heads(out, "out", shape, q.dtype)
         if out is not None or not count:
             lse.fill_(float("-inf"))
-        ws, p, n = self._attn_scratch(s, q, False)
-        rc = self.lib.he_attention(self.ctx, s, qh, kh, vh, oh, lse.data_ptr(), p, n, self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_attention")
+        self._with_scratch(self.lib.he_attention, lambda: self._attn_bytes(s, False), "he_attention", q, s, qh, kh, vh, oh, lse.data_ptr())
         return o, lse
 
     def attention_backward(self, do, q, k, v, o, lse, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None,
@@ -978,8 +980,10 @@ class HE:
         else:
             dq, dk, dv = out
             gq, gk, gv = self._heads(dq, "dq", shape, dtype), self._heads(dk, "dk", k.shape, dtype), self._heads(dv, "dv", k.shape, dtype)
-        ws, p, n = self._attn_scratch(s, q, True)
-        rc = self.lib.he_attention_grad(self.ctx, s, gh, qh, kh, vh, oh, lse.data_ptr(), gq, gk, gv, p, n, self._raw_stream(self.device))
+        n = self._attn_bytes(s, True)
+        ws = self._scratch(q, n)
+        rc = self.lib.he_attention_grad(self.ctx, s, gh, qh, kh, vh, oh, lse.data_ptr(), gq, gk, gv, ws.data_ptr() if ws is not None else None, n,
+                                        self._raw_stream(self.device))
         if rc:
             self._chk(rc, "he_attention_grad")
         return dq, dk, dv
