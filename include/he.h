@@ -309,7 +309,7 @@ int32_t he_rotate_sum_batch(he_ctx *ctx, const he_evk *const *rots, int32_t n_ro
 /* The data owner's half of the paper's pipeline (Section 2.1): what turns the states of a sentence's tokens into the embedding that is
  * encoded and encrypted, and the gradients of it, for fitting an encoder in the clear.  These functions work on floating-point rows, use
  * nothing of a context but its device, run on it whatever device is current, and keep the conventions above: caller-owned buffers, work
- * enqueued on `stream` alone, no allocation, no synchronisation.  Inputs are not written; outputs must not overlap inputs or one another.
+ * enqueued on `stream` alone, no allocation, no synchronisation.  Addresses are multiples of their element's size.  Inputs are not written; outputs must not overlap inputs or one another.
  * Sums, statistics and softmax are in 32 bits; a result is rounded to its type once.  No sequences (count 0): nothing is written. */
 #define HE_F32 0
 #define HE_F16 1
@@ -331,12 +331,13 @@ typedef struct {
  * the device and are not checked: ones that break the rule give results without meaning (no access outside the buffers). */
 typedef struct {
     const int32_t *d_begin, *d_end; /* [count] */
-    int32_t count;
+    int32_t count;                  /* at most 2^23 */
     int64_t rows; /* at most 2^31 - 65536 */
 } he_spans;
 
 /* Layer norm over the last dimension: s = x + residual, rounded to the type (no residual: s = x); m and v its mean and variance over the width;
- * rstd = (v + eps)^-1/2; y = (s - m) rstd w + b.  Weights have the rows' type or HE_F32.  HE_EINVAL: width above 16384, eps negative. */
+ * rstd = (v + eps)^-1/2; y = (s - m) rstd w + b.  Weights have the rows' type or HE_F32.  HE_EINVAL: width above 16384, more
+ * than 2^31 - 65536 rows, eps negative. */
 typedef struct {
     int32_t type, weight_type;
     int64_t rows;
@@ -366,11 +367,12 @@ int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width
  *   lse = log sum exp(s);  o = sum exp(s - lse) v;  a row whose sequence has no keys: o = 0, lse = -inf
  * Query head h reads key head h / (heads / kv_heads).  The last query stands at the last key's position (where both have the same rows:
  * row i of each at the same one).  d_lse [heads][q.rows].  dim: a multiple of 8 up to 128.  fill: query rows of no sequence get o = 0,
- * lse = -inf (backward: gradient rows of no sequence zeros), else they are left as they are. */
+ * lse = -inf (backward: gradient rows of no sequence zeros), else they are left as they are.  HE_EINVAL: more than 2^23 work-groups (tiles of 128
+ * rows, 32 to 256 with the lengths, times heads). */
 typedef struct {
     int32_t type, heads, kv_heads, dim;
     he_spans q, k;         /* the same count */
-    double scale, cap;     /* scale > 0, cap >= 0, both finite in 32 bits */
+    double scale, cap;     /* scale > 0, cap >= 0, both and scale / cap finite in 32 bits */
     const float *d_slopes; /* [heads]; NULL: no bias */
     int32_t fill;
 } he_attn;

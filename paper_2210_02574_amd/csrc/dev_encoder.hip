@@ -75,7 +75,8 @@ int32_t norm_check(const he_norm *n)
     if (n->rows < 0 || n->rows > MAX_ROWS || n->width < 1 || n->width > NORM_MAX_WIDTH) return HE_EINVAL;
     return HE_OK;
 }
-bool rows_ok(const he_rows *r, int64_t width) { return r && r->d && r->stride >= width; }
+bool rows_ok(const he_rows *r, int64_t width, int32_t type) { return r && r->d && aligned(r->d, type_size(type)) && r->stride >= width; }
+bool words_ok(const void *p, size_t size = 4) { return p && aligned(p, size); }
 
 // Work-groups of the backward pass: each writes a partial row of dw and db, so two for each of the 256 CUs and no more than rows need.
 int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
@@ -84,19 +85,21 @@ int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t
 
 int32_t spans_check(const he_spans *s)
 {
-    if (!s || s->count < 0 || s->rows < 0 || s->rows > MAX_ROWS || s->count > (1 << 24)) return HE_EINVAL;
-    if (s->count > 0 && (!s->d_begin || !s->d_end)) return HE_EINVAL;
+    if (!s || s->count < 0 || s->rows < 0 || s->rows > MAX_ROWS || s->count > (1 << 23)) return HE_EINVAL;
+    if (s->count > 0 && (!words_ok(s->d_begin) || !words_ok(s->d_end))) return HE_EINVAL;
     return HE_OK;
 }
 Spans spans_of(const he_spans *s) { return Spans{s->d_begin, s->d_end, s->count, (int32_t)s->rows}; }
 
-// A work-group per sequence while their rows are few; else tiles of equal length, about 2048 of them, whatever the lengths are, and a second launch that joins
+// A work-group per sequence while they and their rows are few; else tiles of equal length, about 2048 of them, whatever the lengths are, and a second launch that joins
 // them.
 int pool_tile(const he_spans *s)
 {
-    if (s->count == 0 || (s->rows <= 8192 && s->rows / s->count <= 256)) return 0;
+    if (s->count == 0 || (s->rows <= 8192 && s->count <= 8192 && s->rows / s->count <= 256)) return 0;
     return (int)std::max<int64_t>(64, (s->rows / 2048 + 15) / 16 * 16);
 }
+// 32 rows, more from 2^27 rows on: a launch holds 2^24 work-groups, of which sequences, 2^23 at most, may take one each.
+int pool_grad_tile(const he_spans *s) { return (int)std::max<int64_t>(32, (s->rows >> 22) + 1); }
 size_t pool_bytes(const he_spans *s, int32_t width)
 {
     const int tile = pool_tile(s);
@@ -112,6 +115,8 @@ int32_t attn_check(const he_attn *s)
     if (spans_check(&s->q) != HE_OK || spans_check(&s->k) != HE_OK || s->q.count != s->k.count) return HE_EINVAL;
     if (!(s->scale > 0.0) || !std::isfinite((float)s->scale) || !((float)s->scale > 0.f)) return HE_EINVAL;
     if (!(s->cap >= 0.0) || !std::isfinite((float)s->cap) || (s->cap > 0.0 && !((float)s->cap > 0.f))) return HE_EINVAL;
+    if (s->cap > 0.0 && !std::isfinite((float)s->scale / (float)s->cap * 3.f)) return HE_EINVAL; // what scores are multiplied with under tanh
+    if (s->d_slopes && !aligned(s->d_slopes, 4)) return HE_EINVAL;
     return HE_OK;
 }
 bool heads_ok(const he_heads *h, int32_t type)
@@ -211,8 +216,10 @@ extern "C" int32_t he_layer_norm(he_ctx *ctx, const he_norm *n, const he_rows *x
         NEEDS_DEVICE(ctx);
         return HE_OK;
     }
-    if (!rows_ok(x, n->width) || !rows_ok(y, n->width) || !d_w || !d_b || !d_mean || !d_rstd) return HE_EINVAL;
-    if (residual && (!rows_ok(residual, n->width) || !rows_ok(sum, n->width))) return HE_EINVAL;
+    const size_t size_w = type_size(n->weight_type);
+    if (!rows_ok(x, n->width, n->type) || !rows_ok(y, n->width, n->type)) return HE_EINVAL;
+    if (!words_ok(d_w, size_w) || !words_ok(d_b, size_w) || !words_ok(d_mean) || !words_ok(d_rstd)) return HE_EINVAL;
+    if (residual && (!rows_ok(residual, n->width, n->type) || !rows_ok(sum, n->width, n->type))) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     if (!residual) sum = nullptr;
     NormArgs a;
@@ -240,14 +247,16 @@ extern "C" int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_ro
                                       const float *d_rstd, const he_rows *add, const he_rows *ds, void *d_dw, void *d_db, void *d_ws, size_t ws_bytes,
                                       void *stream)
 {
-    if (!ctx || norm_check(n) != HE_OK || !d_w || !d_dw || !d_db) return HE_EINVAL;
+    if (!ctx || norm_check(n) != HE_OK) return HE_EINVAL;
+    const size_t size_w = type_size(n->weight_type);
+    if (!words_ok(d_w, size_w) || !words_ok(d_dw, size_w) || !words_ok(d_db, size_w)) return HE_EINVAL;
     NormGradArgs a;
     memset(&a, 0, sizeof(a));
     a.rows = (int)n->rows, a.width = n->width;
     const int parts = n->rows ? norm_parts(n->rows) : 0;
     if (n->rows) {
-        if (!rows_ok(dy, n->width) || !rows_ok(s, n->width) || !rows_ok(ds, n->width) || !d_mean || !d_rstd) return HE_EINVAL;
-        if (add && !rows_ok(add, n->width)) return HE_EINVAL;
+        if (!rows_ok(dy, n->width, n->type) || !rows_ok(s, n->width, n->type) || !rows_ok(ds, n->width, n->type)) return HE_EINVAL;
+        if (!words_ok(d_mean) || !words_ok(d_rstd) || (add && !rows_ok(add, n->width, n->type))) return HE_EINVAL;
         if (!d_ws || ws_bytes < (size_t)parts * 2 * n->width * sizeof(float)) return HE_EWORKSPACE;
         if (!aligned(d_ws, 4)) return HE_EINVAL;
         a.dy = dy->d, a.dy_row = dy->stride, a.s = s->d, a.s_row = s->stride, a.ds = ds->d, a.ds_row = ds->stride;
@@ -280,7 +289,7 @@ extern "C" int32_t he_pool(he_ctx *ctx, int32_t type, const he_spans *s, int32_t
         NEEDS_DEVICE(ctx);
         return HE_OK;
     }
-    if (!d_e || (s->rows > 0 && !rows_ok(x, width))) return HE_EINVAL;
+    if (!words_ok(d_e) || (s->rows > 0 && !rows_ok(x, width, type))) return HE_EINVAL;
     PoolArgs a;
     memset(&a, 0, sizeof(a));
     if (s->rows > 0) a.x = x->d, a.x_row = x->stride;
@@ -304,15 +313,15 @@ extern "C" int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, in
         NEEDS_DEVICE(ctx);
         return HE_OK;
     }
-    if (!d_de || !rows_ok(dx, width)) return HE_EINVAL;
+    if (!words_ok(d_de) || !rows_ok(dx, width, type)) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     PoolGradArgs a;
     memset(&a, 0, sizeof(a));
-    a.de = d_de, a.dx = dx->d, a.dx_row = dx->stride, a.s = spans_of(s), a.width = width, a.fill = fill;
+    a.de = d_de, a.dx = dx->d, a.dx_row = dx->stride, a.s = spans_of(s), a.width = width, a.fill = fill, a.tile = pool_grad_tile(s);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
     rows_launch(type).pool_grad(ctx, (hipStream_t)stream, (double)s->rows * width * type_size(type) + 4.0 * s->count * width,
-                                (unsigned)tile_slots(s->rows, s->count, POOL_TILE), a);
+                                (unsigned)tile_slots(s->rows, s->count, a.tile), a);
     return launched(ctx);
 }
 
@@ -331,7 +340,7 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
         NEEDS_DEVICE(ctx);
         return HE_OK;
     }
-    if (!heads_ok(q, s->type) || !out_ok(o, s, s->q.rows, s->heads) || !d_lse) return HE_EINVAL;
+    if (!heads_ok(q, s->type) || !out_ok(o, s, s->q.rows, s->heads) || !words_ok(d_lse)) return HE_EINVAL;
     if (s->k.rows > 0 && (!heads_ok(k, s->type) || !heads_ok(v, s->type))) return HE_EINVAL;
     const size_t need = attn_bytes(s, false);
     if (need && (!d_ws || ws_bytes < need)) return HE_EWORKSPACE;
@@ -349,7 +358,6 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
     unsigned grid;
     if (!attn_grid(a, p.slots, (int64_t)s->heads * p.splits, grid)) return HE_EINVAL;
     const int64_t rows = s->q.rows * s->heads;
-    if (p.splits > 1 && rows >= (int64_t)4 << 23) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
@@ -371,7 +379,8 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
         return HE_OK;
     }
     const bool some_q = s->q.rows > 0, some_k = s->k.rows > 0;
-    if (some_q && (!heads_ok(q, s->type) || !heads_ok(o, s->type) || !heads_ok(go, s->type) || !out_ok(dq, s, s->q.rows, s->heads) || !d_lse)) return HE_EINVAL;
+    if (some_q && (!heads_ok(q, s->type) || !heads_ok(o, s->type) || !heads_ok(go, s->type) || !out_ok(dq, s, s->q.rows, s->heads) || !words_ok(d_lse)))
+        return HE_EINVAL;
     if (some_k && (!heads_ok(k, s->type) || !heads_ok(v, s->type) || !out_ok(dk, s, s->k.rows, s->kv_heads) ||
                    !out_ok(dv, s, s->k.rows, s->kv_heads)))
         return HE_EINVAL;
@@ -397,7 +406,6 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, tile_q), s->heads, grid_q)) return HE_EINVAL;
     if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, tile_k), (int64_t)s->kv_heads * b.splits, grid_kv)) return HE_EINVAL;
     const int64_t rows_kv = s->k.rows * s->kv_heads;
-    if (b.splits > 1 && rows_kv >= (int64_t)4 << 23) return HE_EINVAL;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;

@@ -14,7 +14,7 @@ struct NormArgs {
     void *y, *s;
     float *mean, *rstd;
     int64_t x_row, r_row, y_row, s_row; // row strides, in elements
-    int rows, width;
+    int rows, width, first; // rows, of them the first one of this launch
     float eps;
 };
 struct NormGradArgs {
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
     __shared__ float red[THREADS / 64];
-    const int t = threadIdx.x % TPR, row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR, row = a.first + blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
     const bool live = row < a.rows; // a row's lanes are live or not together; all of them take part in the sums, on the last row
     const int64_t r = min(row, a.rows - 1);
     Vec<T, VEC> x[NC], res[NC];

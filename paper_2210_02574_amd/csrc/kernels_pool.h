@@ -18,6 +18,7 @@ struct PoolGradArgs {
     int64_t dx_row;
     Spans s;
     int width, fill;
+    int tile; // rows of a tile
 };
 
 // grid (sequences or tile slots, column blocks).  A thread has one vector of columns and every RG-th row; CL = threads along the columns.
@@ -89,10 +90,9 @@ static __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 }
 
 // grid (tile slots, column blocks): the rows of one tile get the sequence's row, rows of no sequence zeros if `fill`.
-#define POOL_TILE 32
 template <class T, int VEC> __global__ __launch_bounds__(256) void k_pool_grad(PoolGradArgs a, int CL)
 {
-    const TileRows t = tile_rows(a.s, a.s, blockIdx.x, POOL_TILE);
+    const TileRows t = tile_rows(a.s, a.s, blockIdx.x, a.tile);
     if (t.first >= t.top) return;
     const int RG = 256 / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
     const int col = (blockIdx.y * CL + cl) * VEC, n = t.end - t.begin;

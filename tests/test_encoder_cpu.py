@@ -48,6 +48,10 @@ def test_layer_norm_refusals(he):
                {"rstd": None}, {"residual": (P, 64)}, {"residual": (P, 63), "sum_": (P, 64)}, {"residual": (P, 64), "sum_": (P, 63)}):
         assert _norm(he, **kw) == EINVAL, kw
     assert he.lib.he_layer_norm(None, *[None] * 10) == EINVAL
+    for kw in ({"x": (P + 1, 64)}, {"y": (P + 1, 64)}, {"w": P + 1}, {"b": P + 1}, {"mean": P + 2}, {"rstd": P + 2},
+               {"residual": (P + 1, 64), "sum_": (P, 64)}, {"residual": (P, 64), "sum_": (P + 1, 64)}):  # not at a multiple of the element's size
+        assert _norm(he, _C.he_norm(2, 2, 5, 64, 1e-5), **kw) == EINVAL, kw
+    assert _norm(he, _C.he_norm(2, 0, 5, 64, 1e-5), w=P + 2) == EINVAL and _norm(he, _C.he_norm(2, 2, 5, 64, 1e-5), w=P + 2) == ENODEV
     assert _norm(he, _C.he_norm(2, 0, 0, 64, 1e-5), x=None, y=None) == ENODEV  # no rows: buffers are not looked at
 
 
@@ -65,6 +69,9 @@ def test_layer_norm_grad_refusals(he):
     assert call() == ENODEV
     for kw in ({"dy": None}, {"s": None}, {"s": (P, 8)}, {"w": None}, {"mean": None}, {"rstd": None}, {"add": (P, 63)}, {"add": (0, 64)},
                {"ds": None}, {"dw": None}, {"db": None}, {"ws": P + 2}):
+        assert call(**kw) == EINVAL, kw
+    for kw in ({"dy": (P + 1, 64)}, {"s": (P + 1, 64)}, {"add": (P + 1, 64)}, {"ds": (P + 1, 64)}, {"w": P + 1}, {"dw": P + 1}, {"db": P + 1},
+               {"mean": P + 2}, {"rstd": P + 2}):
         assert call(**kw) == EINVAL, kw
     assert call(ws=None) == EWORKSPACE and call(size=need.value - 1) == EWORKSPACE
 
@@ -87,16 +94,18 @@ def test_pool_refusals(he):
     grad = lambda s, width=64, x=x, e=P, type=0: he.lib.he_pool_grad(he.ctx, type, _ref(s), width, e, _ref(x), 1, None)  # noqa: E731
     assert pool(_spans()) == ENODEV and grad(_spans()) == ENODEV
     assert pool(_spans(0, 40)) == ENODEV and grad(_spans(0, 40)) == ENODEV
-    for s in (None, _spans(-1), _spans((1 << 24) + 1), _spans(3, -1), _spans(3, 1 << 31), _spans(begin=None), _spans(end=None)):
+    assert pool(_spans(1 << 23), size=1 << 40) == ENODEV and grad(_spans(1 << 23)) == ENODEV
+    for s in (None, _spans(-1), _spans((1 << 23) + 1), _spans((1 << 24) + 1), _spans(begin=P + 2), _spans(end=P + 1), _spans(3, -1), _spans(3, 1 << 31), _spans(begin=None), _spans(end=None)):
         assert pool(s) == EINVAL and grad(s) == EINVAL
         assert he.lib.he_pool_workspace_bytes(he.ctx, _ref(s), 64, _ref(need)) == EINVAL
-    for kw in ({"width": 0}, {"width": (1 << 20) + 1}, {"x": None}, {"x": _C.he_rows(P, 63)}, {"e": None}, {"type": 3}):
+    for kw in ({"width": 0}, {"width": (1 << 20) + 1}, {"x": None}, {"x": _C.he_rows(P, 63)}, {"x": _C.he_rows(P + 2, 64)}, {"e": None}, {"e": P + 2},
+               {"type": 3}):
         assert pool(_spans(), **kw) == EINVAL and grad(_spans(), **kw) == EINVAL, kw
     assert pool(long, ws=None) == EWORKSPACE and pool(long, size=64) == EWORKSPACE and pool(long, ws=P + 2) == EINVAL
 
 
-def _attn(type=2, heads=4, kv=2, dim=64, q=None, k=None, scale=0.125, cap=0.0):
-    return bd._ATTN.pack(type, heads, kv, dim, *(q or _span()), *(k or _span()), scale, cap, 0, 1)
+def _attn(type=2, heads=4, kv=2, dim=64, q=None, k=None, scale=0.125, cap=0.0, slopes=0):
+    return bd._ATTN.pack(type, heads, kv, dim, *(q or _span()), *(k or _span()), scale, cap, slopes, 1)
 
 
 def test_attention_refusals(he):
@@ -114,7 +123,7 @@ def test_attention_refusals(he):
     inf, nan = float("inf"), float("nan")
     for s in (None, _attn(type=3), _attn(heads=0), _attn(kv=0), _attn(heads=5), _attn(heads=65536, kv=1), _attn(dim=0), _attn(dim=12),
               _attn(dim=136), _attn(scale=0.0), _attn(scale=-1.0), _attn(scale=nan), _attn(scale=inf), _attn(scale=1e-60), _attn(scale=1e60), _attn(cap=-1.0),
-              _attn(cap=nan), _attn(cap=inf), _attn(cap=1e-60), _attn(q=_span(2)), _attn(q=_span(-1), k=_span(-1)), _attn(q=_span(3, -1)),
+              _attn(cap=nan), _attn(cap=inf), _attn(cap=1e-60), _attn(scale=1e30, cap=1e-30), _attn(q=_span(2)), _attn(q=_span(-1), k=_span(-1)), _attn(q=_span(3, -1)),
               _attn(q=_span(3, 1 << 31)), _attn(q=_span(begin=None)), _attn(k=_span(end=None))):
         assert fwd(s) == EINVAL and bwd(s) == EINVAL
         assert he.lib.he_attention_workspace_bytes(he.ctx, _ref(s), 0, _ref(need)) == EINVAL
@@ -123,6 +132,8 @@ def test_attention_refusals(he):
             assert fwd(_attn(), **{name: bad}) == EINVAL, (name, bad)
         for name in ("go", "q", "k", "v", "o", "dq", "dk", "dv"):
             assert bwd(_attn(), **{name: bad}) == EINVAL, (name, bad)
+    assert fwd(_attn(), lse=P + 2) == EINVAL and bwd(_attn(), lse=P + 2) == EINVAL
+    assert fwd(_attn(slopes=P + 4)) == ENODEV and fwd(_attn(slopes=P + 2)) == EINVAL and bwd(_attn(slopes=P + 2)) == EINVAL
     assert fwd(_attn(), lse=None) == EINVAL and bwd(_attn(), lse=None) == EINVAL
     assert bwd(_attn(), ws=None) == EWORKSPACE and bwd(_attn(), size=40 * 4 * 4 - 1) == EWORKSPACE and bwd(_attn(), ws=P + 4) == EINVAL
     long = _attn(q=_span(1, 1), k=_span(1, 1 << 20))  # one query of many keys: cut along the keys

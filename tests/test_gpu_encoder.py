@@ -80,6 +80,17 @@ def test_layer_norm_of_no_rows(he):
     assert y.shape == dx.shape == (0, 64) and not dw.any() and not db.any()
 
 
+def test_layer_norm_of_more_rows_than_a_launch_holds(he):
+    """2^32 threads are too many, and 32 of them are a row's here.  Every row has the same numbers in another order of its two halves."""
+    rows, row = (1 << 27) + 37, rand(1, 8, dtype=BF16)
+    x = row.expand(rows, 8).contiguous()
+    x[1::2] = row.roll(4)
+    y, _, mean, rstd = he.layer_norm(x, torch.ones(8, device="cuda"), torch.zeros(8, device="cuda"))
+    small = he.layer_norm(x[:2], torch.ones(8, device="cuda"), torch.zeros(8, device="cuda"))
+    for k in range(2):
+        assert (y[k::2] == small[0][k]).all() and (mean[k::2] == small[2][k]).all() and (rstd[k::2] == small[3][k]).all()
+
+
 def test_layer_norm_weight_gradient_of_many_rows_repeats(he):
     x, dy = rand(1, 70001, 64, dtype=F16), rand(2, 70001, 64, dtype=F16)
     w = rand(3, 64)
@@ -123,6 +134,24 @@ def test_pool_mean_of_padded_rows(he):
     out = torch.full_like(dx, 3.0)
     he.pool_mean_backward(de, (begin, end), 63, BF16, out=out)
     assert (out[~keep.cuda()] == 3).all() and torch.equal(out[keep.cuda()], dx[keep.cuda()])
+
+
+def test_pool_mean_of_more_rows_and_sequences_than_a_launch_holds(he):
+    rows = (1 << 29) + 40  # tiles of 32 rows would take 2^32 threads
+    de = torch.full((1, 1), float(rows), device="cuda")
+    dx = he.pool_mean_backward(de, i32(0, rows), rows, BF16)
+    assert dx.shape == (rows, 1) and (dx == 1).all()
+    assert he.pool_mean(dx, i32(0, rows)) == 1  # sums of 2^18 each, whose sum is rounded as the length is
+    del dx
+    count = (1 << 22) + 9  # work-groups of 1024 threads would take 2^32 of them
+    off = torch.full((count + 1,), 5, dtype=torch.int32, device="cuda")
+    off[:count - 3] = 0  # sequence count - 4 has all rows
+    x = rand(1, 5, 8)
+    e = he.pool_mean(x, off)
+    assert not e[:count - 4].any() and not e[count - 3:].any()
+    assert (e[count - 4].double() - x.double().mean(0)).abs().max() <= 5 * 2.0**-24 * x.abs().max()
+    want = e[count - 4].double() / 5  # one rounding of the quotient
+    assert ((he.pool_mean_backward(e, off, 5, F32) - want).abs() <= 2.0**-24 * want.abs()).all()
 
 
 def test_pool_mean_of_no_sequences_and_no_rows(he):
