@@ -979,6 +979,9 @@ class HE:
             gq, gk, gv = (_HEADS.pack(t.data_ptr(), n, shape[2]) for t, n in ((dq, shape[1] * shape[2]), (dk, kv), (dv, kv)))
         else:
             dq, dk, dv = out
+            if not count and fill:  # the library writes nothing without sequences
+                for t in out:
+                    t.zero_()
             gq, gk, gv = self._heads(dq, "dq", shape, dtype), self._heads(dk, "dk", k.shape, dtype), self._heads(dv, "dv", k.shape, dtype)
         n = self._attn_bytes(s, True)
         ws = self._scratch(q, n)

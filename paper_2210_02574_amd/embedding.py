@@ -3,6 +3,7 @@ x -> F_emb(x), then encryption), with gradients, so that an encoder can be fitte
 
 The operators are the library's (HE.attention, HE.layer_norm, HE.pool_mean); the functions here make them differentiable, and SentenceEncoder puts them
 together.  Matrix products with weights are plain library products.  Sentences are packed back to back or padded, as HE's offsets say.
+Gradients are of the first order: a backward pass that is to be differentiated again is refused.
 """
 from __future__ import annotations
 
@@ -11,9 +12,17 @@ from typing import Dict, List, Sequence
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 from torch.nn import functional as F
 
 from .classifier import BLOCK, pack_samples
+
+
+def _kept(offsets):
+    """Offsets as tensors to save for a backward pass, which then notices if they have been written since, and as what HE takes from those."""
+    if isinstance(offsets, (tuple, list)):
+        return tuple(offsets), tuple
+    return (offsets,), lambda t: t[0]
 
 
 class _Norm(torch.autograd.Function):
@@ -26,6 +35,7 @@ class _Norm(torch.autograd.Function):
         return (y, s) if ctx.residual else (y, None)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, ds):
         s, weight, mean, rstd = ctx.saved_tensors
         if dy is None:  # only the sum was used
@@ -44,15 +54,17 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, he, q, k, v, offsets, offsets_k, scale, cap, slopes):
         o, lse = he.attention(q, k, v, offsets, offsets_k=offsets_k, scale=scale, cap=cap, slopes=slopes)
-        ctx.he, ctx.args = he, (offsets, offsets_k, scale, cap, slopes)
-        ctx.save_for_backward(q, k, v, o, lse)
+        (a, join), (b, join_k) = _kept(offsets), ((None,), lambda t: None) if offsets_k is None else _kept(offsets_k)
+        ctx.he, ctx.args = he, (len(a), join, join_k, scale, cap)
+        ctx.save_for_backward(q, k, v, o, lse, slopes, *a, *b)
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
-        offsets, offsets_k, scale, cap, slopes = ctx.args
-        q, k, v, o, lse = ctx.saved_tensors
-        grads = ctx.he.attention_backward(do.contiguous(), q, k, v, o, lse, offsets, offsets_k=offsets_k, scale=scale, cap=cap, slopes=slopes)
+        n, join, join_k, scale, cap = ctx.args
+        q, k, v, o, lse, slopes, *off = ctx.saved_tensors
+        grads = ctx.he.attention_backward(do.contiguous(), q, k, v, o, lse, join(off[:n]), offsets_k=join_k(off[n:]), scale=scale, cap=cap, slopes=slopes)
         return (None, *grads, None, None, None, None, None)
 
 
@@ -70,30 +82,36 @@ class _SelfAttention(torch.autograd.Function):
     def forward(ctx, he, qkv, kv_heads, offsets, cap, slopes):
         h = qkv.shape[1] - 2 * kv_heads
         o, lse = he.attention(qkv[:, :h], qkv[:, h:h + kv_heads], qkv[:, h + kv_heads:], offsets, cap=cap, slopes=slopes)
-        ctx.he, ctx.args = he, (kv_heads, offsets, cap, slopes)
-        ctx.save_for_backward(qkv, o, lse)
+        off, join = _kept(offsets)
+        ctx.he, ctx.args = he, (kv_heads, join, cap)
+        ctx.save_for_backward(qkv, o, lse, slopes, *off)
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
-        kv, offsets, cap, slopes = ctx.args
-        qkv, o, lse = ctx.saved_tensors
+        kv, join, cap = ctx.args
+        qkv, o, lse, slopes, *off = ctx.saved_tensors
         h = qkv.shape[1] - 2 * kv
         d = torch.empty_like(qkv)
         cut = lambda t: (t[:, :h], t[:, h:h + kv], t[:, h + kv:])  # noqa: E731
-        ctx.he.attention_backward(do.contiguous(), *cut(qkv), o, lse, offsets, cap=cap, slopes=slopes, out=cut(d), fill=True)
+        ctx.he.attention_backward(do.contiguous(), *cut(qkv), o, lse, join(off), cap=cap, slopes=slopes, out=cut(d), fill=True)
         return None, d, None, None, None, None
 
 
 class _Pool(torch.autograd.Function):
     @staticmethod
     def forward(ctx, he, x, offsets):
-        ctx.he, ctx.offsets, ctx.rows, ctx.dtype = he, offsets, x.shape[0], x.dtype
+        off, join = _kept(offsets)
+        ctx.he, ctx.args = he, (join, x.shape[0], x.dtype)
+        ctx.save_for_backward(*off)
         return he.pool_mean(x, offsets)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, de):
-        return None, ctx.he.pool_mean_backward(de.contiguous(), ctx.offsets, ctx.rows, ctx.dtype), None
+        join, rows, dtype = ctx.args
+        return None, ctx.he.pool_mean_backward(de.contiguous(), join(ctx.saved_tensors), rows, dtype), None
 
 
 def pool_mean(he, x, offsets):
@@ -115,6 +133,8 @@ class SentenceEncoder:
                  slopes=None, eps: float = 1e-5):
         if pool not in ("mean", "first"):
             raise ValueError(f"pool: {pool!r}, want 'mean' or 'first'")
+        if slopes is not None and slopes.requires_grad:
+            raise ValueError("slopes are constants: they have no gradient")
         for i, w in enumerate(layers):
             missing = [n for n in self.NAMES if n not in w]
             if missing:

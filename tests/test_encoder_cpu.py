@@ -169,6 +169,8 @@ def test_encoder_refusals(he):
         SentenceEncoder(he, [w], 2, pool="max")
     with pytest.raises(ValueError, match="lacks norm2"):
         SentenceEncoder(he, [{k: v for k, v in w.items() if k != "norm2"}], 2)
+    with pytest.raises(ValueError, match="constants"):
+        SentenceEncoder(he, [w], 2, slopes=torch.ones(2, requires_grad=True))
     from paper_2210_02574_amd.embedding import attention as diff_attention
 
     with pytest.raises(ValueError, match="constants"):

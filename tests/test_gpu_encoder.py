@@ -499,6 +499,42 @@ def test_gradients_against_differences(he):
         assert abs(diff - want) < 2.0**-11 * (1 + float(grads[i].norm())), (i, diff, want)
 
 
+def test_gradients_of_no_sentences_are_zeros(he):
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    layer, x = SentenceEncoder.random_layer(64, 2, 96, 5, F32, "cuda"), rand(1, 6, 64).requires_grad_(True)
+    torch.full((6 * 384,), float("nan"), device="cuda")  # what memory that is not written may hold
+    layer["qkv"].requires_grad_(True)
+    e = SentenceEncoder(he, [layer], 2)(x, i32(0))
+    assert e.shape == (0, 64)
+    e.sum().backward()
+    assert not x.grad.any() and not layer["qkv"].grad.any()
+    d = [torch.full((6, 2, 32), float("nan"), device="cuda") for _ in range(3)]
+    q = rand(2, 6, 2, 32)
+    o, lse = he.attention(q, q, q, i32(0))
+    he.attention_backward(q, q, q, q, o, lse, i32(0), out=d, fill=True)
+    assert not any(t.any() for t in d)
+
+
+def test_refusals_of_the_differentiable_functions(he):
+    """A second derivative, and offsets that are written between the two passes."""
+    from paper_2210_02574_amd.embedding import attention, layer_norm, pool_mean
+
+    w = torch.ones(64, device="cuda")
+    fns = (lambda x, o: layer_norm(he, x, w, w)[0], lambda x, o: attention(he, *[x.view(6, 2, 32)] * 3, o), lambda x, o: pool_mean(he, x, o),
+           lambda x, o: attention(he, *[x.view(6, 2, 32)] * 3, (o[:1], o[1:]), offsets_k=(o[:1], o[1:])))
+    for k, f in enumerate(fns):
+        off, x = i32(0, 6), rand(1, 6, 64).requires_grad_(True)
+        g, = torch.autograd.grad(f(x, off).square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.sum().backward()
+        y = f(x, off).square().sum()
+        off[0] = 1
+        if k:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward()
+
+
 def test_sentences_to_encrypted_logits(he):
     """The whole path: token states -> embeddings -> packed, encrypted -> encrypted classifier -> logits, against the same in the clear."""
     from paper_2210_02574_amd.classifier import EncryptedInference, logits_from_slots
