@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import List, Sequence
 
 import numpy as np
@@ -18,7 +17,6 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhe_gfx950.so")
 
 HE_OK = 0
-HE_EWORKSPACE = -4
 ERRORS = {
     -1: "HE_EINVAL", -2: "HE_ELEVEL", -3: "HE_ENOKEY", -4: "HE_EWORKSPACE",
     -5: "HE_EHIP", -6: "HE_ENODEV", -7: "HE_ENOMEM", -8: "HE_ESCRATCH",
@@ -54,14 +52,6 @@ class he_kernel_stat(ctypes.Structure):
         ("name", ctypes.c_char * 48), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
         ("bytes", ctypes.c_double),
     ]
-
-
-# descriptors of the operators on token states, laid out as C does
-_ROWS = struct.Struct("@Pq")               # he_rows: d, stride
-_HEADS = struct.Struct("@Pqq")             # he_heads: d, row, head
-_SPANS = struct.Struct("@PPiq")            # he_spans: d_begin, d_end, count, rows
-_NORM = struct.Struct("@iiqid")            # he_norm: type, weight_type, rows, width, eps
-_ATTN = struct.Struct("@4iPPiqPPiqddPi4x") # he_attn: type, heads, kv_heads, dim, q, k, scale, cap, d_slopes, fill
 
 
 class he_params(ctypes.Structure):
@@ -184,6 +174,23 @@ def _hp(a: np.ndarray):
     return ctypes.c_void_p(a.ctypes.data)
 
 
+_tensors = None
+
+
+def load_tensors():
+    """The extension module for torch tensors (csrc/tensors.cpp), built with the library."""
+    global _tensors
+    if _tensors is None:
+        load_library()
+        import importlib.util
+
+        spec = importlib.util.spec_from_file_location("he_tensors", os.path.join(_HERE, "he_tensors.so"))
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _tensors = module
+    return _tensors
+
+
 class SecretKey:
     def __init__(self, he, handle):
         self.he, self.handle = he, handle
@@ -240,7 +247,7 @@ class HE:
             raise HeError(rc, "he_ctx_create")
         self.ctx = h
         self._ws = None
-        self._type_of = None
+        self._ctx, self._tensors, self._raw_stream = h.value, None, lambda device: 0
 
     @classmethod
     def from_params(cls, params, device: int = -1):
@@ -733,263 +740,51 @@ class HE:
     # Floating-point rows on this context's device.  Sequences: an int32 tensor [count + 1] of offsets (sequence i is the rows
     # offsets[i] .. offsets[i + 1]), or a pair (begin, end) of int32 tensors [count] where rows between them belong to none (a
     # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.
-    # Calls on short sentences last as long as this code does, so descriptors are packed as bytes (a ctypes structure takes
-    # several times as long to fill) and tensors are asked for each number once.
-    def _types(self):
-        import torch
+    # Tensors are checked and made in he_tensors (csrc/tensors.cpp): calls on short sentences last as long as the host needs for them.
+    def _on_tensors(self, name: str, where: str, *args):
+        if self._tensors is None:
+            self._tensors = load_tensors()
+            if self.device >= 0:
+                import torch
 
-        self._t32, self._i32 = torch.float32, torch.int32
-        self._empty_like, self._dense = torch.empty_like, torch.contiguous_format
-        self._type_of = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # HE_F32, HE_F16, HE_BF16
-        self._raw_stream = torch._C._cuda_getCurrentRawStream  # of torch.cuda.current_stream, without an object around it
-        return self._type_of
-
-    def _type(self, dtype) -> int:
-        code = (self._type_of or self._types()).get(dtype)
-        if code is None:
-            raise ValueError(f"{dtype}: rows are float32, float16 or bfloat16")
-        return code
-
-    def _placed(self, t, what: str, dtype=None):
-        if t.get_device() != self.device or self.device < 0:
-            raise ValueError(f"{what}: on {t.device}, the context is on device {self.device}")
-        if dtype is not None and t.dtype != dtype:
-            raise ValueError(f"{what}: {t.dtype}, want {dtype}")
-
-    def _rows(self, t, what: str, shape, dtype=None) -> bytes:
-        """[rows][width], dense along the width: he_rows."""
-        if t.shape != shape or len(shape) != 2:
-            raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][width]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
-        rows, width = shape
-        stride, dense = t.stride()
-        if dense != 1 and width > 1:
-            raise ValueError(f"{what}: want rows that are dense along the width")
-        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
-            self._placed(t, what, dtype)
-        return _ROWS.pack(t.data_ptr(), stride if rows > 1 else width)
-
-    def _vector(self, t, what: str, n: int, dtype) -> int:
-        shape = t.shape
-        if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
-            raise ValueError(f"{what}: want a dense vector of {n}")
-        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
-            self._placed(t, what, dtype)
-        return t.data_ptr()
-
-    def _spans(self, offsets, rows: int, what: str = "offsets"):
-        """The fields of he_spans."""
-        if self._type_of is None:
-            self._types()
-        if isinstance(offsets, (tuple, list)):
-            begin, end = offsets
-            if begin.dim() != 1 or end.shape != begin.shape:
-                raise ValueError(f"{what}: begin and end are vectors of one length")
-            count = begin.shape[0]
-            return self._vector(begin, what, count, self._i32), self._vector(end, what, count, self._i32), count, rows
-        shape = offsets.shape
-        if len(shape) != 1 or shape[0] < 1:
-            raise ValueError(f"{what}: want a vector of count + 1 offsets, or a pair of vectors (begin, end)")
-        n = shape[0]
-        p = self._vector(offsets, what, n, self._i32)
-        return p, p + 4, n - 1, rows
-
-    def _scratch(self, like, need: int):
-        """A workspace of this call's own, from torch's allocator: calls on other streams and captured graphs have theirs."""
-        return like.new_empty((need + 3) // 4, dtype=self._t32) if need else None
+                self._raw_stream = torch._C._cuda_getCurrentRawStream  # of torch.cuda.current_stream, without an object around it
+        r = getattr(self._tensors, name)(self._ctx, self.device, self._raw_stream(self.device), *args)
+        if r.__class__ is int:
+            self._chk(r, where)
+        return r
 
     def layer_norm(self, x, weight, bias, residual=None, eps: float = 1e-5, out=None):
         """(x - mean) rstd weight + bias over the last dimension of x [rows][width], of s = x + residual with one (rounded to the type).
         Returns (y, s, mean, rstd); s is x itself without a residual.  Keep s, mean and rstd for layer_norm_backward."""
-        dtype, shape = x.dtype, x.shape
-        code = self._type(dtype)
-        xr = self._rows(x, "x", shape)
-        rows, width = shape
-        wd = weight.dtype
-        w, b = self._vector(weight, "weight", width, None), self._vector(bias, "bias", width, wd)
-        rr = sr = None
-        s = x
-        if residual is not None:
-            rr = self._rows(residual, "residual", shape, dtype)
-            s = self._empty_like(x, memory_format=self._dense)
-            sr = _ROWS.pack(s.data_ptr(), width)
-        if out is None:
-            y = self._empty_like(x, memory_format=self._dense)
-            yr = _ROWS.pack(y.data_ptr(), width)
-        else:
-            y, yr = out, self._rows(out, "out", shape, dtype)
-        mean, rstd = x.new_empty((2, rows), dtype=self._t32).unbind(0)
-        rc = self.lib.he_layer_norm(self.ctx, _NORM.pack(code, self._type(wd), rows, width, eps), xr, rr, w, b, yr, sr, mean.data_ptr(), rstd.data_ptr(),
-                                    self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_layer_norm")
-        return y, s, mean, rstd
+        return self._on_tensors("layer_norm", "he_layer_norm", x, weight, bias, residual, eps, out)
 
     def layer_norm_backward(self, dy, s, weight, mean, rstd, ds=None):
         """(dx, dweight, dbias) from the gradient of y; ds: a gradient that reaches s from elsewhere, added to dx.  dx is the gradient of x and
         of the residual both."""
-        dtype, shape = s.dtype, s.shape
-        code = self._type(dtype)
-        sr = self._rows(s, "s", shape)
-        rows, width = shape
-        dyr, ar = self._rows(dy, "dy", shape, dtype), None if ds is None else self._rows(ds, "ds", shape, dtype)
-        w, m, r = self._vector(weight, "weight", width, None), self._vector(mean, "mean", rows, self._t32), self._vector(rstd, "rstd", rows, self._t32)
-        n = _NORM.pack(code, self._type(weight.dtype), rows, width, 0.0)
-        need = ctypes.c_size_t()
-        rc = self.lib.he_layer_norm_workspace_bytes(self.ctx, n, need)
-        if rc:
-            self._chk(rc, "he_layer_norm_workspace_bytes")
-        dx = self._empty_like(s, memory_format=self._dense)
-        dw, db = weight.new_empty((2, width)).unbind(0)
-        ws = self._scratch(s, need.value)
-        rc = self.lib.he_layer_norm_grad(self.ctx, n, dyr, sr, w, m, r, ar, _ROWS.pack(dx.data_ptr(), width), dw.data_ptr(), db.data_ptr(),
-                                         ws.data_ptr() if ws is not None else None, need.value, self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_layer_norm_grad")
-        return dx, dw, db
+        return self._on_tensors("layer_norm_backward", "he_layer_norm_grad", dy, s, weight, mean, rstd, ds)
 
     def pool_mean(self, x, offsets, out=None):
         """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence."""
-        code, shape = self._type(x.dtype), x.shape
-        xr = self._rows(x, "x", shape)
-        rows, width = shape
-        span = self._spans(offsets, rows)
-        count, sp = span[2], _SPANS.pack(*span)
-        if out is None:
-            e = x.new_empty((count, width), dtype=self._t32)
-        else:
-            e = out
-            if e.shape != (count, width) or not e.is_contiguous():
-                raise ValueError(f"out: want a dense [{count}][{width}]")
-            self._placed(e, "out", self._t32)
-
-        def sizes():
-            need = ctypes.c_size_t()
-            self._chk(self.lib.he_pool_workspace_bytes(self.ctx, sp, width, need), "he_pool_workspace_bytes")
-            return need.value
-
-        self._with_scratch(self.lib.he_pool, sizes, "he_pool", x, code, sp, width, xr, e.data_ptr())
-        return e
+        return self._on_tensors("pool_mean", "he_pool", x, offsets, out)
 
     def pool_mean_backward(self, de, offsets, rows: int, dtype, out=None):
         """Gradient of pool_mean's x [rows][width], of type dtype, from de [count][width]."""
-        code, span = self._type(dtype), self._spans(offsets, rows)
-        count = span[2]
-        if de.dim() != 2 or de.shape[0] != count or not de.is_contiguous():
-            raise ValueError(f"de: want a dense [{count}][width]")
-        width = de.shape[1]
-        self._placed(de, "de", self._t32)
-        if out is None:
-            dx = de.new_empty((rows, width), dtype=dtype) if count else de.new_zeros((rows, width), dtype=dtype)
-            xr = _ROWS.pack(dx.data_ptr(), width)
-        else:
-            dx = out
-            if tuple(dx.shape) != (rows, width):
-                raise ValueError(f"out: want [{rows}][{width}]")
-            xr = self._rows(dx, "out", dx.shape, dtype)
-        rc = self.lib.he_pool_grad(self.ctx, code, _SPANS.pack(*span), width, de.data_ptr(), xr, out is None, self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_pool_grad")
-        return dx
-
-    def _heads(self, t, what: str, shape, dtype=None) -> bytes:
-        """[rows][heads][dim] with a dense last dimension: he_heads."""
-        if t.shape != shape or len(shape) != 3:
-            raise ValueError(f"{what}: {tuple(t.shape)}, want [rows][heads][dim]" + (f" = {tuple(shape)}" if shape != t.shape else ""))
-        row, head, dense = t.stride()
-        p = t.data_ptr()
-        if t.get_device() != self.device or self.device < 0 or (dtype is not None and t.dtype is not dtype):
-            self._placed(t, what, dtype)
-        if dense != 1 and shape[2] > 1:
-            raise ValueError(f"{what}: the last dimension is not dense")
-        if (p | (row | head) * t.element_size()) & 15 and t.numel():
-            raise ValueError(f"{what}: address {p:#x} or strides {t.stride()} not in multiples of 16 bytes")
-        return _HEADS.pack(p, row, head)
-
-    def _attn(self, q, k, v, offsets, offsets_k, scale, cap, slopes, fill):
-        """(he_attn, count of sequences, he_heads of q, k, v)"""
-        dtype, shape, kshape = q.dtype, q.shape, k.shape
-        code, qh = self._type(dtype), self._heads(q, "q", shape)
-        rows, heads, dim = shape
-        if len(kshape) != 3 or kshape[2] != dim:
-            raise ValueError(f"k: {tuple(kshape)}, want [rows][heads][{dim}]")
-        rows_k, kv, _ = kshape
-        kh, vh = self._heads(k, "k", kshape, dtype), self._heads(v, "v", kshape, dtype)
-        if kv == 0 or heads % kv:
-            raise ValueError(f"{heads} query heads on {kv} key heads")
-        sq = sk = self._spans(offsets, rows)
-        if offsets_k is not None and (offsets_k is not offsets or rows_k != rows):
-            sk = self._spans(offsets_k, rows_k, "offsets_k")
-            if sk[2] != sq[2]:
-                raise ValueError("offsets and offsets_k: another number of sequences")
-        elif rows_k != rows:
-            raise ValueError("keys of another length than the queries need offsets_k")
-        sl = 0 if slopes is None else self._vector(slopes, "slopes", heads, self._t32)
-        return _ATTN.pack(code, heads, kv, dim, *sq, *sk, dim**-0.5 if scale is None else scale, cap, sl, fill), sq[2], qh, kh, vh
-
-    def _with_scratch(self, fn, sizes, where: str, like, *args):
-        """fn(ctx, *args, workspace, bytes, stream), first without a workspace: most calls take none, and one that does says so before it enqueues
-        anything.  sizes() gives the bytes then."""
-        rc = fn(self.ctx, *args, None, 0, self._raw_stream(self.device))
-        if rc == HE_EWORKSPACE:
-            need = sizes()
-            ws = self._scratch(like, need)
-            rc = fn(self.ctx, *args, ws.data_ptr(), need, self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, where)
-
-    def _attn_bytes(self, s, backward: bool) -> int:
-        need = ctypes.c_size_t()
-        rc = self.lib.he_attention_workspace_bytes(self.ctx, s, backward, need)
-        if rc:
-            self._chk(rc, "he_attention_workspace_bytes")
-        return need.value
+        return self._on_tensors("pool_mean_backward", "he_pool_grad", de, offsets, rows, dtype, out)
 
     def attention(self, q, k, v, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None):
         """Attention inside each sequence: q [rows][heads][dim], k and v [rows_k][kv_heads][dim] (strided views of a joint projection are fine;
         query head h reads key head h // (heads / kv_heads)).  offsets_k: the sequences of the keys, where they are not the queries'.
         scale: of the products, 1 / sqrt(dim) by default; cap > 0: cap tanh(score / cap); slopes [heads] float32: minus slope times distance.
         Returns (o, lse): o like q, lse [heads][rows] float32."""
-        s, count, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None)
-        shape = q.shape
-        lse = q.new_empty((shape[1], shape[0]), dtype=self._t32)
-        if out is None:
-            o = self._empty_like(q, memory_format=self._dense) if count else q.new_zeros(shape)
-            oh = _HEADS.pack(o.data_ptr(), shape[1] * shape[2], shape[2])
-        else:
-            o, oh = out, self._heads(out, "out", shape, q.dtype)
-        if out is not None or not count:
-            lse.fill_(float("-inf"))
-        self._with_scratch(self.lib.he_attention, lambda: self._attn_bytes(s, False), "he_attention", q, s, qh, kh, vh, oh, lse.data_ptr())
-        return o, lse
+        return self._on_tensors("attention", "he_attention", q, k, v, offsets, offsets_k, scale, cap, slopes, out)
 
     def attention_backward(self, do, q, k, v, o, lse, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None,
                            fill=None):
         """(dq, dk, dv) from the gradient of o, with o and lse of the forward call and its other arguments.  out: three tensors (strided views are
         fine) to write them to; fill: whether their rows of no sequence become zeros (by default where they are made here).  Slopes are constants:
         they have no gradient."""
-        s, count, qh, kh, vh = self._attn(q, k, v, offsets, offsets_k, scale, cap, slopes, out is None if fill is None else bool(fill))
-        dtype, shape = q.dtype, q.shape
-        gh, oh = self._heads(do, "do", shape, dtype), self._heads(o, "o", shape, dtype)
-        if lse.shape != (shape[1], shape[0]) or not lse.is_contiguous():
-            raise ValueError("lse: want a dense [heads][rows]")
-        self._placed(lse, "lse", self._t32)
-        if out is None:
-            dq, dk, dv = [self._empty_like(t, memory_format=self._dense) if count else t.new_zeros(t.shape) for t in (q, k, v)]
-            kv = k.shape[1] * shape[2]
-            gq, gk, gv = (_HEADS.pack(t.data_ptr(), n, shape[2]) for t, n in ((dq, shape[1] * shape[2]), (dk, kv), (dv, kv)))
-        else:
-            dq, dk, dv = out
-            if not count and fill:  # the library writes nothing without sequences
-                for t in out:
-                    t.zero_()
-            gq, gk, gv = self._heads(dq, "dq", shape, dtype), self._heads(dk, "dk", k.shape, dtype), self._heads(dv, "dv", k.shape, dtype)
-        n = self._attn_bytes(s, True)
-        ws = self._scratch(q, n)
-        rc = self.lib.he_attention_grad(self.ctx, s, gh, qh, kh, vh, oh, lse.data_ptr(), gq, gk, gv, ws.data_ptr() if ws is not None else None, n,
-                                        self._raw_stream(self.device))
-        if rc:
-            self._chk(rc, "he_attention_grad")
-        return dq, dk, dv
+        return self._on_tensors("attention_backward", "he_attention_grad", do, q, k, v, o, lse, offsets, offsets_k, scale, cap, slopes,
+                                None if out is None else tuple(out), out is None if fill is None else fill)
 
     # ---- measurement -------------------------------------------------------------------------------------------------
     def profile_start(self):

@@ -12,6 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhe_gfx950.so")
+TENSORS = os.path.join(HERE, "he_tensors.so")  # the extension module for torch tensors
 # one object per ring size and kernel family: they compile in parallel
 SOURCES = (
     # (source, extra defines, object name), the slowest first
@@ -45,6 +46,21 @@ CODEGEN_FLAGS = [
 ]
 
 
+TENSORS_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-shared", "-Wall"]
+
+
+def _tensors_command() -> list:
+    """Host code alone: torch's and Python's headers, linked to the library beside it."""
+    import importlib.util
+    import sysconfig
+
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    return (["g++"] + TENSORS_FLAGS + ["-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch, "include"),
+                                       "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+                                       os.path.join(CSRC, "tensors.cpp"), "-o", TENSORS + ".tmp", "-L", HERE, "-l:" + os.path.basename(LIB),
+                                       "-L", os.path.join(torch, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined"])
+
+
 def _flags():
     # HE_EXTRA_HIPCC_FLAGS: diagnostics such as -Rpass-analysis=kernel-resource-usage (not part of the source hash)
     return CODEGEN_FLAGS + [
@@ -66,6 +82,7 @@ def source_hash() -> str:
             h.update(fh.read())
     h.update(" ".join(CODEGEN_FLAGS).encode())
     h.update(repr(SOURCES).encode())
+    h.update(" ".join(TENSORS_FLAGS).encode())
     return h.hexdigest()
 
 
@@ -94,6 +111,11 @@ def build(verbose: bool = False, jobs: int | None = None, only=None) -> str:
         print(" ".join(link), flush=True)
     subprocess.check_call(link)
     os.replace(LIB + ".tmp", LIB)
+    if only is None or "tensors" in only or not os.path.exists(TENSORS):
+        if verbose:
+            print(" ".join(_tensors_command()), flush=True)
+        subprocess.check_call(_tensors_command())
+        os.replace(TENSORS + ".tmp", TENSORS)
     with open(STAMP, "w") as fh:
         fh.write(stamp + "\n")
     return LIB
@@ -101,7 +123,7 @@ def build(verbose: bool = False, jobs: int | None = None, only=None) -> str:
 
 def is_stale() -> bool:
     """True when no library is built or its sources have changed since (by content, not by time stamp)."""
-    if not os.path.exists(LIB) or not os.path.exists(STAMP):
+    if not all(os.path.exists(f) for f in (LIB, TENSORS, STAMP)):
         return True
     with open(STAMP) as fh:
         return fh.read().strip() != source_hash()
@@ -110,7 +132,7 @@ def is_stale() -> bool:
 def ensure_built() -> str:
     """Loads what is built; compiles only when nothing is.  A library built from other sources than the present ones is an error
     rather than a silent run of stale kernels (rebuild with ``python -m paper_2210_02574_amd.build``)."""
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(TENSORS):
         return build()
     if is_stale() and not os.environ.get("HE_ALLOW_STALE_LIB"):
         raise RuntimeError(

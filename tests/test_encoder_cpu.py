@@ -1,6 +1,7 @@
 """The operators on token states without a GPU: what the C entry points and the binding refuse, and the reference that the GPU tests compare with,
 against differences and torch's own formulas."""
 import ctypes
+import struct
 
 import numpy as np
 import pytest
@@ -9,7 +10,6 @@ import torch
 import paper_2210_02574_amd as pkg
 import workloads as wl
 from encoder_reference import attention, layer_norm, pool_mean
-from paper_2210_02574_amd import binding as bd
 from paper_2210_02574_amd.embedding import SentenceEncoder, pack_embeddings
 
 EINVAL, EWORKSPACE, ENODEV = -1, -4, -6
@@ -22,9 +22,13 @@ def he():
 
 
 class _C:
-    """Descriptors as bytes."""
+    """Descriptors as bytes, laid out as C does."""
 
-    he_rows, he_heads, he_spans, he_norm = bd._ROWS.pack, bd._HEADS.pack, bd._SPANS.pack, bd._NORM.pack
+    he_rows = struct.Struct("@Pq").pack                # d, stride
+    he_heads = struct.Struct("@Pqq").pack              # d, row, head
+    he_spans = struct.Struct("@PPiq").pack             # d_begin, d_end, count, rows
+    he_norm = struct.Struct("@iiqid").pack             # type, weight_type, rows, width, eps
+    he_attn = struct.Struct("@4iPPiqPPiqddPi4x").pack  # type, heads, kv_heads, dim, q, k, scale, cap, d_slopes, fill
 
 
 def _ref(x):
@@ -105,7 +109,7 @@ def test_pool_refusals(he):
 
 
 def _attn(type=2, heads=4, kv=2, dim=64, q=None, k=None, scale=0.125, cap=0.0, slopes=0):
-    return bd._ATTN.pack(type, heads, kv, dim, *(q or _span()), *(k or _span()), scale, cap, slopes, 1)
+    return _C.he_attn(type, heads, kv, dim, *(q or _span()), *(k or _span()), scale, cap, slopes, 1)
 
 
 def test_attention_refusals(he):
@@ -156,11 +160,12 @@ def test_binding_refusals(he):
         with pytest.raises(ValueError, match="device|want"):
             f()  # CPU tensors: there is no fallback
     for f in (lambda: he.layer_norm(x[0], w, w), lambda: he.layer_norm(x.t(), w, w), lambda: he.pool_mean(x.view(2, 2, 8), off), lambda: he.attention(x, x, x, off),
-              lambda: he._spans(off.view(1, 2), 4), lambda: he._spans((off, off[:1]), 4), lambda: he._heads(x.view(4, 1, 8).transpose(0, 2), "q", (8, 1, 4))):
+              lambda: he.layer_norm(x, None, w), lambda: he.pool_mean_backward(x, off, 4, 5), lambda: he.pool_mean_backward(x, off, -1, torch.float32)):
         with pytest.raises(ValueError):
             f()
-    with pytest.raises(ValueError, match="float32, float16 or bfloat16"):
-        he._type(torch.float64)
+    for f in (lambda: he.layer_norm(x.double(), w, w), lambda: he.pool_mean(x.long(), off), lambda: he.pool_mean_backward(x, off, 4, torch.float64)):
+        with pytest.raises(ValueError, match="float32, float16 or bfloat16"):
+            f()
 
 
 def test_encoder_refusals(he):

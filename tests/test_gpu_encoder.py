@@ -223,15 +223,15 @@ def test_attention_is_cut_where_it_should_be(he):
     """Sizes that test_attention_of_other_keys_and_few_queries (one query of many keys) and test_attention_of_long_sequences (few tiles of keys under many
     queries) run really are cut and joined."""
     import ctypes
-
-    from paper_2210_02574_amd import binding as bd
+    import struct
 
     need = ctypes.c_size_t()
-    sq, sk = he._spans(i32(0, 1), 1), he._spans(i32(0, 4000), 4000)
-    s = bd._ATTN.pack(2, 4, 2, 64, *sq, *sk, 0.125, 0.0, 0, 1)
+    attn = struct.Struct("@4iPPiqPPiqddPi4x").pack  # he_attn
+    sq, sk = (64, 64, 1, 1), (64, 64, 1, 4000)  # begin, end (only their count is looked at), count, rows
+    s = attn(2, 4, 2, 64, *sq, *sk, 0.125, 0.0, 0, 1)
     assert he.lib.he_attention_workspace_bytes(he.ctx, s, 0, ctypes.byref(need)) == 0 and need.value > 0
-    both = he._spans(i32(0, 1100, 3161), 3161)
-    s = bd._ATTN.pack(2, 8, 4, 64, *both, *both, 0.125, 15.0, 0, 1)
+    both = (64, 64, 2, 3161)
+    s = attn(2, 8, 4, 64, *both, *both, 0.125, 15.0, 0, 1)
     assert he.lib.he_attention_workspace_bytes(he.ctx, s, 1, ctypes.byref(need)) == 0 and need.value > 2 * 2 * 4 * 3161 * 64 * 4
 
 
