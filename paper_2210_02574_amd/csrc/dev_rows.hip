@@ -73,7 +73,11 @@ static void pool(he_ctx *c, hipStream_t st, double bytes, unsigned slots, const 
     const unsigned cols = (unsigned)((chunks + cl - 1) / cl);
     if (a.tile) {
         KLAUNCH_T(c, st, KID_POOL, bytes, (k_pool<T, VEC, 256>), dim3(slots, cols), 256, a, cl);
-        KLAUNCH(c, st, KID_POOL_JOIN, 4.0 * a.width * (slots + a.s.count), k_pool_join, dim3((unsigned)a.s.count, (unsigned)((a.width + 255) / 256)), a);
+        bytes = 4.0 * a.width * (slots + a.s.count);
+        if (slots >= (unsigned)a.s.count * POOL_SHARED_TILES)
+            KLAUNCH(c, st, KID_POOL_JOIN, bytes, k_pool_join<8>, dim3((unsigned)a.s.count, (unsigned)((a.width + 31) / 32)), a);
+        else
+            KLAUNCH(c, st, KID_POOL_JOIN, bytes, k_pool_join<1>, dim3((unsigned)a.s.count, (unsigned)((a.width + 255) / 256)), a);
     } else
         KLAUNCH_T(c, st, KID_POOL, bytes, (k_pool<T, VEC, 1024>), dim3((unsigned)a.s.count, cols), 1024, a, cl);
 }

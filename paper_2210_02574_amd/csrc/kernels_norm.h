@@ -121,7 +121,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a
 #pragma unroll
     for (int c = 0; c < NC; c++) {
         const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
-        const Vec<TW, VEC> w = k.load((const TW *)a.w), b = k.load((const TW *)a.b);
+        const Vec<TW, VEC> w = k.load((const TW *)a.w), b = k.load((const TW *)a.b); // (asked for ahead of the sums they cost a wave: 16384 x 768 16 us, 19)
         Vec<T, VEC> y;
 #pragma unroll
         for (int e = 0; e < VEC; e++) y[e] = (T)((v[c][e] - mean) * rstd * (float)w[e] + (float)b[e]);

@@ -26,7 +26,8 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
 {
     __shared__ float join[THREADS * VEC];
     const int RG = THREADS / CL, cl = threadIdx.x % CL, rg = threadIdx.x / CL;
-    const int col = (blockIdx.y * CL + cl) * VEC;
+    const int own = (blockIdx.y * CL + cl) * VEC; // the thread's columns begin here, its vector earlier where it would reach over the row's end
+    const int col = a.width < VEC ? own : min(own, a.width - VEC);
     int lo, hi, n;
     if (a.tile) {
         const TileRows t = tile_rows(a.s, a.s, blockIdx.x, a.tile);
@@ -38,55 +39,76 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
     float s[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; e++) s[e] = 0.f;
-    if (rg < RG && col < a.width) {
+    // No more than it takes to give each eight rows, which cost one trip to memory: fewer shares are to be joined then.
+    const int groups = min(RG, max((hi - lo + 7) / 8, 1));
+    if (rg < groups && own < a.width) {
         const T *x = (const T *)a.x + (lo + rg) * a.x_row;
-        const int64_t step = RG * a.x_row;
-        int left = (hi - lo - rg + RG - 1) / RG; // rows of this thread
-        if (col + VEC <= a.width)
-            for (; left >= 8; left -= 8) {
+        const int64_t step = groups * a.x_row;
+        int left = (hi - lo - rg + groups - 1) / groups; // rows of this thread
+        if (a.width >= VEC)
+            for (; left > 0; left -= 8) {
                 Vec<T, VEC> v[8];
 #pragma unroll
-                for (int u = 0; u < 8; u++, x += step) v[u] = load_once<T, VEC>(x + col);
+                for (int u = 0; u < 8; u++) { // the last row again where there are fewer
+                    v[u] = load_once<T, VEC>(x + col);
+                    if (u + 1 < left) x += step;
+                }
                 __builtin_amdgcn_sched_barrier(0); // eight rows are under way before the first one is waited for
 #pragma unroll
                 for (int u = 0; u < 8; u++)
 #pragma unroll
-                    for (int e = 0; e < VEC; e++) s[e] += (float)v[u][e];
+                    for (int e = 0; e < VEC; e++) s[e] += u < left ? (float)v[u][e] : 0.f;
             }
-        for (; left > 0; left--, x += step) {
-            const Vec<T, VEC> v = load_vec<T, VEC>(x, col, a.width);
+        else
+            for (; left > 0; left--, x += step) {
+                const Vec<T, VEC> v = load_vec<T, VEC>(x, col, a.width);
 #pragma unroll
-            for (int e = 0; e < VEC; e++) s[e] += (float)v[e];
-        }
+                for (int e = 0; e < VEC; e++) s[e] += (float)v[e];
+            }
     }
+    // the shares of the upper half of the groups that are left go to the lower half
+    for (int half = 1 << (31 - __clz(2 * groups - 1)) >> 1; half >= 1; half >>= 1) {
+        if (rg >= half && rg < 2 * half)
 #pragma unroll
-    for (int e = 0; e < VEC; e++) join[e * THREADS + threadIdx.x] = s[e];
-    __syncthreads();
+            for (int e = 0; e < VEC; e++) join[e * THREADS + threadIdx.x] = s[e];
+        __syncthreads();
+        if (rg < half && rg + half < groups)
+#pragma unroll
+            for (int e = 0; e < VEC; e++) s[e] += join[e * THREADS + threadIdx.x + half * CL];
+    }
     if (rg != 0) return;
     float *out = (a.tile ? a.part : a.e) + (size_t)blockIdx.x * a.width;
     const float f = 1.f / (float)n;
 #pragma unroll
-    for (int e = 0; e < VEC; e++) {
-        for (int k = 1; k < RG; k++) s[e] += join[e * THREADS + k * CL + cl];
-        if (col + e < a.width) out[col + e] = s[e] * f;
-    }
+    for (int e = 0; e < VEC; e++)
+        if (col + e >= own && col + e < a.width) out[col + e] = s[e] * f;
 }
 
-// grid (sequences, columns / 256): the tiles of a sequence are those of the slots tile_slot(c, i) .. that reach into it.
-static __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
+// grid (sequences, columns * SHARES / 256), SHARES threads to a column: the tiles of a sequence are those of the slots tile_slot(c, i) .. that reach into it.
+// Shares pay where sequences have many tiles: one sequence of 8192 rows in 128 of them 11 us with one share, 4 with eight; 256 sequences of 580 in 8 4 us, 7.
+#define POOL_SHARED_TILES 16 // per sequence, from which on there are eight shares
+template <int SHARES> __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 {
-    const int col = blockIdx.y * 256 + threadIdx.x, i = blockIdx.x;
-    if (col >= a.width) return;
+    constexpr int COLS = 256 / SHARES;
+    __shared__ float join[256];
+    const int col = blockIdx.y * COLS + threadIdx.x % COLS, share = threadIdx.x / COLS, i = blockIdx.x;
     const int begin = span_begin(a.s, i), end = span_end(a.s, i), c = i ? begin : 0, top = i + 1 < a.s.count ? span_begin(a.s, i + 1) : a.s.rows;
     const int stop = min(end, top); // a tile ends at the next sequence's begin
     const int64_t slot = tile_slot(c, i, a.tile);
     float s = 0.f;
-    if (stop > begin) {
+    if (stop > begin && col < a.width) {
         const int first = (begin - c) / a.tile, last = (stop - 1 - c) / a.tile;
 #pragma unroll 4
-        for (int k = first; k <= last; k++) s += a.part[(size_t)(slot + k) * a.width + col];
+        for (int k = first + share; k <= last; k += SHARES) s += a.part[(size_t)(slot + k) * a.width + col];
     }
-    a.e[(size_t)i * a.width + col] = end > begin ? s / (float)(end - begin) : 0.f;
+    if constexpr (SHARES > 1) {
+        join[threadIdx.x] = s;
+        __syncthreads();
+        if (share) return;
+#pragma unroll
+        for (int k = 1; k < SHARES; k++) s += join[COLS * k + threadIdx.x];
+    }
+    if (col < a.width) a.e[(size_t)i * a.width + col] = end > begin ? s / (float)(end - begin) : 0.f;
 }
 
 // grid (tile slots, column blocks): the rows of one tile get the sequence's row, rows of no sequence zeros if `fill`.

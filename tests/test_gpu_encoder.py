@@ -141,7 +141,9 @@ def test_pool_mean_of_more_rows_and_sequences_than_a_launch_holds(he):
     de = torch.full((1, 1), float(rows), device="cuda")
     dx = he.pool_mean_backward(de, i32(0, rows), rows, BF16)
     assert dx.shape == (rows, 1) and (dx == 1).all()
-    assert he.pool_mean(dx, i32(0, rows)) == 1  # sums of 2^18 each, whose sum is rounded as the length is
+    # Tiles sum up to 2^18 ones exactly, and eighths of them to 2^26 or 2^26 + 40 (a multiple of 8).  Joining the eighths takes seven roundings above
+    # 2^26, the length in 32 bits is one and the quotient one: 9 * 2^-24.
+    assert (he.pool_mean(dx, i32(0, rows)).double() - 1).abs() <= 9 * 2.0**-24
     del dx
     count = (1 << 22) + 9  # work-groups of 1024 threads would take 2^32 of them
     off = torch.full((count + 1,), 5, dtype=torch.int32, device="cuda")
