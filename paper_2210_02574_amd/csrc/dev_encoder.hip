@@ -149,7 +149,7 @@ AttnPlan attn_plan(const he_attn *s)
     if (groups(p.tile) < 128 || (mean_q <= 32 && mean_k > 128)) p.tile = 32;
     if (mean_q >= 1024 && s->cap == 0.0 && attn_wide(type_size(s->type), s->dim) && groups(256) >= 768) p.tile = 256;
     p.slots = tile_slots(s->q.rows, s->q.count, p.tile);
-    if (p.tile == 32 && p.slots > 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / groups(32), mean_k / 512, 64}));
+    if (p.tile == 32 && p.slots > 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / groups(32), mean_k / 512, ATTN_SPLITS}));
     return p;
 }
 
