@@ -131,25 +131,34 @@ bool out_ok(const he_heads *h, const he_attn *s, int64_t rows, int heads)
 }
 
 struct AttnPlan {
-    int tile, splits; // queries of a work-group; parts that the keys are cut into
-    int64_t slots;
+    int tile, splits; // rows of a work-group; parts that the keys are cut into
+    int pack;         // query heads to a tile
+    int64_t slots;    // tiles
+    int64_t groups;   // work-groups
 };
 // Tiles by the sequences' mean length: 128 queries, 64 for short sequences, 256 where attn_wide() says so, no cap keeps the vector instructions busy
 // anyway (one sequence of 8192, 12 heads of 64, capped: 496 us, with 128 426) and three rounds of them fill the card.  Tiles of 32, whose four waves
 // share the keys, where tiles of 128 would leave half of the CUs without one, or few queries meet many keys.  12 heads of 64 in bf16, tiles of 32,
 // 64, 128: 64 tokens 5.4, 6.0, 5.4 us; 512 tokens 8.2, 8.8, 10; 1024 16, 17, 15; 4 x 512 14, 13, 13; 64 x 64 13, 9.2, 9.5; 256 x 24 24, 18, 21.
-// The keys are cut where even so there are few work-groups: two launches cost 4 to 10 us more than one (512 tokens cut in two: 14 us instead of 8.2).
+// Query heads that share a key head go into one tile where their queries fit it: 64 sequences of one query and 1152 keys, 12 heads of 64 on 4, 17 us in bf16 (38
+// apart) and 51 in 32 bits (95); 16 of them, heads of 128, 32 on 4, 19 and 43 us (28, 124); 10 queries, 1000 keys, 12 heads on 4, 12 and 30 us (16, 46).
+// The keys are cut where even so there are few work-groups: the second launch costs 4 us (16 sequences of one query and 1152 keys, 12 heads of 64, cut in
+// two: 20 us instead of 14.5).
 AttnPlan attn_plan(const he_attn *s)
 {
-    AttnPlan p{128, 1, 0};
+    AttnPlan p{128, 1, 1, 0, 0};
     if (s->q.count == 0) return p;
     const int64_t mean_q = s->q.rows / s->q.count, mean_k = s->k.rows / s->q.count;
     const auto groups = [&](int tile) { return tile_slots(s->q.rows, s->q.count, tile) * s->heads; };
     if (mean_q <= 64) p.tile = 64;
     if (groups(p.tile) < 128 || (mean_q <= 32 && mean_k > 128)) p.tile = 32;
     if (mean_q >= 1024 && s->cap == 0.0 && attn_wide(type_size(s->type), s->dim) && groups(256) >= 768) p.tile = 256;
-    p.slots = tile_slots(s->q.rows, s->q.count, p.tile);
-    if (p.tile == 32 && p.slots > 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / groups(32), mean_k / 512, ATTN_SPLITS}));
+    const int group = s->heads / s->kv_heads;
+    if (group > 1 && mean_q * group <= 32 && group <= 32) p.tile = 32, p.pack = group;
+    p.slots = tile_slots(s->q.rows, s->q.count, p.tile / p.pack);
+    p.groups = p.slots * (s->heads / p.pack);
+    if (p.tile == 32 && p.slots > 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / p.groups, mean_k / 512, ATTN_SPLITS}));
+    p.groups *= p.splits;
     return p;
 }
 
@@ -195,9 +204,8 @@ AttnArgs attn_args(const he_attn *s)
     return a;
 }
 // work-groups, a multiple of eight for the eight dies; false: more than a launch holds
-bool attn_grid(AttnArgs &a, int64_t slots, int64_t per_slot, unsigned &grid)
+bool attn_grid(AttnArgs &a, int64_t slots, int64_t w, unsigned &grid)
 {
-    const int64_t w = slots * per_slot;
     if (w >= ((int64_t)1 << 31) / ATTN_THREADS) return false;
     a.slots = (int)slots;
     a.work = (unsigned)w;
@@ -347,7 +355,7 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
     if (need && !aligned(d_ws, 16)) return HE_EINVAL;
     const AttnPlan p = attn_plan(s);
     AttnArgs a = attn_args(s);
-    a.q = q->d, a.o = o->d, a.lse = d_lse, a.splits = p.splits;
+    a.q = q->d, a.o = o->d, a.lse = d_lse, a.splits = p.splits, a.pack = p.pack;
     SET(q, q), SET(o, o);
     if (s->k.rows > 0) {
         a.k = k->d, a.v = v->d;
@@ -356,7 +364,7 @@ extern "C" int32_t he_attention(he_ctx *ctx, const he_attn *s, const he_heads *q
     a.part_o = (float *)d_ws;
     a.part_lse = a.part_o + (size_t)p.splits * s->heads * s->q.rows * s->dim;
     unsigned grid;
-    if (!attn_grid(a, p.slots, (int64_t)s->heads * p.splits, grid)) return HE_EINVAL;
+    if (!attn_grid(a, p.slots, p.groups, grid)) return HE_EINVAL;
     const int64_t rows = s->q.rows * s->heads;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
@@ -403,8 +411,8 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     b.part_o = a.delta + (s->q.rows * s->heads + 3) / 4 * 4;
     unsigned grid_q = 0, grid_kv = 0;
     const int tile_q = grad_tile_q(s->q), tile_k = grad_tile_k(s->k);
-    if (!attn_grid(a, tile_slots(s->q.rows, s->q.count, tile_q), s->heads, grid_q)) return HE_EINVAL;
-    if (!attn_grid(b, tile_slots(s->k.rows, s->k.count, tile_k), (int64_t)s->kv_heads * b.splits, grid_kv)) return HE_EINVAL;
+    const int64_t slots_q = tile_slots(s->q.rows, s->q.count, tile_q), slots_k = tile_slots(s->k.rows, s->k.count, tile_k);
+    if (!attn_grid(a, slots_q, slots_q * s->heads, grid_q) || !attn_grid(b, slots_k, slots_k * s->kv_heads * b.splits, grid_kv)) return HE_EINVAL;
     const int64_t rows_kv = s->k.rows * s->kv_heads;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);

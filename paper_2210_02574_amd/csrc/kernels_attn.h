@@ -33,6 +33,7 @@ struct AttnArgs {
     int heads, group, dim; // group: query heads that share a key head
     float scale, cap;
     int slots, splits, fill;
+    int pack; // few queries: query heads of one key head that lie side by side in a tile, `group` or 1
     unsigned work; // work-groups that have something to do
 };
 
@@ -485,7 +486,8 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 }
 
 // Few queries: NWQ of the four waves along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: so that 32 queries
-// still keep four waves busy.
+// still keep four waves busy.  With NWQ = 1 a tile may hold the a.pack query heads that share a key head, row r being query r / a.pack of head r % a.pack, so
+// that keys are read once for all of them.
 template <class T, int DP, int NWQ> struct AttnFew {
     static constexpr int NWK = 4 / NWQ, BM = 32 * NWQ, BN = 32 * NWK;
     static constexpr int TILE = BN * DP; // elements of a tile
@@ -500,17 +502,18 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
     __shared__ __attribute__((aligned(16))) char lds[F::LDS];
     T *const lk = (T *)lds, *const lv = lk + F::TILE;
 
-    int head, slot, split;
-    if (!attn_work(a, a.slots * a.splits, head, slot, split)) return;
-    const TileRows t = tile_rows(a.sq, a.sk, slot, F::BM);
+    int first, slot, split; // first: key head of a packed tile, or query head
+    if (!attn_work(a, a.slots * a.splits, first, slot, split)) return;
+    const int pack = NWQ == 1 ? a.pack : 1;
+    const TileRows t = tile_rows(a.sq, a.sk, slot, F::BM / pack);
     if (t.first >= t.top) return;
     const FwdRange g(a, t, split, BN);
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wq = wave % NWQ, wk = wave / NWQ;
-    const int row = t.first + 32 * wq + (lane & 31);
+    const int row = t.first + (32 * wq + (lane & 31)) / pack, head = first * pack + (lane & 31) % pack, kh = pack > 1 ? first : first / a.group;
 
     const T *const q = (const T *)a.q + head * a.q_head;
-    const T *const k = (const T *)a.k + (head / a.group) * a.k_head, *const v = (const T *)a.v + (head / a.group) * a.v_head;
+    const T *const k = (const T *)a.k + kh * a.k_head, *const v = (const T *)a.v + kh * a.v_head;
     typename L::Chunk ck[L::template per<BN, ATTN_THREADS>()], cv[L::template per<BN, ATTN_THREADS>()];
     const typename L::template Reads<BN, ATTN_THREADS> reads_k(a.k_row, a.dim, tid), reads_v(a.v_row, a.dim, tid);
     reads_k.load(ck, k, a.k_row, g.lo, g.hi, a.dim);

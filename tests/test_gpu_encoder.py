@@ -221,6 +221,22 @@ def test_attention_of_other_keys_and_few_queries(he, queries, keys, dtype):
         compare(he, q, k, v, oq, do, offsets_k=ok, slopes=sl)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("heads,kv,queries,keys", [(6, 2, [1, 1, 0, 3], [200, 0, 50, 33]), (8, 1, [4, 1, 2], [1, 129, 300]), (32, 1, [1, 1], [5, 2100]),
+                                                   (33, 1, [1, 1], [40, 70]), (12, 4, [10, 20, 3, 7], [40, 128, 1, 500]), (4, 2, [1], [3000])])
+def test_attention_of_few_queries_and_shared_heads(he, heads, kv, queries, keys, dtype):
+    """Query heads that share a key head lie in one tile, some of which reach over a tile's end; of rows of no sequence as well."""
+    off, off_k = np.cumsum([2] + queries).tolist(), offsets_of(keys)
+    rows, sl = off[-1] + 3, torch.linspace(0.0, 0.2, heads, device="cuda")
+    q, do = (rand(i, rows, heads, 32, dtype=dtype) for i in (1, 4))
+    k, v = (rand(i, sum(keys), kv, 32, dtype=dtype) for i in (2, 3))
+    for cap, slopes in ((0.0, None), (9.0, sl)):
+        compare(he, q, k, v, (i32(*off[:-1]), i32(*off[1:])), do, offsets_k=off_k, cap=cap, slopes=slopes)
+    out = torch.full_like(q, 7.0)
+    he.attention(q, k, v, (i32(*off[:-1]), i32(*off[1:])), offsets_k=off_k, out=out)
+    assert (out[:2] == 7).all() and (out[-3:] == 7).all() and not (out[2:-3] == 7).all()
+
+
 def test_attention_is_cut_where_it_should_be(he):
     """Sizes that test_attention_of_other_keys_and_few_queries (one query of many keys) and test_attention_of_long_sequences (few tiles of keys under many
     queries) run really are cut and joined."""
