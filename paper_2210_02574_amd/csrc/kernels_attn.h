@@ -13,8 +13,10 @@
 // The operand A of that product is a transposed tile: 16-bit types read it from LDS with the transposing read, 32-bit ones word by word.
 //
 // Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
-// everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  fp16 holds it down to 6e-8: gradients as small as that need a
-// scaled loss, as everywhere in fp16.
+// everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  Rounding both the terms and the result leaves 1.4
+// times the error of rounding the result alone.  delta takes o as it was rounded: where few keys carry a row's weight (a steep distance bias) that adds a
+// tenth to dq and dk; without it a pass over all keys would have to come first.  fp16 holds dt down to 6e-8: gradients as small as that need a scaled
+// loss, as everywhere in fp16.
 #pragma once
 #include "enc_common.h"
 #include <type_traits>
@@ -310,6 +312,12 @@ __device__ __forceinline__ float col_max(const f32x16 &s)
 // Many queries: four waves with 32 QB queries each, all of which read all keys.  A step takes 32 keys: the products of the next step's scores are
 // independent of this step's exponentials, so that matrix and vector instructions of one wave overlap.  Tiles of BN keys pass through three LDS
 // stages, which takes one barrier a tile: the stage that a wave overwrites is the one that every wave has left before the last barrier.
+// 12 heads of 128 on 4 key heads, 16384 rows of bf16: 1.70 ms, 970 TF, 0.80 of what a library product of 8192^3 reaches on the card (1208); matrix instructions
+// take 0.47 of the cycles, vector instructions 0.50, at the clock that the power limit leaves (1.7 to 1.9 GHz).  64 sequences of 290 rows on average, 12 heads of
+// 64: 44 us: a work-group has 9 steps then, and spends a third of its time on its first loads and its store.
+// Tried and not kept: no maximum per step, weights watched by their sums instead (heads of 32 1.1 times as fast, of 64 and 128 1.02, a steep distance bias 0.87);
+// the weighted sum one step later, so that all of a step's products and exponentials are independent (85 registers more, 0.85); waves without rows
+// skipping their products (full tiles 0.93).
 template <class T, int DP, int QB> struct AttnFwd {
     // Two blocks of queries halve what is read of LDS for a product; heads above 64 then take the registers of one wave per SIMD, everything
     // else leaves room for two or three, and its stages for as many work-groups.
@@ -487,7 +495,9 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 
 // Few queries: NWQ of the four waves along the queries, 32 each, 4 / NWQ along the keys, whose shares are joined in LDS at the end: so that 32 queries
 // still keep four waves busy.  With NWQ = 1 a tile may hold the a.pack query heads that share a key head, row r being query r / a.pack of head r % a.pack, so
-// that keys are read once for all of them.
+// that keys are read once for all of them.  Bound by latency where there is little to read (23 rows in 32 bits 7.6 us: sequence numbers, rows, products, store),
+// then by memory: 16 sequences of one query and 1152 keys, 12 heads of 64 in bf16 14.5 us (3.9 TB/s), 64 of them 40 (5.7).  (Two tiles under way instead of
+// one: 5 % slower.)
 template <class T, int DP, int NWQ> struct AttnFew {
     static constexpr int NWK = 4 / NWQ, BM = 32 * NWQ, BN = 32 * NWK;
     static constexpr int TILE = BN * DP; // elements of a tile
@@ -674,6 +684,8 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
 // registers are kept for more of them: three per SIMD for dq and two for dk and dv, with heads up to 64.  (Row operands read a block ahead, at the
 // price of a wave: dq of one sequence of 8192, 12 heads of 64, 484 us instead of 424.)  The next block goes to LDS ahead of the barrier at the block's
 // beginning for dq, in its middle for dk and dv, whose barrier is there too (at the beginning: 578 us instead of 500).
+// One sequence of 4096, 12 heads of 64 in bf16: dq 110 us (706 TF), dk and dv 124 (829); capped and biased 158 and 161 us: vector instructions.  64 sequences of
+// 290 rows on average: 56 and 71 us.
 template <class T, int DP> struct AttnGrad {
     static constexpr int TILE = 32 * DP;
     static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : DP > 64 ? 2 : 3, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2; // per SIMD
