@@ -9,7 +9,9 @@
  * slot rotation (ModUp, inner product with the evaluation key, ModDown),
  * rescale, and rotate-and-sum.  Key generation, encoding, encryption and
  * decryption run on the host; everything else runs in HIP kernels (gfx950) on
- * device buffers owned by the caller.
+ * device buffers owned by the caller.  The operators that make the embeddings
+ * which are encrypted (attention inside sequences, layer norm, mean over
+ * sequences, with gradients) are a section of their own near the end.
  *
  * Conventions
  *  - Moduli: q_0..q_{L-1} (ciphertext primes) then p_0..p_{K-1} (special primes),
