@@ -57,6 +57,8 @@ static void attn_grad_kv(he_ctx *c, hipStream_t st, double bytes, int tile, unsi
     by_mode(a, [&](auto mode) {
         if (tile == 32)
             KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 1, mode>), grid, 64, a);
+        else if (tile == 64)
+            KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 2, mode>), grid, 128, a);
         else
             KLAUNCH_T(c, st, KID_ATTN_GRAD_KV, bytes, (k_attn_grad_kv<T, HE_DIM, 4, mode>), grid, 256, a);
     });

@@ -163,19 +163,22 @@ AttnPlan attn_plan(const he_attn *s)
 }
 
 // Rows of a work-group of the backward pass.  Short sequences leave a part of a tile empty and a work-group little to do between its first loads and its last
-// stores: small ones then waste less and more of them are resident.  12 heads of 64 in bf16, dq with 64 rows against 128: 1000 sequences of 18 rows on average
-// 49 us, 79; 200 of 56 30, 34; 64 of 290 62, 63; 32 of 570 92, 88; one of 8192 415, 366.  dk and dv with 32 against 128: 42 us, 101; 30, 42; 77, 85; 123, 129;
-// with 64 the last one 607, 500.
+// stores: small ones then waste less and more of them are resident.  12 heads of 64 in bf16, dq with 64 rows against 128: 1000 sequences of 17 rows on average
+// 49 us, 79; 128 of 138 45, 48; 64 of 288 59, 58; 32 of 577 92, 89; 4 of 2525 192, 170.  dk and dv with 32, 64, 128: 44 us, 60, 102; 52, 52, 62; 75, 72, 79; 124,
+// 116, 119; 250, 232, 220.
 int grad_tile_q(const he_spans &s) { return s.rows / s.count < 256 ? 64 : 128; }
-int grad_tile_k(const he_spans &s) { return s.rows / s.count < 512 ? 32 : 128; }
-// Parts that the queries of a tile of 128 keys are cut into, where those tiles are few for 256 CUs that hold two each: shared key heads have long work and few
-// tiles (one sequence of 8192, heads of 64 in bf16, 12 on 4: 636 us whole, 472 in two or three; 2 of 2048, heads of 128, 8 on 2: 291, 105; of one of 4096 with
-// heads of their own 148, 150).
+int grad_tile_k(const he_spans &s) { return s.rows / s.count < 192 ? 32 : s.rows / s.count < 640 ? 64 : 128; }
+// Parts that the queries of a tile of keys are cut into, each a work-group of its own, until there are 2560 waves (two and a half for each SIMD): shared key heads have
+// long work and few tiles.  Joining costs 4 to 14 us, so parts keep 512 query rows, or 128 where there is not even a wave for half of the SIMDs.  One sequence of
+// 8192, heads of 64 in bf16, 12 on 4: 636 us whole, 472 in two or three; one of 4096 with heads of their own 148, 150; one of 336, 12 on 4, 27 whole, 13 in seven; one of 167,
+// 12 on 2, 32, 12; two of 576, heads of 96 of their own, 28, 30.
 int grad_splits(const he_attn *s)
 {
-    if (s->k.count == 0 || s->k.rows == 0 || grad_tile_k(s->k) != 128) return 1;
-    const int64_t groups = tile_slots(s->k.rows, s->k.count, 128) * s->kv_heads, work = s->q.rows / s->q.count * (s->heads / s->kv_heads);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(640 + groups / 2) / groups, work / 512, 8}));
+    if (s->k.count == 0 || s->k.rows == 0) return 1;
+    const int tile = grad_tile_k(s->k);
+    const int64_t waves = tile_slots(s->k.rows, s->k.count, tile) * s->kv_heads * (tile / 32), work = s->q.rows / s->q.count * (s->heads / s->kv_heads);
+    if (work < 640) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(2560 + waves / 2) / waves, work / (waves < 512 ? 128 : 512), 8}));
 }
 size_t attn_bytes(const he_attn *s, bool backward)
 {

@@ -76,7 +76,7 @@ int32_t type_of(at::ScalarType t)
 
 void placed(const Args &a, const Tensor &t, const char *what, at::ScalarType type)
 {
-    if (t.layout() != at::kStrided) refuse(what, ": want a strided tensor");
+    if (t.layout() != at::kStrided || t.is_neg()) refuse(what, ": want a strided tensor that holds its values as they are");
     if (a.device < 0 || !t.is_cuda() || t.get_device() != a.device) refuse(what, ": on ", t.device(), ", the context is on device ", a.device);
     if (t.scalar_type() != type) refuse(what, ": ", t.scalar_type(), ", want ", type);
 }

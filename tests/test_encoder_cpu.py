@@ -160,7 +160,8 @@ def test_binding_refusals(he):
         with pytest.raises(ValueError, match="device|want"):
             f()  # CPU tensors: there is no fallback
     for f in (lambda: he.layer_norm(x[0], w, w), lambda: he.layer_norm(x.t(), w, w), lambda: he.pool_mean(x.view(2, 2, 8), off), lambda: he.attention(x, x, x, off),
-              lambda: he.layer_norm(x, None, w), lambda: he.pool_mean_backward(x, off, 4, 5), lambda: he.pool_mean_backward(x, off, -1, torch.float32)):
+              lambda: he.layer_norm(x, None, w), lambda: he.layer_norm(x.to_sparse(), w, w),
+              lambda: he.layer_norm(torch.complex(x, x).conj().imag, w, w), lambda: he.pool_mean_backward(x, off, 4, 5), lambda: he.pool_mean_backward(x, off, -1, torch.float32)):
         with pytest.raises(ValueError):
             f()
     for f in (lambda: he.layer_norm(x.double(), w, w), lambda: he.pool_mean(x.long(), off), lambda: he.pool_mean_backward(x, off, 4, torch.float64)):

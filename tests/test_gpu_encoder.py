@@ -222,6 +222,22 @@ def test_attention_of_other_keys_and_few_queries(he, queries, keys, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("lengths,heads,kv,dim", [([150, 0, 120], 32, 1, 32), ([300, 261], 8, 2, 64), ([230, 1, 410], 12, 2, 40), ([90], 96, 8, 128)])
+def test_attention_gradients_of_cut_queries(he, lengths, heads, kv, dim, dtype):
+    """Short sequences whose key heads are shared by many: the queries of a tile of 32 or 64 keys are cut into parts."""
+    import ctypes
+    import struct
+
+    rows = sum(lengths)
+    need, span = ctypes.c_size_t(), (64, 64, len(lengths), rows + 5)
+    s = struct.Struct("@4iPPiqPPiqddPi4x").pack({F32: 0, F16: 1, BF16: 2}[dtype], heads, kv, dim, *span, *span, 1.0, 0.0, 0, 1)
+    assert he.lib.he_attention_workspace_bytes(he.ctx, s, 1, ctypes.byref(need)) == 0 and need.value > 2 * 2 * kv * rows * dim * 4
+    q, do = (rand(i, rows + 5, heads, dim, dtype=dtype) for i in (1, 4))
+    k, v = (rand(i, rows + 5, kv, dim, dtype=dtype) for i in (2, 3))
+    compare(he, q, k, v, offsets_of(lengths), do, slopes=torch.linspace(0.0, 0.1, heads, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("heads,kv,queries,keys", [(6, 2, [1, 1, 0, 3], [200, 0, 50, 33]), (8, 1, [4, 1, 2], [1, 129, 300]), (32, 1, [1, 1], [5, 2100]),
                                                    (33, 1, [1, 1], [40, 70]), (12, 4, [10, 20, 3, 7], [40, 128, 1, 500]), (4, 2, [1], [3000])])
 def test_attention_of_few_queries_and_shared_heads(he, heads, kv, queries, keys, dtype):
