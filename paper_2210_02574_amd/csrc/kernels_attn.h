@@ -14,8 +14,9 @@
 //
 // Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
 // everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  Rounding both the terms and the result leaves 1.4
-// times the error of rounding the result alone.  delta takes o as it was rounded: where few keys carry a row's weight (a steep distance bias) that adds a
-// tenth to dq and dk; without it a pass over all keys would have to come first.  fp16 holds dt down to 6e-8: gradients as small as that need a scaled
+// times the error of rounding the result alone.  delta takes o as it was rounded: where few keys of many carry a row's weight (a steep distance bias) that
+// adds a tenth to dq and dk; without it a pass over all keys would have to come first (up to 32 keys of short sequences are at hand at once, and delta is exact).  Its error
+// alone, sum p (dp - delta), would mend dk but not dq: 10 % of dq's time under a cap.  fp16 holds dt down to 6e-8: gradients as small as that need a scaled
 // loss, as everywhere in fp16.
 #pragma once
 #include "enc_common.h"
@@ -768,7 +769,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     for (int db = 0; db < DB; db++) dq[db] = f32x16{};
 
     int stage = 0;
-    const auto block = [&](int j, auto tail) { // the 32 keys from j on
+    const auto block = [&](int j, auto tail, auto lone) { // the 32 keys from j on; lone: the only ones
         L::template store<32, NT>(ck, lds[stage][0], tid);
         L::template store<32, NT>(cv, lds[stage][1], tid);
         __syncthreads();
@@ -783,14 +784,27 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         }
         const float pos = (float)(pos0 - (j - kb) - 4 * h);
         Vec<T, 8> d[2];
+        float ps[lone ? 16 : 1], fs[lone ? 16 : 1], by = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
             const int m = 8 * (r >> 2) + (r & 3);
             float f = 1.f, p = score.p(s[r], rest, pos - (float)m, f);
             if (tail && m + 4 * h >= ke - j) p = 0.f; // a missing key's score may be anything
+            if constexpr (lone) {
+                ps[r] = p, fs[r] = f;
+                by += p * dp[r];
+                continue;
+            }
             p *= dp[r];
             if (MODE & MODE_CAP) p *= f;
             d[r >> 3][r & 7] = (T)p; // the scale is put on at the end
+        }
+        if constexpr (lone) {
+            // All weights of the row are at hand: sum p (dp - delta) is what delta lacks for o as it was before its rounding.
+            by = pair_sum(by) * (1.f / GradScore<T, MODE>::LIFT);
+            delta -= by;
+#pragma unroll
+            for (int r = 0; r < 16; r++) d[r >> 3][r & 7] = (T)(ps[r] * (dp[r] - by) * fs[r]);
         }
 #pragma unroll
         for (int half = 0; half < 2; half++)
@@ -799,8 +813,14 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         stage ^= 1;
     };
     int j = kb;
-    for (; j + 32 <= ke; j += 32) block(j, std::false_type{});
-    if (j < ke) block(j, std::true_type{});
+    if constexpr (NW == 2) // tiles of short sequences (its registers would cost the other tile 5 %)
+        if (ke - kb <= 32 && ke > kb) {
+            block(j, std::true_type{}, std::true_type{});
+            if (in && h == 0) a.delta[at] = delta;
+            j = ke;
+        }
+    for (; j + 32 <= ke; j += 32) block(j, std::false_type{}, std::false_type{});
+    if (j < ke) block(j, std::true_type{}, std::false_type{});
     if (row >= t.top || (!in && !a.fill)) return;
     if (!in || ke == kb)
 #pragma unroll
