@@ -323,7 +323,8 @@ typedef struct {
     int64_t stride;
 } he_rows;
 /* [rows][heads][dim], the last dimension dense: element (r, h, c) is at r * row + h * head + c.  Base and strides are multiples of 16
- * bytes; strides of an output are at least dim (inputs may repeat: 0), row strides are below 2^24 bytes. */
+ * bytes, row strides below 2^24 bytes.  Inputs may repeat (stride 0); an output's rows and heads are apart: strides of at least dim, and
+ * row >= (heads - 1) head + dim or head >= (rows - 1) row + dim. */
 typedef struct {
     void *d;
     int64_t row, head;

@@ -122,12 +122,14 @@ int32_t attn_check(const he_attn *s)
 bool heads_ok(const he_heads *h, int32_t type)
 {
     const int64_t size = (int64_t)type_size(type);
-    return h && h->d && aligned(h->d, 16) && h->row >= 0 && h->head >= 0 && h->row < (1 << 24) / size && (h->row * size) % 16 == 0 && (h->head * size) % 16 == 0;
+    if (!h || !h->d || !aligned(h->d, 16) || h->row < 0 || h->row >= (1 << 24) / size || h->head < 0 || h->head >= (int64_t)1 << 46) return false;
+    return (h->row * size) % 16 == 0 && (h->head * size) % 16 == 0;
 }
-// Buffers that are written: elements of different rows or heads have different addresses if the strides hold a row of a head each.
+// Buffers that are written: elements of different rows and heads have different addresses.
 bool out_ok(const he_heads *h, const he_attn *s, int64_t rows, int heads)
 {
-    return heads_ok(h, s->type) && (rows <= 1 || h->row >= s->dim) && (heads <= 1 || h->head >= s->dim);
+    if (!heads_ok(h, s->type) || (rows > 1 && h->row < s->dim) || (heads > 1 && h->head < s->dim)) return false;
+    return rows <= 1 || heads <= 1 || h->row >= (heads - 1) * h->head + s->dim || h->head >= (rows - 1) * h->row + s->dim;
 }
 
 struct AttnPlan {

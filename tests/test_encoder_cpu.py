@@ -145,11 +145,15 @@ def test_attention_refusals(he):
     assert fwd(long) == ENODEV and fwd(long, ws=None) == EWORKSPACE and fwd(long, size=need.value - 1) == EWORKSPACE and fwd(long, ws=P + 4) == EINVAL
     huge = _attn(heads=4096, kv=4096, q=_span(1, 1 << 30), k=_span(1, 1 << 30))  # more work-groups than a launch holds
     assert fwd(huge, size=1 << 62) == EINVAL and bwd(huge, size=1 << 62) == EINVAL
-    for bad in (_C.he_heads(P, 32, 64), _C.he_heads(P, 512, 32), _C.he_heads(P, 0, 64), _C.he_heads(P, 512, 0)):  # outputs that overlap themselves
+    for bad in (_C.he_heads(P, 32, 64), _C.he_heads(P, 512, 32), _C.he_heads(P, 0, 64), _C.he_heads(P, 512, 0), _C.he_heads(P, 64, 64), _C.he_heads(P, 72, 64),
+                _C.he_heads(P, 128, 1024)):  # outputs that overlap themselves
         assert fwd(_attn(), o=bad) == EINVAL
         for name in ("dq", "dk", "dv"):
             assert bwd(_attn(), **{name: bad}) == EINVAL, name
         assert fwd(_attn(), q=bad, k=bad, v=bad) == ENODEV  # inputs may
+    apart = _C.he_heads(P, 64, 40 * 64)  # one head after the other
+    assert fwd(_attn(), o=apart) == ENODEV and bwd(_attn(), dq=apart, dk=apart, dv=apart) == ENODEV
+    assert fwd(_attn(), q=_C.he_heads(P, 512, 1 << 46)) == EINVAL
 
 
 def test_binding_refusals(he):
