@@ -253,6 +253,27 @@ def test_attention_of_few_queries_and_shared_heads(he, heads, kv, queries, keys,
     assert (out[:2] == 7).all() and (out[-3:] == 7).all() and not (out[2:-3] == 7).all()
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_of_drawn_shapes(he, seed):
+    """Types, heads, sizes, gaps between sequences, lengths of queries and keys, caps and biases as they come."""
+    r = np.random.default_rng(seed)
+    dtype, kv, group, dim = [F32, F16, BF16][seed % 3], int(r.integers(1, 4)), int(r.choice([1, 2, 4, 7])), 8 * int(r.integers(1, 17))
+    gap, longest = int(r.choice([0, 0, 5])), int(r.choice([1, 8, 40, 150, 700]))
+
+    def spans(n):
+        at = np.cumsum(np.r_[r.integers(0, gap + 1), n + r.integers(0, gap + 1, len(n))])
+        return (i32(*at[:-1].tolist()), i32(*(at[:-1] + n).tolist())), int(at[-1]) + gap
+
+    nq = r.integers(0, longest + 1, r.integers(1, 13))
+    (off, rows), (off_k, rows_k) = spans(nq), spans(r.integers(0, r.choice([4, 60, 900]), len(nq)))
+    if r.random() < 0.5:
+        off_k, rows_k = off, rows
+    q, do = (rand(i, rows, kv * group, dim, dtype=dtype) for i in (1, 4))
+    k, v = (rand(i, rows_k, kv, dim, dtype=dtype) for i in (2, 3))
+    slopes = None if r.random() < 0.5 else 0.3 * torch.rand(kv * group, device="cuda", generator=torch.Generator("cuda").manual_seed(seed))
+    compare(he, q, k, v, off, do, offsets_k=off_k, cap=float(r.choice([0.0, 8.0])), slopes=slopes)
+
+
 def test_attention_is_cut_where_it_should_be(he):
     """Sizes that test_attention_of_other_keys_and_few_queries (one query of many keys) and test_attention_of_long_sequences (few tiles of keys under many
     queries) run really are cut and joined."""
