@@ -12,6 +12,8 @@ features at block offsets 4 .. 771 and zeros elsewhere.
 """
 from __future__ import annotations
 
+import hashlib
+import struct
 from typing import Dict, List, Sequence
 
 import numpy as np
@@ -46,6 +48,14 @@ def weight_diagonals(W: np.ndarray, n_slots: int) -> List[np.ndarray]:
     return out
 
 
+def _ciphertext_seed(seed: int, i: int) -> int:
+    """The seed of the i-th ciphertext of a call: a hash, since mask and error are functions of an encryption's seed alone, and seed + i of one call
+    would be seed + i - 1 of the next one's neighbour.  Two ciphertexts under one mask give the difference of their messages to anybody."""
+    if not 0 <= seed < 1 << 64:
+        raise ValueError(f"seed: {seed}, want 64 bits")
+    return int.from_bytes(hashlib.blake2b(struct.pack("<QQ", seed, i), digest_size=8).digest(), "little")
+
+
 INFER_HOISTED = (1, 2, 3)
 INFER_SUM_SHIFTS = tuple(4 << k for k in range(8))  # 4 .. 512
 
@@ -69,11 +79,12 @@ class EncryptedInference:
 
     def encrypt_sentences(self, sk, encoder, states, offsets, scale: float, seed: int):
         """The data owner's side: token states -> embeddings (embedding.SentenceEncoder) -> packed slots -> ciphertexts for run(), n / 1024
-        sentences each."""
+        sentences each.  seed, of 64 bits: every ciphertext of a call is masked under a seed of its own that is made from it, so that calls with
+        different seeds, neighbouring ones too, share none.  Under one key a seed must not be used again."""
         from .embedding import pack_embeddings
 
         he = self.he
-        return [he.to_device(he.encrypt_coeffs(sk, he.encode(z, scale), self.level, seed + i))
+        return [he.to_device(he.encrypt_coeffs(sk, he.encode(z, scale), self.level, _ciphertext_seed(seed, i)))
                 for i, z in enumerate(pack_embeddings(encoder(states, offsets), he.n))]
 
     def run(self, ct, pts, keys):

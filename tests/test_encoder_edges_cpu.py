@@ -1,0 +1,33 @@
+"""Token states to embeddings and ciphertexts without a GPU: calls at the edge of what is documented."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2210_02574_amd as pkg
+import workloads as wl
+from paper_2210_02574_amd.classifier import EncryptedInference
+
+
+@pytest.fixture(scope="module")
+def he():
+    return pkg.HE.from_params(wl.C1B)
+
+
+def test_ciphertexts_of_calls_with_neighbouring_seeds_share_no_mask(he, monkeypatch):
+    monkeypatch.setattr(he, "to_device", lambda x: x, raising=False)
+    inf, sk = EncryptedInference(he, 2), he.keygen_secret(3)
+    encoder = lambda states, offsets: states  # noqa: E731
+    e = torch.rand(3 * he.n // 1024, 768, generator=torch.Generator().manual_seed(4))
+    calls = [inf.encrypt_sentences(sk, encoder, e, None, 2.0**30, s) for s in (10, 11, 12, 0, 2**64 - 1)]
+    cts = [c for call in calls for c in call]
+    assert len(cts) == 15
+    for a, b in itertools.combinations(cts, 2):
+        assert not np.array_equal(a[1][0], b[1][0])  # the mask
+        assert not np.array_equal(a[0][0], b[0][0])
+    again = inf.encrypt_sentences(sk, encoder, e, None, 2.0**30, 10)
+    assert all(np.array_equal(a, b) for a, b in zip(again, calls[0]))  # the same seed: the same ciphertexts
+    for bad in (-1, 2**64):
+        with pytest.raises(ValueError, match="seed"):
+            inf.encrypt_sentences(sk, encoder, e, None, 2.0**30, bad)
