@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from typing import List, Sequence
 
 import numpy as np
@@ -174,20 +175,21 @@ def _hp(a: np.ndarray):
     return ctypes.c_void_p(a.ctypes.data)
 
 
-_tensors = None
+_tensors, _tensors_lock = None, threading.Lock()
 
 
 def load_tensors():
-    """The extension module for torch tensors (csrc/tensors.cpp), built with the library."""
+    """The extension module for torch tensors (csrc/tensors.cpp), built with the library; loaded once, whichever threads ask for it."""
     global _tensors
-    if _tensors is None:
-        load_library()
-        import importlib.util
+    with _tensors_lock:
+        if _tensors is None:
+            load_library()
+            import importlib.util
 
-        spec = importlib.util.spec_from_file_location("he_tensors", os.path.join(_HERE, "he_tensors.so"))
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        _tensors = module
+            spec = importlib.util.spec_from_file_location("he_tensors", os.path.join(_HERE, "he_tensors.so"))
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
+            _tensors = module
     return _tensors
 
 
@@ -247,7 +249,9 @@ class HE:
             raise HeError(rc, "he_ctx_create")
         self.ctx = h
         self._ws = None
-        self._ctx, self._tensors, self._raw_stream = h.value, None, lambda device: 0
+        self._ctx, self._tensors = h.value, None
+        # of torch.cuda.current_stream, without an object around it
+        self._raw_stream = torch._C._cuda_getCurrentRawStream if device >= 0 else lambda device: 0
 
     @classmethod
     def from_params(cls, params, device: int = -1):
@@ -744,10 +748,6 @@ class HE:
     def _on_tensors(self, name: str, where: str, *args):
         if self._tensors is None:
             self._tensors = load_tensors()
-            if self.device >= 0:
-                import torch
-
-                self._raw_stream = torch._C._cuda_getCurrentRawStream  # of torch.cuda.current_stream, without an object around it
         r = getattr(self._tensors, name)(self._ctx, self.device, self._raw_stream(self.device), *args)
         if r.__class__ is int:
             self._chk(r, where)

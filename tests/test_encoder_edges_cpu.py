@@ -1,5 +1,8 @@
 """Token states to embeddings and ciphertexts without a GPU: calls at the edge of what is documented."""
+import importlib.util
 import itertools
+import threading
+import time
 
 import numpy as np
 import pytest
@@ -7,6 +10,7 @@ import torch
 
 import paper_2210_02574_amd as pkg
 import workloads as wl
+from paper_2210_02574_amd import binding
 from paper_2210_02574_amd.classifier import EncryptedInference
 
 
@@ -31,3 +35,24 @@ def test_ciphertexts_of_calls_with_neighbouring_seeds_share_no_mask(he, monkeypa
     for bad in (-1, 2**64):
         with pytest.raises(ValueError, match="seed"):
             inf.encrypt_sentences(sk, encoder, e, None, 2.0**30, bad)
+
+
+def test_two_threads_load_the_extension_once(monkeypatch):
+    """Both ask for it before it is there; the first one is held up while it loads."""
+    pkg.load_library()
+    monkeypatch.setattr(binding, "_tensors", None)
+    loads, plain = [], importlib.util.module_from_spec
+
+    def slow(spec):
+        loads.append(spec.name)
+        time.sleep(0.3)
+        return plain(spec)
+
+    monkeypatch.setattr(importlib.util, "module_from_spec", slow)
+    got = []
+    threads = [threading.Thread(target=lambda: got.append(binding.load_tensors())) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert loads == ["he_tensors"] and got[0] is got[1]
