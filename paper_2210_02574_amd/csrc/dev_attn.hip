@@ -35,7 +35,7 @@ static void attn_fwd(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned
             KLAUNCH_T(c, st, KID_ATTN_FEW, bytes, (k_attn_few<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
         else if (tile == 128)
             KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 1, mode>), grid, ATTN_THREADS, a);
-        else if constexpr (ATTN_WIDE)
+        else if constexpr (ATTN_WIDE && !(mode & MODE_CAP)) // (no plan has wide tiles under a cap)
             KLAUNCH_T(c, st, KID_ATTN, bytes, (k_attn<T, HE_DIM, 2, mode>), grid, ATTN_THREADS, a);
     });
 }

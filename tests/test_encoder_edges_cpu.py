@@ -1,6 +1,7 @@
 """Token states to embeddings and ciphertexts without a GPU: calls at the edge of what is documented."""
 import importlib.util
 import itertools
+import re
 import threading
 import time
 
@@ -56,3 +57,11 @@ def test_two_threads_load_the_extension_once(monkeypatch):
     for t in threads:
         t.join()
     assert loads == ["he_tensors"] and got[0] is got[1]
+
+
+def test_wide_tiles_are_built_for_the_modes_that_plans_give_them():
+    """Tiles of 256 queries (two blocks to a wave) go with heads up to 64 in 16 bits and no cap; other ones would be kernels that no call reaches."""
+    with open(pkg.LIB_PATH, "rb") as f:
+        names = {m.decode() for m in re.findall(rb"_Z6k_attnI\w+", f.read())}
+    wide = {m.groups() for m in (re.match(r"_Z6k_attnI(f|DF16_|DF16b)Li(\d+)ELi2ELi(\d+)EE", n) for n in names) if m}
+    assert wide == {(t, d, mode) for t in ("DF16_", "DF16b") for d in ("32", "64") for mode in ("0", "2")}
