@@ -375,7 +375,7 @@ int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width
 typedef struct {
     int32_t type, heads, kv_heads, dim;
     he_spans q, k;         /* the same count */
-    double scale, cap;     /* scale > 0, cap >= 0, both and scale / cap finite in 32 bits */
+    double scale, cap;     /* scale > 0, cap >= 0, both at most 2^127, and scale / cap finite in 32 bits */
     const float *d_slopes; /* [heads]; NULL: no bias */
     int32_t fill;
 } he_attn;

@@ -12,10 +12,15 @@ typedef bf16 T;
 
 static constexpr bool ATTN_WIDE = attn_wide(sizeof(T), HE_DIM);
 
-// F with the variant of cap and distance bias
+// f with the variant of cap and distance bias
 template <class F> static void by_mode(const AttnArgs &a, F f)
 {
     const int mode = (a.cap > 0.f ? MODE_CAP : 0) | (a.slope ? MODE_SLOPE : 0);
+    if constexpr (sizeof(T) == 2)
+        if (a.cap > ATTN_FAST_CAP) {
+            if (a.slope) return f(std::integral_constant<int, MODE_CAP | MODE_SLOPE | MODE_EXACT>{});
+            return f(std::integral_constant<int, MODE_CAP | MODE_EXACT>{});
+        }
     if (mode == 0)
         f(std::integral_constant<int, 0>{});
     else if (mode == MODE_CAP)

@@ -113,8 +113,9 @@ int32_t attn_check(const he_attn *s)
     if (!s || !type_ok(s->type) || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads || s->heads > 65535) return HE_EINVAL;
     if (s->dim < 8 || s->dim > 128 || s->dim % 8) return HE_EINVAL;
     if (spans_check(&s->q) != HE_OK || spans_check(&s->k) != HE_OK || s->q.count != s->k.count) return HE_EINVAL;
-    if (!(s->scale > 0.0) || !std::isfinite((float)s->scale) || !((float)s->scale > 0.f)) return HE_EINVAL;
-    if (!(s->cap >= 0.0) || !std::isfinite((float)s->cap) || (s->cap > 0.0 && !((float)s->cap > 0.f))) return HE_EINVAL;
+    constexpr double most = 0x1p127; // times log2(e) still finite in 32 bits
+    if (!(s->scale > 0.0) || !(s->scale <= most) || !((float)s->scale > 0.f)) return HE_EINVAL;
+    if (!(s->cap >= 0.0) || !(s->cap <= most) || (s->cap > 0.0 && !((float)s->cap > 0.f))) return HE_EINVAL;
     if (s->cap > 0.0 && !std::isfinite((float)s->scale / (float)s->cap * 3.f)) return HE_EINVAL; // what scores are multiplied with under tanh
     if (s->d_slopes && !aligned(s->d_slopes, 4)) return HE_EINVAL;
     return HE_OK;

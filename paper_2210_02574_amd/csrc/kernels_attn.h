@@ -214,8 +214,13 @@ __device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, 
 }
 
 // Scores of 32 x 32 blocks, x = log2(e) s, from products c = q . k.  MODE: MODE_CAP, MODE_SLOPE, both or neither.  16-bit types take tanh(y) =
-// 1 - 2 / (1 + e^2y) by the hardware's exponential and reciprocal (off by 2^-22 at most, absolutely: cap times that in a score), 32 bits the library's.
-enum { MODE_CAP = 1, MODE_SLOPE = 2 };
+// 1 - 2 / (1 + e^2y) by the hardware's exponential and reciprocal: it is off by 2^-22 at most, but absolutely, so that a score is off by that times the
+// cap, however small it is.  Up to caps of 64 that is 2^-16, an eighth of what rounding its weight to fp16 costs (bf16: a 64th).  Above (MODE_EXACT),
+// and in 32 bits, tanh is the library's, which keeps small values: a cap may be far above all scores.  3 sequences of 4000, 16 heads of 64 on 8 in fp16, biased,
+// caps of 64 and 65: 386 us forward and 1035 backward, 469 and 1380; 32 of 300, 12 heads of 64: 32 and 84, 41 and 111.
+enum { MODE_CAP = 1, MODE_SLOPE = 2, MODE_EXACT = 4 };
+#define ATTN_FAST_CAP 64.f
+template <class T, int MODE> constexpr bool attn_fast_tanh() { return sizeof(T) == 2 && (MODE & MODE_CAP) && !(MODE & MODE_EXACT); }
 template <class T, int MODE> struct Scores {
     float in, out, slope; // of c before tanh, of tanh (or of c), of the distance
 
@@ -224,7 +229,7 @@ template <class T, int MODE> struct Scores {
         out = a.scale * LOG2E;
         if (MODE & MODE_CAP) {
             out = a.cap * LOG2E;
-            in = sizeof(T) == 4 ? a.scale / a.cap : a.scale / a.cap * (2.f * LOG2E);
+            in = attn_fast_tanh<T, MODE>() ? a.scale / a.cap * (2.f * LOG2E) : a.scale / a.cap;
         }
         if (MODE & MODE_SLOPE) slope = a.slope[head] * LOG2E;
     }
@@ -239,12 +244,12 @@ template <class T, int MODE> struct Scores {
             for (int r = 0; r < 16; r++) {
                 float x;
                 if constexpr (MODE & MODE_CAP) {
-                    if constexpr (sizeof(T) == 4) {
-                        x = tanhf(c[r] * in);
-                        x *= out;
-                    } else {
+                    if constexpr (attn_fast_tanh<T, MODE>()) {
                         const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c[r] * in));
                         x = fmaf(-2.f * out, g, out);
+                    } else {
+                        x = tanhf(c[r] * in);
+                        x *= out;
                     }
                 } else
                     x = c[r] * out;
@@ -687,15 +692,16 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
 // beginning for dq, in its middle for dk and dv, whose barrier is there too (at the beginning: 578 us instead of 500).
 // One sequence of 4096, 12 heads of 64 in bf16: dq 110 us (706 TF), dk and dv 124 (829); capped and biased 158 and 161 us: vector instructions.  64 sequences of
 // 290 rows on average: 56 and 71 us.
-template <class T, int DP> struct AttnGrad {
+template <class T, int DP, int MODE> struct AttnGrad {
     static constexpr int TILE = 32 * DP;
-    static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : DP > 64 ? 2 : 3, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2; // per SIMD
+    static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave
+    static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : (DP > 64 ? 2 : 3) - LESS, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2 - LESS; // per SIMD
 };
 // What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p and the factor of ds, 1 - tanh^2 under
-// a cap.  16-bit types have tanh as 1 - 2 g, g = 1 / (1 + e^2y), and 1 - tanh^2 as 4 g (1 - g): the 4 is in p there (LIFT), so that ds keeps the size that fp16
+// a cap.  Where tanh is 1 - 2 g, g = 1 / (1 + e^2y), 1 - tanh^2 is 4 g (1 - g): the 4 is in p there (LIFT), so that ds keeps the size that fp16
 // was chosen for, and dv is divided by it.
 template <class T, int MODE> struct GradScore {
-    static constexpr bool FAST = (MODE & MODE_CAP) && sizeof(T) == 2;
+    static constexpr bool FAST = attn_fast_tanh<T, MODE>();
     static constexpr float LIFT = FAST ? 4.f : 1.f;
     float in, out, slope;
     __device__ __forceinline__ GradScore(const AttnArgs &a, int head)
@@ -723,11 +729,11 @@ template <class T, int MODE> struct GradScore {
 };
 
 // dq: queries as columns.  Also leaves -delta for the kernel of dk and dv, which runs after it.
-template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP>::WAVES_Q)) void k_attn_grad_q(AttnArgs a)
+template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP, MODE>::WAVES_Q)) void k_attn_grad_q(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
     constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP>::TILE];
+    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP, MODE>::TILE];
 
     int head, slot, split;
     if (!attn_work(a, a.slots, head, slot, split)) return;
@@ -830,11 +836,11 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
 
 // dk, dv: keys as columns, the queries of all heads that share the key head stream by, one head after the other.  Where that leaves too few work-groups
 // their blocks are cut into a.splits parts, whose sums k_attn_grad_join adds up.
-template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP>::WAVES_KV)) void k_attn_grad_kv(AttnArgs a)
+template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP, MODE>::WAVES_KV)) void k_attn_grad_kv(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
     constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP>::TILE];
+    __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP, MODE>::TILE];
     __shared__ __attribute__((aligned(16))) float stat[2][2][32]; // what is added to scores, -delta
 
     int kh, slot, split;

@@ -1,7 +1,9 @@
 """Token states to embeddings and ciphertexts without a GPU: calls at the edge of what is documented."""
+import ctypes
 import importlib.util
 import itertools
 import re
+import struct
 import threading
 import time
 
@@ -65,3 +67,13 @@ def test_wide_tiles_are_built_for_the_modes_that_plans_give_them():
         names = {m.decode() for m in re.findall(rb"_Z6k_attnI\w+", f.read())}
     wide = {m.groups() for m in (re.match(r"_Z6k_attnI(f|DF16_|DF16b)Li(\d+)ELi2ELi(\d+)EE", n) for n in names) if m}
     assert wide == {(t, d, mode) for t in ("DF16_", "DF16b") for d in ("32", "64") for mode in ("0", "2")}
+
+
+def test_scales_and_caps_are_taken_up_to_2_to_the_127(he):
+    """Products with log2(e) are made of them: what is finite only without it is refused."""
+    pack, span = struct.Struct("@4iPPiqPPiqddPi4x").pack, (1 << 20, 1 << 20, 3, 40)  # he_attn
+    need = ctypes.c_size_t()
+    call = lambda scale, cap: he.lib.he_attention_workspace_bytes(he.ctx, pack(2, 4, 2, 64, *span, *span, scale, cap, 0, 1), 0, ctypes.byref(need))  # noqa: E731
+    assert call(0.125, 2.0**127) == 0 and call(2.0**127, 0.0) == 0
+    for bad in ((0.125, 2.0**127 * 1.01), (2.0**127 * 1.01, 0.0), (0.125, 3.4e38), (3.4e38, 0.0)):
+        assert call(*bad) == -1, bad

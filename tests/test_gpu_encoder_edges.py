@@ -48,3 +48,33 @@ def test_a_context_knows_its_stream_before_it_says_that_it_is_ready():
         he.pool_mean(x, i32(0, 3))
     torch.cuda.synchronize()
     assert streams == [side.cuda_stream]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("cap", [1e3, 1e5, 1e8, 1e30])
+@pytest.mark.parametrize("lengths,heads,kv,bias", [([40, 0, 130], 4, 2, True), ([1100], 16, 8, False), ([700, 460], 12, 12, True)])
+def test_attention_under_caps_that_scores_never_reach(he, lengths, heads, kv, bias, cap, dtype):
+    """A cap far above the scores changes nothing, so what is granted is what is granted without one."""
+    off, rows = offsets_of(lengths), sum(lengths)
+    q, do = rand(1, rows, heads, 64, dtype=dtype, scale=2.0), rand(4, rows, heads, 64, dtype=dtype)
+    k, v = (rand(i, rows, kv, 64, dtype=dtype) for i in (2, 3))
+    slopes = torch.linspace(0.0, 0.1, heads, device="cuda") if bias else None
+    free = ref.attention(q, k, v, off, do=do, slopes=slopes, device="cuda")
+    want = ref.attention(q, k, v, off, do=do, slopes=slopes, cap=cap, device="cuda")
+    o, lse = he.attention(q, k, v, off, cap=cap, slopes=slopes)
+    grads = he.attention_backward(do, q, k, v, o, lse, off, cap=cap, slopes=slopes)
+    for name, got in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *grads)):
+        ref.check(got, (want[name][0], free[name][1]), name)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("cap", [63.0, 64.0, 65.0, 200.0])
+def test_attention_under_caps_on_both_sides_of_the_rule(he, cap, dtype):
+    """Scores that reach the cap, on both sides of 64, where the tanh is made in another way."""
+    off = offsets_of([90, 1, 300])
+    q, do = rand(1, 391, 4, 64, dtype=dtype, scale=60.0), rand(4, 391, 4, 64, dtype=dtype)
+    k, v = (rand(i, 391, 2, 64, dtype=dtype) for i in (2, 3))
+    want = ref.attention(q, k, v, off, do=do, cap=cap, device="cuda")
+    o, lse = he.attention(q, k, v, off, cap=cap)
+    for name, got in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *he.attention_backward(do, q, k, v, o, lse, off, cap=cap))):
+        ref.check(got, want[name], name)
