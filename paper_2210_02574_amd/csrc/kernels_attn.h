@@ -278,6 +278,11 @@ struct FwdRange {
     }
 };
 
+// Weights refer to the running maximum, which may be 8 behind: they are at most 2^8.  In fp16, whose numbers end at 2^-25, they are lifted by 2^7 more, as far as
+// its 65504 allow, so that many small weights beside a large one still count: a weight is off by 2^-32 of the largest (not lifted, 60000 weights of 2^-25.2
+// were zeros, 0.0016 of the sum).  It costs nothing: the lift is in what the exponent is taken less of.
+template <class T> constexpr float attn_lift() { return std::is_same<T, f16>::value ? 7.f : 0.f; }
+
 // A row's result: its sum of weights, the maximum that they refer to (in units of log2) and the weighted sum of values in o.
 template <class T, int DB> __device__ __forceinline__ void fwd_store(const AttnArgs &a, const FwdRange &g, int head, int split, int row, float top, float sum, f32x16 (&o)[DB], int lane)
 {
@@ -285,7 +290,7 @@ template <class T, int DB> __device__ __forceinline__ void fwd_store(const AttnA
     if (row >= g.t.top || (!in && !a.fill)) return;
     // a row without keys, and a row of no sequence: zeros
     const bool some = in && g.hi > g.lo;
-    const float f = some ? 1.f / sum : 0.f, lse = some ? (top + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    const float f = some ? 1.f / sum : 0.f, lse = some ? (top - attn_lift<T>() + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
     const int64_t at = (int64_t)head * a.sq.rows + row;
     if (a.splits > 1) {
         const int64_t part = (int64_t)split * a.heads * a.sq.rows + at;
@@ -399,7 +404,7 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 #pragma unroll
         for (int b = 0; b < QB; b++) scores(x[b], (float)(row0 + 32 * b + g.back - (j - g.kb)), h);
     };
-    // The maximum that the sums refer to moves only when it is left 8 behind (2^8 fits every type): most steps skip the rescaling.
+    // The maximum that the sums refer to moves only when it is left 8 behind (attn_lift): most steps skip the rescaling.
     const auto rescale = [&]() {
         bool far = false;
 #pragma unroll
@@ -421,7 +426,7 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
     const auto exponentials = [&](int half) {
 #pragma unroll
         for (int b = 0; b < QB; b++) {
-            const float ref = top[b] == -INFINITY ? 0.f : top[b];
+            const float ref = (top[b] == -INFINITY ? 0.f : top[b]) - attn_lift<T>();
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[b][8 * half + e], c2, -ref));
@@ -570,7 +575,7 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
 #pragma unroll
                 for (int r = 0; r < 16; r++) o[db][r] *= f;
         }
-        const float ref = top == -INFINITY ? 0.f : top;
+        const float ref = (top == -INFINITY ? 0.f : top) - attn_lift<T>();
 #pragma unroll
         for (int half = 0; half < 2; half++) {
             Vec<T, 8> p;

@@ -78,3 +78,22 @@ def test_attention_under_caps_on_both_sides_of_the_rule(he, cap, dtype):
     o, lse = he.attention(q, k, v, off, cap=cap)
     for name, got in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *he.attention_backward(do, q, k, v, o, lse, off, cap=cap))):
         ref.check(got, want[name], name)
+
+
+@pytest.mark.parametrize("seqs,queries,keys", [(1, 1100, 60000), (20, 20, 3000)])
+def test_fp16_weights_far_below_the_largest(he, seqs, queries, keys):
+    """One key's weight is 2^25.2 times each of the others', which alone carry a value.  A weight is held down to 2^-31 of the largest, so it is off by 2^-32 of
+    that at most."""
+    u, heads = 2.0**-11, 16
+    k, v = torch.zeros(seqs * keys, 1, 8, dtype=F16, device="cuda"), torch.ones(seqs * keys, 1, 8, dtype=F16, device="cuda")
+    k[..., 0] = -17.46875
+    k[::keys] = 0
+    v[::keys] = 0
+    q = torch.zeros(seqs * queries, heads, 8, dtype=F16, device="cuda")
+    q[..., 0] = 1
+    at = torch.arange(seqs + 1, dtype=torch.int32, device="cuda")
+    o, _ = he.attention(q, k.expand(-1, heads, 8), v.expand(-1, heads, 8), at * queries, offsets_k=at * keys, scale=1.0)
+    w = (keys - 1) * np.exp(-17.46875)
+    p = w / (1 + w)
+    e = 16 * ref.F32 * 17.5 + 4 * ref.F32 * 17.5 + 2.0**-22
+    assert (o.double() - p).abs().max() <= (u + 2 * e + 2.0**-14) * p + keys * 2.0**-32 + u * p
