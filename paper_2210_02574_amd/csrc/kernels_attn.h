@@ -427,12 +427,14 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 #pragma unroll
         for (int b = 0; b < QB; b++) {
             const float ref = (top[b] == -INFINITY ? 0.f : top[b]) - attn_lift<T>();
+            float eight = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[b][8 * half + e], c2, -ref));
-                sum[b] += x;
+                eight += x;
                 p[half][b][e] = (T)x;
             }
+            sum[b] += eight; // one by one, weights below 2^-25 of the sum would leave it as it is
         }
     };
     const auto weigh = [&](int half) {
@@ -579,12 +581,14 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
 #pragma unroll
         for (int half = 0; half < 2; half++) {
             Vec<T, 8> p;
+            float eight = 0.f; // as in k_attn
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * half + e], c2, -ref));
-                sum += x;
+                eight += x;
                 p[e] = (T)x;
             }
+            sum += eight;
 #pragma unroll
             for (int db = 0; db < DB; db++) o[db] = AttnType<T>::mma(L::cols(lv, 32 * wk + 16 * half, db, lane), p, o[db]);
         }

@@ -97,3 +97,20 @@ def test_fp16_weights_far_below_the_largest(he, seqs, queries, keys):
     p = w / (1 + w)
     e = 16 * ref.F32 * 17.5 + 4 * ref.F32 * 17.5 + 2.0**-22
     assert (o.double() - p).abs().max() <= (u + 2 * e + 2.0**-14) * p + keys * 2.0**-32 + u * p
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("seqs,queries,keys", [(1, 1100, 60000), (20, 20, 3000)])
+def test_sums_of_many_small_weights(he, seqs, queries, keys, dtype):
+    """The same weights: each is too small to change a sum in 32 bits of which the largest is a part.  A lane's sum takes eight at a time and meets half of the
+    keys or fewer, so it is off by half a step, 2^-24 below 2, keys / 16 times.  2^-20: two steps of a logarithm below 8, fp16's lift."""
+    k = torch.zeros(seqs * keys, 1, 8, dtype=dtype, device="cuda")
+    k[..., 0] = -17.5
+    k[::keys] = 0
+    q = torch.zeros(seqs * queries, 16, 8, dtype=dtype, device="cuda")
+    q[..., 0] = 1
+    at = torch.arange(seqs + 1, dtype=torch.int32, device="cuda")
+    lse = he.attention(q, k.expand(-1, 16, 8), k.expand(-1, 16, 8), at * queries, offsets_k=at * keys, scale=1.0)[1]
+    e = 16 * ref.F32 * 17.5 + 4 * ref.F32 * 17.5 + 2.0**-22
+    w = (keys - 1) * np.exp(-17.5)
+    assert (lse.double() - np.log1p(w)).abs().max() <= 2 * e * w + 2.0**-20 + keys / 16 * 2.0**-24
