@@ -48,6 +48,10 @@ static void attn_join(he_ctx *c, hipStream_t st, double bytes, unsigned grid, co
 {
     KLAUNCH(c, st, KID_ATTN_JOIN, bytes, (k_attn_join<T>), grid, a);
 }
+static void attn_grad_size(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a)
+{
+    if constexpr (grad_lifted<T>()) KLAUNCH(c, st, KID_ATTN_GRAD_SIZE, bytes, (k_attn_grad_size<T, HE_DIM>), grid, a);
+}
 static void attn_grad_q(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a)
 {
     by_mode(a, [&](auto mode) {
@@ -79,6 +83,7 @@ void NAME(HE_TYPE, HE_DIM)(AttnLaunch &t)
 {
     t.fwd = attn_fwd;
     t.join = attn_join;
+    t.grad_size = grad_lifted<T>() ? attn_grad_size : nullptr;
     t.grad_q = attn_grad_q;
     t.grad_kv = attn_grad_kv;
     t.grad_join = attn_grad_join;

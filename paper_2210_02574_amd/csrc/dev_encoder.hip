@@ -183,12 +183,17 @@ int grad_splits(const he_attn *s)
     if (work < 640) return 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>({(2560 + waves / 2) / waves, work / (waves < 512 ? 128 : 512), 8}));
 }
+int64_t grad_slots_q(const he_attn *s) { return tile_slots(s->q.rows, s->q.count, grad_tile_q(s->q)); }
+int64_t grad_slots_k(const he_attn *s) { return tile_slots(s->k.rows, s->k.count, grad_tile_k(s->k)); }
+// numbers of k_attn_grad_size, in whole vectors of 16 bytes
+size_t grad_sizes(const he_attn *s) { return s->type == HE_F16 ? (size_t)((grad_slots_q(s) + grad_slots_k(s)) * s->kv_heads + 3) / 4 * 4 : 0; }
 size_t attn_bytes(const he_attn *s, bool backward)
 {
     const size_t rows = (size_t)s->q.rows * s->heads;
     if (backward) {
+        if (s->q.count == 0) return 0;
         const int splits = grad_splits(s);
-        return (rows + 3) / 4 * 16 + (splits > 1 ? (size_t)splits * 2 * s->kv_heads * s->k.rows * s->dim * 4 : 0);
+        return (rows + 3) / 4 * 16 + grad_sizes(s) * 4 + (splits > 1 ? (size_t)splits * 2 * s->kv_heads * s->k.rows * s->dim * 4 : 0);
     }
     const AttnPlan p = attn_plan(s);
     return p.splits > 1 ? rows * p.splits * (s->dim + 1) * 4 : 0;
@@ -411,13 +416,16 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
         SET(k, k), SET(v, v), SET(dk, dk), SET(dv, dv);
     }
     a.lse = const_cast<float *>(d_lse);
+    const int64_t slots_q = grad_slots_q(s), slots_k = grad_slots_k(s);
+    const int tile_q = grad_tile_q(s->q), tile_k = grad_tile_k(s->k);
     a.delta = (float *)d_ws;
+    a.v_size = a.delta + (s->q.rows * s->heads + 3) / 4 * 4;
+    a.go_size = a.v_size + slots_k * s->kv_heads;
+    a.slots_q = (int)std::min<int64_t>(slots_q, INT32_MAX), a.tile_q = tile_q, a.slots_k = (int)std::min<int64_t>(slots_k, INT32_MAX), a.tile_k = tile_k;
     AttnArgs b = a;
     b.splits = grad_splits(s);
-    b.part_o = a.delta + (s->q.rows * s->heads + 3) / 4 * 4;
+    b.part_o = a.v_size + grad_sizes(s);
     unsigned grid_q = 0, grid_kv = 0;
-    const int tile_q = grad_tile_q(s->q), tile_k = grad_tile_k(s->k);
-    const int64_t slots_q = tile_slots(s->q.rows, s->q.count, tile_q), slots_k = tile_slots(s->k.rows, s->k.count, tile_k);
     if (!attn_grid(a, slots_q, slots_q * s->heads, grid_q) || !attn_grid(b, slots_k, slots_k * s->kv_heads * b.splits, grid_kv)) return HE_EINVAL;
     const int64_t rows_kv = s->k.rows * s->kv_heads;
     NEEDS_DEVICE(ctx);
@@ -425,6 +433,8 @@ extern "C" int32_t he_attention_grad(he_ctx *ctx, const he_attn *s, const he_hea
     if (dg.rc != HE_OK) return dg.rc;
     const AttnLaunch &l = attn_launch(s->type, s->dim);
     const double size = (double)type_size(s->type) * s->dim, qb = s->q.rows * s->heads * size, kb = s->k.rows * s->kv_heads * size;
+    if (l.grad_size && some_q && some_k)
+        l.grad_size(ctx, (hipStream_t)stream, qb + kb, (unsigned)std::min<int64_t>(((slots_q + slots_k) * s->kv_heads + 3) / 4, 1 << 22), a);
     if (some_q) l.grad_q(ctx, (hipStream_t)stream, 4 * qb + 2 * kb + 8.0 * s->q.rows * s->heads, tile_q, grid_q, a);
     if (some_k) l.grad_kv(ctx, (hipStream_t)stream, 2 * qb + 4 * kb + 8.0 * s->q.rows * s->heads, tile_k, grid_kv, b);
     if (some_k && b.splits > 1) l.grad_join(ctx, (hipStream_t)stream, 2.0 * rows_kv * (size + 4.0 * b.splits * s->dim), (unsigned)((rows_kv + 3) / 4), b);

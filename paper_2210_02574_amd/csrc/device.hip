@@ -182,7 +182,7 @@ static const char *const kKernelNames[KID_COUNT] = {
     "k_ntt_fwd_blocks",
     "k_ntt_fwd_blocks_fin", "k_ntt_inv_blocks", "k_ntt_inv_cols", "k_limbwise", "k_cmult", "k_copy_limbs", "k_inner_special", "k_inner_finished",
     "k_inner_fin", "k_ntt_fwd12", "k_ntt_fwd12_modup", "k_ntt_fwd12_rescale", "k_ntt_inv12", "k_inner12", "k_fin12",
-    "k_attn", "k_attn_few", "k_attn_join", "k_attn_grad_q", "k_attn_grad_kv", "k_attn_grad_join", "k_layer_norm", "k_layer_norm_grad", "k_norm_weight_grad", "k_pool", "k_pool_join", "k_pool_grad"};
+    "k_attn", "k_attn_few", "k_attn_join", "k_attn_grad_size", "k_attn_grad_q", "k_attn_grad_kv", "k_attn_grad_join", "k_layer_norm", "k_layer_norm_grad", "k_norm_weight_grad", "k_pool", "k_pool_join", "k_pool_grad"};
 
 bool prof_events(he_ctx *c, int kid, double bytes, ProfRecord &r)
 {

@@ -18,6 +18,7 @@ struct AttnLaunch {
     // tile: queries of a work-group, 32, 64, 128 or 256
     void (*fwd)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);
     void (*join)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a);
+    void (*grad_size)(he_ctx *c, hipStream_t st, double bytes, unsigned grid, const AttnArgs &a); // fp16, else null
     // tile: rows of a work-group, 64 or 128 queries, 32, 64 or 128 keys
     void (*grad_q)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);
     void (*grad_kv)(he_ctx *c, hipStream_t st, double bytes, int tile, unsigned grid, const AttnArgs &a);

@@ -16,8 +16,8 @@
 // everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  Rounding both the terms and the result leaves 1.4
 // times the error of rounding the result alone.  delta takes o as it was rounded: where few keys of many carry a row's weight (a steep distance bias) that
 // adds a tenth to dq and dk; without it a pass over all keys would have to come first (up to 32 keys of short sequences are at hand at once, and delta is exact).  Its error
-// alone, sum p (dp - delta), would mend dk but not dq: 10 % of dq's time under a cap.  fp16 holds dt down to 6e-8: gradients as small as that need a scaled
-// loss, as everywhere in fp16.
+// alone, sum p (dp - delta), would mend dk but not dq: 10 % of dq's time under a cap.  fp16 has the bits for it but not the range: there all factors are
+// lifted by powers of two, weights by constants (attn_lift, GRAD_LIFT), ds by what k_attn_grad_size finds.
 #pragma once
 #include "enc_common.h"
 #include <type_traits>
@@ -27,6 +27,7 @@ struct AttnArgs {
     void *o, *dq, *dk, *dv;
     float *lse;         // [heads][rows_q], natural logarithm
     float *delta;       // [heads][rows_q]
+    float *v_size, *go_size; // fp16, backward: [slots of keys or queries][kv_heads], k_attn_grad_size
     float *part_o;      // forward: [splits][heads][rows_q][dim]; dk and dv: [splits][2][kv_heads][rows_k][dim]
     float *part_lse;    // [splits][heads][rows_q]
     const float *slope; // [heads] or null
@@ -38,6 +39,7 @@ struct AttnArgs {
     int slots, splits, fill;
     int pack; // few queries: query heads of one key head that lie side by side in a tile, `group` or 1
     unsigned work; // work-groups that have something to do
+    int slots_q, tile_q, slots_k, tile_k; // of the backward pass, in both of its kernels
 };
 
 template <class T> struct AttnType;
@@ -706,12 +708,11 @@ template <class T, int DP, int MODE> struct AttnGrad {
     static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave
     static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : (DP > 64 ? 2 : 3) - LESS, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2 - LESS; // per SIMD
 };
-// What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p and the factor of ds, 1 - tanh^2 under
-// a cap.  Where tanh is 1 - 2 g, g = 1 / (1 + e^2y), 1 - tanh^2 is 4 g (1 - g): the 4 is in p there (LIFT), so that ds keeps the size that fp16
-// was chosen for, and dv is divided by it.
+// What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p, times 2^lift, and the factor of ds, 1 - tanh^2 under
+// a cap.  Where tanh is 1 - 2 g, g = 1 / (1 + e^2y), 1 - tanh^2 is 4 g (1 - g): the 4 (BACK) comes with the scale.
 template <class T, int MODE> struct GradScore {
     static constexpr bool FAST = attn_fast_tanh<T, MODE>();
-    static constexpr float LIFT = FAST ? 4.f : 1.f;
+    static constexpr float BACK = FAST ? 4.f : 1.f;
     float in, out, slope;
     __device__ __forceinline__ GradScore(const AttnArgs &a, int head)
     {
@@ -734,8 +735,87 @@ template <class T, int MODE> struct GradScore {
         }
         return __builtin_amdgcn_exp2f(fmaf(x, out, rest));
     }
-    __device__ __forceinline__ float rest(float lse) const { return FAST ? out + 2.f - lse * LOG2E : -lse * LOG2E; }
+    __device__ __forceinline__ float rest(float lse, float lift) const { return (FAST ? out + lift : lift) - lse * LOG2E; }
 };
+
+// fp16 has numbers from 2^-24 to 2^16, and eleven bits of them from 2^-14 on: p of long rows is below that, and ds, which no scaling of a loss keeps in place for
+// every sequence and head, on either side.  So p is lifted by GRAD_LIFT (it is at most 1: eleven bits down to 2^-26), and ds by the power of two that brings
+// its bound to 2^12: |ds_ij| = p |do . (v_j - o)| <= p (1 - p) |do| 2 max|v| <= |do| max|v| / 2, with max|v| over the sequence's keys (k_attn_grad_size).  16 are
+// left for the roundings of p, lse and delta.  dq has the own |do| of each query row in it, dk and dv, whose sums go over queries, the sequence's largest.
+#define GRAD_LIFT 12
+template <class T> constexpr bool grad_lifted() { return std::is_same<T, f16>::value; }
+// the power of two for ds; fast: ds lacks a factor of 4
+__device__ __forceinline__ int ds_lift(float go, float v, bool fast)
+{
+    const int e = __builtin_amdgcn_frexp_expf(0.5f * go * v); // bound <= 2^e; of 0, infinities and NaN 0
+    return min(max((fast ? 14 : 12) - e, -60), 60);
+}
+// The largest of a sequence's sizes as k_attn_grad_size left them: of the slots that its rows begin .. end - 1 have tiles in.  The first 64 are asked for at once, for a
+// caller that has other things to ask for before it needs them.
+struct SeqSize {
+    const float *size; // of the key head in slot 0
+    int64_t slot, top; // the sequence's first slot, the last slot of all
+    int kv_heads, next, last;
+    float most;
+    __device__ __forceinline__ SeqSize(const float *of, int seq, int begin, int end, int tile, int slots, int kv_heads, int kh) : size(of + kh), top(slots - 1), kv_heads(kv_heads), most(0.f)
+    {
+        const int c = seq ? begin : 0;
+        slot = tile_slot(c, seq, tile);
+        next = (begin - c) / tile + (threadIdx.x & 63), last = end > begin ? (end - 1 - c) / tile : -1;
+        take();
+    }
+    __device__ __forceinline__ void take()
+    {
+        if (next <= last) most = fmaxf(most, size[min(slot + next, top) * kv_heads]);
+        next += 64;
+    }
+    __device__ __forceinline__ float largest()
+    {
+        while (next <= last) take();
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s, 64));
+        return most;
+    }
+};
+
+// fp16: the largest norm of a row of v in each tile of keys, and of do in each tile of queries over the heads of a group.  A wave per slot and key head, the keys' slots
+// first; the lanes of a row have 16 bytes each, and each lane eight rows under way.  No more than 2^22 work-groups, each of which takes its share.
+// It takes 8.5 us for 3 sequences of 4000, 16 heads of 64 on 8 (the whole backward pass 789, 740 in bf16, which needs none of this), 7.9 for 32 of 300, 12 heads of 64 (86, 77), and
+// 4.3 for one of 23, a launch and two trips (15, 9.5).
+template <class T, int DP> __global__ __launch_bounds__(256) void k_attn_grad_size(AttnArgs a)
+{
+    constexpr int LANES = DP > 64 ? 16 : DP / 8, STEP = 64 / LANES; // lanes and rows at once
+    const int kv_heads = a.heads / a.group, sub = (threadIdx.x & 63) / LANES, col = (threadIdx.x % LANES) * 8;
+    const int64_t of_keys = (int64_t)a.slots_k * kv_heads, all = of_keys + (int64_t)a.slots_q * kv_heads;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < all; w += (int64_t)gridDim.x * 4) {
+        const bool keys = w < of_keys;
+        const int64_t item = keys ? w : w - of_keys;
+        const int slot = item / kv_heads, kh = item % kv_heads;
+        const TileRows t = keys ? tile_rows(a.sk, a.sq, slot, a.tile_k) : tile_rows(a.sq, a.sk, slot, a.tile_q);
+        const int lo = max(t.first, t.begin), hi = min(t.top, t.end);
+        const int64_t row = keys ? a.v_row : a.go_row;
+        float most = 0.f;
+        for (int g = 0; g < (keys ? 1 : a.group); g++) {
+            // lanes behind the row's end read its last vector and count nothing
+            const T *const base = (keys ? (const T *)a.v + kh * a.v_head : (const T *)a.go + ((int64_t)kh * a.group + g) * a.go_head) + min(col, a.dim - 8);
+            for (int r0 = lo; r0 < hi; r0 += 8 * STEP) {
+                Vec<T, 8> x[8];
+#pragma unroll
+                for (int u = 0; u < 8; u++) x[u] = *(const Vec<T, 8> *)(base + min(r0 + u * STEP + sub, hi - 1) * row); // the last row again where there are fewer
+#pragma unroll
+                for (int u = 0; u < 8; u++) {
+                    float sq = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) sq = fmaf((float)x[u][e], (float)x[u][e], sq);
+                    most = fmaxf(most, lanes_sum<LANES>(col < a.dim ? sq : 0.f));
+                }
+            }
+        }
+#pragma unroll
+        for (int k = LANES; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k, 64));
+        if ((threadIdx.x & 63) == 0) (keys ? a.v_size : a.go_size)[item] = sqrtf(most);
+    }
+}
 
 // dq: queries as columns.  Also leaves -delta for the kernel of dk and dv, which runs after it.
 template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP, MODE>::WAVES_Q)) void k_attn_grad_q(AttnArgs a)
@@ -764,21 +844,26 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         reads_v.load(cv, v, a.v_row, j, ke, a.dim);
     };
     load(kb);
+    SeqSize size(a.v_size, t.seq, kb, grad_lifted<T>() ? ke : kb, a.tile_k, a.slots_k, a.heads / a.group, head / a.group);
     Vec<T, 8> fq[KK], fg[KK];
-    float delta = 0.f;
+    float delta = 0.f, sq = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
         fq[kk] = L::own(q, a.q_row, row, in, kk, a.dim, lane);
         fg[kk] = L::own(go, a.go_row, row, in, kk, a.dim, lane);
         const Vec<T, 8> x = L::own(oi, a.oi_row, row, in, kk, a.dim, lane);
 #pragma unroll
-        for (int e = 0; e < 8; e++) delta -= (float)x[e] * (float)fg[kk][e];
+        for (int e = 0; e < 8; e++) {
+            delta -= (float)x[e] * (float)fg[kk][e];
+            if (grad_lifted<T>()) sq = fmaf((float)fg[kk][e], (float)fg[kk][e], sq);
+        }
     }
     delta = pair_sum(delta);
+    const int lift = grad_lifted<T>() ? ds_lift(sqrtf(pair_sum(sq)), size.largest(), GradScore<T, MODE>::FAST) : 0;
     const GradScore<T, MODE> score(a, head);
     const int64_t at = (int64_t)head * a.sq.rows + row;
     if (in && h == 0) a.delta[at] = delta;
-    const float rest = in ? score.rest(a.lse[at]) : -INFINITY; // rows of no sequence: p = 0
+    const float rest = in ? score.rest(a.lse[at], (float)lift) : -INFINITY; // rows of no sequence: p = 0
     f32x16 dq[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dq[db] = f32x16{};
@@ -816,7 +901,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         }
         if constexpr (lone) {
             // All weights of the row are at hand: sum p (dp - delta) is what delta lacks for o as it was before its rounding.
-            by = pair_sum(by) * (1.f / GradScore<T, MODE>::LIFT);
+            by = ldexpf(pair_sum(by), -lift);
             delta -= by;
 #pragma unroll
             for (int r = 0; r < 16; r++) d[r >> 3][r & 7] = (T)(ps[r] * (dp[r] - by) * fs[r]);
@@ -840,7 +925,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     if (!in || ke == kb)
 #pragma unroll
         for (int db = 0; db < DB; db++) dq[db] = f32x16{};
-    store_row<T, DB>(dq, a.scale, (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
+    store_row<T, DB>(dq, ldexpf(a.scale * GradScore<T, MODE>::BACK, -lift), (T *)a.dq + head * a.dq_head + row * a.dq_row, a.dim, lane);
 }
 
 // dk, dv: keys as columns, the queries of all heads that share the key head stream by, one head after the other.  Where that leaves too few work-groups
@@ -848,7 +933,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
 template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP, MODE>::WAVES_KV)) void k_attn_grad_kv(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
-    constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32;
+    constexpr int NT = 64 * NW, KK = DP / 16, DB = DP / 32, P_LIFT = grad_lifted<T>() ? GRAD_LIFT : 0;
     __shared__ __attribute__((aligned(16))) T lds[2][2][AttnGrad<T, DP, MODE>::TILE];
     __shared__ __attribute__((aligned(16))) float stat[2][2][32]; // what is added to scores, -delta
 
@@ -874,14 +959,19 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     const auto store = [&](int stage, int head, int i) {
         L::template store<32, NT>(cq, lds[stage][0], tid);
         L::template store<32, NT>(cg, lds[stage][1], tid);
-        if (tid < 64) stat[stage][h][lane & 31] = h ? cs : i + lane < qe ? GradScore<T, MODE>(a, head).rest(cs) : -INFINITY; // a missing query: p = 0
+        if (tid < 64) stat[stage][h][lane & 31] = h ? cs : i + lane < qe ? GradScore<T, MODE>(a, head).rest(cs, P_LIFT) : -INFINITY; // a missing query: p = 0
     };
+    const bool sized = grad_lifted<T>() && qe > qb;
+    SeqSize size_go(a.go_size, t.seq, qb, sized ? qe : qb, a.tile_q, a.slots_q, a.heads / a.group, kh);
+    SeqSize size_v(a.v_size, t.seq, t.begin, sized ? t.end : t.begin, a.tile_k, a.slots_k, a.heads / a.group, kh);
     Vec<T, 8> fk[KK], fv[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
         fk[kk] = L::own(k, a.k_row, row, in, kk, a.dim, lane);
         fv[kk] = L::own(v, a.v_row, row, in, kk, a.dim, lane);
     }
+    const int lift = sized ? ds_lift(size_go.largest(), size_v.largest(), GradScore<T, MODE>::FAST) : 0;
+    const float ds_rest = ldexpf(1.f, lift - P_LIFT); // what ds lacks when p has its lift
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
@@ -944,6 +1034,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
                 const float w = score.p(s[r], rest[r >> 2][r & 3], pos - (float)(8 * (r >> 2) + (r & 3)), f);
                 float x = w * dp[r];
                 if (MODE & MODE_CAP) x *= f;
+                if (grad_lifted<T>()) x *= ds_rest;
                 p[r >> 3][r & 7] = (T)w;
                 d[r >> 3][r & 7] = (T)x;
             }
@@ -963,15 +1054,16 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     if (!in || blocks <= 0)
 #pragma unroll
         for (int db = 0; db < DB; db++) dk[db] = dv[db] = f32x16{};
+    const float back_k = ldexpf(a.scale * GradScore<T, MODE>::BACK, -lift), back_v = ldexpf(1.f, -P_LIFT);
     if (a.splits > 1) {
         float *part = a.part_o + (((int64_t)split * 2 * (a.heads / a.group) + kh) * a.sk.rows + row) * a.dim;
-        store_row<float, DB>(dk, a.scale, part, a.dim, lane);
-        store_row<float, DB>(dv, 1.f / GradScore<T, MODE>::LIFT, part + (int64_t)(a.heads / a.group) * a.sk.rows * a.dim, a.dim, lane);
+        store_row<float, DB>(dk, back_k, part, a.dim, lane);
+        store_row<float, DB>(dv, back_v, part + (int64_t)(a.heads / a.group) * a.sk.rows * a.dim, a.dim, lane);
         return;
     }
     if (!in && !a.fill) return;
-    store_row<T, DB>(dk, a.scale, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
-    store_row<T, DB>(dv, 1.f / GradScore<T, MODE>::LIFT, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
+    store_row<T, DB>(dk, back_k, (T *)a.dk + kh * a.dk_head + row * a.dk_row, a.dim, lane);
+    store_row<T, DB>(dv, back_v, (T *)a.dv + kh * a.dv_head + row * a.dv_row, a.dim, lane);
 }
 
 // dk and dv from the parts: a wave per row and key head, blockIdx.x * 4 + wave over [kv_heads][rows].

@@ -114,3 +114,70 @@ def test_sums_of_many_small_weights(he, seqs, queries, keys, dtype):
     e = 16 * ref.F32 * 17.5 + 4 * ref.F32 * 17.5 + 2.0**-22
     w = (keys - 1) * np.exp(-17.5)
     assert (lse.double() - np.log1p(w)).abs().max() <= 2 * e * w + 2.0**-20 + keys / 16 * 2.0**-24
+
+
+def _gradients(q, k, v, do, scale):
+    """{name: (value, bound)} of dq, dk and dv of one sequence with one head, [rows][dim] each, in 64 bits on the device.  As encoder_reference has them, but
+    for what a factor of small size is off by: with G and V the largest norms of a row of do and of v, ds is at most G V / 2, and is lifted by a power of
+    two to between 2^11 and 2^12 of that or less; p is lifted by 2^12.  So half a step of fp16 is 2^-37 G V of a ds and 2^-37 of a p.  A result's own
+    half step is 2^-25."""
+    u, f = 2.0**-11, ref.F32
+    q, k, v, do = (t.double() for t in (q, k, v, do))
+    d = q.shape[1]
+    t, t_abs = scale * q @ k.T, scale * q.abs() @ k.abs().T
+    e = ((d + 8) * f * t_abs + 4 * f * t.abs()).amax(1, keepdim=True) + 2.0**-22
+    p = torch.softmax(t, 1)
+    del t, t_abs
+    rel = u + 2 * e + 2.0**-14
+    o, dp = p @ v, do @ v.T
+    ob = (rel * p) @ v.abs() + u * o.abs()
+    size = do.abs() @ v.abs().T + (do * o).abs().sum(1, keepdim=True)
+    db = (do.abs() * ob).sum(1, keepdim=True) + (d + 8) * f * size
+    dt = p * (dp - (do * o).sum(1, keepdim=True)) * scale
+    most = float(do.norm(dim=1).max() * v.norm(dim=1).max())
+    te = rel * dt.abs() + p * db * scale + 2.0**-37 * most * scale
+    out = {"dq": (dt @ k, te @ k.abs()), "dk": (dt.T @ q, te.T @ q.abs()), "dv": (p.T @ do, (rel * p + 2.0**-37).T @ do.abs())}
+    return {n: (a.cpu(), (b + u * a.abs() + 2.0**-25).cpu()) for n, (a, b) in out.items()}
+
+
+def _check_gradients(he, q, k, v, do, scale, cap=0.0):
+    q, k, v, do = (t.to(F16).contiguous() for t in (q, k, v, do))
+    args = [t[:, None] for t in (q, k, v)]
+    extra = {"offsets_k": i32(0, len(k)), "scale": scale, "cap": cap}
+    o, lse = he.attention(*args, i32(0, len(q)), **extra)
+    got = he.attention_backward(do[:, None], *args, o, lse, i32(0, len(q)), **extra)
+    want = _gradients(q, k, v, do, scale)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        ref.check(g[:, 0], want[name], name)
+
+
+def test_fp16_gradients_of_long_rows_with_equal_weights(he):
+    """Weights of 1 / 166940: 100.5 of fp16's smallest steps, so that each of them rounds the same way by 2^-7.7 of itself."""
+    n, ones = 166940, torch.ones(8, device="cuda")
+    s = torch.ones(n, 1, device="cuda")
+    s[1::2] = -1
+    r = s[:512]
+    _check_gradients(he, 0 * r * ones, s * 2.0**-12 * ones, s * ones, 0.125 * ones.expand(512, 8), 8**-0.5)  # dv and dq
+    _check_gradients(he, 8 * r * ones, s * 2.0**-12 * ones, s * ones, 0.125 * r * ones, 8**-0.5)  # dk and dq
+
+
+@pytest.mark.parametrize("size", [2.0**-12, 1.0, 2.0**10])
+@pytest.mark.parametrize("cap", [0.0, 1e6])
+def test_fp16_gradients_of_long_rows_and_of_any_size(he, size, cap):
+    """Gradients whose terms are below fp16's smallest number, and large ones."""
+    q, do = rand(1, 300, 64), rand(2, 300, 64, scale=size)
+    k, v = rand(3, 20000, 64), rand(4, 20000, 64)
+    _check_gradients(he, q, k, v, do, 0.125, cap)
+
+
+@pytest.mark.parametrize("keys", [2, 40, 700])
+def test_fp16_gradients_near_the_largest_number(he, keys):
+    """ds passes 65504, dq, dk and dv do not."""
+    s = torch.ones(keys, 1, device="cuda")
+    s[1::2] = -1
+    ones = torch.ones(64, device="cuda")
+    r = torch.ones(30, 1, device="cuda")
+    r[1::2] = -1
+    q, do = 2.0**-9 * r * ones, 30000 * r * ones  # a dp of 1.9e6
+    do[3] = 2.0**-10
+    _check_gradients(he, q, s * 2.0**-4 * ones, s * ones, do, 0.125)
