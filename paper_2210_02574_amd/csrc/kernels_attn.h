@@ -14,9 +14,11 @@
 //
 // Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
 // everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  Rounding both the terms and the result leaves 1.4
-// times the error of rounding the result alone.  delta takes o as it was rounded: where few keys of many carry a row's weight (a steep distance bias) that
-// adds a tenth to dq and dk; without it a pass over all keys would have to come first (up to 32 keys of short sequences are at hand at once, and delta is exact).  Its error
-// alone, sum p (dp - delta), would mend dk but not dq: 10 % of dq's time under a cap.  fp16 has the bits for it but not the range: there all factors are
+// times the error of rounding the result alone.  delta takes o as it was rounded: its error has the size of that rounding, |do . o| 2^-9 or 2^-12 and less, and matters where
+// o is not small beside the values' own spread: under a steep distance bias, which leaves few keys with a weight whatever the data are, dq and dk had 1.55 times the error of
+// rounding the result alone.  With a bias it is therefore mended (k_attn_grad_q, which also says what it is otherwise), and for up to 32 keys of short sequences, which are at hand
+// at once, delta is exact.
+// fp16 has the bits for it but not the range: there all factors are
 // lifted by powers of two, weights by constants (attn_lift, GRAD_LIFT), ds by what k_attn_grad_size finds.
 #pragma once
 #include "enc_common.h"
@@ -705,8 +707,9 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
 // 290 rows on average: 56 and 71 us.
 template <class T, int DP, int MODE> struct AttnGrad {
     static constexpr int TILE = 32 * DP;
-    static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave
-    static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : (DP > 64 ? 2 : 3) - LESS, WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2 - LESS; // per SIMD
+    static constexpr bool MEND = sizeof(T) == 2 && (MODE & MODE_SLOPE); // delta and dq are mended, as the comment at k_attn_grad_q says
+    static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave, the sums that mend too
+    static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : (DP > 64 ? 2 : 3) - (LESS || MEND), WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2 - LESS; // per SIMD
 };
 // What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p, times 2^lift, and the factor of ds, 1 - tanh^2 under
 // a cap.  Where tanh is 1 - 2 g, g = 1 / (1 + e^2y), 1 - tanh^2 is 4 g (1 - g): the 4 (BACK) comes with the scale.
@@ -818,6 +821,11 @@ template <class T, int DP> __global__ __launch_bounds__(256) void k_attn_grad_si
 }
 
 // dq: queries as columns.  Also leaves -delta for the kernel of dk and dv, which runs after it.
+// MEND: what delta lacks, off = sum p (dp - delta), is known when all keys have passed.  So the weighted mean of the keys, sum p k (1 - tanh^2), is summed beside dq, which is
+// then less by off times that; dk and dv get the right delta from the start.  That is one product in four, two or three vector instructions per score and a wave per SIMD:
+// the whole backward pass of 3 sequences of 4000, 16 heads of 64 on 8, biased, 845 us in bf16 (772 without), of 4096 rows, 12 heads of 128, 594 (449).  Relative error of dq
+// over 600 rows in bf16, values of mean 0, 1, 4 and 16 times their spread: 0.0024 each; without it (and so without a bias, where it would take 83 us instead of 75
+// for 32 sequences of 300, 577 instead of 429 for heads of 128) 0.0024, 0.0044, 0.016 and 0.061.
 template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * NW, (AttnGrad<T, DP, MODE>::WAVES_Q)) void k_attn_grad_q(AttnArgs a)
 {
     typedef AttnTile<T, DP> L;
@@ -862,11 +870,18 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
     const int lift = grad_lifted<T>() ? ds_lift(sqrtf(pair_sum(sq)), size.largest(), GradScore<T, MODE>::FAST) : 0;
     const GradScore<T, MODE> score(a, head);
     const int64_t at = (int64_t)head * a.sq.rows + row;
-    if (in && h == 0) a.delta[at] = delta;
+    if (!AttnGrad<T, DP, MODE>::MEND && in && h == 0) a.delta[at] = delta;
     const float rest = in ? score.rest(a.lse[at], (float)lift) : -INFINITY; // rows of no sequence: p = 0
-    f32x16 dq[DB];
+    constexpr bool MEND = AttnGrad<T, DP, MODE>::MEND;
+    constexpr int W_LIFT = grad_lifted<T>() ? GRAD_LIFT : 0;
+    const float w_rest = ldexpf(1.f, W_LIFT - lift); // what p lacks as a weight of the mean when it has ds's lift
+    float off = 0.f; // times 2^lift
+    f32x16 dq[DB], mean[MEND ? DB : 1];
 #pragma unroll
-    for (int db = 0; db < DB; db++) dq[db] = f32x16{};
+    for (int db = 0; db < DB; db++) {
+        dq[db] = f32x16{};
+        if constexpr (MEND) mean[db] = f32x16{};
+    }
 
     int stage = 0;
     const auto block = [&](int j, auto tail, auto lone) { // the 32 keys from j on; lone: the only ones
@@ -883,7 +898,7 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
             dp = AttnType<T>::mma(L::rows(lds[stage][1], 0, kk, lane), fg[kk], dp);
         }
         const float pos = (float)(pos0 - (j - kb) - 4 * h);
-        Vec<T, 8> d[2];
+        Vec<T, 8> d[2], w[2];
         float ps[lone ? 16 : 1], fs[lone ? 16 : 1], by = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
@@ -895,10 +910,18 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
                 by += p * dp[r];
                 continue;
             }
+            if constexpr (MEND) {
+                by = fmaf(p, dp[r], by);
+                if (MODE & MODE_CAP) p *= f;
+                w[r >> 3][r & 7] = (T)(grad_lifted<T>() ? p * w_rest : p); // (its rounding is one of the correction alone)
+                d[r >> 3][r & 7] = (T)(p * dp[r]);
+                continue;
+            }
             p *= dp[r];
             if (MODE & MODE_CAP) p *= f;
             d[r >> 3][r & 7] = (T)p; // the scale is put on at the end
         }
+        if constexpr (MEND) off += by;
         if constexpr (lone) {
             // All weights of the row are at hand: sum p (dp - delta) is what delta lacks for o as it was before its rounding.
             by = ldexpf(pair_sum(by), -lift);
@@ -909,11 +932,15 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
 #pragma unroll
         for (int half = 0; half < 2; half++)
 #pragma unroll
-            for (int db = 0; db < DB; db++) dq[db] = AttnType<T>::mma(L::cols(lds[stage][0], 16 * half, db, lane), d[half], dq[db]);
+            for (int db = 0; db < DB; db++) {
+                const Vec<T, 8> x = L::cols(lds[stage][0], 16 * half, db, lane);
+                dq[db] = AttnType<T>::mma(x, d[half], dq[db]);
+                if constexpr (MEND) mean[db] = AttnType<T>::mma(x, w[half], mean[db]);
+            }
         stage ^= 1;
     };
     int j = kb;
-    if constexpr (NW == 2) // tiles of short sequences (its registers would cost the other tile 5 %)
+    if constexpr (NW == 2 && !MEND) // tiles of short sequences (its registers would cost the other tile 5 %)
         if (ke - kb <= 32 && ke > kb) {
             block(j, std::true_type{}, std::true_type{});
             if (in && h == 0) a.delta[at] = delta;
@@ -921,6 +948,16 @@ template <class T, int DP, int NW, int MODE> __global__ __launch_bounds__(64 * N
         }
     for (; j + 32 <= ke; j += 32) block(j, std::false_type{}, std::false_type{});
     if (j < ke) block(j, std::true_type{}, std::false_type{});
+    if constexpr (MEND) {
+        off = pair_sum(off);
+        delta -= ldexpf(off, -lift);
+        if (in && h == 0) a.delta[at] = delta;
+        off = ldexpf(off, -W_LIFT); // off has 2^lift, as dq has, and the mean 2^W_LIFT
+#pragma unroll
+        for (int db = 0; db < DB; db++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) dq[db][r] = fmaf(-off, mean[db][r], dq[db][r]);
+    }
     if (row >= t.top || (!in && !a.fill)) return;
     if (!in || ke == kb)
 #pragma unroll

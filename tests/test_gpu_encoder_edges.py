@@ -181,3 +181,46 @@ def test_fp16_gradients_near_the_largest_number(he, keys):
     q, do = 2.0**-9 * r * ones, 30000 * r * ones  # a dp of 1.9e6
     do[3] = 2.0**-10
     _check_gradients(he, q, s * 2.0**-4 * ones, s * ones, do, 0.125)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("cap,lengths,heads,kv,dim", [(0.0, [20, 333, 1, 200], 4, 2, 64), (25.0, [20, 333, 1, 200], 4, 2, 64), (1e4, [700], 3, 3, 32), (0.0, [1500, 90], 6, 2, 128)])
+def test_biased_gradients_do_not_depend_on_how_o_was_rounded(he, cap, lengths, heads, kv, dim, dtype):
+    """Values with a large part in common: dp - delta is small beside both.  o is rounded to 16 bits, delta must not be.  Bounds as in encoder_reference without
+    that rounding; what takes its place is the sum p (dp - delta), off by 2 e + 2^-14 of its terms (weights and 4096 additions at most), and the
+    mean that it is multiplied with, off by u of a correction of |do| |o| u."""
+    u, f, off = ref.half_step(dtype), ref.F32, offsets_of(lengths)
+    rows = sum(lengths)
+    q, do = rand(1, rows, heads, dim, dtype=dtype), rand(2, rows, heads, dim, dtype=dtype)
+    k, v = rand(3, rows, kv, dim, dtype=dtype), (16 + rand(4, rows, kv, dim)).to(dtype)
+    slopes = 2.0 ** -torch.arange(1, heads + 1).float().cuda()
+    o, lse = he.attention(q, k, v, off, cap=cap, slopes=slopes)
+    dq, dk, _ = he.attention_backward(do, q, k, v, o, lse, off, cap=cap, slopes=slopes)
+    scale, at = dim**-0.5, np.cumsum([0] + lengths)
+    want_k, bound_k = (torch.zeros(rows, kv, dim, dtype=torch.float64, device="cuda") for _ in range(2))
+    for b, e in zip(at[:-1], at[1:]):
+        dist = (torch.arange(e - b, device="cuda")[:, None] - torch.arange(e - b, device="cuda")[None]).abs().double()
+        for i in range(heads):
+            c = i // (heads // kv)
+            Q, K, V, G = (t.double() for t in (q[b:e, i], k[b:e, c], v[b:e, c], do[b:e, i]))
+            t, err = scale * Q @ K.T, (dim + 8) * f * scale * Q.abs() @ K.abs().T
+            th = torch.zeros_like(t)
+            if cap:
+                th = torch.tanh(t / cap)
+                t, err = cap * th, err + 2 * 2.0**-23 * min(cap, 64)
+            t = t - float(slopes[i]) * dist
+            err = (err + 4 * f * t.abs()).amax(1, keepdim=True) + 2.0**-22
+            p = torch.softmax(t, 1)
+            slope = 1 - th**2
+            dp, size = G @ V.T, G.abs() @ V.abs().T
+            d = dp - (p * dp).sum(1, keepdim=True)
+            rounded = u * u * (G.abs() * (p @ V).abs()).sum(1, keepdim=True)
+            db = (dim + 8) * f * 2 * size + (2 * err + 2.0**-14) * (p * d.abs()).sum(1, keepdim=True) + 2 * rounded
+            dt = p * d * slope * scale
+            te = (u + 2 * err + 2.0**-14) * dt.abs() + p * db * slope * scale
+            if cap:
+                te = te + (p * d).abs() * scale * 2 * (2.0**-22 + err / cap)
+            ref.check(dq[b:e, i], ((dt @ K).cpu(), (te @ K.abs() + u * (dt @ K).abs() + 2.0**-25).cpu()), f"dq of head {i}")
+            want_k[b:e, c] += dt.T @ Q
+            bound_k[b:e, c] += te.T @ Q.abs()
+    ref.check(dk, (want_k.cpu(), (bound_k + u * want_k.abs() + 2.0**-25).cpu()), "dk")
