@@ -25,6 +25,12 @@ def _kept(offsets):
     return (offsets,), lambda t: t[0]
 
 
+def _dense(grad):
+    """A gradient as HE.attention_backward takes it, dense and at a multiple of 16 bytes: it may be any part of what the program behind made."""
+    grad = grad.contiguous()
+    return grad.clone() if grad.data_ptr() % 16 else grad
+
+
 class _Norm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, he, x, weight, bias, residual, eps):
@@ -64,7 +70,7 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, do):
         n, join, join_k, scale, cap = ctx.args
         q, k, v, o, lse, slopes, *off = ctx.saved_tensors
-        grads = ctx.he.attention_backward(do.contiguous(), q, k, v, o, lse, join(off[:n]), offsets_k=join_k(off[n:]), scale=scale, cap=cap, slopes=slopes)
+        grads = ctx.he.attention_backward(_dense(do), q, k, v, o, lse, join(off[:n]), offsets_k=join_k(off[n:]), scale=scale, cap=cap, slopes=slopes)
         return (None, *grads, None, None, None, None, None)
 
 
@@ -95,7 +101,7 @@ class _SelfAttention(torch.autograd.Function):
         h = qkv.shape[1] - 2 * kv
         d = torch.empty_like(qkv)
         cut = lambda t: (t[:, :h], t[:, h:h + kv], t[:, h + kv:])  # noqa: E731
-        ctx.he.attention_backward(do.contiguous(), *cut(qkv), o, lse, join(off), cap=cap, slopes=slopes, out=cut(d), fill=True)
+        ctx.he.attention_backward(_dense(do), *cut(qkv), o, lse, join(off), cap=cap, slopes=slopes, out=cut(d), fill=True)
         return None, d, None, None, None, None
 
 

@@ -224,3 +224,17 @@ def test_biased_gradients_do_not_depend_on_how_o_was_rounded(he, cap, lengths, h
             want_k[b:e, c] += dt.T @ Q
             bound_k[b:e, c] += te.T @ Q.abs()
     ref.check(dk, (want_k.cpu(), (bound_k + u * want_k.abs() + 2.0**-25).cpu()), "dk")
+
+
+def test_gradients_that_begin_between_two_vectors(he):
+    """The gradient that reaches the operator is what the program behind it makes: here a part of a longer buffer, at no multiple of 16 bytes."""
+    from paper_2210_02574_amd.embedding import _SelfAttention, attention
+
+    off = i32(0, 9, 20)
+    for dtype in (BF16, F32):
+        x = rand(1, 20, 6, 32, dtype=dtype).requires_grad_(True)
+        one, g = rand(2, 1, dtype=dtype), rand(3, 1 + 20 * 2 * 32, dtype=dtype)
+        for f in (lambda: attention(he, x[:, :2], x[:, 2:4], x[:, 4:], off), lambda: _SelfAttention.apply(he, x, 2, off, 0.0, None)):
+            got, = torch.autograd.grad(torch.cat([one, f().flatten()]), x, g)
+            want, = torch.autograd.grad(f().flatten(), x, g[1:].clone())
+            assert torch.equal(got, want)
