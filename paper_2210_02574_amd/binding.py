@@ -743,7 +743,8 @@ class HE:
     # ---- device: from token states to embeddings ------------------------------------------------------------------
     # Floating-point rows on this context's device.  Sequences: an int32 tensor [count + 1] of offsets (sequence i is the rows
     # offsets[i] .. offsets[i + 1]), or a pair (begin, end) of int32 tensors [count] where rows between them belong to none (a
-    # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.
+    # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.  Autograd and forward-mode
+    # differentiation have no part in these calls: results have neither history nor tangents, and an `out` must not require gradients.
     # Tensors are checked and made in he_tensors (csrc/tensors.cpp): calls on short sentences last as long as the host needs for them.
     def _on_tensors(self, name: str, where: str, *args):
         if self._tensors is None:
@@ -755,7 +756,8 @@ class HE:
 
     def layer_norm(self, x, weight, bias, residual=None, eps: float = 1e-5, out=None):
         """(x - mean) rstd weight + bias over the last dimension of x [rows][width], of s = x + residual with one (rounded to the type).
-        Returns (y, s, mean, rstd); s is x itself without a residual.  Keep s, mean and rstd for layer_norm_backward."""
+        Returns (y, s, mean, rstd); s is x itself without a residual.  Keep s, mean and rstd for layer_norm_backward.
+        Results have no history, whatever the inputs have: embedding.layer_norm is the differentiable form."""
         return self._on_tensors("layer_norm", "he_layer_norm", x, weight, bias, residual, eps, out)
 
     def layer_norm_backward(self, dy, s, weight, mean, rstd, ds=None):
@@ -764,7 +766,8 @@ class HE:
         return self._on_tensors("layer_norm_backward", "he_layer_norm_grad", dy, s, weight, mean, rstd, ds)
 
     def pool_mean(self, x, offsets, out=None):
-        """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence."""
+        """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence.
+        No history, whatever x has: embedding.pool_mean is the differentiable form."""
         return self._on_tensors("pool_mean", "he_pool", x, offsets, out)
 
     def pool_mean_backward(self, de, offsets, rows: int, dtype, out=None):
@@ -775,7 +778,8 @@ class HE:
         """Attention inside each sequence: q [rows][heads][dim], k and v [rows_k][kv_heads][dim] (strided views of a joint projection are fine;
         query head h reads key head h // (heads / kv_heads)).  offsets_k: the sequences of the keys, where they are not the queries'.
         scale: of the products, 1 / sqrt(dim) by default; cap > 0: cap tanh(score / cap); slopes [heads] float32: minus slope times distance.
-        Returns (o, lse): o like q, lse [heads][rows] float32."""
+        Returns (o, lse): o like q, lse [heads][rows] float32.
+        No history, whatever the inputs have: embedding.attention is the differentiable form."""
         return self._on_tensors("attention", "he_attention", q, k, v, offsets, offsets_k, scale, cap, slopes, out)
 
     def attention_backward(self, do, q, k, v, o, lse, offsets, offsets_k=None, scale=None, cap: float = 0.0, slopes=None, out=None,

@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <cmath>
 #include <limits>
 
@@ -128,6 +129,19 @@ he_spans spans_of(const Args &a, PyObject *o, int64_t rows, const char *what)
     return {p, p + 1, (int32_t)n, rows};
 }
 
+// A buffer of the caller's to write to: autograd has no part in that, so one that it tracks is refused where it is switched on, ..
+const Tensor &out_of(PyObject *o, const char *what)
+{
+    const Tensor &t = tensor(o, what);
+    if (t.requires_grad() && c10::GradMode::is_enabled()) refuse(what, ": buffers to write to must not require gradients");
+    return t;
+}
+// .. and one that it may have saved gets another version, so that it notices.
+void written(const Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 Tensor dense(at::IntArrayRef shape, const Tensor &like, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
 // A workspace of this call's own, from torch's allocator: calls on other streams and captured graphs have theirs.
 Tensor scratch(const Tensor &like, size_t bytes) { return bytes ? dense({(int64_t)(bytes + 3) / 4}, like, at::kFloat) : Tensor(); }
@@ -172,11 +186,12 @@ PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             y = dense(x.sizes(), x, type);
             yr = {y.data_ptr(), width};
         } else
-            yr = rows_of(a, tensor(a.at[5], "out"), "out", x.sizes(), type);
+            yr = rows_of(a, out_of(a.at[5], "out"), "out", x.sizes(), type);
         Tensor mean = dense({rows}, x, at::kFloat), rstd = dense({rows}, x, at::kFloat);
         const int32_t rc = he_layer_norm(a.ctx, &n, &xr, residual ? &rr : nullptr, wp, bp, &yr, residual ? &sr : nullptr, (float *)mean.data_ptr(),
                                          (float *)rstd.data_ptr(), a.stream);
         if (rc != HE_OK) return status(rc);
+        if (!y.defined()) written(tensor(a.at[5], "out"));
         return pack(y.defined() ? wrap(y) : same(a.at[5]), residual ? wrap(s) : same(a.at[0]), wrap(mean), wrap(rstd));
     });
 }
@@ -225,7 +240,7 @@ PyObject *pool_mean(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         if (none(a.at[2]))
             e = dense({sp.count, width}, x, at::kFloat);
         else {
-            e = tensor(a.at[2], "out");
+            e = out_of(a.at[2], "out");
             if (e.dim() != 2 || e.size(0) != sp.count || e.size(1) != width || !e.is_contiguous())
                 refuse("out: ", e.sizes(), ", want a dense [", sp.count, "][", width, "]");
             placed(a, e, "out", at::kFloat);
@@ -239,7 +254,9 @@ PyObject *pool_mean(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             rc = he_pool(a.ctx, type, &sp, (int32_t)width, &xr, (float *)e.data_ptr(), address(ws), need, a.stream);
         }
         if (rc != HE_OK) return status(rc);
-        return none(a.at[2]) ? wrap(e) : same(a.at[2]);
+        if (none(a.at[2])) return wrap(e);
+        written(e);
+        return same(a.at[2]);
     });
 }
 
@@ -268,10 +285,12 @@ PyObject *pool_mean_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
             if (!sp.count) dx.zero_(); // the library writes nothing without sequences
             xr = {dx.data_ptr(), width};
         } else
-            xr = rows_of(a, tensor(a.at[4], "out"), "out", shape, dtype);
+            xr = rows_of(a, out_of(a.at[4], "out"), "out", shape, dtype);
         const int32_t rc = he_pool_grad(a.ctx, type, &sp, (int32_t)width, (const float *)de.data_ptr(), &xr, fill, a.stream);
         if (rc != HE_OK) return status(rc);
-        return fill ? wrap(dx) : same(a.at[4]);
+        if (fill) return wrap(dx);
+        written(tensor(a.at[4], "out"));
+        return same(a.at[4]);
     });
 }
 
@@ -324,7 +343,7 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             o = dense(q.sizes(), q, t.type);
             oh = dense_heads(o);
         } else
-            oh = heads_of(a, tensor(a.at[8], "out"), "out", q.sizes(), t.type);
+            oh = heads_of(a, out_of(a.at[8], "out"), "out", q.sizes(), t.type);
         if (!made || !t.s.q.count) lse.fill_(-std::numeric_limits<float>::infinity()); // rows that the library leaves as they are
         if (made && !t.s.q.count) o.zero_();
         // most calls take no workspace, and one that does says so before it enqueues anything
@@ -336,6 +355,7 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             rc = he_attention(a.ctx, &t.s, &t.q, &t.k, &t.v, &oh, (float *)lse.data_ptr(), address(ws), need, a.stream);
         }
         if (rc != HE_OK) return status(rc);
+        if (!made) written(tensor(a.at[8], "out"));
         return pack(made ? wrap(o) : same(a.at[8]), wrap(lse));
     });
 }
@@ -361,7 +381,7 @@ PyObject *attention_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
         if (!made && (!PyTuple_Check(a.at[11]) || PyTuple_GET_SIZE(a.at[11]) != 3)) refuse("out: want dq, dk and dv");
         for (int i = 0; i < 3; i++) {
             const Tensor &like = i ? k : q;
-            d[i] = made ? dense(like.sizes(), like, t.type) : tensor(PyTuple_GET_ITEM(a.at[11], i), names[i]);
+            d[i] = made ? dense(like.sizes(), like, t.type) : out_of(PyTuple_GET_ITEM(a.at[11], i), names[i]);
             g[i] = made ? dense_heads(d[i]) : heads_of(a, d[i], names[i], like.sizes(), t.type);
         }
         if (fill && !t.s.q.count) // the library writes nothing without sequences
@@ -372,6 +392,8 @@ PyObject *attention_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
         const int32_t rc = he_attention_grad(a.ctx, &t.s, &gh, &t.q, &t.k, &t.v, &oh, (const float *)lse.data_ptr(), &g[0], &g[1], &g[2], address(ws), need,
                                              a.stream);
         if (rc != HE_OK) return status(rc);
+        if (!made)
+            for (const Tensor &x : d) written(x);
         return made ? pack(wrap(d[0]), wrap(d[1]), wrap(d[2])) : same(a.at[11]);
     });
 }

@@ -238,3 +238,38 @@ def test_gradients_that_begin_between_two_vectors(he):
             got, = torch.autograd.grad(torch.cat([one, f().flatten()]), x, g)
             want, = torch.autograd.grad(f().flatten(), x, g[1:].clone())
             assert torch.equal(got, want)
+
+
+def _written(he):
+    """Every call that takes buffers to write to: (the call, what its buffers are like)."""
+    off, x, w = i32(0, 3, 8), rand(1, 8, 2, 32), rand(2, 64)
+    o, lse = he.attention(x, x, x, off)
+    rows = x.view(8, 64)
+    return [(lambda out: he.layer_norm(rows, w, w, out=out[0]), [rows]), (lambda out: he.pool_mean(rows, off, out=out[0]), [rows[:2]]),
+            (lambda out: he.pool_mean_backward(rows[:2], off, 8, F32, out=out[0]), [rows]), (lambda out: he.attention(x, x, x, off, out=out[0]), [x]),
+            (lambda out: he.attention_backward(x, x, x, x, o, lse, off, out=out), [x, x, x])]
+
+
+@pytest.mark.parametrize("call", range(5))
+def test_autograd_notices_buffers_that_are_written(he, call):
+    f, like = _written(he)[call]
+    for i in range(len(like)):
+        out, x = [torch.ones_like(t) for t in like], torch.ones_like(like[i], requires_grad=True)
+        y = (x * out[i]).sum()  # keeps out[i] for its gradient
+        f(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    with torch.inference_mode():
+        f([torch.ones_like(t) for t in like])  # tensors without a version
+
+
+@pytest.mark.parametrize("call", range(5))
+def test_buffers_that_autograd_tracks_are_refused(he, call):
+    f, like = _written(he)[call]
+    for i in range(len(like)):
+        out = [torch.ones_like(t) for t in like]
+        out[i].requires_grad_(True)
+        with pytest.raises(ValueError, match="require gradients"):
+            f(out)
+        with torch.no_grad():
+            f(out)  # as torch's own writing operations have it
