@@ -744,7 +744,8 @@ class HE:
     # Floating-point rows on this context's device.  Sequences: an int32 tensor [count + 1] of offsets (sequence i is the rows
     # offsets[i] .. offsets[i + 1]), or a pair (begin, end) of int32 tensors [count] where rows between them belong to none (a
     # padded batch).  An `out` that is given keeps its rows of no sequence; one that is made here has zeros there.  Autograd and forward-mode
-    # differentiation have no part in these calls: results have neither history nor tangents, and an `out` must not require gradients.
+    # differentiation have no part in these calls: results have neither history nor tangents, and an `out` must not require gradients.  An `out` overlaps no other tensor of its call; the rows of both may
+    # take turns in one buffer.
     # Tensors are checked and made in he_tensors (csrc/tensors.cpp): calls on short sentences last as long as the host needs for them.
     def _on_tensors(self, name: str, where: str, *args):
         if self._tensors is None:

@@ -11,7 +11,9 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <limits>
 
 #include "he.h"
@@ -142,6 +144,53 @@ void written(const Tensor &t)
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
+// What a call reads or writes: n[0] x n[1] pieces of `bytes`, step[0] and step[1] apart.
+struct Part {
+    int64_t at, bytes, n[2], step[2];
+    // the last dimension is one piece; a step that is never taken is 0
+    explicit Part(const Tensor &t) : at((int64_t)t.data_ptr()), bytes(t.element_size()), n{1, 1}, step{0, 0}
+    {
+        const int64_t size = t.element_size(), d = t.dim();
+        bytes = t.numel() ? t.size(d - 1) * size : 0;
+        for (int64_t i = 0; i + 1 < d; i++)
+            if (t.size(i) > 1 && t.stride(i)) n[i] = t.size(i), step[i] = t.stride(i) * size;
+    }
+    int64_t end() const { return at + (n[0] - 1) * step[0] + (n[1] - 1) * step[1] + bytes; }
+};
+// Whether two of them share an address.  Rows of the same step, as the parts of one buffer have, are looked at head by head; rows of different steps
+// in one place are taken to overlap.
+bool overlap(const Part &a, const Part &b)
+{
+    if (!a.bytes || !b.bytes || a.end() <= b.at || b.end() <= a.at) return false;
+    const int64_t step = a.step[0] ? a.step[0] : b.step[0], lowest = 1 - b.n[0], highest = a.n[0] - 1; // of the row of a minus the row of b
+    if (a.step[0] && b.step[0] && a.step[0] != b.step[0]) return true;
+    const auto near = [&](int64_t d) { // a row d bytes from its place in b's rows: d + i step in (-a.bytes, b.bytes) for some i
+        if (!step) return d > -a.bytes && d < b.bytes;
+        const int64_t low = -a.bytes + 1 - d, i = std::max(low >= 0 ? (low + step - 1) / step : -(-low / step), lowest);
+        return i <= highest && d + i * step < b.bytes;
+    };
+    const int64_t d = a.at - b.at;
+    if (a.step[1] == b.step[1] || !a.step[1] || !b.step[1]) { // heads of one step: by their differences
+        const int64_t head = a.step[1] ? a.step[1] : b.step[1];
+        for (int64_t j = 1 - b.n[1]; j < a.n[1]; j++)
+            if (near(d + j * head)) return true;
+        return false;
+    }
+    for (int64_t i = 0; i < a.n[1]; i++)
+        for (int64_t j = 0; j < b.n[1]; j++)
+            if (near(d + i * a.step[1] - j * b.step[1])) return true;
+    return false;
+}
+// A buffer of the caller's and what the same call reads, or writes as well.  (One that repeats itself is for the library to refuse.)
+void apart(const Tensor &out, const char *what, std::initializer_list<PyObject *> others)
+{
+    for (int64_t i = 0; i < out.dim(); i++)
+        if (out.size(i) > 1 && !out.stride(i)) return;
+    const Part p(out);
+    for (PyObject *o : others)
+        if (!none(o) && overlap(p, Part(THPVariable_Unpack(o)))) refuse(what, ": the buffer overlaps another tensor of the call");
+}
+
 Tensor dense(at::IntArrayRef shape, const Tensor &like, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
 // A workspace of this call's own, from torch's allocator: calls on other streams and captured graphs have theirs.
 Tensor scratch(const Tensor &like, size_t bytes) { return bytes ? dense({(int64_t)(bytes + 3) / 4}, like, at::kFloat) : Tensor(); }
@@ -185,8 +234,11 @@ PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         if (none(a.at[5])) {
             y = dense(x.sizes(), x, type);
             yr = {y.data_ptr(), width};
-        } else
-            yr = rows_of(a, out_of(a.at[5], "out"), "out", x.sizes(), type);
+        } else {
+            const Tensor &out = out_of(a.at[5], "out");
+            yr = rows_of(a, out, "out", x.sizes(), type);
+            apart(out, "out", {a.at[0], a.at[1], a.at[2], a.at[3]});
+        }
         Tensor mean = dense({rows}, x, at::kFloat), rstd = dense({rows}, x, at::kFloat);
         const int32_t rc = he_layer_norm(a.ctx, &n, &xr, residual ? &rr : nullptr, wp, bp, &yr, residual ? &sr : nullptr, (float *)mean.data_ptr(),
                                          (float *)rstd.data_ptr(), a.stream);
@@ -244,6 +296,7 @@ PyObject *pool_mean(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             if (e.dim() != 2 || e.size(0) != sp.count || e.size(1) != width || !e.is_contiguous())
                 refuse("out: ", e.sizes(), ", want a dense [", sp.count, "][", width, "]");
             placed(a, e, "out", at::kFloat);
+            apart(e, "out", {a.at[0]});
         }
         // most calls take no workspace, and one that does says so before it enqueues anything
         int32_t rc = he_pool(a.ctx, type, &sp, (int32_t)width, &xr, (float *)e.data_ptr(), nullptr, 0, a.stream);
@@ -284,8 +337,11 @@ PyObject *pool_mean_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
             dx = dense(shape, de, dtype);
             if (!sp.count) dx.zero_(); // the library writes nothing without sequences
             xr = {dx.data_ptr(), width};
-        } else
-            xr = rows_of(a, out_of(a.at[4], "out"), "out", shape, dtype);
+        } else {
+            const Tensor &out = out_of(a.at[4], "out");
+            xr = rows_of(a, out, "out", shape, dtype);
+            apart(out, "out", {a.at[0]});
+        }
         const int32_t rc = he_pool_grad(a.ctx, type, &sp, (int32_t)width, (const float *)de.data_ptr(), &xr, fill, a.stream);
         if (rc != HE_OK) return status(rc);
         if (fill) return wrap(dx);
@@ -342,8 +398,11 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         if (made) {
             o = dense(q.sizes(), q, t.type);
             oh = dense_heads(o);
-        } else
-            oh = heads_of(a, out_of(a.at[8], "out"), "out", q.sizes(), t.type);
+        } else {
+            const Tensor &out = out_of(a.at[8], "out");
+            oh = heads_of(a, out, "out", q.sizes(), t.type);
+            apart(out, "out", {a.at[0], a.at[1], a.at[2], a.at[7]});
+        }
         if (!made || !t.s.q.count) lse.fill_(-std::numeric_limits<float>::infinity()); // rows that the library leaves as they are
         if (made && !t.s.q.count) o.zero_();
         // most calls take no workspace, and one that does says so before it enqueues anything
@@ -384,6 +443,11 @@ PyObject *attention_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
             d[i] = made ? dense(like.sizes(), like, t.type) : out_of(PyTuple_GET_ITEM(a.at[11], i), names[i]);
             g[i] = made ? dense_heads(d[i]) : heads_of(a, d[i], names[i], like.sizes(), t.type);
         }
+        if (!made)
+            for (int i = 0; i < 3; i++) {
+                apart(d[i], names[i], {a.at[0], a.at[1], a.at[2], a.at[3], a.at[4], a.at[5], a.at[10]});
+                for (int j = 0; j < i; j++) apart(d[i], names[i], {PyTuple_GET_ITEM(a.at[11], j)});
+            }
         if (fill && !t.s.q.count) // the library writes nothing without sequences
             for (Tensor &x : d) x.zero_();
         size_t need = 0;

@@ -273,3 +273,46 @@ def test_buffers_that_autograd_tracks_are_refused(he, call):
             f(out)
         with torch.no_grad():
             f(out)  # as torch's own writing operations have it
+
+
+def test_buffers_that_overlap_are_refused(he):
+    off, buf = i32(0, 3, 8), rand(1, 4096)
+    rows, w = buf[:512].view(8, 64), rand(2, 64)
+    x = buf[:512].view(8, 2, 32)
+    o, lse = he.attention(x, x, x, off)
+    joint = rand(3, 8, 6, 32)
+    cut = lambda *at: [joint[:, a:a + 2] for a in at]  # noqa: E731
+    for f in (lambda: he.layer_norm(rows, w, w, out=rows), lambda: he.layer_norm(rows, w, w, out=buf[32:544].view(8, 64)),
+              lambda: he.layer_norm(rows[:, :32], w[:32], w[:32], residual=rows[:, 32:], out=buf[16:528].view(8, 64)[:, :32]),
+              lambda: he.layer_norm(rows, buf[1024:1088], w, out=buf[1000:1512].view(8, 64)), lambda: he.pool_mean(rows, off, out=buf[64:192].view(2, 64)),
+              lambda: he.pool_mean_backward(buf[:128].view(2, 64), off, 8, F32, out=rows), lambda: he.attention(x, x, x, off, out=x),
+              lambda: he.attention(x, x, x, off, out=buf[256:768].view(2, 8, 32).transpose(0, 1)), lambda: he.attention(x, joint[:, :2], joint[:, 2:4], off, out=joint[:, 1:3]),
+              lambda: he.attention_backward(x, x, x, x, o, lse, off, out=cut(0, 1, 4)), lambda: he.attention_backward(x, x, x, x, o, lse, off, out=cut(0, 2, 3)),
+              lambda: he.attention_backward(x, *cut(0, 2, 4), o, lse, off, out=[torch.ones_like(x), *cut(0, 2)]),
+              lambda: he.attention_backward(x, x, x, x, o, lse, off, out=[torch.ones_like(x), o, torch.ones_like(x)]),
+              lambda: he.attention_backward(x, x, x, x, o, lse, off, out=[torch.ones_like(x)] + [torch.ones_like(x)] * 2)):
+        with pytest.raises(ValueError, match="overlap"):
+            f()
+
+
+def test_buffers_beside_one_another_are_taken(he):
+    """Rows and heads that take turns in one buffer, and parts of one: none of them overlaps."""
+    off, w, r = i32(0, 3, 8), rand(2, 64), rand(4, 8, 64)
+    want = he.layer_norm(r, w, w)[0]
+    both = torch.cat([r, torch.zeros_like(r)], 1)
+    assert torch.equal(he.layer_norm(both[:, :64], w, w, out=both[:, 64:])[0], want) and torch.equal(both[:, :64], r)
+    one = torch.cat([r, r, torch.zeros_like(r)])
+    assert torch.equal(he.layer_norm(one[:8], w, w, residual=one[8:16], out=one[16:])[0], he.layer_norm(r, w, w, residual=r)[0])
+    assert torch.equal(he.layer_norm(both[:1, :64], w, w, out=both[1:2, :64])[0], want[:1])  # rows of one, whose strides nothing asks for
+    q, k, v = (rand(i, 8, 2, 32) for i in (5, 6, 7))
+    o, lse = he.attention(q, k, v, off)
+    joint = torch.cat([q, k, v, torch.zeros_like(q)], 1)
+    assert torch.equal(he.attention(joint[:, :2], joint[:, 2:4], joint[:, 4:6], off, out=joint[:, 6:])[0], o) and torch.equal(joint[:, :2], q)
+    heads = torch.stack([q, k, v, torch.zeros_like(q)]).transpose(1, 2).contiguous().transpose(1, 2)  # one head after the other
+    assert torch.equal(he.attention(*heads[:3], off, out=heads[3])[0], o)
+    mixed = torch.stack([q, k, v, torch.zeros_like(q)], 2)  # [rows][heads][4][dim]
+    assert torch.equal(he.attention(*(mixed[:, :, i] for i in range(3)), off, out=mixed[:, :, 3])[0], o) and torch.equal(mixed[:, :, 0], q)
+    grads = he.attention_backward(q, q, k, v, o, lse, off)
+    d = torch.empty(8, 6, 32, device="cuda")
+    he.attention_backward(q, q, k, v, o, lse, off, out=[d[:, i:i + 2] for i in (0, 2, 4)])
+    assert all(torch.equal(d[:, 2 * i:2 * i + 2], g) for i, g in enumerate(grads))
