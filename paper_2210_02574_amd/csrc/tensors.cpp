@@ -98,14 +98,14 @@ void *vector_of(const Args &a, const Tensor &t, const char *what, int64_t n, at:
     placed(a, t, what, type);
     return t.data_ptr();
 }
-// [rows][heads][dim] with a dense last dimension, at multiples of 16 bytes
+// [rows][heads][dim] with a dense last dimension, at multiples of 16 bytes; the stride of one row or one head, which may be any number, is none
 he_heads heads_of(const Args &a, const Tensor &t, const char *what, at::IntArrayRef shape, at::ScalarType type)
 {
     if (shape.size() != 3 || t.sizes() != shape) refuse(what, ": ", t.sizes(), ", want [rows][heads][dim]", shape.size() == 3 ? c10::str(" = ", shape) : "");
     placed(a, t, what, type);
     if (t.stride(2) != 1 && shape[2] > 1) refuse(what, ": the last dimension is not dense");
     void *const p = t.data_ptr();
-    const int64_t row = t.stride(0), head = t.stride(1);
+    const int64_t row = shape[0] > 1 ? t.stride(0) : 0, head = shape[1] > 1 ? t.stride(1) : 0;
     if ((((int64_t)p | (row | head) * (int64_t)t.element_size()) & 15) && t.numel())
         refuse(what, ": address ", p, " or strides ", t.strides(), " not in multiples of 16 bytes");
     return {p, row, head};

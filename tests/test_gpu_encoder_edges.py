@@ -316,3 +316,20 @@ def test_buffers_beside_one_another_are_taken(he):
     d = torch.empty(8, 6, 32, device="cuda")
     he.attention_backward(q, q, k, v, o, lse, off, out=[d[:, i:i + 2] for i in (0, 2, 4)])
     assert all(torch.equal(d[:, 2 * i:2 * i + 2], g) for i, g in enumerate(grads))
+
+
+def test_attention_of_one_row_or_one_head_whose_stride_nothing_takes(he):
+    """The stride of a dimension of one element is no address: it may be any number."""
+    k, v, off = rand(2, 7, 2, 32, dtype=BF16), rand(3, 7, 2, 32, dtype=BF16), (i32(0, 1), i32(0, 7))
+    q = rand(1, 1, 2, 32, dtype=BF16)
+    o, lse = he.attention(q, k, v, off[0], offsets_k=off[1])
+    grads = he.attention_backward(q, q, k, v, o, lse, off[0], offsets_k=off[1])
+    odd = torch.as_strided(q, (1, 2, 32), (101, 32, 1))
+    far = torch.as_strided(q, (1, 2, 32), (1 << 24, 32, 1))
+    for one in (odd, far):
+        out = torch.as_strided(torch.empty_like(q), one.shape, one.stride())
+        assert torch.equal(he.attention(one, k, v, off[0], offsets_k=off[1], out=out)[0], o) and torch.equal(he.attention(one, k, v, off[0], offsets_k=off[1])[0], o)
+        assert all(torch.equal(a, b) for a, b in zip(he.attention_backward(one, one, k, v, o, lse, off[0], offsets_k=off[1]), grads))
+    lone = torch.as_strided(k[:, :1].contiguous(), (7, 1, 32), (32, 5, 1))
+    want = he.attention(q[:, :1], k[:, :1], k[:, :1], off[0], offsets_k=off[1])[0]
+    assert torch.equal(he.attention(q[:, :1], lone, lone, off[0], offsets_k=off[1])[0], want)
