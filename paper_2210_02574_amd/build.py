@@ -74,6 +74,14 @@ def _inputs():
     return sorted(glob.glob(os.path.join(CSRC, "*")) + glob.glob(os.path.join(ROOT, "include", "*.h")))
 
 
+def _binds_to() -> str:
+    """What the extension module's binary interface hangs on besides its sources: torch's version and Python's."""
+    import importlib.metadata
+    import sysconfig
+
+    return f"torch {importlib.metadata.version('torch')} python {sysconfig.get_config_var('SOABI')}"
+
+
 def source_hash() -> str:
     h = hashlib.sha256()
     for f in _inputs():
@@ -83,6 +91,7 @@ def source_hash() -> str:
     h.update(" ".join(CODEGEN_FLAGS).encode())
     h.update(repr(SOURCES).encode())
     h.update(" ".join(TENSORS_FLAGS).encode())
+    h.update(_binds_to().encode())
     return h.hexdigest()
 
 
@@ -122,7 +131,7 @@ def build(verbose: bool = False, jobs: int | None = None, only=None) -> str:
 
 
 def is_stale() -> bool:
-    """True when no library is built or its sources have changed since (by content, not by time stamp)."""
+    """True when no library is built, or its sources (by content, not by time stamp), torch or Python have changed since."""
     if not all(os.path.exists(f) for f in (LIB, TENSORS, STAMP)):
         return True
     with open(STAMP) as fh:

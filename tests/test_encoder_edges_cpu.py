@@ -1,5 +1,7 @@
 """Token states to embeddings and ciphertexts without a GPU: calls at the edge of what is documented."""
 import ctypes
+import importlib
+import importlib.metadata
 import importlib.util
 import itertools
 import re
@@ -13,7 +15,7 @@ import torch
 
 import paper_2210_02574_amd as pkg
 import workloads as wl
-from paper_2210_02574_amd import binding
+from paper_2210_02574_amd import binding, build
 from paper_2210_02574_amd.classifier import EncryptedInference
 
 
@@ -77,3 +79,13 @@ def test_scales_and_caps_are_taken_up_to_2_to_the_127(he):
     assert call(0.125, 2.0**127) == 0 and call(2.0**127, 0.0) == 0
     for bad in ((0.125, 2.0**127 * 1.01), (2.0**127 * 1.01, 0.0), (0.125, 3.4e38), (3.4e38, 0.0)):
         assert call(*bad) == -1, bad
+
+
+@pytest.mark.parametrize("where,name,other", [("importlib.metadata", "version", "0.0"), ("sysconfig", "get_config_var", "cpython-0")])
+def test_a_library_built_for_another_torch_or_python_is_stale(monkeypatch, where, name, other):
+    """The extension module holds their binary interfaces: loading it into another one would be undefined."""
+    module = importlib.import_module(where)
+    before, plain = build.source_hash(), getattr(module, name)
+    assert not build.is_stale()
+    monkeypatch.setattr(module, name, lambda key: other if key in ("torch", "SOABI") else plain(key))
+    assert build.source_hash() != before and build.is_stale()
