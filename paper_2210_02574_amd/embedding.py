@@ -131,7 +131,7 @@ class SentenceEncoder:
     layers: per layer a dict of weights: qkv [(heads + 2 kv_heads) dim][width] and qkv_bias, out [width][heads dim] and out_bias, up and up_bias,
     down and down_bias (the products of the feed-forward part, with a Gaussian error unit between), norm1, norm1_bias, norm2, norm2_bias.
     pool: "mean" of a sentence's rows, or its "first" row; the last layer then computes that row of each sentence alone.
-    cap, slopes: as HE.attention takes them, the same in every layer."""
+    cap, slopes: as HE.attention takes them, the same in every layer; no slopes with pool "first"."""
 
     NAMES = ("qkv", "qkv_bias", "out", "out_bias", "up", "up_bias", "down", "down_bias", "norm1", "norm1_bias", "norm2", "norm2_bias")
 
@@ -141,6 +141,8 @@ class SentenceEncoder:
             raise ValueError(f"pool: {pool!r}, want 'mean' or 'first'")
         if slopes is not None and slopes.requires_grad:
             raise ValueError("slopes are constants: they have no gradient")
+        if slopes is not None and pool == "first":
+            raise ValueError("pool='first' with a distance bias: a lone query stands at its sentence's last position, not its first")
         for i, w in enumerate(layers):
             missing = [n for n in self.NAMES if n not in w]
             if missing:
@@ -192,8 +194,6 @@ class SentenceEncoder:
     def _last_first(self, w, x, offsets, dim):
         """The last layer on the first row of each sentence: one query to a sentence's keys."""
         begin, some = self._first(x, offsets)
-        if self.slopes is not None:
-            raise ValueError("pool='first' with a distance bias: a lone query stands at its sentence's last position, not its first")
         rows, cut = x[begin], self.heads * dim
         q = F.linear(rows, w["qkv"][:cut], w["qkv_bias"][:cut]).unflatten(1, (self.heads, dim))
         kvs = F.linear(x, w["qkv"][cut:], w["qkv_bias"][cut:]).unflatten(1, (2 * self.kv_heads, dim))

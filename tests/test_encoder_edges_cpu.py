@@ -17,6 +17,7 @@ import paper_2210_02574_amd as pkg
 import workloads as wl
 from paper_2210_02574_amd import binding, build
 from paper_2210_02574_amd.classifier import EncryptedInference
+from paper_2210_02574_amd.embedding import SentenceEncoder
 
 
 @pytest.fixture(scope="module")
@@ -89,3 +90,12 @@ def test_a_library_built_for_another_torch_or_python_is_stale(monkeypatch, where
     assert not build.is_stale()
     monkeypatch.setattr(module, name, lambda key: other if key in ("torch", "SOABI") else plain(key))
     assert build.source_hash() != before and build.is_stale()
+
+
+def test_a_distance_bias_with_first_rows_is_refused_before_any_layer_runs(he):
+    w = SentenceEncoder.random_layer(16, 2, 24, 1, torch.float32, "cpu")
+    for layers in ([w], [w, w]):
+        with pytest.raises(ValueError, match="distance bias"):
+            SentenceEncoder(he, layers, 2, pool="first", slopes=torch.ones(2))
+    SentenceEncoder(he, [w], 2, pool="mean", slopes=torch.ones(2))
+    SentenceEncoder(he, [w], 2, pool="first")
