@@ -333,3 +333,80 @@ def test_attention_of_one_row_or_one_head_whose_stride_nothing_takes(he):
     lone = torch.as_strided(k[:, :1].contiguous(), (7, 1, 32), (32, 5, 1))
     want = he.attention(q[:, :1], k[:, :1], k[:, :1], off[0], offsets_k=off[1])[0]
     assert torch.equal(he.attention(q[:, :1], lone, lone, off[0], offsets_k=off[1])[0], want)
+
+
+def _fp16_inputs(seed, rows=223):
+    return [rand(seed + i, rows, 2, 64, dtype=F16) for i in range(4)]
+
+
+def test_fp16_gradients_keep_sequences_and_padding_apart(he):
+    """The powers of two that lift ds come from the rows of a sequence alone: neither its neighbours' NaN and infinities nor those of rows of no
+    sequence change a bit of it."""
+    begin, end = i32(3, 53, 90, 103, 153), i32(40, 53, 100, 150, 154)
+    keep = torch.zeros(223, dtype=torch.bool, device="cuda")
+    for b, e in zip(begin.tolist(), end.tolist()):
+        keep[b:e] = True
+    q, k, v, do = _fp16_inputs(1)
+    for sl in (None, torch.tensor([0.5, 0.01], device="cuda")):
+        want = ref.attention(q, k, v, (begin, end), do=do, slopes=sl)
+        o, lse = he.attention(q, k, v, (begin, end), slopes=sl)
+        clean = he.attention_backward(do, q, k, v, o, lse, (begin, end), slopes=sl)
+        for name, g in zip(("dq", "dk", "dv"), clean):
+            ref.check(g, want[name], name)
+        bad = [t.clone() for t in (q, k, v, do)]
+        for t, x in zip(bad, ("nan", "inf", "nan", "-inf")):
+            t[~keep] = float(x)
+            t[95] = float(x)  # the third sequence
+        o2, lse2 = he.attention(*bad[:3], (begin, end), slopes=sl)
+        mine = keep.clone()
+        mine[90:100] = False
+        for g, c in zip(he.attention_backward(bad[3], *bad[:3], o2, lse2, (begin, end), slopes=sl), clean):
+            assert torch.equal(g[mine], c[mine]) and not g[~keep].any()
+
+
+def test_fp16_gradients_in_a_captured_graph(he):
+    """The powers of two are found again in every replay."""
+    off, sl = offsets_of([1, 60, 0, 162]), torch.tensor([0.5, 0.01], device="cuda")
+
+    def run(q, k, v, do):
+        o, lse = he.attention(q, k, v, off, slopes=sl)
+        return (o, lse, *he.attention_backward(do, q, k, v, o, lse, off, slopes=sl), *he.attention_backward(do, q, k, v, *he.attention(q, k, v, off), off))
+
+    ins, side, graph = _fp16_inputs(1), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run(*ins)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        outs = run(*ins)
+    for rep, size in enumerate((1.0, 2.0**-10, 2.0**9, 1.0)):
+        for t, new in zip(ins, _fp16_inputs(10 * rep)):
+            t.copy_(new)
+        ins[3].mul_(size)
+        want = [t.clone() for t in run(*ins)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
+
+
+def test_fp16_gradients_of_offsets_that_break_the_rule_stay_in_the_buffers(he):
+    q = rand(1, 64, 2, 32, dtype=F16)
+    sl = torch.tensor([0.5, 0.01], device="cuda")
+    for off in (i32(0, 500, 64), i32(-9, 30, 64), i32(0, 40, 10, 64), (i32(10, 0), i32(5, 100))):
+        o, lse = he.attention(q, q, q, off)
+        he.attention_backward(q, q, q, q, o, lse, off)
+        he.attention_backward(q, q, q, q, o, lse, off, slopes=sl)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("lengths", [[9000], [30, 7000, 2, 900]])
+def test_fp16_gradients_of_sequences_of_many_tiles(he, lengths):
+    """More tiles than a wave has lanes: their sizes take several trips."""
+    rows, off = sum(lengths), offsets_of(lengths)
+    q, k, v, do = _fp16_inputs(5, rows)
+    v[-3:] *= 100  # the largest in the last tile
+    want = ref.attention(q, k, v, off, do=do, device="cuda")
+    o, lse = he.attention(q, k, v, off)
+    for name, g in zip(("dq", "dk", "dv"), he.attention_backward(do, q, k, v, o, lse, off)):
+        ref.check(g, want[name], name)
