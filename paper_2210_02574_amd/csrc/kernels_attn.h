@@ -743,15 +743,15 @@ template <class T, int MODE> struct GradScore {
 
 // fp16 has numbers from 2^-24 to 2^16, and eleven bits of them from 2^-14 on: p of long rows is below that, and ds, which no scaling of a loss keeps in place for
 // every sequence and head, on either side.  So p is lifted by GRAD_LIFT (it is at most 1: eleven bits down to 2^-26), and ds by the power of two that brings
-// its bound to 2^12: |ds_ij| = p |do . (v_j - o)| <= p (1 - p) |do| 2 max|v| <= |do| max|v| / 2, with max|v| over the sequence's keys (k_attn_grad_size).  16 are
-// left for the roundings of p, lse and delta.  dq has the own |do| of each query row in it, dk and dv, whose sums go over queries, the sequence's largest.
+// its bound to 2^15: |ds_ij| = p |do . (v_j - o)| <= p (1 - p) |do| 2 max|v| <= |do| max|v| / 2, with max|v| over the sequence's keys (k_attn_grad_size).  A factor of
+// two is left for the roundings of p, lse and delta.  dq has the own |do| of each query row in it, dk and dv, whose sums go over queries, the sequence's largest.
 #define GRAD_LIFT 12
 template <class T> constexpr bool grad_lifted() { return std::is_same<T, f16>::value; }
 // the power of two for ds; fast: ds lacks a factor of 4
 __device__ __forceinline__ int ds_lift(float go, float v, bool fast)
 {
     const int e = __builtin_amdgcn_frexp_expf(0.5f * go * v); // bound <= 2^e; of 0, infinities and NaN 0
-    return min(max((fast ? 14 : 12) - e, -60), 60);
+    return min(max((fast ? 17 : 15) - e, -60), 60);
 }
 // The largest of a sequence's sizes as k_attn_grad_size left them: of the slots that its rows begin .. end - 1 have tiles in.  The first 64 are asked for at once, for a
 // caller that has other things to ask for before it needs them.

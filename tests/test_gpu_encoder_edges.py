@@ -119,7 +119,7 @@ def test_sums_of_many_small_weights(he, seqs, queries, keys, dtype):
 def _gradients(q, k, v, do, scale):
     """{name: (value, bound)} of dq, dk and dv of one sequence with one head, [rows][dim] each, in 64 bits on the device.  As encoder_reference has them, but
     for what a factor of small size is off by: with G and V the largest norms of a row of do and of v, ds is at most G V / 2, and is lifted by a power of
-    two to between 2^11 and 2^12 of that or less; p is lifted by 2^12.  So half a step of fp16 is 2^-37 G V of a ds and 2^-37 of a p.  A result's own
+    two that brings this to 2^14 or more; p is lifted by 2^12.  So half a step of fp16, 2^-25, is 2^-40 G V of a ds and 2^-37 of a p.  A result's own
     half step is 2^-25."""
     u, f = 2.0**-11, ref.F32
     q, k, v, do = (t.double() for t in (q, k, v, do))
@@ -135,7 +135,7 @@ def _gradients(q, k, v, do, scale):
     db = (do.abs() * ob).sum(1, keepdim=True) + (d + 8) * f * size
     dt = p * (dp - (do * o).sum(1, keepdim=True)) * scale
     most = float(do.norm(dim=1).max() * v.norm(dim=1).max())
-    te = rel * dt.abs() + p * db * scale + 2.0**-37 * most * scale
+    te = rel * dt.abs() + p * db * scale + 2.0**-40 * most * scale
     out = {"dq": (dt @ k, te @ k.abs()), "dk": (dt.T @ q, te.T @ q.abs()), "dv": (p.T @ do, (rel * p + 2.0**-37).T @ do.abs())}
     return {n: (a.cpu(), (b + u * a.abs() + 2.0**-25).cpu()) for n, (a, b) in out.items()}
 
@@ -410,3 +410,9 @@ def test_fp16_gradients_of_sequences_of_many_tiles(he, lengths):
     o, lse = he.attention(q, k, v, off)
     for name, g in zip(("dq", "dk", "dv"), he.attention_backward(do, q, k, v, o, lse, off)):
         ref.check(g, want[name], name)
+
+
+def test_fp16_gradients_of_keys_without_much_weight(he):
+    """Large do and v, and scores that leave some keys with next to nothing: their part of dk is small, and still right to fp16's smallest steps."""
+    q, do = rand(1, 1, 112, scale=8.0), rand(2, 1, 112, scale=64.0)  # one query: no errors that cancel
+    _check_gradients(he, q, rand(3, 500, 112), rand(4, 500, 112, scale=8.0), do, 112**-0.5)
