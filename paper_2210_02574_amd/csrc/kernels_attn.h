@@ -12,9 +12,9 @@
 // slot (l / 32, e) holds row 4 (l / 32) + e for e < 4 and 8 + 4 (l / 32) + e - 4 above.  Nothing moves between lanes on the way.
 // The operand A of that product is a transposed tile: 16-bit types read it from LDS with the transposing read, 32-bit ones word by word.
 //
-// Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-9 or 2^-11 of each term, as the inputs themselves have),
+// Roundings: products take p and dt in the type of the inputs (16 bits: relative 2^-8 or 2^-11 of each term at most, as the inputs themselves have),
 // everything else, sums and statistics included, is in 32 bits.  (dt is rounded before its factor scale.)  Rounding both the terms and the result leaves 1.4
-// times the error of rounding the result alone.  delta takes o as it was rounded: its error has the size of that rounding, |do . o| 2^-9 or 2^-12 and less, and matters where
+// times the error of rounding the result alone.  delta takes o as it was rounded: its error has the size of that rounding, |do . o| 2^-8 or 2^-11 at most, and matters where
 // o is not small beside the values' own spread: under a steep distance bias, which leaves few keys with a weight whatever the data are, dq and dk had 1.55 times the error of
 // rounding the result alone.  With a bias it is therefore mended (k_attn_grad_q, which also says what it is otherwise), and for up to 32 keys of short sequences, which are at hand
 // at once, delta is exact.
@@ -219,7 +219,7 @@ __device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, 
 
 // Scores of 32 x 32 blocks, x = log2(e) s, from products c = q . k.  MODE: MODE_CAP, MODE_SLOPE, both or neither.  16-bit types take tanh(y) =
 // 1 - 2 / (1 + e^2y) by the hardware's exponential and reciprocal: it is off by 2^-22 at most, but absolutely, so that a score is off by that times the
-// cap, however small it is.  Up to caps of 64 that is 2^-16, an eighth of what rounding its weight to fp16 costs (bf16: a 64th).  Above (MODE_EXACT),
+// cap, however small it is.  Up to caps of 64 that is 2^-16, a 32nd of what rounding its weight to fp16 costs (bf16: a 256th).  Above (MODE_EXACT),
 // and in 32 bits, tanh is the library's, which keeps small values: a cap may be far above all scores.  3 sequences of 4000, 16 heads of 64 on 8 in fp16, biased,
 // caps of 64 and 65: 386 us forward and 1035 backward, 469 and 1380; 32 of 300, 12 heads of 64: 32 and 84, 41 and 111.
 enum { MODE_CAP = 1, MODE_SLOPE = 2, MODE_EXACT = 4 };
@@ -227,20 +227,24 @@ enum { MODE_CAP = 1, MODE_SLOPE = 2, MODE_EXACT = 4 };
 template <class T, int MODE> constexpr bool attn_fast_tanh() { return sizeof(T) == 2 && (MODE & MODE_CAP) && !(MODE & MODE_EXACT); }
 template <class T, int MODE> struct Scores {
     float in, out, slope; // of c before tanh, of tanh (or of c), of the distance
+    float unit;           // of c: to score / cap
 
     __device__ __forceinline__ Scores(const AttnArgs &a, int head)
     {
         out = a.scale * LOG2E;
         if (MODE & MODE_CAP) {
             out = a.cap * LOG2E;
-            in = attn_fast_tanh<T, MODE>() ? a.scale / a.cap * (2.f * LOG2E) : a.scale / a.cap;
+            unit = a.scale / a.cap;
+            in = attn_fast_tanh<T, MODE>() ? unit * (2.f * LOG2E) : unit;
         }
         if (MODE & MODE_SLOPE) slope = a.slope[head] * LOG2E;
     }
     // what is left to multiply scores with: without a cap or a bias the exponential's fma does it
     __device__ __forceinline__ float rest() const { return MODE ? 1.f : out; }
     // pos: position of the lane's own row minus the one of row 0 of the block: the distance of row m is |pos - m|
-    __device__ __forceinline__ void operator()(f32x16 &c, float pos, int h) const
+    // lone: they are all that a row has.  lse in 32 bits is as exact as they are then (of two keys under a cap of 50 it was off by 2e-6 of itself; from 32 on errors
+    // of the scores cancel), so tanh is the library's.
+    __device__ __forceinline__ void operator()(f32x16 &c, float pos, int h, bool lone) const
     {
         if constexpr (MODE != 0) {
             const float p = pos - (float)(4 * h);
@@ -248,11 +252,11 @@ template <class T, int MODE> struct Scores {
             for (int r = 0; r < 16; r++) {
                 float x;
                 if constexpr (MODE & MODE_CAP) {
-                    if constexpr (attn_fast_tanh<T, MODE>()) {
+                    if (attn_fast_tanh<T, MODE>() && !lone) {
                         const float g = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c[r] * in));
                         x = fmaf(-2.f * out, g, out);
                     } else {
-                        x = tanhf(c[r] * in);
+                        x = tanhf(c[r] * unit);
                         x *= out;
                     }
                 } else
@@ -404,9 +408,9 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
 #pragma unroll
             for (int b = 0; b < QB; b++) x[b] = AttnType<T>::mma(fk[kk], fq[b][kk], x[b]);
     };
-    const auto finish = [&](f32x16 (&x)[QB], int j) { // of the keys from j on
+    const auto finish = [&](f32x16 (&x)[QB], int j, auto lone) { // of the keys from j on
 #pragma unroll
-        for (int b = 0; b < QB; b++) scores(x[b], (float)(row0 + 32 * b + g.back - (j - g.kb)), h);
+        for (int b = 0; b < QB; b++) scores(x[b], (float)(row0 + 32 * b + g.back - (j - g.kb)), h, lone);
     };
     // The maximum that the sums refer to moves only when it is left 8 behind (attn_lift): most steps skip the rescaling.
     const auto rescale = [&]() {
@@ -455,10 +459,12 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
         __syncthreads();
         read_keys(lds[0][0], 0);
         products(s);
-        finish(s, g.lo);
-        if (blocks > 1)
+        if (blocks > 1) {
+            finish(s, g.lo, std::false_type{});
 #pragma unroll
             for (int b = 0; b < QB; b++) m[b] = col_max(s[b]);
+        } else
+            finish(s, g.lo, std::true_type{});
         int stage = 0, i = 0;
         while (i + 1 < blocks) {
 #pragma unroll
@@ -481,7 +487,7 @@ template <class T, int DP, int QB, int MODE> __global__ __launch_bounds__(ATTN_T
                 weigh(0);
                 exponentials(1);
                 weigh(1);
-                finish(n, g.lo + 32 * (i + 1));
+                finish(n, g.lo + 32 * (i + 1), std::false_type{});
 #pragma unroll
                 for (int b = 0; b < QB; b++) {
                     s[b] = n[b];
@@ -568,7 +574,10 @@ template <class T, int DP, int NWQ, int MODE> __global__ __launch_bounds__(ATTN_
         f32x16 s = {};
 #pragma unroll
         for (int kk = 0; kk < KK; kk++) s = AttnType<T>::mma(L::rows(lk, 32 * wk, kk, lane), fq[kk], s);
-        scores(s, (float)(row + g.back - (j - g.kb)), h);
+        if (g.ke - g.kb <= 32)
+            scores(s, (float)(row + g.back - (j - g.kb)), h, true);
+        else
+            scores(s, (float)(row + g.back - (j - g.kb)), h, false);
         if (g.hi - j < 32) mask_rows(s, g.hi - j, h);
         const float m = col_max(s) * c2;
         if (__any(m > top + 8.f)) { // as in k_attn

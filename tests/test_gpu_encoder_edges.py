@@ -416,3 +416,25 @@ def test_fp16_gradients_of_keys_without_much_weight(he):
     """Large do and v, and scores that leave some keys with next to nothing: their part of dk is small, and still right to fp16's smallest steps."""
     q, do = rand(1, 1, 112, scale=8.0), rand(2, 1, 112, scale=64.0)  # one query: no errors that cancel
     _check_gradients(he, q, rand(3, 500, 112), rand(4, 500, 112, scale=8.0), do, 112**-0.5)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("cap", [8.0, 50.0, 64.0, 1e5])
+@pytest.mark.parametrize("queries", [7, 1400])
+def test_capped_scores_of_few_keys(he, queries, cap, dtype):
+    """lse of up to 32 keys in 32 bits.  Products have one term each, so a score is off by a few roundings (four of 2^-24 are granted, the library's tanh among them), and
+    lse by that, by two steps of a logarithm below 8 (fp16's lift: 2^-20) and by its own rounding."""
+    keys = [1, 2, 3, 17, 32, 33, 40]
+    per = queries // 7
+    q, k = torch.zeros(queries, 16, 32, dtype=dtype, device="cuda"), torch.zeros(sum(keys), 16, 32, dtype=dtype, device="cuda")
+    q[..., 0], k[..., 0] = rand(1, queries, 16, dtype=dtype, scale=2.0), rand(2, sum(keys), 16, dtype=dtype, scale=2.0)
+    lse = he.attention(q, k, k, offsets_of([per] * 7), offsets_k=offsets_of(keys), scale=0.5, cap=cap)[1].double()
+    at = 0
+    for i, n in enumerate(keys):
+        t = 0.5 * q[i * per:(i + 1) * per, :, 0].double()[:, :, None] * k[at:at + n, :, 0].double().t()[None]
+        t, at = cap * torch.tanh(t / cap), at + n
+        want = torch.logsumexp(t, -1)
+        # above 32 keys tanh is off by 2^-22 of the cap where that is at most 64
+        bound = 4 * ref.F32 * t.abs().amax(-1) + 2.0**-20 + ref.F32 * want.abs() + (2.0**-22 * cap if n > 32 and cap <= 64 else 0.0)
+        got = lse[:, i * per:(i + 1) * per].t()
+        assert ((got - want).abs() <= bound).all(), (n, float((got - want).abs().max()))
