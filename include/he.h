@@ -365,7 +365,10 @@ int32_t he_pool(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, con
                 void *stream);
 int32_t he_pool_grad(he_ctx *ctx, int32_t type, const he_spans *s, int32_t width, const float *d_de, const he_rows *dx, int32_t fill, void *stream);
 
-/* Attention of the queries of each sequence over the keys of the same sequence (both directions, no other mask):
+/* Attention of the queries of each sequence over the keys of the same sequence (both directions, no other mask).  16-bit types: weights and the
+ * gradients of scores are rounded to the type as factors of products; tanh under caps up to 64 is off by 2^-22, times the cap in a score, for more
+ * than 32 keys and in the backward pass; without slopes the backward pass takes do . o from o as it was rounded.
+ *
  *   t = scale q . k;  u = cap tanh(t / cap) (cap 0: u = t);  s = u - slope_h |position of q - position of k|
  *   lse = log sum exp(s);  o = sum exp(s - lse) v;  a row whose sequence has no keys: o = 0, lse = -inf
  * Query head h reads key head h / (heads / kv_heads).  The last query stands at the last key's position (where both have the same rows:

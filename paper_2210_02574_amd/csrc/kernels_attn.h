@@ -18,8 +18,8 @@
 // o is not small beside the values' own spread: under a steep distance bias, which leaves few keys with a weight whatever the data are, dq and dk had 1.55 times the error of
 // rounding the result alone.  With a bias it is therefore mended (k_attn_grad_q, which also says what it is otherwise), and for up to 32 keys of short sequences, which are at hand
 // at once, delta is exact.
-// fp16 has the bits for it but not the range: there all factors are
-// lifted by powers of two, weights by constants (attn_lift, GRAD_LIFT), ds by what k_attn_grad_size finds.
+// fp16 has the bits for all of this but not the range: there factors are lifted by powers of two, weights by constants (attn_lift, GRAD_LIFT), ds by what
+// k_attn_grad_size finds.
 #pragma once
 #include "enc_common.h"
 #include <type_traits>
@@ -221,7 +221,7 @@ __device__ __forceinline__ bool attn_work(const AttnArgs &a, unsigned per_head, 
 // 1 - 2 / (1 + e^2y) by the hardware's exponential and reciprocal: it is off by 2^-22 at most, but absolutely, so that a score is off by that times the
 // cap, however small it is.  Up to caps of 64 that is 2^-16, a 32nd of what rounding its weight to fp16 costs (bf16: a 256th).  Above (MODE_EXACT),
 // and in 32 bits, tanh is the library's, which keeps small values: a cap may be far above all scores.  3 sequences of 4000, 16 heads of 64 on 8 in fp16, biased,
-// caps of 64 and 65: 386 us forward and 1035 backward, 469 and 1380; 32 of 300, 12 heads of 64: 32 and 84, 41 and 111.
+// caps of 64 and 65: 375 us forward and 1106 backward, 446 and 1468; 32 of 300, 12 heads of 64: 32 and 96, 41 and 126.
 enum { MODE_CAP = 1, MODE_SLOPE = 2, MODE_EXACT = 4 };
 #define ATTN_FAST_CAP 64.f
 template <class T, int MODE> constexpr bool attn_fast_tanh() { return sizeof(T) == 2 && (MODE & MODE_CAP) && !(MODE & MODE_EXACT); }
@@ -332,7 +332,7 @@ __device__ __forceinline__ float col_max(const f32x16 &s)
 // independent of this step's exponentials, so that matrix and vector instructions of one wave overlap.  Tiles of BN keys pass through three LDS
 // stages, which takes one barrier a tile: the stage that a wave overwrites is the one that every wave has left before the last barrier.
 // 12 heads of 128 on 4 key heads, 16384 rows of bf16: 1.70 ms, 970 TF, 0.80 of what a library product of 8192^3 reaches on the card (1208); matrix instructions
-// take 0.47 of the cycles, vector instructions 0.50, at the clock that the power limit leaves (1.7 to 1.9 GHz).  64 sequences of 290 rows on average, 12 heads of
+// take 0.47 of the cycles, vector instructions 0.50, at the clock that the power limit leaves (1.7 to 1.9 GHz).  64 sequences of 277 rows on average, 12 heads of
 // 64: 44 us: a work-group has 9 steps then, and spends a third of its time on its first loads and its store.
 // Tried and not kept: no maximum per step, weights watched by their sums instead (heads of 32 1.1 times as fast, of 64 and 128 1.02, a steep distance bias 0.87);
 // the weighted sum one step later, so that all of a step's products and exponentials are independent (85 registers more, 0.85); waves without rows
@@ -709,15 +709,16 @@ template <class T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a
 //
 // NW waves of 32 rows each (queries for dq, keys for dk and dv); the other axis streams by in blocks of 32 rows through two LDS stages, one barrier a
 // block.  delta is where the sums of do . v begin, lse is part of the exponential's fma: one subtraction less each.  A lone wave hides little, so
-// registers are kept for more of them: three per SIMD for dq and two for dk and dv, with heads up to 64.  (Row operands read a block ahead, at the
+// registers are kept for more of them: three per SIMD for dq (two under a bias) and two for dk and dv, with heads up to 64.  (Row operands read a block ahead, at the
 // price of a wave: dq of one sequence of 8192, 12 heads of 64, 484 us instead of 424.)  The next block goes to LDS ahead of the barrier at the block's
 // beginning for dq, in its middle for dk and dv, whose barrier is there too (at the beginning: 578 us instead of 500).
-// One sequence of 4096, 12 heads of 64 in bf16: dq 110 us (706 TF), dk and dv 124 (829); capped and biased 158 and 161 us: vector instructions.  64 sequences of
-// 290 rows on average: 56 and 71 us.
+// One sequence of 4096, 12 heads of 64 in bf16: dq 109 us (709 TF), dk and dv 124 (831); capped and biased 178 and 168 us: vector instructions.  64 sequences of
+// 277 rows on average: 56 and 68 us.  Of the 16-bit kernels those for dq of short sequences with heads of 128, without a bias, keep 12 to 15 registers in scratch memory
+// (of 64 one at most); of the 32-bit ones those for dk and dv with heads above 64.
 template <class T, int DP, int MODE> struct AttnGrad {
     static constexpr int TILE = 32 * DP;
     static constexpr bool MEND = sizeof(T) == 2 && (MODE & MODE_SLOPE); // delta and dq are mended, as the comment at k_attn_grad_q says
-    static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave, the sums that mend too
+    static constexpr int LESS = sizeof(T) == 2 && (MODE & MODE_EXACT) ? 1 : 0; // the library's tanh takes the registers of a wave, the sums that mend (MEND) too
     static constexpr int WAVES_Q = sizeof(T) == 4 ? 1 : (DP > 64 ? 2 : 3) - (LESS || MEND), WAVES_KV = sizeof(T) == 4 || DP > 64 ? 1 : 2 - LESS; // per SIMD
 };
 // What the backward pass makes of one score x, from the product x = q . k and `rest`, which has -lse in it: p, times 2^lift, and the factor of ds, 1 - tanh^2 under

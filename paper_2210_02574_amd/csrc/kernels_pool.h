@@ -21,7 +21,7 @@ struct PoolGradArgs {
     int tile; // rows of a tile
 };
 
-// 256 sequences of 580 rows of 768 on average, bf16: 39 us (5.6 TB/s), and 4 us to join; 32 of 72 rows 6 us: the sequence's numbers, then one or two trips.
+// 256 sequences of 555 rows of 768 on average, bf16: 38 us (5.8 TB/s), and 4 us to join; 32 of 68 rows 6 us: the sequence's numbers, then one or two trips.
 // grid (sequences or tile slots, column blocks).  A thread has one vector of columns and every RG-th row; CL = threads along the columns.
 template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) void k_pool(PoolArgs a, int CL)
 {
@@ -86,7 +86,7 @@ template <class T, int VEC, int THREADS> __global__ __launch_bounds__(THREADS) v
 }
 
 // grid (sequences, columns * SHARES / 256), SHARES threads to a column: the tiles of a sequence are those of the slots tile_slot(c, i) .. that reach into it.
-// Shares pay where sequences have many tiles: one sequence of 8192 rows in 128 of them 11 us with one share, 4 with eight; 256 sequences of 580 in 8 4 us, 7.
+// Shares pay where sequences have many tiles: one sequence of 8192 rows in 128 of them 11 us with one share, 4 with eight; 256 sequences of 555 in 8 4 us, 7.
 #define POOL_SHARED_TILES 16 // per sequence, from which on there are eight shares
 template <int SHARES> __global__ __launch_bounds__(256) void k_pool_join(PoolArgs a)
 {
@@ -112,7 +112,7 @@ template <int SHARES> __global__ __launch_bounds__(256) void k_pool_join(PoolArg
     if (col < a.width) a.e[(size_t)i * a.width + col] = end > begin ? s / (float)(end - begin) : 0.f;
 }
 
-// 256 sequences of 580 rows of 768, bf16: 35 us (6.3 TB/s).
+// 256 sequences of 555 rows of 768 on average, bf16: 35 us (6.3 TB/s).
 // grid (tile slots, column blocks): the rows of one tile get the sequence's row, rows of no sequence zeros if `fill`.
 template <class T, int VEC> __global__ __launch_bounds__(256) void k_pool_grad(PoolGradArgs a, int CL)
 {
