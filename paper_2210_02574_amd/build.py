@@ -79,7 +79,11 @@ def _binds_to() -> str:
     import importlib.metadata
     import sysconfig
 
-    return f"torch {importlib.metadata.version('torch')} python {sysconfig.get_config_var('SOABI')}"
+    try:
+        torch = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:  # a torch that was not installed as a package
+        torch = "unknown"
+    return f"torch {torch} python {sysconfig.get_config_var('SOABI')}"
 
 
 def source_hash() -> str:

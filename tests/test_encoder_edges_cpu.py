@@ -99,3 +99,11 @@ def test_a_distance_bias_with_first_rows_is_refused_before_any_layer_runs(he):
             SentenceEncoder(he, layers, 2, pool="first", slopes=torch.ones(2))
     SentenceEncoder(he, [w], 2, pool="mean", slopes=torch.ones(2))
     SentenceEncoder(he, [w], 2, pool="first")
+
+
+def test_a_torch_without_package_data_is_no_error(monkeypatch):
+    def missing(name):
+        raise importlib.metadata.PackageNotFoundError(name)
+
+    monkeypatch.setattr(importlib.metadata, "version", missing)
+    assert build.is_stale() and build.source_hash() == build.source_hash()
