@@ -107,3 +107,18 @@ def test_a_torch_without_package_data_is_no_error(monkeypatch):
 
     monkeypatch.setattr(importlib.metadata, "version", missing)
     assert build.is_stale() and build.source_hash() == build.source_hash()
+
+
+def test_the_workspace_of_fp16_gradients_has_room_for_the_rows_sizes(he):
+    """A number for each tile of queries and of keys, and each key head, beside what other types take; one byte less is refused."""
+    attn, heads = struct.Struct("@4iPPiqPPiqddPi4x").pack, struct.Struct("@Pqq").pack(1 << 20, 512, 64)
+    for count, rows in ((3, 40), (1, 5000), (200, 4000)):
+        span, need = (1 << 20, 1 << 20, count, rows), {}
+        for t in (1, 2):
+            s, size = attn(t, 4, 2, 64, *span, *span, 0.125, 0.0, 0, 1), ctypes.c_size_t()
+            assert he.lib.he_attention_workspace_bytes(he.ctx, s, 1, ctypes.byref(size)) == 0
+            need[t] = size.value
+            for room, rc in ((need[t], -6), (need[t] - 1, -4)):  # all but a device; too little
+                assert he.lib.he_attention_grad(he.ctx, s, *[heads] * 5, 1 << 20, *[heads] * 3, 1 << 20, room, None) == rc
+        tiles = -(-rows // 128) + count - 1  # of 128 rows; smaller ones are more
+        assert need[1] - need[2] >= 2 * 2 * 4 * tiles
