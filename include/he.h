@@ -358,6 +358,39 @@ int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, con
                            const float *d_rstd, const he_rows *add, const he_rows *ds, void *d_dw, void *d_db, void *d_ws, size_t ws_bytes,
                            void *stream);
 
+/* Root-mean-square norm over the last dimension: s as in he_layer_norm; rstd = (mean(s^2) + eps)^-1/2; y = s rstd w.  Limits as there; the squares
+ * are summed in 32 bits (a sum beyond them: y = 0). */
+int32_t he_rms_norm(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows *y,
+                    const he_rows *sum, float *d_rstd, void *stream);
+/* With g = dy w: ds = rstd (g - s rstd^2 mean(g s)) + add, dw = sum over rows of dy s rstd; otherwise as he_layer_norm_grad. */
+int32_t he_rms_norm_workspace_bytes(const he_ctx *ctx, const he_norm *n, size_t *out);
+int32_t he_rms_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, const he_rows *s, const void *d_w, const float *d_rstd,
+                         const he_rows *add, const he_rows *ds, void *d_dw, void *d_ws, size_t ws_bytes, void *stream);
+
+/* Rows of `width` 8-bit integers, `stride` bytes from row to row, each integer standing for itself times d_scale[row].  Rows that are read begin at multiples of 16
+ * bytes and are read by whole pieces of 16: the buffer holds the last piece of its last row too (what it has behind the width does not count). */
+typedef struct {
+    int8_t *d;
+    int64_t stride;
+    float *d_scale;
+} he_rows8;
+/* Rows in 8 bits: t = max |f|, integers rint(127 f / t) (ties to the even one), scale = t / 127, in the order of these operations; for a row of zeros both are 0.  A row with
+ * an infinity or a NaN: scale NaN, integers 0, so that nothing made of it is finite.
+ *   he_quantize8: f = x, or the Gaussian error unit x Phi(x) of it with gelu != 0, within 2^-20 (1 + x^2 / 8) of itself.  width at most 16384.
+ *   he_rms_norm8: f = s w in he_rms_norm, unrounded; the scale is (t rstd) / 127.  The integers hang on s w alone. */
+int32_t he_quantize8(he_ctx *ctx, int32_t type, int64_t rows, int32_t width, int32_t gelu, const he_rows *x, const he_rows8 *y, void *stream);
+int32_t he_rms_norm8(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows8 *y,
+                     const he_rows *sum, void *stream);
+/* Product of 8-bit rows and 8-bit weights: o[m][n] = (sum over k of x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n], of type `type`.  The sums are exact; a result
+ * takes four roundings to 32 bits, in this order, and one to its type.  width (of k) at most 65536, strides below 2^23 bytes; HE_EINVAL also: more than 2^31 - 65536
+ * rows or 2^24 channels.  bias_type: HE_F32 or `type`; d_bias NULL: no bias. */
+typedef struct {
+    int32_t type, bias_type;
+    int64_t rows;
+    int32_t width, channels;
+} he_product8;
+int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *stream);
+
 /* Mean over the rows of each sequence, d_e [count][width] in 32 bits, zeros for an empty one; and its gradient, dx = de / length on the rows of
  * each sequence.  fill: rows of no sequence are set to zero, else left as they are.  width at most 2^20. */
 int32_t he_pool_workspace_bytes(const he_ctx *ctx, const he_spans *s, int32_t width, size_t *out);

@@ -38,6 +38,7 @@ SYMBOLS = [
     "he_hrot_noalloc",
     "he_layer_norm", "he_layer_norm_workspace_bytes", "he_layer_norm_grad", "he_pool", "he_pool_workspace_bytes", "he_pool_grad",
     "he_attention", "he_attention_workspace_bytes", "he_attention_grad",
+    "he_rms_norm", "he_rms_norm_workspace_bytes", "he_rms_norm_grad", "he_rms_norm8", "he_quantize8", "he_linear8",
     "he_profile_start", "he_profile_stop",
 ]
 
@@ -86,7 +87,7 @@ def load_library() -> ctypes.CDLL:
         import torch  # noqa: F401
 
         lib = ctypes.CDLL(LIB_PATH)
-        vp, i32, u64, sz, dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_double
+        vp, i32, i64, u64, sz, dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_double
         ds = ctypes.c_char_p
         sig = {
             "he_ctx_create": [ctypes.POINTER(he_params), i32, ctypes.POINTER(vp)],
@@ -153,6 +154,12 @@ def load_library() -> ctypes.CDLL:
             "he_pool": [vp, i32, ds, i32, ds, vp, vp, sz, vp],
             "he_pool_workspace_bytes": [vp, ds, i32, ctypes.POINTER(sz)],
             "he_pool_grad": [vp, i32, ds, i32, vp, ds, i32, vp],
+            "he_rms_norm": [vp, ds, ds, ds, vp, ds, ds, vp, vp],
+            "he_rms_norm_workspace_bytes": [vp, ds, ctypes.POINTER(sz)],
+            "he_rms_norm_grad": [vp, ds, ds, ds, vp, vp, ds, ds, vp, vp, sz, vp],
+            "he_rms_norm8": [vp, ds, ds, ds, vp, ds, ds, vp],
+            "he_quantize8": [vp, i32, i64, i32, i32, ds, ds, vp],
+            "he_linear8": [vp, ds, ds, ds, vp, ds, vp],
             "he_attention": [vp, ds, ds, ds, ds, ds, vp, vp, sz, vp],
             "he_attention_workspace_bytes": [vp, ds, i32, ctypes.POINTER(sz)],
             "he_attention_grad": [vp, ds, ds, ds, ds, ds, ds, vp, ds, ds, ds, vp, sz, vp],
@@ -765,6 +772,36 @@ class HE:
         """(dx, dweight, dbias) from the gradient of y; ds: a gradient that reaches s from elsewhere, added to dx.  dx is the gradient of x and
         of the residual both."""
         return self._on_tensors("layer_norm_backward", "he_layer_norm_grad", dy, s, weight, mean, rstd, ds)
+
+    def rms_norm(self, x, weight, residual=None, eps: float = 1e-5, out=None):
+        """x rstd weight over the last dimension of x [rows][width], rstd = (mean(x^2) + eps)^-1/2, of s = x + residual with one (rounded to the type).
+        Returns (y, s, rstd); s is x itself without a residual.  Keep s and rstd for rms_norm_backward.
+        No history, whatever the inputs have: embedding.rms_norm is the differentiable form."""
+        return self._on_tensors("rms_norm", "he_rms_norm", x, weight, residual, eps, out)
+
+    def rms_norm_backward(self, dy, s, weight, rstd, ds=None):
+        """(dx, dweight) from the gradient of y; ds: a gradient that reaches s from elsewhere, added to dx.  dx is the gradient of x and of the
+        residual both."""
+        return self._on_tensors("rms_norm_backward", "he_rms_norm_grad", dy, s, weight, rstd, ds)
+
+    # Rows in 8 bits: int8 integers, each standing for itself times its row's scale (float32), with max |row| at +-127.  A row with an infinity or a NaN has the
+    # scale NaN, so that all that is made of it is NaN.  No gradients pass through them.
+    def rms_norm8(self, x, weight, residual=None, eps: float = 1e-5):
+        """rms_norm with y in 8 bits: (y8 [rows][width], scale [rows], s)."""
+        return self._on_tensors("rms_norm8", "he_rms_norm8", x, weight, residual, eps)
+
+    def quantize8(self, x, gelu: bool = False):
+        """Rows x [rows][width], or Gaussian error units of them, in 8 bits: (x8 [rows][width], scale [rows]).  Weights of a product too: a row is a channel."""
+        return self._on_tensors("quantize8", "he_quantize8", x, gelu)
+
+    def linear8(self, x8, scale, w8, w_scale, bias=None, dtype=None, out=None):
+        """x8 scale (w8 w_scale)^T + bias, of type dtype (bfloat16 by default): x8 [rows][width] with a scale for each row, w8 [channels][width] with one for each
+        channel, bias [channels] float32 or of type dtype.  Sums are exact.  Rows of x8 and w8 begin at multiples of 16 bytes, as quantize8 and rms_norm8 make them."""
+        import torch
+
+        if dtype is None:
+            dtype = torch.bfloat16 if out is None else out.dtype
+        return self._on_tensors("linear8", "he_linear8", x8, scale, w8, w_scale, bias, dtype, out)
 
     def pool_mean(self, x, offsets, out=None):
         """Mean of the rows of each sequence of x [rows][width]: [count][width] in 32 bits, zeros for an empty sequence.

@@ -25,6 +25,8 @@ SOURCES = (
     # (matrix instructions with their sums in ordinary registers, where the exponentials read them: accumulation registers cost a move per value)
     + [("dev_attn.hip", ["-DHE_TYPE=%d" % t, "-DHE_DIM=%d" % d, "-mllvm", "-amdgpu-mfma-vgpr-form"], "dev_attn%d_%d" % (t, d)) for d in (128, 96, 64, 32) for t in (0, 1, 2)]
     + [("dev_rows.hip", ["-DHE_TYPE=%d" % t], "dev_rows%d" % t) for t in (0, 1, 2)]
+    + [("dev_rows8.hip", ["-DHE_TYPE=%d" % t], "dev_rows8_%d" % t) for t in (0, 1, 2)]
+    + [("dev_linear8.hip", ["-DHE_TYPE=%d" % t], "dev_linear8_%d" % t) for t in (0, 1, 2)]
     + [("dev_encoder.hip", [], "dev_encoder")]
     + [(s, [], os.path.splitext(s)[0]) for s in ("dev_n12.hip", "dev_n16_blocks.hip", "dev_n17_blocks.hip", "device.hip", "host.cpp")]
 )

@@ -1,11 +1,14 @@
-// Entry points of the operators on token states: attention inside sequences, layer norm, mean over sequences.
+// Entry points of the operators on token states: attention inside sequences, layer norm and root-mean-square norm, mean over sequences, rows in 8 bits and their
+// products.
 #include <cmath>
 #include <cstring>
 
 #include "enc_launch.h"
 #include "kernels_attn.h"
+#include "kernels_linear8.h"
 #include "kernels_norm.h"
 #include "kernels_pool.h"
+#include "kernels_rows8.h"
 
 namespace {
 
@@ -80,6 +83,30 @@ bool words_ok(const void *p, size_t size = 4) { return p && aligned(p, size); }
 
 // Work-groups of the backward pass: each writes a partial row of dw and db, so two for each of the 256 CUs and no more than rows need.
 int norm_parts(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
+
+// ---- rows in 8 bits ----------------------------------------------------------------------------------------------------------
+
+const Rows8Launch &rows8_launch(int32_t t)
+{
+    static const Rows8Launch tables[3] = {
+        [] { Rows8Launch x{}; rows8_launch_0(x); return x; }(),
+        [] { Rows8Launch x{}; rows8_launch_1(x); return x; }(),
+        [] { Rows8Launch x{}; rows8_launch_2(x); return x; }(),
+    };
+    return tables[t];
+}
+const Linear8Launch &linear8_launch(int32_t t)
+{
+    static const Linear8Launch tables[3] = {
+        [] { Linear8Launch x{}; linear8_launch_0(x); return x; }(),
+        [] { Linear8Launch x{}; linear8_launch_1(x); return x; }(),
+        [] { Linear8Launch x{}; linear8_launch_2(x); return x; }(),
+    };
+    return tables[t];
+}
+// rows that are written, and rows that a product reads by pieces of 16 bytes
+bool rows8_ok(const he_rows8 *r, int64_t width) { return r && r->d && words_ok(r->d_scale) && r->stride >= width; }
+bool pieces_ok(const he_rows8 *r, int64_t width) { return rows8_ok(r, width) && aligned(r->d, 16) && r->stride % 16 == 0 && r->stride < 1 << 23; }
 
 // ---- mean ----------------------------------------------------------------------------------------------------------------
 
@@ -292,6 +319,159 @@ extern "C" int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_ro
     const double row = (double)n->width * type_size(n->type), part = (double)parts * 2 * n->width * 4;
     if (n->rows) l.norm_grad(ctx, (hipStream_t)stream, n->rows * (row * (add ? 4 : 3) + 8) + part, ww, parts, a);
     l.weight_grad(ctx, (hipStream_t)stream, part + 2.0 * n->width * type_size(n->weight_type), ww, (const float *)d_ws, parts, n->width, d_dw, d_db);
+    return launched(ctx);
+}
+
+namespace {
+
+// What both forms of the root-mean-square norm take; `y` and `out` are the caller's to set.
+int32_t rms_args(RmsArgs &a, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows *sum)
+{
+    memset(&a, 0, sizeof(a));
+    if (!rows_ok(x, n->width, n->type) || !words_ok(d_w, type_size(n->weight_type))) return HE_EINVAL;
+    if (residual && (!rows_ok(residual, n->width, n->type) || !rows_ok(sum, n->width, n->type))) return HE_EINVAL;
+    a.x = x->d, a.x_row = x->stride, a.w = d_w;
+    if (residual) a.r = residual->d, a.r_row = residual->stride, a.s = sum->d, a.s_row = sum->stride;
+    a.rows = (int)n->rows, a.width = n->width, a.eps = (float)n->eps;
+    return HE_OK;
+}
+bool eps_ok(const he_norm *n) { return n->eps >= 0.0 && std::isfinite((float)n->eps); }
+
+} // namespace
+
+extern "C" int32_t he_rms_norm(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows *y,
+                               const he_rows *sum, float *d_rstd, void *stream)
+{
+    if (!ctx || norm_check(n) != HE_OK || !eps_ok(n)) return HE_EINVAL;
+    if (n->rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    RmsArgs a;
+    if (rms_args(a, n, x, residual, d_w, sum) != HE_OK || !rows_ok(y, n->width, n->type) || !words_ok(d_rstd)) return HE_EINVAL;
+    a.y = y->d, a.y_row = y->stride, a.out = d_rstd;
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const double row = (double)n->width * type_size(n->type);
+    rows8_launch(n->type).rms(ctx, (hipStream_t)stream, n->rows * (row * (residual ? 4 : 2) + 4) + (double)n->width * type_size(n->weight_type),
+                              n->weight_type == HE_F32, a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_rms_norm8(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows8 *y,
+                                const he_rows *sum, void *stream)
+{
+    if (!ctx || norm_check(n) != HE_OK || !eps_ok(n)) return HE_EINVAL;
+    if (n->rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    RmsArgs a;
+    if (rms_args(a, n, x, residual, d_w, sum) != HE_OK || !rows8_ok(y, n->width)) return HE_EINVAL;
+    a.y = y->d, a.y_row = y->stride, a.out = y->d_scale;
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const double row = (double)n->width * type_size(n->type);
+    rows8_launch(n->type).rms8(ctx, (hipStream_t)stream, n->rows * (row * (residual ? 3 : 1) + n->width + 4) + (double)n->width * type_size(n->weight_type),
+                               n->weight_type == HE_F32, a);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_rms_norm_workspace_bytes(const he_ctx *ctx, const he_norm *n, size_t *out)
+{
+    if (!ctx || !out || norm_check(n) != HE_OK) return HE_EINVAL;
+    *out = n->rows ? (size_t)norm_parts(n->rows) * n->width * sizeof(float) : 0;
+    return HE_OK;
+}
+
+extern "C" int32_t he_rms_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, const he_rows *s, const void *d_w, const float *d_rstd,
+                                    const he_rows *add, const he_rows *ds, void *d_dw, void *d_ws, size_t ws_bytes, void *stream)
+{
+    if (!ctx || norm_check(n) != HE_OK) return HE_EINVAL;
+    const size_t size_w = type_size(n->weight_type);
+    if (!words_ok(d_w, size_w) || !words_ok(d_dw, size_w)) return HE_EINVAL;
+    RmsGradArgs a;
+    memset(&a, 0, sizeof(a));
+    a.rows = (int)n->rows, a.width = n->width;
+    const int parts = n->rows ? norm_parts(n->rows) : 0;
+    if (n->rows) {
+        if (!rows_ok(dy, n->width, n->type) || !rows_ok(s, n->width, n->type) || !rows_ok(ds, n->width, n->type)) return HE_EINVAL;
+        if (!words_ok(d_rstd) || (add && !rows_ok(add, n->width, n->type))) return HE_EINVAL;
+        if (!d_ws || ws_bytes < (size_t)parts * n->width * sizeof(float)) return HE_EWORKSPACE;
+        if (!aligned(d_ws, 4)) return HE_EINVAL;
+        a.dy = dy->d, a.dy_row = dy->stride, a.s = s->d, a.s_row = s->stride, a.ds = ds->d, a.ds_row = ds->stride;
+        if (add) a.add = add->d, a.add_row = add->stride;
+        a.w = d_w, a.rstd = d_rstd, a.part = (float *)d_ws;
+    }
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const Rows8Launch &l = rows8_launch(n->type);
+    const bool ww = n->weight_type == HE_F32;
+    const double row = (double)n->width * type_size(n->type), part = (double)parts * n->width * 4;
+    if (n->rows) l.rms_grad(ctx, (hipStream_t)stream, n->rows * (row * (add ? 4 : 3) + 4) + part, ww, parts, a);
+    l.weight_grad(ctx, (hipStream_t)stream, part + (double)n->width * type_size(n->weight_type), ww, (const float *)d_ws, parts, n->width, d_dw);
+    return launched(ctx);
+}
+
+extern "C" int32_t he_quantize8(he_ctx *ctx, int32_t type, int64_t rows, int32_t width, int32_t gelu, const he_rows *x, const he_rows8 *y, void *stream)
+{
+    if (!ctx || !type_ok(type) || rows < 0 || rows > MAX_ROWS || width < 1 || width > NORM_MAX_WIDTH) return HE_EINVAL;
+    if (rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!rows_ok(x, width, type) || !rows8_ok(y, width)) return HE_EINVAL;
+    NEEDS_DEVICE(ctx);
+    Rows8Args a;
+    memset(&a, 0, sizeof(a));
+    a.x = x->d, a.x_row = x->stride, a.y = y->d, a.y_row = y->stride, a.scale = y->d_scale, a.rows = (int)rows, a.width = width;
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    rows8_launch(type).quantize(ctx, (hipStream_t)stream, rows * ((double)width * (type_size(type) + 1) + 4), gelu != 0, a);
+    return launched(ctx);
+}
+
+namespace {
+
+int32_t product8_check(const he_product8 *p)
+{
+    if (!p || !type_ok(p->type) || (p->bias_type != p->type && p->bias_type != HE_F32)) return HE_EINVAL;
+    if (p->rows < 0 || p->rows > MAX_ROWS || p->width < 1 || p->width > LINEAR8_MAX_WIDTH || p->channels < 1 || p->channels > 1 << 24) return HE_EINVAL;
+    return HE_OK;
+}
+int64_t product8_tiles(const he_product8 *p, int tile) { return ((p->rows + tile - 1) / tile) * ((p->channels + tile - 1) / tile); }
+
+} // namespace
+
+extern "C" int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *stream)
+{
+    if (!ctx || product8_check(p) != HE_OK || !pieces_ok(w, p->width)) return HE_EINVAL;
+    if (d_bias && !words_ok(d_bias, type_size(p->bias_type))) return HE_EINVAL;
+    if (p->rows == 0) {
+        NEEDS_DEVICE(ctx);
+        return HE_OK;
+    }
+    if (!pieces_ok(x, p->width) || !rows_ok(o, p->channels, p->type)) return HE_EINVAL;
+    Linear8Args a;
+    memset(&a, 0, sizeof(a));
+    a.x = x->d, a.x_row = x->stride, a.x_scale = x->d_scale, a.w = w->d, a.w_row = w->stride, a.w_scale = w->d_scale;
+    a.bias = d_bias, a.bias32 = p->bias_type == HE_F32, a.o = o->d, a.o_row = o->stride;
+    a.rows = (int)p->rows, a.width = p->width, a.channels = p->channels;
+    const int tile = product8_tiles(p, 256) >= 192 ? 256 : product8_tiles(p, 128) >= 192 ? 128 : 64;
+    if (product8_tiles(p, tile) > 1 << 23) return HE_EINVAL; // more than a launch holds
+    NEEDS_DEVICE(ctx);
+    DeviceGuard dg(ctx);
+    if (dg.rc != HE_OK) return dg.rc;
+    const double bytes = (double)p->rows * (p->width + 4) + (double)p->channels * (p->width + 4) + (double)p->rows * p->channels * type_size(p->type) +
+                         (d_bias ? (double)p->channels * type_size(p->bias_type) : 0.0);
+    const Linear8Launch &l = linear8_launch(p->type);
+    if (p->rows <= 64)
+        l.few(ctx, (hipStream_t)stream, bytes, p->rows <= 16 ? 1 : p->rows <= 32 ? 2 : 4, (int)std::min<int64_t>(16, (p->width + 255) / 256), a);
+    else
+        l.tiles(ctx, (hipStream_t)stream, bytes, tile, a);
     return launched(ctx);
 }
 

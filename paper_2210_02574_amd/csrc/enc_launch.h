@@ -8,6 +8,10 @@ struct NormArgs;
 struct NormGradArgs;
 struct PoolArgs;
 struct PoolGradArgs;
+struct RmsArgs;
+struct RmsGradArgs;
+struct Rows8Args;
+struct Linear8Args;
 
 // Whether there are tiles of 256 queries, two blocks of 32 to a wave: they halve what is read of LDS for a product, and pay where the registers still
 // hold two waves per SIMD.  12 heads of 64 in bf16, tiles of 256 against 128: one sequence of 16384 1013 us, 1086; 16 of 2048 300, 312; 32 of 1024 146, 150;
@@ -46,4 +50,26 @@ void rows_launch_0(RowsLaunch &t);
 void rows_launch_1(RowsLaunch &t);
 void rows_launch_2(RowsLaunch &t);
 
+struct Rows8Launch {
+    void (*rms)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const RmsArgs &a);
+    void (*rms8)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const RmsArgs &a);
+    void (*rms_grad)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, int parts, const RmsGradArgs &a);
+    void (*weight_grad)(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const float *part, int parts, int width, void *dw);
+    void (*quantize)(he_ctx *c, hipStream_t st, double bytes, bool gelu, const Rows8Args &a);
+};
+void rows8_launch_0(Rows8Launch &t);
+void rows8_launch_1(Rows8Launch &t);
+void rows8_launch_2(Rows8Launch &t);
+
+struct Linear8Launch {
+    // tile: rows and channels of a work-group, 64, 128 or 256
+    void (*tiles)(he_ctx *c, hipStream_t st, double bytes, int tile, const Linear8Args &a);
+    // blocks: of 16 rows to a work-group, 1, 2 or 4; waves that share a sum, up to 16
+    void (*few)(he_ctx *c, hipStream_t st, double bytes, int blocks, int waves, const Linear8Args &a);
+};
+void linear8_launch_0(Linear8Launch &t);
+void linear8_launch_1(Linear8Launch &t);
+void linear8_launch_2(Linear8Launch &t);
+
 #define NORM_MAX_WIDTH 16384
+#define LINEAR8_MAX_WIDTH 65536

@@ -1,0 +1,327 @@
+// Root-mean-square norm over rows of token states, forward and backward, and rows in 8 bits.
+//
+//   s = x + r (rounded to the type, where there is a residual r; else s = x), rstd = (mean(s^2) + eps)^-1/2, y = s rstd w.
+//   With g = dy w:  ds = rstd (g - s rstd^2 mean(g s)) + ds', dw = sum over rows of dy s rstd.
+//   A row f in 8 bits: t = max |f|, integers rint(127 f / t), scale t / 127.  Of y it takes f = s w alone, as rstd is common to the row: scale t rstd / 127.
+//
+// As in layer norm a row stays in the registers of its TPR threads and is read once; sums are in 32 bits.  All of it is bound by memory.
+#pragma once
+#include "kernels_norm.h"
+
+struct RmsArgs {
+    const void *x, *r, *w;
+    void *y, *s;  // y: the rows' type, or 8-bit integers
+    float *out;   // [rows]: rstd, or the scales
+    int64_t x_row, r_row, y_row, s_row; // row strides, in elements
+    int rows, width, first; // rows, of them the first one of this launch
+    float eps;
+};
+struct RmsGradArgs {
+    const void *dy, *s, *w, *add;
+    void *ds;
+    const float *rstd;
+    float *part; // [gridDim.x][width]: every work-group's share of dw
+    int64_t dy_row, s_row, add_row, ds_row;
+    int rows, width;
+};
+
+// The sum of v and the largest m over the TPR threads of a row, the same in each; red: two words per wave.
+template <int TPR> __device__ __forceinline__ void row_sum_max(float &v, unsigned &m, float *red)
+{
+    constexpr int LANES = TPR < 64 ? TPR : 64;
+#pragma unroll
+    for (int s = LANES / 2; s > 0; s >>= 1) {
+        v += __shfl_xor(v, s, 64);
+        m = max(m, (unsigned)__shfl_xor((int)m, s, 64));
+    }
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            red[2 * (threadIdx.x >> 6)] = v;
+            red[2 * (threadIdx.x >> 6) + 1] = __uint_as_float(m);
+        }
+        __syncthreads();
+        v = 0.f, m = 0;
+#pragma unroll
+        for (int k = 0; k < TPR / 64; k++) {
+            v += red[2 * k];
+            m = max(m, __float_as_uint(red[2 * k + 1]));
+        }
+    }
+}
+
+// x Phi(x).  With z = |x|: Phi(-z) = exp(-z^2 / 2) t p(t), t = 1 / (1 + c z); p is a fit of degree 8 to the function that this leaves, within 2e-8 of it, so that the lower tail is
+// as exact, relatively, as the exponential: 1 + erf would lose it.
+__device__ __forceinline__ float gelu(float x)
+{
+    const float z = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(z, 0.21f, 1.f));
+    float p = -0.07129527628421783f;
+    p = fmaf(p, t, 0.28180667757987976f);
+    p = fmaf(p, t, -0.32649728655815125f);
+    p = fmaf(p, t, 0.34499093890190125f);
+    p = fmaf(p, t, -0.09077534824609756f);
+    p = fmaf(p, t, 0.12347319722175598f);
+    p = fmaf(p, t, 0.06956949084997177f);
+    p = fmaf(p, t, 0.08501247316598892f);
+    p = fmaf(p, t, 0.08371514827013016f);
+    const float tail = p * t * __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); // log2(e) / 2
+    return x * (x > 0.f ? 1.f - tail : tail);
+}
+
+// The row's numbers for its integers, from the bits of max |f| (largest as an integer: a NaN is above an infinity is above all others).  Values and maximum are
+// taken times a power of two that brings the maximum into [1/2, 1): 127 / t then neither overflows nor loses bits.
+struct Eight {
+    float top, inv; // the maximum in [1/2, 1), and 127 / top
+    int exp;        // the power of two
+    float t;        // the maximum
+    bool bad;       // not finite
+    __device__ __forceinline__ explicit Eight(unsigned bits)
+    {
+        bad = bits >= 0x7f800000u;
+        t = __uint_as_float(bits);
+        const float one = bad || !bits ? 1.f : t;
+        exp = -__builtin_amdgcn_frexp_expf(one);
+        top = __builtin_amdgcn_frexp_mantf(one);
+        inv = 127.f / top;
+    }
+    __device__ __forceinline__ float scale(float rstd) const { return bad ? __builtin_nanf("") : t == 0.f ? 0.f : t * rstd / 127.f; }
+    // f / t * 127 to the nearest integer, in the low byte of the result: the sum with 1.5 2^23 rounds to whole numbers, ties to the even one.
+    static constexpr float MAGIC = 12582912.f;
+    __device__ __forceinline__ unsigned near(float f, float &far) const
+    {
+        const float p = __builtin_amdgcn_ldexpf(f, exp), m = fmaf(p, inv, MAGIC);
+        far = fmaxf(far, fabsf(fmaf(p, inv, MAGIC - m)));
+        return __float_as_uint(m);
+    }
+    // The same where the quotient, off by up to 2^-17 as inv is rounded, may lie on the other side of a border, or on it: the rest 127 f - n t decides, with
+    // no rounding that could change its sign for 16-bit rows and weights.
+    __device__ __forceinline__ unsigned exact(float f) const
+    {
+        const float p = __builtin_amdgcn_ldexpf(f, exp), m = fmaf(p, inv, MAGIC), n = m - MAGIC;
+        const float h = 127.f * p, rest = 2.f * (fmaf(-n, top, h) + fmaf(127.f, p, -h));
+        const unsigned i = __float_as_uint(m), odd = i & 1;
+        return i + (rest > top || (rest == top && odd) ? 1u : 0u) - (rest < -top || (rest == -top && odd) ? 1u : 0u);
+    }
+};
+// VEC values of a row in 8 bits.
+template <int VEC> __device__ __forceinline__ Vec<int8_t, VEC> eight_vec(const float (&f)[VEC], const Eight &q)
+{
+    unsigned b[VEC];
+    float far = 0.f;
+#pragma unroll
+    for (int e = 0; e < VEC; e++) b[e] = q.near(f[e], far);
+    if (!(far < 0.4999f))
+#pragma unroll
+        for (int e = 0; e < VEC; e++) b[e] = q.exact(f[e]);
+    unsigned w[VEC / 4];
+#pragma unroll
+    for (int i = 0; i < VEC / 4; i++) {
+        const unsigned lo = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u);
+        w[i] = q.bad ? 0u : lo | hi << 16;
+    }
+    Vec<int8_t, VEC> v;
+    __builtin_memcpy(&v, w, VEC);
+    return v;
+}
+
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm(RmsArgs a)
+{
+    constexpr int THREADS = TPR > 256 ? TPR : 256;
+    __shared__ float red[THREADS / 32];
+    const int t = threadIdx.x % TPR, row = a.first + blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    const bool live = row < a.rows; // a row's lanes are live or not together; all of them take part in the sums, on the last row
+    const int64_t r = min(row, a.rows - 1);
+    Vec<T, VEC> x[NC], res[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        x[c] = k.load((const T *)a.x + r * a.x_row);
+        if (a.r) res[c] = k.load((const T *)a.r + r * a.r_row);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float v[NC][VEC];
+    float sq = 0.f;
+    unsigned top = 0;
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        Vec<TW, VEC> w;
+        if constexpr (EIGHT) w = k.load((const TW *)a.w);
+        if (a.r) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++) x[c][e] = (T)((float)x[c][e] + (float)res[c][e]);
+            if (live) k.store(x[c], (T *)a.s + r * a.s_row);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            v[c][e] = (float)x[c][e];
+            sq += k.count(e) ? v[c][e] * v[c][e] : 0.f;
+            if constexpr (EIGHT) {
+                v[c][e] *= (float)w[e];
+                top = max(top, __float_as_uint(v[c][e]) & 0x7fffffffu); // (elements that are a neighbour's as well, or zeros behind the end, do no harm)
+            }
+        }
+    }
+    const float inv_w = 1.f / (float)a.width;
+    if constexpr (EIGHT) {
+        row_sum_max<TPR>(sq, top, red);
+        if (!live) return;
+        const Eight q(top);
+        const float rstd = rsqrtf(sq * inv_w + a.eps);
+        if (t == 0) a.out[row] = q.scale(rstd);
+#pragma unroll
+        for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC>(v[c], q), (int8_t *)a.y + r * a.y_row);
+    } else {
+        const float rstd = rsqrtf(row_sum<TPR>(sq, red) * inv_w + a.eps);
+        if (!live) return;
+        if (t == 0) a.out[row] = rstd;
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+            const Vec<TW, VEC> w = k.load((const TW *)a.w);
+            Vec<T, VEC> y;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) y[e] = (T)(v[c][e] * rstd * (float)w[e]);
+            k.store(y, (T *)a.y + r * a.y_row);
+        }
+    }
+}
+
+// Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows.  No atomics: a run repeats bit for bit.
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGradArgs a)
+{
+    constexpr int THREADS = TPR > 256 ? TPR : 256, RPW = THREADS / TPR;
+    __shared__ float red[THREADS / 64];
+    __shared__ float join[RPW > 1 ? (RPW - 1) * TPR * VEC : 1];
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    float dw[NC][VEC];
+    Vec<TW, VEC> w[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        w[c] = Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).load((const TW *)a.w);
+#pragma unroll
+        for (int e = 0; e < VEC; e++) dw[c][e] = 0.f;
+    }
+    const float inv_w = 1.f / (float)a.width;
+    for (int row0 = blockIdx.x * RPW; row0 < a.rows; row0 += gridDim.x * RPW) {
+        Vec<T, VEC> d[NC], s[NC], add[NC];
+        const int64_t r = min(row0 + sub, a.rows - 1);
+        const float rstd = a.rstd[r];
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+            d[c] = k.load((const T *)a.dy + r * a.dy_row);
+            s[c] = k.load((const T *)a.s + r * a.s_row);
+            if (a.add) add[c] = k.load((const T *)a.add + r * a.add_row);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int row = row0 + sub;
+        const bool live = row < a.rows;
+        float c2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                if (!live || !k.count(e)) continue; // (a product with an infinity of no account would not be zero)
+                const float dy = (float)d[c][e], xh = (float)s[c][e] * rstd;
+                c2 += dy * (float)w[c][e] * xh;
+                dw[c][e] += dy * xh;
+            }
+        }
+        c2 = row_sum<TPR>(c2, red) * inv_w;
+        if (!live) continue; // rows of one wave or more: all of its threads; the barriers are behind
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+            const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+            Vec<T, VEC> o;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                float u = rstd * ((float)d[c][e] * (float)w[c][e] - (float)s[c][e] * rstd * c2);
+                if (a.add) u += (float)add[c][e];
+                o[e] = (T)u;
+            }
+            k.store(o, (T *)a.ds + row * a.ds_row);
+        }
+    }
+    float *part = a.part + (size_t)blockIdx.x * a.width;
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        const Cols<VEC, WIDTH> k((c * TPR + t) * VEC, a.width);
+        if constexpr (RPW > 1) {
+            __syncthreads();
+            if (sub > 0)
+#pragma unroll
+                for (int e = 0; e < VEC; e++) join[((sub - 1) * VEC + e) * TPR + t] = dw[c][e];
+            __syncthreads();
+        }
+        if (sub == 0)
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                if (!k.count(e)) continue;
+                float u = dw[c][e];
+                if constexpr (RPW > 1)
+#pragma unroll
+                    for (int i = 0; i < RPW - 1; i++) u += join[(i * VEC + e) * TPR + t];
+                part[k.at + e] = u;
+            }
+    }
+}
+
+// dw from the partial rows: 16 columns per work-group, 16 threads to a column.
+template <class TW> __global__ __launch_bounds__(256) void k_rms_weight_grad(const float *__restrict__ part, int parts, int width, TW *dw)
+{
+    __shared__ float red[256];
+    const int c = threadIdx.x & 15, k0 = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+    const float *p = part + col;
+    float s = 0.f;
+    if (col < width)
+#pragma unroll 8
+        for (int k = k0; k < parts; k += 16) s += p[(size_t)k * width];
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x >= 16 || col >= width) return;
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; k++) s += red[k * 16 + c];
+    dw[col] = (TW)s;
+}
+
+struct Rows8Args {
+    const void *x;
+    int8_t *y;
+    float *scale;
+    int64_t x_row, y_row;
+    int rows, width, first;
+};
+template <class T, int VEC, int TPR, int NC, int WIDTH, bool GELU>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize8(Rows8Args a)
+{
+    constexpr int THREADS = TPR > 256 ? TPR : 256;
+    __shared__ float red[THREADS / 32];
+    const int t = threadIdx.x % TPR, row = a.first + blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    const bool live = row < a.rows;
+    const int64_t r = min(row, a.rows - 1);
+    Vec<T, VEC> x[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) x[c] = Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).load((const T *)a.x + r * a.x_row);
+    __builtin_amdgcn_sched_barrier(0);
+    float v[NC][VEC], none = 0.f;
+    unsigned top = 0;
+#pragma unroll
+    for (int c = 0; c < NC; c++)
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            v[c][e] = (float)x[c][e];
+            if constexpr (GELU) v[c][e] = gelu(v[c][e]);
+            // (elements that are a neighbour's as well, or zeros behind the row's end, do no harm)
+            top = max(top, __float_as_uint(v[c][e]) & 0x7fffffffu);
+        }
+    row_sum_max<TPR>(none, top, red);
+    if (!live) return;
+    const Eight q(top);
+    if (t == 0) a.scale[row] = q.scale(1.f);
+#pragma unroll
+    for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC>(v[c], q), a.y + r * a.y_row);
+}

@@ -277,6 +277,176 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t narg
     });
 }
 
+// x, weight, residual and eps, as both forms of the root-mean-square norm take them; the residual sum
+struct Rms {
+    he_norm n;
+    he_rows x, r, sum;
+    const void *w;
+    bool residual;
+    Tensor s;
+    at::ScalarType type;
+    Rms(const Args &a, PyObject *const *in) : r{}, sum{}
+    {
+        const Tensor &tx = tensor(in[0], "x"), &tw = tensor(in[1], "weight");
+        type = tx.scalar_type();
+        n = {type_of(type), 0, 0, 0, number(in[3])};
+        x = rows_of(a, tx, "x", tx.sizes(), type);
+        if (tx.size(1) > INT32_MAX) refuse("x: ", tx.sizes(), ", rows are too wide");
+        n.weight_type = type_of(tw.scalar_type()), n.rows = tx.size(0), n.width = (int32_t)tx.size(1);
+        w = vector_of(a, tw, "weight", n.width, tw.scalar_type());
+        residual = !none(in[2]);
+        if (residual) {
+            r = rows_of(a, tensor(in[2], "residual"), "residual", tx.sizes(), type);
+            s = dense(tx.sizes(), tx, type);
+            sum = {s.data_ptr(), n.width};
+        }
+    }
+    PyObject *kept(PyObject *x) { return residual ? wrap(s) : same(x); }
+};
+// 8-bit rows begin at multiples of 64 bytes, so that products read them by whole lines; the integers of a row are a view of its `width`.
+struct Eight {
+    Tensor rows, scale, view;
+    he_rows8 d;
+    Eight(const Tensor &like, int64_t n, int64_t width)
+    {
+        const int64_t stride = (width + 63) / 64 * 64;
+        rows = dense({n, stride}, like, at::kChar), scale = dense({n}, like, at::kFloat);
+        view = stride == width ? rows : rows.narrow(1, 0, width);
+        d = {(int8_t *)rows.data_ptr(), stride, (float *)scale.data_ptr()};
+    }
+};
+// 8-bit rows that a product reads, by pieces of 16 bytes
+he_rows8 eight_of(const Args &a, const Tensor &t, const char *what, const Tensor &scale, const char *what_scale)
+{
+    if (t.dim() != 2) refuse(what, ": ", t.sizes(), ", want [rows][width]");
+    const he_rows r = rows_of(a, t, what, t.sizes(), at::kChar);
+    const int64_t rows = t.size(0), width = t.size(1), stride = rows > 1 ? r.stride : (width + 15) / 16 * 16;
+    if (((int64_t)r.d & 15 || stride % 16) && t.numel()) refuse(what, ": address ", r.d, " or stride ", stride, " is not a multiple of 16");
+    if (t.numel() && t.storage().nbytes() < (size_t)(t.storage_offset() + (rows - 1) * stride + (width + 15) / 16 * 16))
+        refuse(what, ": the buffer ends inside a piece of 16 bytes of the last row");
+    return {(int8_t *)r.d, stride, (float *)vector_of(a, scale, what_scale, rows, at::kFloat)};
+}
+
+// x, weight, residual, eps, out
+PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        const Args a(args, nargs, 8);
+        Rms t(a, a.at);
+        const Tensor &x = tensor(a.at[0], "x");
+        Tensor y;
+        he_rows yr;
+        if (none(a.at[4])) {
+            y = dense(x.sizes(), x, t.type);
+            yr = {y.data_ptr(), t.n.width};
+        } else {
+            const Tensor &out = out_of(a.at[4], "out");
+            yr = rows_of(a, out, "out", x.sizes(), t.type);
+            apart(out, "out", {a.at[0], a.at[1], a.at[2]});
+        }
+        Tensor rstd = dense({t.n.rows}, x, at::kFloat);
+        const int32_t rc = he_rms_norm(a.ctx, &t.n, &t.x, t.residual ? &t.r : nullptr, t.w, &yr, t.residual ? &t.sum : nullptr, (float *)rstd.data_ptr(), a.stream);
+        if (rc != HE_OK) return status(rc);
+        if (!y.defined()) written(tensor(a.at[4], "out"));
+        return pack(y.defined() ? wrap(y) : same(a.at[4]), t.kept(a.at[0]), wrap(rstd));
+    });
+}
+
+// dy, s, weight, rstd, ds
+PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        const Args a(args, nargs, 8);
+        const Tensor &s = tensor(a.at[1], "s"), &w = tensor(a.at[2], "weight");
+        const at::ScalarType type = s.scalar_type(), wt = w.scalar_type();
+        he_norm n{type_of(type), type_of(wt), 0, 0, 0.0};
+        const he_rows sr = rows_of(a, s, "s", s.sizes(), type), dyr = rows_of(a, tensor(a.at[0], "dy"), "dy", s.sizes(), type);
+        const int64_t rows = s.size(0), width = s.size(1);
+        if (width > INT32_MAX) refuse("s: ", s.sizes(), ", rows are too wide");
+        n.rows = rows, n.width = (int32_t)width;
+        he_rows ar{};
+        if (!none(a.at[4])) ar = rows_of(a, tensor(a.at[4], "ds"), "ds", s.sizes(), type);
+        const void *wp = vector_of(a, w, "weight", width, wt);
+        const float *rstd = (const float *)vector_of(a, tensor(a.at[3], "rstd"), "rstd", rows, at::kFloat);
+        size_t need = 0;
+        if (const int32_t rc = he_rms_norm_workspace_bytes(a.ctx, &n, &need)) return status(rc);
+        Tensor dx = dense(s.sizes(), s, type), dw = dense({width}, w, wt);
+        const Tensor ws = scratch(s, need);
+        const he_rows xr{dx.data_ptr(), width};
+        const int32_t rc = he_rms_norm_grad(a.ctx, &n, &dyr, &sr, wp, rstd, none(a.at[4]) ? nullptr : &ar, &xr, dw.data_ptr(), address(ws), need, a.stream);
+        if (rc != HE_OK) return status(rc);
+        return pack(wrap(dx), wrap(dw));
+    });
+}
+
+// x, weight, residual, eps
+PyObject *rms_norm8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        const Args a(args, nargs, 7);
+        Rms t(a, a.at);
+        Eight y(tensor(a.at[0], "x"), t.n.rows, t.n.width);
+        const int32_t rc = he_rms_norm8(a.ctx, &t.n, &t.x, t.residual ? &t.r : nullptr, t.w, &y.d, t.residual ? &t.sum : nullptr, a.stream);
+        if (rc != HE_OK) return status(rc);
+        return pack(wrap(y.view), wrap(y.scale), t.kept(a.at[0]));
+    });
+}
+
+// x, gelu
+PyObject *quantize8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        const Args a(args, nargs, 5);
+        const Tensor &x = tensor(a.at[0], "x");
+        const int gelu = PyObject_IsTrue(a.at[1]);
+        if (gelu < 0) throw python_error();
+        const int32_t type = type_of(x.scalar_type());
+        const he_rows xr = rows_of(a, x, "x", x.sizes(), x.scalar_type());
+        if (x.size(1) > INT32_MAX) refuse("x: ", x.sizes(), ", rows are too wide");
+        Eight y(x, x.size(0), x.size(1));
+        const int32_t rc = he_quantize8(a.ctx, type, x.size(0), (int32_t)x.size(1), gelu, &xr, &y.d, a.stream);
+        if (rc != HE_OK) return status(rc);
+        return pack(wrap(y.view), wrap(y.scale));
+    });
+}
+
+// x8, scale, w8, w_scale, bias, dtype, out
+PyObject *linear8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        const Args a(args, nargs, 10);
+        const Tensor &x = tensor(a.at[0], "x8"), &w = tensor(a.at[2], "w8");
+        const he_rows8 xr = eight_of(a, x, "x8", tensor(a.at[1], "scale"), "scale"), wr = eight_of(a, w, "w8", tensor(a.at[3], "w_scale"), "w_scale");
+        const int64_t rows = x.size(0), width = x.size(1), channels = w.size(0), shape[2] = {rows, channels};
+        if (w.size(1) != width) refuse("w8: ", w.sizes(), ", want [channels][", width, "]");
+        if (width > INT32_MAX || channels > INT32_MAX) refuse("w8: ", w.sizes(), " is too large");
+        if (!THPDtype_Check(a.at[5])) refuse("dtype: want a torch.dtype");
+        const at::ScalarType dtype = ((THPDtype *)a.at[5])->scalar_type;
+        he_product8 p{type_of(dtype), HE_F32, rows, (int32_t)width, (int32_t)channels};
+        const void *bias = nullptr;
+        if (!none(a.at[4])) {
+            const Tensor &b = tensor(a.at[4], "bias");
+            p.bias_type = type_of(b.scalar_type());
+            bias = vector_of(a, b, "bias", channels, b.scalar_type());
+        }
+        Tensor o;
+        he_rows orows;
+        if (none(a.at[6])) {
+            o = dense(shape, x, dtype);
+            orows = {o.data_ptr(), channels};
+        } else {
+            const Tensor &out = out_of(a.at[6], "out");
+            orows = rows_of(a, out, "out", shape, dtype);
+            apart(out, "out", {a.at[0], a.at[1], a.at[2], a.at[3], a.at[4]});
+        }
+        const int32_t rc = he_linear8(a.ctx, &p, &xr, &wr, bias, &orows, a.stream);
+        if (rc != HE_OK) return status(rc);
+        if (o.defined()) return wrap(o);
+        written(tensor(a.at[6], "out"));
+        return same(a.at[6]);
+    });
+}
+
 // x, offsets, out
 PyObject *pool_mean(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -464,7 +634,8 @@ PyObject *attention_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(layer_norm), ENTRY(layer_norm_backward), ENTRY(pool_mean), ENTRY(pool_mean_backward),
-                         ENTRY(attention),  ENTRY(attention_backward),  {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(attention),  ENTRY(attention_backward),  ENTRY(rms_norm), ENTRY(rms_norm_backward),
+                         ENTRY(rms_norm8),  ENTRY(quantize8),           ENTRY(linear8),   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "he_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
