@@ -10,40 +10,32 @@ typedef f16 T;
 typedef bf16 T;
 #endif
 
-template <int MB, int NB> static void tiles(he_ctx *c, hipStream_t st, double bytes, Linear8Args a)
+template <int MB, int NB, int WM, int WN, int G, int OCC, bool PART = false> static void tiles(he_ctx *c, hipStream_t st, double bytes, Linear8Args a)
 {
-    a.tiles_m = (a.rows + 64 * MB - 1) / (64 * MB), a.tiles_n = (a.channels + 64 * NB - 1) / (64 * NB);
-    KLAUNCH_T(c, st, KID_LINEAR8, bytes, (k_linear8<T, MB, NB>), (unsigned)(a.tiles_m * a.tiles_n), 256, a);
+    constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN;
+    a.tiles_m = (a.rows + BM - 1) / BM, a.tiles_n = (a.channels + BN - 1) / BN;
+    KLAUNCH_T(c, st, KID_LINEAR8, bytes, (k_linear8<T, MB, NB, WM, WN, G, OCC, PART>), dim3((unsigned)(a.tiles_m * a.tiles_n), PART ? a.splits : 1), 64 * WM * WN * G, a);
 }
-template <int MB> static void few(he_ctx *c, hipStream_t st, double bytes, int waves, const Linear8Args &a)
-{
-    const dim3 grid((unsigned)((a.channels + 15) / 16), (unsigned)((a.rows + 16 * MB - 1) / (16 * MB)));
-    KLAUNCH_T(c, st, KID_LINEAR8_FEW, bytes, (k_linear8_few<T, MB>), grid, 64 * waves, a);
-}
-
 static void product(he_ctx *c, hipStream_t st, double bytes, int tile, const Linear8Args &a)
 {
-    if (tile == 256)
-        tiles<4, 4>(c, st, bytes, a);
-    else if (tile == 128)
-        tiles<2, 2>(c, st, bytes, a);
-    else
-        tiles<1, 1>(c, st, bytes, a);
-}
-static void product_few(he_ctx *c, hipStream_t st, double bytes, int blocks, int waves, const Linear8Args &a)
-{
-    if (blocks == 1)
-        few<1>(c, st, bytes, waves, a);
-    else if (blocks == 2)
-        few<2>(c, st, bytes, waves, a);
-    else
-        few<4>(c, st, bytes, waves, a);
+    if (tile == LINEAR8_256)
+        tiles<4, 2, 2, 4, 1, 2>(c, st, bytes, a);
+    else if (tile == LINEAR8_128)
+        tiles<2, 1, 2, 4, 1, 4>(c, st, bytes, a);
+    else if (tile == LINEAR8_64)
+        tiles<1, 1, 2, 2, 1, 4>(c, st, bytes, a);
+    else if (a.splits == 1)
+        tiles<1, 1, 2, 2, 4, 4>(c, st, bytes, a);
+    else {
+        tiles<1, 1, 2, 2, 4, 4, true>(c, st, bytes, a);
+        const double part = 4.0 * a.splits * a.rows * a.channels;
+        KLAUNCH(c, st, KID_LINEAR8_JOIN, part + (double)sizeof(T) * a.rows * a.channels, (k_linear8_join<T>), (unsigned)((a.rows * (int64_t)((a.channels + 3) / 4) + 255) / 256), a);
+    }
 }
 
 #define NAME_(t) linear8_launch_##t
 #define NAME(t) NAME_(t)
 void NAME(HE_TYPE)(Linear8Launch &t)
 {
-    t.tiles = product;
-    t.few = product_few;
+    t.product = product;
 }

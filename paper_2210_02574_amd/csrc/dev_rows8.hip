@@ -23,15 +23,26 @@ template <int TPR, class A, class F> static void by_rows(const A &a, F f)
     }
 }
 
-template <bool EIGHT> static void rms(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const RmsArgs &a)
+static void rms(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const RmsArgs &a)
 {
     row_shape(a.width, [&](auto tpr, auto nc, auto kind) {
         by_rows<tpr>(a, [&](int threads, unsigned grid, const RmsArgs &part) {
-            constexpr int kid = EIGHT ? KID_RMS8 : KID_RMS;
             if (wide_w)
-                KLAUNCH_T(c, st, kid, bytes, (k_rms_norm<T, float, VEC, tpr, nc, kind, EIGHT>), grid, threads, part);
+                KLAUNCH_T(c, st, KID_RMS, bytes, (k_rms_norm<T, float, VEC, tpr, nc, kind>), grid, threads, part);
             else
-                KLAUNCH_T(c, st, kid, bytes, (k_rms_norm<T, T, VEC, tpr, nc, kind, EIGHT>), grid, threads, part);
+                KLAUNCH_T(c, st, KID_RMS, bytes, (k_rms_norm<T, T, VEC, tpr, nc, kind>), grid, threads, part);
+            bytes = 0.0; // the profile counts them once
+        });
+    });
+}
+static void rms8(he_ctx *c, hipStream_t st, double bytes, bool wide_w, const RmsArgs &a)
+{
+    row_shape(a.width, [&](auto tpr, auto nc, auto kind) {
+        by_rows<tpr>(a, [&](int threads, unsigned grid, const RmsArgs &part) {
+            if (wide_w)
+                KLAUNCH_T(c, st, KID_RMS8, bytes, (k_rms_norm8<T, float, VEC, tpr, nc, kind>), grid, threads, part);
+            else
+                KLAUNCH_T(c, st, KID_RMS8, bytes, (k_rms_norm8<T, T, VEC, tpr, nc, kind>), grid, threads, part);
             bytes = 0.0; // the profile counts them once
         });
     });
@@ -71,8 +82,8 @@ static void quantize(he_ctx *c, hipStream_t st, double bytes, bool gelu, const R
 #define NAME(t) NAME_(t)
 void NAME(HE_TYPE)(Rows8Launch &t)
 {
-    t.rms = rms<false>;
-    t.rms8 = rms<true>;
+    t.rms = rms;
+    t.rms8 = rms8;
     t.rms_grad = rms_grad;
     t.weight_grad = weight_grad;
     t.quantize = quantize;

@@ -61,11 +61,10 @@ void rows8_launch_0(Rows8Launch &t);
 void rows8_launch_1(Rows8Launch &t);
 void rows8_launch_2(Rows8Launch &t);
 
+// Tiles of a product: rows and channels of a work-group; LINEAR8_LONG: 64 of each, with four groups of waves on the sum.
+enum { LINEAR8_256, LINEAR8_128, LINEAR8_64, LINEAR8_LONG };
 struct Linear8Launch {
-    // tile: rows and channels of a work-group, 64, 128 or 256
-    void (*tiles)(he_ctx *c, hipStream_t st, double bytes, int tile, const Linear8Args &a);
-    // blocks: of 16 rows to a work-group, 1, 2 or 4; waves that share a sum, up to 16
-    void (*few)(he_ctx *c, hipStream_t st, double bytes, int blocks, int waves, const Linear8Args &a);
+    void (*product)(he_ctx *c, hipStream_t st, double bytes, int tile, const Linear8Args &a);
 };
 void linear8_launch_0(Linear8Launch &t);
 void linear8_launch_1(Linear8Launch &t);

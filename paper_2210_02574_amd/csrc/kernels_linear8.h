@@ -1,8 +1,8 @@
 // Product of 8-bit rows and 8-bit weights, both dense along the sum: o[m][n] = (sum over k of x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n].
 //
-// Sums are exact in 32-bit integers.  A sum over 32 (or 64) numbers is one matrix instruction, whose operands are 16 bytes of a row for each lane: bytes of x and w
-// that a lane holds side by side are multiplied, so any order along k serves as long as both use it.
-// Weights are operand A, rows of x operand B: a lane then holds neighbouring channels of one row, which it can write together.
+// Sums are exact in 32-bit integers.  A matrix instruction multiplies blocks of 32 x 32 numbers, whose operands are 16 bytes of a row for each lane: bytes of x and w
+// that lanes hold in the same places are multiplied, so any order along k serves as long as both use it.
+// Weights are operand A, rows of x operand B: a lane then holds four neighbouring channels of one row, which it can write together.
 #pragma once
 #include "enc_common.h"
 
@@ -18,36 +18,10 @@ struct Linear8Args {
     int rows, width, channels;
     int tiles_m, tiles_n;
     int bias32;
+    int *part;  // [splits][rows][channels], where the sum is cut: the sums of each part
+    int splits; // parts of the sum, each of `stages` stages of it
+    int stages;
 };
-
-// Results of one row, N neighbouring channels from n on.
-template <class T, int N> __device__ __forceinline__ Vec<T, N> linear8_results(const Linear8Args &a, const int (&sum)[N], float xs, int n)
-{
-    Vec<T, N> y;
-    Vec<float, N> ws = {}, b = {};
-    if (n + N <= a.channels) {
-        ws = *(const typename UnalignedVec<float, N>::type *)(a.w_scale + n);
-        if (a.bias && a.bias32) b = *(const typename UnalignedVec<float, N>::type *)((const float *)a.bias + n);
-        if (a.bias && !a.bias32) {
-            const Vec<T, N> t = *(const typename UnalignedVec<T, N>::type *)((const T *)a.bias + n);
-#pragma unroll
-            for (int e = 0; e < N; e++) b[e] = (float)t[e];
-        }
-    } else
-#pragma unroll
-        for (int e = 0; e < N; e++)
-            if (n + e < a.channels) {
-                ws[e] = a.w_scale[n + e];
-                if (a.bias) b[e] = a.bias32 ? ((const float *)a.bias)[n + e] : (float)((const T *)a.bias)[n + e];
-            }
-#pragma unroll
-    for (int e = 0; e < N; e++) {
-        float f = (float)sum[e] * xs * ws[e];
-        if (a.bias) f += b[e];
-        y[e] = (T)f;
-    }
-    return y;
-}
 
 // 16 bytes for each lane from `at` of a buffer (zeros behind its end) to LDS, lane i's at to + 16 i, with no register in between.
 // (Not in the template itself: the host's pass knows no such size and would drop the instance.)
@@ -57,71 +31,78 @@ __device__ __forceinline__ void fetch_lds(__amdgpu_buffer_rsrc_t from, unsigned 
 }
 
 #define LINEAR8_K 128 // numbers of a row that a stage holds
+// Chunk c of 16 bytes of row r lies at c ^ (r / 2 mod 8) of the row's 128 bytes in LDS: the 16 rows that a 16-byte read takes at a time then lie in 16 different places.
+__device__ __forceinline__ int linear8_twist(int row) { return row >> 1 & 7; }
 
-// Tiles of 64 MB rows by 64 NB channels, 2 x 2 waves with MB x NB blocks of 32 x 32 each.  A stage is 128 bytes of every row of both, written to LDS by
-// the loads themselves, chunk c of row r at c ^ (r / 2 mod 8): the 16 rows that a 16-byte read of LDS takes at a time then lie in 16 different places.  There are two stages; the loads of one
-// are under way for the whole of the other.  Per stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
-template <class T, int MB, int NB> __global__ __launch_bounds__(256) void k_linear8(Linear8Args a)
+// Tiles of 32 MB WM rows by 32 NB WN channels, WM x WN waves with MB x NB blocks of 32 x 32 each; G such groups of waves share the sum, each taking every G-th
+// stage; PART: blockIdx.y's part of the sum alone, left as it is.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
+// stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
+template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
 {
-    constexpr int BM = 64 * MB, BN = 64 * NB, STAGE = (BM + BN) * LINEAR8_K;
-    constexpr int OUT_PITCH = 32 * NB * (int)sizeof(T) + 16; // of a row of results in LDS, bytes
-    constexpr int OUT_BYTES = 4 * 32 * OUT_PITCH, LDS = 2 * STAGE > OUT_BYTES ? 2 * STAGE : OUT_BYTES;
+    static_assert(G == 1 ? !PART : G == 4 && MB == 1 && NB == 1, "");
+    constexpr int W = WM * WN, THREADS = 64 * W * G, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * LINEAR8_K;
+    constexpr int SIZE = (int)sizeof(T), VEC = 16 / SIZE;
+    constexpr int COLS = G == 1 ? 32 * NB : BN, PITCH = COLS * SIZE + 16; // of a row of results in LDS, bytes
+    constexpr int OUT = G == 1 ? W * 32 * PITCH : G * W * 4096 + BM * PITCH, LDS = G * 2 * STAGE > OUT ? G * 2 * STAGE : OUT;
     __shared__ __attribute__((aligned(1024))) int8_t lds[LDS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+    __shared__ __attribute__((aligned(16))) float sx[BM], sw[BN], sb[BN];
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % W, group = all / W, wm = wave % WM, wn = wave / WM;
 
     // Each of the eight dies takes a run of tiles that follow one another, in bands of eight tiles of rows, so that they share operands in its L2.
-    const int tiles = a.tiles_m * a.tiles_n, per = tiles / 8, extra = tiles % 8, die = blockIdx.x % 8, at = blockIdx.x / 8;
-    const int id = die * per + min(die, extra) + at;
+    const int tiles = a.tiles_m * a.tiles_n, per = tiles / 8, extra = tiles % 8, die = blockIdx.x % 8;
+    const int id = die * per + min(die, extra) + blockIdx.x / 8;
     constexpr int BAND = 8;
     const int band = id / (BAND * a.tiles_n), first = band * BAND, high = min(BAND, a.tiles_m - first), in = id - band * BAND * a.tiles_n;
     const int m0 = (first + in % high) * BM, n0 = in / high * BN;
 
-    const int steps = (a.width + LINEAR8_K - 1) / LINEAR8_K;
-    const int whole = (a.width + 15) / 16 * 16; // bytes of a row that may be read
-    const int rows_m = min(BM, a.rows - m0), rows_n = min(BN, a.channels - n0);
-    const int8_t *const xb = a.x + m0 * a.x_row, *const wb = a.w + n0 * a.w_row;
-    const int bytes_m = (rows_m - 1) * (int)a.x_row + whole, bytes_n = (rows_n - 1) * (int)a.w_row + whole; // below 2^31, as strides are below 2^23
-    // One load of a wave brings eight rows; wave v takes every fourth eight of them.
-    constexpr int LM = BM / 32, LN = BN / 32;
+    const int k0 = PART ? blockIdx.y * a.stages * LINEAR8_K : 0, width = PART ? min(a.width - k0, a.stages * LINEAR8_K) : a.width;
+    const int steps = (width + LINEAR8_K - 1) / LINEAR8_K, rounds = (steps + G - 1) / G, tail = width % LINEAR8_K;
+    const int whole = (width + 15) / 16 * 16; // bytes of a row that may be read
+    const int8_t *const xb = a.x + m0 * a.x_row + k0, *const wb = a.w + n0 * a.w_row + k0;
+    const int bytes_m = (min(BM, a.rows - m0) - 1) * (int)a.x_row + whole, bytes_n = (min(BN, a.channels - n0) - 1) * (int)a.w_row + whole; // below 2^31: strides are below 2^23
+    // One load of a wave brings eight rows.
+    constexpr int LM = BM / 8 / W, LN = BN / 8 / W;
+    static_assert(LM * 8 * W == BM && LN * 8 * W == BN, "");
     unsigned at_m[LM], at_n[LN];
 #pragma unroll
     for (int i = 0; i < LM; i++) {
-        const int row = 8 * (4 * i + wave) + lane / 8, c = (lane % 8) ^ (row >> 1 & 7);
-        at_m[i] = (unsigned)row * (unsigned)a.x_row + 16 * c;
+        const int row = 8 * (W * i + wave) + lane / 8;
+        at_m[i] = (unsigned)row * (unsigned)a.x_row + 16 * (lane % 8 ^ linear8_twist(row));
     }
 #pragma unroll
     for (int i = 0; i < LN; i++) {
-        const int row = 8 * (4 * i + wave) + lane / 8, c = (lane % 8) ^ (row >> 1 & 7);
-        at_n[i] = (unsigned)row * (unsigned)a.w_row + 16 * c;
+        const int row = 8 * (W * i + wave) + lane / 8;
+        at_n[i] = (unsigned)row * (unsigned)a.w_row + 16 * (lane % 8 ^ linear8_twist(row));
     }
-    const auto fetch = [&](int step, int8_t *stage) {
-        const int k = step * LINEAR8_K; // below the width
+    int8_t *const mine = lds + group * 2 * STAGE;
+    const auto fetch = [&](int step, int8_t *stage) { // step < steps
+        const int k = step * LINEAR8_K;
         const __amdgpu_buffer_rsrc_t rm = __builtin_amdgcn_make_buffer_rsrc((void *)(xb + k), 0, bytes_m - k, 0x00027000);
         const __amdgpu_buffer_rsrc_t rn = __builtin_amdgcn_make_buffer_rsrc((void *)(wb + k), 0, bytes_n - k, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < LM; i++)
-            fetch_lds(rm, at_m[i], stage + (4 * i + wave) * 1024);
+        for (int i = 0; i < LM; i++) fetch_lds(rm, at_m[i], stage + (W * i + wave) * 1024);
 #pragma unroll
-        for (int i = 0; i < LN; i++)
-            fetch_lds(rn, at_n[i], stage + BM * LINEAR8_K + (4 * i + wave) * 1024);
+        for (int i = 0; i < LN; i++) fetch_lds(rn, at_n[i], stage + BM * LINEAR8_K + (W * i + wave) * 1024);
     };
-    // Behind the end of the sum: weights of a stage's numbers from `left` on become zeros, so that what x's rows have there does not count.
-    const auto cut = [&](int8_t *stage, int left) {
-        for (int row = threadIdx.x; row < BN; row += 256) {
-            int8_t *const r = stage + BM * LINEAR8_K + row * LINEAR8_K;
-            for (int c = left / 16; c < 8; c++) {
-                int8_t *const p = r + 16 * (c ^ (row >> 1 & 7));
-                for (int b = max(left - 16 * c, 0); b < 16; b++) p[b] = 0;
-            }
-        }
-        __syncthreads();
-    };
-
     // Loads that write to LDS are waited for by hand: the barrier's own wait does not cover them.
     const auto arrive = [&] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
+    // Behind the end of the sum: weights of its last stage from number `tail` on become zeros, so that what x's rows have there does not count.  All of a work-group
+    // take part.
+    const auto cut = [&](int8_t *stage) {
+        for (int row = threadIdx.x; row < BN; row += THREADS) {
+            int8_t *const r = stage + (BM + row) * LINEAR8_K;
+            for (int c = tail / 16; c < 8; c++) {
+                int8_t *const p = r + 16 * (c ^ linear8_twist(row));
+                for (int b = max(tail - 16 * c, 0); b < 16; b++) p[b] = 0;
+            }
+        }
+        __syncthreads();
+    };
+    const int last_round = (steps - 1) / G, last_group = (steps - 1) % G; // where the last stage is
+    int8_t *const last_stage = lds + (last_group * 2 + (last_round & 1)) * STAGE;
 
     i32x16 acc[MB][NB];
 #pragma unroll
@@ -131,114 +112,140 @@ template <class T, int MB, int NB> __global__ __launch_bounds__(256) void k_line
     i32x4 fx[2][MB], fw[2][NB];
     // operands of the numbers 32 kk .. of a stage: lane's row l mod 32 of each block, 16 numbers
     const auto read = [&](const int8_t *stage, int kk, int to) {
-        const int row = lane % 32, c = (2 * kk + lane / 32) ^ (row >> 1 & 7);
-#pragma unroll
-        for (int i = 0; i < MB; i++) fx[to][i] = *(const i32x4 *)(stage + (32 * (MB * wm + i) + row) * LINEAR8_K + 16 * c);
+        const int row = lane % 32, c = (2 * kk + lane / 32) ^ linear8_twist(row);
 #pragma unroll
         for (int j = 0; j < NB; j++) fw[to][j] = *(const i32x4 *)(stage + (BM + 32 * (NB * wn + j) + row) * LINEAR8_K + 16 * c);
+#pragma unroll
+        for (int i = 0; i < MB; i++) fx[to][i] = *(const i32x4 *)(stage + (32 * (MB * wm + i) + row) * LINEAR8_K + 16 * c);
     };
 
-    fetch(0, lds);
-    if (steps > 1) fetch(1, lds + STAGE);
+    if (group < steps) fetch(group, mine);
+    if (group + G < steps) fetch(group + G, mine + STAGE);
+    for (int i = threadIdx.x; !PART && i < BM + BN; i += THREADS) {
+        if (i < BM)
+            sx[i] = a.x_scale[min(m0 + i, a.rows - 1)];
+        else {
+            const int n = min(n0 + i - BM, a.channels - 1);
+            sw[i - BM] = a.w_scale[n];
+            sb[i - BM] = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[n] : (float)((const T *)a.bias)[n];
+        }
+    }
     arrive();
-    if (steps == 1 && a.width % LINEAR8_K) cut(lds, a.width);
-    read(lds, 0, 0);
-    for (int t = 0; t < steps; t++) {
-        int8_t *const here = lds + (t & 1) * STAGE, *const next = lds + (~t & 1) * STAGE;
+    if (last_round == 0 && tail) cut(last_stage);
+    read(mine, 0, 0);
+    for (int t = 0; t < rounds; t++) {
+        int8_t *const here = mine + (t & 1) * STAGE, *const next = mine + (~t & 1) * STAGE;
+        const bool some = G == 1 || t * G + group < steps;
 #pragma unroll
         for (int kk = 0; kk < 4; kk++) {
             if (kk < 3)
                 read(here, kk + 1, (kk + 1) & 1);
             else {
                 arrive(); // the next stage is there, and nobody reads this one any more
-                if (t + 1 < steps) {
-                    if (t + 2 == steps && a.width % LINEAR8_K) cut(next, a.width - (t + 1) * LINEAR8_K);
+                if (t + 1 < rounds) {
+                    if (t + 1 == last_round && tail) cut(last_stage);
                     read(next, 0, 0);
                 }
-                if (t + 2 < steps) fetch(t + 2, here);
+                if ((t + 2) * G + group < steps) fetch((t + 2) * G + group, here);
             }
+            if (some)
 #pragma unroll
-            for (int i = 0; i < MB; i++)
+                for (int i = 0; i < MB; i++)
 #pragma unroll
-                for (int j = 0; j < NB; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][j], fx[kk & 1][i], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < NB; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][j], fx[kk & 1][i], acc[i][j], 0, 0, 0);
         }
     }
 
-    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  32 rows at a time go through a part of LDS that is the wave's own and leave it as whole rows.
-    int8_t *const own = lds + wave * 32 * OUT_PITCH;
-    constexpr int VEC = 16 / (int)sizeof(T), CHUNKS = 32 * NB / VEC; // a row's 16-byte pieces
+    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as whole pieces of rows, with no lines kept: the next kernel begins
+    // with another L2, and what is written early need not be when this one ends.
+    const int row = lane % 32, h = lane / 32;
+    const auto scaled = [&](const i32x4 s, float xs, int col) {
+        const f32x4 ws = *(const f32x4 *)(sw + col), b = *(const f32x4 *)(sb + col);
+        Vec<T, 4> y;
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[e] = (T)fmaf((float)s[e] * xs, ws[e], b[e]);
+        return y;
+    };
+    const auto store = [&](const Vec<T, VEC> y, int m, int n) {
+        if (m >= a.rows) return;
+        T *const to = (T *)a.o + m * a.o_row;
+        if (n + VEC <= a.channels)
+            __builtin_nontemporal_store(y, (typename UnalignedVec<T, VEC>::type *)(to + n));
+        else
+            store_vec<T, VEC>(y, to, n, a.channels);
+    };
     __syncthreads();
+    if constexpr (G == 1) { // 32 rows at a time, by each wave in a part of its own
+        int8_t *const own = lds + wave * 32 * PITCH;
+        constexpr int CHUNKS = COLS / VEC, PER = CHUNKS / 2;
 #pragma unroll
-    for (int i = 0; i < MB; i++) {
-        const int m = m0 + 32 * (MB * wm + i), row = lane % 32;
-        const float xs = a.x_scale[min(m + row, a.rows - 1)];
+        for (int i = 0; i < MB; i++) {
+            const int m = 32 * (MB * wm + i);
+            const float xs = sx[m + row];
 #pragma unroll
-        for (int j = 0; j < NB; j++)
+            for (int j = 0; j < NB; j++)
 #pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const int col = 32 * j + 8 * g + 4 * (lane / 32);
-                int sum[4];
+                for (int g = 0; g < 4; g++) {
+                    const int col = 32 * j + 8 * g + 4 * h;
+                    const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                    *(Vec<T, 4> *)(own + row * PITCH + col * SIZE) = scaled(s, xs, COLS * wn + col);
+                }
+            __builtin_amdgcn_wave_barrier();
+            Vec<T, VEC> y[PER];
 #pragma unroll
-                for (int e = 0; e < 4; e++) sum[e] = acc[i][j][4 * g + e];
-                *(Vec<T, 4> *)(own + row * OUT_PITCH + col * (int)sizeof(T)) = linear8_results<T, 4>(a, sum, xs, n0 + 32 * NB * wn + col);
-            }
-        __builtin_amdgcn_wave_barrier();
-        for (int p = lane; p < 32 * CHUNKS; p += 64) {
-            const int r = p / CHUNKS, c = p % CHUNKS, n = n0 + 32 * NB * wn + c * VEC;
-            const Vec<T, VEC> y = *(const Vec<T, VEC> *)(own + r * OUT_PITCH + 16 * c);
-            if (m + r < a.rows) store_vec<T, VEC>(y, (T *)a.o + (m + r) * a.o_row, n, a.channels);
+            for (int p = 0; p < PER; p++) y[p] = *(const Vec<T, VEC> *)(own + (p * 64 + lane) / CHUNKS * PITCH + 16 * (lane % CHUNKS));
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < PER; p++) store(y[p], m0 + m + (p * 64 + lane) / CHUNKS, n0 + COLS * wn + lane % CHUNKS * VEC);
         }
-        __builtin_amdgcn_wave_barrier();
+    } else { // each group joins a quarter of the groups' sums of each block
+        i32x4 *const join = (i32x4 *)lds + wave * G * G * 64; // [group][quarter][lane]
+#pragma unroll
+        for (int g = 0; g < G; g++) join[(group * G + g) * 64 + lane] = i32x4{acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2], acc[0][0][4 * g + 3]};
+        __syncthreads();
+        i32x4 s = join[group * 64 + lane];
+#pragma unroll
+        for (int g = 1; g < G; g++) s += join[(g * G + group) * 64 + lane];
+        int8_t *const out = lds + G * W * 4096;
+        const int m = 32 * wm + row, col = 32 * wn + 8 * group + 4 * h;
+        if constexpr (PART) {
+            const int n = n0 + col;
+            if (m0 + m >= a.rows) return;
+            store_vec<int, 4>(s, a.part + ((size_t)blockIdx.y * a.rows + m0 + m) * a.channels, n, a.channels);
+            return;
+        }
+        *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
+        __syncthreads();
+        constexpr int CHUNKS = COLS / VEC;
+        for (int p = threadIdx.x; p < BM * CHUNKS; p += THREADS)
+            store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), m0 + p / CHUNKS, n0 + p % CHUNKS * VEC);
     }
 }
 
-// Few rows: 16 channels and 16 MB rows to a work-group, whose waves share the sum; operands come from memory straight into registers, each once, and the waves' sums are
-// joined in LDS.
-template <class T, int MB> __global__ __launch_bounds__(1024) void k_linear8_few(Linear8Args a)
+// The parts' sums joined and scaled: a thread has four channels of a row.
+template <class T> __global__ __launch_bounds__(256) void k_linear8_join(Linear8Args a)
 {
-    __shared__ i32x4 join[16][MB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MB;
-    const int row = lane % 16, part = lane / 16 * 16;
-    const int8_t *const w = a.w + (int64_t)min(n0 + row, a.channels - 1) * a.w_row;
-    const int8_t *x[MB];
+    const int fours = (a.channels + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = i / fours;
+    const int n = (int)(i % fours) * 4;
+    if (m >= a.rows) return;
+    i32x4 s = {};
+    for (int k = 0; k < a.splits; k += 4) { // four parts' reads under way together
+        i32x4 v[4];
 #pragma unroll
-    for (int i = 0; i < MB; i++) x[i] = a.x + (int64_t)min(m0 + 16 * i + row, a.rows - 1) * a.x_row;
-    i32x4 acc[MB];
+        for (int u = 0; u < 4; u++) v[u] = load_vec<int, 4>(a.part + ((size_t)min(k + u, a.splits - 1) * a.rows + m) * a.channels, n, a.channels);
 #pragma unroll
-    for (int i = 0; i < MB; i++) acc[i] = i32x4{};
-    const int last = (a.width - 1) / 16 * 16; // the last piece of a row
-    constexpr int U = 4;
-    for (int k0 = wave * 64; k0 < a.width; k0 += waves * 64 * U) {
-        i32x4 fw[U], fx[U][MB];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int k = min(k0 + u * waves * 64 + part, last); // behind the end the last piece again, which does not count
-            fw[u] = *(const i32x4 *)(w + k);
-#pragma unroll
-            for (int i = 0; i < MB; i++) fx[u][i] = *(const i32x4 *)(x[i] + k);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int left = a.width - (k0 + u * waves * 64 + part); // numbers of the piece that count
-            if (left < 16)
-#pragma unroll
-                for (int e = 0; e < 4; e++) fw[u][e] &= left >= 4 * e + 4 ? -1 : left <= 4 * e ? 0 : (int)((1u << 8 * (left - 4 * e)) - 1);
-#pragma unroll
-            for (int i = 0; i < MB; i++) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u][i], acc[i], 0, 0, 0);
-        }
+        for (int u = 0; u < 4; u++)
+            if (k + u < a.splits) s += v[u];
     }
+    const float xs = a.x_scale[m];
+    Vec<T, 4> y;
 #pragma unroll
-    for (int i = 0; i < MB; i++) join[wave][i][lane] = acc[i];
-    __syncthreads();
-    for (int i = wave; i < MB; i += waves) {
-        i32x4 s = join[0][i][lane];
-        for (int k = 1; k < waves; k++) s += join[k][i][lane];
-        // a lane has channels 4 (l / 16) .. of row l mod 16
-        const int m = m0 + 16 * i + row, n = n0 + lane / 16 * 4;
-        if (m >= a.rows) continue;
-        const int sum[4] = {s[0], s[1], s[2], s[3]};
-        store_vec<T, 4>(linear8_results<T, 4>(a, sum, a.x_scale[m], n), (T *)a.o + m * a.o_row, n, a.channels);
+    for (int e = 0; e < 4; e++) {
+        const int c = min(n + e, a.channels - 1);
+        const float b = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[c] : (float)((const T *)a.bias)[c];
+        y[e] = (T)fmaf((float)s[e] * xs, a.w_scale[c], b);
     }
+    store_vec<T, 4>(y, (T *)a.o + m * a.o_row, n, a.channels);
 }

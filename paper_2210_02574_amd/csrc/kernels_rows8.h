@@ -123,8 +123,7 @@ template <int VEC> __device__ __forceinline__ Vec<int8_t, VEC> eight_vec(const f
     return v;
 }
 
-template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm(RmsArgs a)
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __device__ __forceinline__ void rms_norm_rows(const RmsArgs &a)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
     __shared__ float red[THREADS / 32];
@@ -185,6 +184,17 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm(RmsArgs a)
             k.store(y, (T *)a.y + r * a.y_row);
         }
     }
+}
+
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm(RmsArgs a)
+{
+    rms_norm_rows<T, TW, VEC, TPR, NC, WIDTH, false>(a);
+}
+template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm8(RmsArgs a)
+{
+    rms_norm_rows<T, TW, VEC, TPR, NC, WIDTH, true>(a);
 }
 
 // Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows.  No atomics: a run repeats bit for bit.
