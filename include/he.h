@@ -383,16 +383,14 @@ int32_t he_rms_norm8(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_r
                      const he_rows *sum, void *stream);
 /* Product of 8-bit rows and 8-bit weights: o[m][n] = (sum over k of x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n], of type `type`.  The sums are exact; a result
  * takes three roundings to 32 bits (the sum's, its product with x_scale, that with w_scale together with the bias's addition) and one to its type.  width (of k)
- * at most 65536, strides below 2^23 bytes; HE_EINVAL also: more than 2^31 - 65536 rows, 2^24 channels or 2^22 work-groups (tiles of 64 to 256 rows and channels).
+ * at most 65536, strides below 2^23 bytes; HE_EINVAL also: more than 2^31 - 65536 rows, 2^24 channels or 2^22 work-groups (tiles of up to 256 rows and channels).
  * bias_type: HE_F32 or `type`; d_bias NULL: no bias. */
 typedef struct {
     int32_t type, bias_type;
     int64_t rows;
     int32_t width, channels;
 } he_product8;
-int32_t he_linear8_workspace_bytes(const he_ctx *ctx, const he_product8 *p, size_t *out);
-int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *d_ws, size_t ws_bytes,
-                   void *stream);
+int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *stream);
 
 /* Mean over the rows of each sequence, d_e [count][width] in 32 bits, zeros for an empty one; and its gradient, dx = de / length on the rows of
  * each sequence.  fill: rows of no sequence are set to zero, else left as they are.  width at most 2^20. */

@@ -38,7 +38,7 @@ SYMBOLS = [
     "he_hrot_noalloc",
     "he_layer_norm", "he_layer_norm_workspace_bytes", "he_layer_norm_grad", "he_pool", "he_pool_workspace_bytes", "he_pool_grad",
     "he_attention", "he_attention_workspace_bytes", "he_attention_grad",
-    "he_rms_norm", "he_rms_norm_workspace_bytes", "he_rms_norm_grad", "he_rms_norm8", "he_quantize8", "he_linear8_workspace_bytes", "he_linear8",
+    "he_rms_norm", "he_rms_norm_workspace_bytes", "he_rms_norm_grad", "he_rms_norm8", "he_quantize8", "he_linear8",
     "he_profile_start", "he_profile_stop",
 ]
 
@@ -159,8 +159,7 @@ def load_library() -> ctypes.CDLL:
             "he_rms_norm_grad": [vp, ds, ds, ds, vp, vp, ds, ds, vp, vp, sz, vp],
             "he_rms_norm8": [vp, ds, ds, ds, vp, ds, ds, vp],
             "he_quantize8": [vp, i32, i64, i32, i32, ds, ds, vp],
-            "he_linear8_workspace_bytes": [vp, ds, ctypes.POINTER(sz)],
-            "he_linear8": [vp, ds, ds, ds, vp, ds, vp, sz, vp],
+            "he_linear8": [vp, ds, ds, ds, vp, ds, vp],
             "he_attention": [vp, ds, ds, ds, ds, ds, vp, vp, sz, vp],
             "he_attention_workspace_bytes": [vp, ds, i32, ctypes.POINTER(sz)],
             "he_attention_grad": [vp, ds, ds, ds, ds, ds, ds, vp, ds, ds, ds, vp, sz, vp],

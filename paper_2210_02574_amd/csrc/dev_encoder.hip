@@ -444,42 +444,33 @@ int32_t product8_check(const he_product8 *p)
 }
 
 struct Product8Plan {
-    int tile, splits, stages; // LINEAR8_..; parts that the sum is cut into, of so many stages each
-    int64_t tiles;            // work-groups of a part
+    int tile, groups; // rows and channels of a work-group, groups of waves that share its sums
+    int64_t tiles;
 };
-// Rules go by the number of tiles.  Times in us, results in bf16, tiles of 256, 128, 64 rows and channels, and of 64 with the sum shared by four groups of waves:
-//   16384 x 4096 x 4096 (rows, width, channels) 236, 281, 400, 582; 4096 x 4096 x 4096 63, 73, 112; 2048 x 4096 x 4096 50, 37, 54; 768 x 4096 x 4096 44, 24, 21;
-//   16384 x 2048 x 768 30, 32, 43; 16384 x 768 x 768 15.8, 15.3, 21; 4096 x 768 x 2304 15, 14, 17; 4096 x 768 x 768 14, 6.9, 7.0; 1000 x 768 x 768 13, 5.9, 4.8, 4.9;
-//   1000 x 4096 x 1024 42, 23, 12, 9.9; 300 x 2048 x 2048 24, 9.8, 7.4, 6.3; 32 x 2048 x 768 23, 9.3, 7.1, 5.9; 23 x 768 x 768 12, 5.5, 4.4, 4.5.
-// 256: from three quarters of a round of the 256 CUs on, unless a short sum meets a last round with few tiles (16384 x 768 x 2304, 2.25 rounds: 49, 41) or an edge
-// leaves an eighth more of the tiles empty than those of 128 would (65536 x 2048 x 64: 34, 23, 22).  128: from a tile for each CU on.
-// A sum of 6144 and more under few tiles is cut, and its parts joined by a second launch: 32 x 8192 x 1024 13 us whole, 9.0 in four, 8.5 in eight, 9.6 in 16; 100 x
-// 8192 x 1024 13, 9.8, 9.9, 15; 1000 x 8192 x 300 19, in two 16, in four 19; at a width of 4096 there is no gain (200 x 4096 x 512: 8.5, in two 9.3, in four 8.6).
+// Rules go by the number of tiles.  Times in us with results in bf16, rows x width x channels: tiles of 256, 128, 64, of 64 with four groups, of 32 with four and with eight:
+//   16384 x 4096 x 4096 236, 281, 400, 582; 4096 x 4096 x 4096 63, 73, 112; 2048 x 4096 x 4096 50, 37, 54; 768 x 4096 x 4096 44, 24, 21; 16384 x 2048 x 768 30, 32, 43;
+//   16384 x 768 x 768 15.8, 15.3, 21; 4096 x 768 x 2304 15, 14, 17; 4096 x 768 x 768 14, 6.9, 7.0; 1000 x 768 x 768 13, 5.9, 4.8, 4.9;
+//   1000 x 4096 x 1024 42, 23, 13, 10, 14, 20; 300 x 2048 x 2048 24, 9.9, 7.6, 6.7, 8.4, 10; 512 x 4096 x 4096 43, 22, 17, 20, 29, 41;
+//   200 x 8192 x 2000 -, 30, 22, 15, 12, 16; 500 x 768 x 768 -, 5.9, 4.6, 5.0, 4.4, 6.0; 64 x 4096 x 4096 41, 16, 12, 9.0, 7.3, 7.1;
+//   100 x 8192 x 1024 75, 28, 20, 14, 9.2, 8.0; 32 x 2048 x 768 23, 9.4, 7.2, 6.2, 4.5, 4.2; 23 x 768 x 768 12, 5.6, 4.5, 4.8, 3.7, 3.6.
+// 256: from three quarters of a round of the 256 CUs on, unless a short sum meets a last round with few tiles (16384 x 768 x 2304, 2.25 rounds: 49, 41) or edges
+// leave an eighth more of the area empty than in tiles of 128 (65536 x 2048 x 64: 34, 23, 22).  128: from a tile for each CU on.  32: as long as all tiles are resident at once,
+// two of them to a CU with four groups, one with eight.
 Product8Plan product8_plan(const he_product8 *p)
 {
     const auto tiles = [&](int tile) { return ((p->rows + tile - 1) / tile) * ((p->channels + tile - 1) / tile); };
-    const int64_t t256 = tiles(256), t128 = tiles(128), t64 = tiles(64);
-    const int steps = (p->width + LINEAR8_K - 1) / LINEAR8_K;
+    const int64_t t256 = tiles(256), t128 = tiles(128), t64 = tiles(64), t32 = tiles(32);
     const bool ragged = p->width < 1024 && t256 > 256 && 10 * ((t256 + 255) / 256 * 256) > 13 * t256;
-    if (t256 >= 192 && !ragged && 4 * t256 * 8 <= 9 * t128) return {LINEAR8_256, 1, steps, t256};
-    if (t128 >= 256 && 4 * t128 * 8 <= 9 * t64) return {LINEAR8_128, 1, steps, t128};
-    if (t64 > 256 || p->width < 1024) return {LINEAR8_64, 1, steps, t64};
-    const int most = steps < 48 || t64 == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({192 / t64, steps / 8, 8})), stages = (steps + most - 1) / most;
-    return {LINEAR8_LONG, (steps + stages - 1) / stages, stages, t64};
+    if (t256 >= 192 && !ragged && 32 * t256 <= 9 * t128) return {256, 1, t256};
+    if (t128 >= 256 && 32 * t128 <= 9 * t64) return {128, 1, t128};
+    if (t32 <= 256) return {32, 8, t32};
+    if (t32 <= 512) return {32, 4, t32};
+    return {64, t64 <= 256 && p->width >= 1024 ? 4 : 1, t64};
 }
-size_t product8_bytes(const he_product8 *p, const Product8Plan &plan) { return plan.splits > 1 ? (size_t)plan.splits * p->rows * p->channels * 4 : 0; }
 
 } // namespace
 
-extern "C" int32_t he_linear8_workspace_bytes(const he_ctx *ctx, const he_product8 *p, size_t *out)
-{
-    if (!ctx || !out || product8_check(p) != HE_OK) return HE_EINVAL;
-    *out = product8_bytes(p, product8_plan(p));
-    return HE_OK;
-}
-
-extern "C" int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *d_ws,
-                              size_t ws_bytes, void *stream)
+extern "C" int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 *x, const he_rows8 *w, const void *d_bias, const he_rows *o, void *stream)
 {
     if (!ctx || product8_check(p) != HE_OK || !pieces_ok(w, p->width)) return HE_EINVAL;
     if (d_bias && !words_ok(d_bias, type_size(p->bias_type))) return HE_EINVAL;
@@ -489,22 +480,18 @@ extern "C" int32_t he_linear8(he_ctx *ctx, const he_product8 *p, const he_rows8 
     }
     if (!pieces_ok(x, p->width) || !rows_ok(o, p->channels, p->type)) return HE_EINVAL;
     const Product8Plan plan = product8_plan(p);
-    const size_t need = product8_bytes(p, plan);
-    if (need && (!d_ws || ws_bytes < need)) return HE_EWORKSPACE;
-    if (need && !aligned(d_ws, 4)) return HE_EINVAL;
     if (plan.tiles > 1 << 22) return HE_EINVAL; // more than a launch holds
     Linear8Args a;
     memset(&a, 0, sizeof(a));
     a.x = x->d, a.x_row = x->stride, a.x_scale = x->d_scale, a.w = w->d, a.w_row = w->stride, a.w_scale = w->d_scale;
     a.bias = d_bias, a.bias32 = p->bias_type == HE_F32, a.o = o->d, a.o_row = o->stride;
     a.rows = (int)p->rows, a.width = p->width, a.channels = p->channels;
-    a.part = (int *)d_ws, a.splits = plan.splits, a.stages = plan.stages;
     NEEDS_DEVICE(ctx);
     DeviceGuard dg(ctx);
     if (dg.rc != HE_OK) return dg.rc;
-    const double bytes = (double)p->rows * (p->width + 4) + (double)p->channels * (p->width + 4) +
-                         (need ? (double)need : (double)p->rows * p->channels * type_size(p->type)) + (d_bias ? (double)p->channels * type_size(p->bias_type) : 0.0);
-    linear8_launch(p->type).product(ctx, (hipStream_t)stream, bytes, plan.tile, a);
+    const double bytes = (double)p->rows * (p->width + 4) + (double)p->channels * (p->width + 4) + (double)p->rows * p->channels * type_size(p->type) +
+                         (d_bias ? (double)p->channels * type_size(p->bias_type) : 0.0);
+    linear8_launch(p->type).product(ctx, (hipStream_t)stream, bytes, plan.tile, plan.groups, a);
     return launched(ctx);
 }
 

@@ -61,10 +61,9 @@ void rows8_launch_0(Rows8Launch &t);
 void rows8_launch_1(Rows8Launch &t);
 void rows8_launch_2(Rows8Launch &t);
 
-// Tiles of a product: rows and channels of a work-group; LINEAR8_LONG: 64 of each, with four groups of waves on the sum.
-enum { LINEAR8_256, LINEAR8_128, LINEAR8_64, LINEAR8_LONG };
 struct Linear8Launch {
-    void (*product)(he_ctx *c, hipStream_t st, double bytes, int tile, const Linear8Args &a);
+    // tile: rows and channels of a work-group; groups: of waves that share a sum.  256, 128 and 64 with one, 64 with four, 32 with four or eight
+    void (*product)(he_ctx *c, hipStream_t st, double bytes, int tile, int groups, const Linear8Args &a);
 };
 void linear8_launch_0(Linear8Launch &t);
 void linear8_launch_1(Linear8Launch &t);

@@ -18,9 +18,6 @@ struct Linear8Args {
     int rows, width, channels;
     int tiles_m, tiles_n;
     int bias32;
-    int *part;  // [splits][rows][channels], where the sum is cut: the sums of each part
-    int splits; // parts of the sum, each of `stages` stages of it
-    int stages;
 };
 
 // 16 bytes for each lane from `at` of a buffer (zeros behind its end) to LDS, lane i's at to + 16 i, with no register in between.
@@ -35,11 +32,11 @@ __device__ __forceinline__ void fetch_lds(__amdgpu_buffer_rsrc_t from, unsigned 
 __device__ __forceinline__ int linear8_twist(int row) { return row >> 1 & 7; }
 
 // Tiles of 32 MB WM rows by 32 NB WN channels, WM x WN waves with MB x NB blocks of 32 x 32 each; G such groups of waves share the sum, each taking every G-th
-// stage; PART: blockIdx.y's part of the sum alone, left as it is.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
+// stage.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
 // stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
-template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
+template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
 {
-    static_assert(G == 1 ? !PART : G == 4 && MB == 1 && NB == 1, "");
+    static_assert(G == 1 || (G % 4 == 0 && MB == 1 && NB == 1), "");
     constexpr int W = WM * WN, THREADS = 64 * W * G, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * LINEAR8_K;
     constexpr int SIZE = (int)sizeof(T), VEC = 16 / SIZE;
     constexpr int COLS = G == 1 ? 32 * NB : BN, PITCH = COLS * SIZE + 16; // of a row of results in LDS, bytes
@@ -55,10 +52,9 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __
     const int band = id / (BAND * a.tiles_n), first = band * BAND, high = min(BAND, a.tiles_m - first), in = id - band * BAND * a.tiles_n;
     const int m0 = (first + in % high) * BM, n0 = in / high * BN;
 
-    const int k0 = PART ? blockIdx.y * a.stages * LINEAR8_K : 0, width = PART ? min(a.width - k0, a.stages * LINEAR8_K) : a.width;
-    const int steps = (width + LINEAR8_K - 1) / LINEAR8_K, rounds = (steps + G - 1) / G, tail = width % LINEAR8_K;
-    const int whole = (width + 15) / 16 * 16; // bytes of a row that may be read
-    const int8_t *const xb = a.x + m0 * a.x_row + k0, *const wb = a.w + n0 * a.w_row + k0;
+    const int steps = (a.width + LINEAR8_K - 1) / LINEAR8_K, rounds = (steps + G - 1) / G, tail = a.width % LINEAR8_K;
+    const int whole = (a.width + 15) / 16 * 16; // bytes of a row that may be read
+    const int8_t *const xb = a.x + m0 * a.x_row, *const wb = a.w + n0 * a.w_row;
     const int bytes_m = (min(BM, a.rows - m0) - 1) * (int)a.x_row + whole, bytes_n = (min(BN, a.channels - n0) - 1) * (int)a.w_row + whole; // below 2^31: strides are below 2^23
     // One load of a wave brings eight rows.
     constexpr int LM = BM / 8 / W, LN = BN / 8 / W;
@@ -92,12 +88,14 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __
     // Behind the end of the sum: weights of its last stage from number `tail` on become zeros, so that what x's rows have there does not count.  All of a work-group
     // take part.
     const auto cut = [&](int8_t *stage) {
-        for (int row = threadIdx.x; row < BN; row += THREADS) {
-            int8_t *const r = stage + (BM + row) * LINEAR8_K;
-            for (int c = tail / 16; c < 8; c++) {
-                int8_t *const p = r + 16 * (c ^ linear8_twist(row));
-                for (int b = max(tail - 16 * c, 0); b < 16; b++) p[b] = 0;
-            }
+        for (int i = threadIdx.x; i < BN * 8; i += THREADS) {
+            const int row = i / 8, left = tail - 16 * (i % 8); // numbers of this piece that count
+            if (left >= 16) continue;
+            i32x4 *const p = (i32x4 *)(stage + (BM + row) * LINEAR8_K + 16 * (i % 8 ^ linear8_twist(row)));
+            i32x4 v = *p;
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] &= left >= 4 * e + 4 ? -1 : left <= 4 * e ? 0 : (int)((1u << 8 * (left - 4 * e)) - 1);
+            *p = v;
         }
         __syncthreads();
     };
@@ -121,7 +119,7 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __
 
     if (group < steps) fetch(group, mine);
     if (group + G < steps) fetch(group + G, mine + STAGE);
-    for (int i = threadIdx.x; !PART && i < BM + BN; i += THREADS) {
+    for (int i = threadIdx.x; i < BM + BN; i += THREADS) {
         if (i < BM)
             sx[i] = a.x_scale[min(m0 + i, a.rows - 1)];
         else {
@@ -198,54 +196,21 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC, bool PART> __
 #pragma unroll
             for (int p = 0; p < PER; p++) store(y[p], m0 + m + (p * 64 + lane) / CHUNKS, n0 + COLS * wn + lane % CHUNKS * VEC);
         }
-    } else { // each group joins a quarter of the groups' sums of each block
-        i32x4 *const join = (i32x4 *)lds + wave * G * G * 64; // [group][quarter][lane]
+    } else { // each of the first four groups joins a quarter of all groups' sums of each block
+        i32x4 *const join = (i32x4 *)lds + wave * G * 256; // [group][quarter][lane]
 #pragma unroll
-        for (int g = 0; g < G; g++) join[(group * G + g) * 64 + lane] = i32x4{acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2], acc[0][0][4 * g + 3]};
+        for (int g = 0; g < 4; g++) join[(group * 4 + g) * 64 + lane] = i32x4{acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2], acc[0][0][4 * g + 3]};
         __syncthreads();
-        i32x4 s = join[group * 64 + lane];
+        i32x4 s = {};
+        if (group < 4)
 #pragma unroll
-        for (int g = 1; g < G; g++) s += join[(g * G + group) * 64 + lane];
+            for (int g = 0; g < G; g++) s += join[(g * 4 + group) * 64 + lane];
         int8_t *const out = lds + G * W * 4096;
         const int m = 32 * wm + row, col = 32 * wn + 8 * group + 4 * h;
-        if constexpr (PART) {
-            const int n = n0 + col;
-            if (m0 + m >= a.rows) return;
-            store_vec<int, 4>(s, a.part + ((size_t)blockIdx.y * a.rows + m0 + m) * a.channels, n, a.channels);
-            return;
-        }
-        *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
+        if (group < 4) *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
         __syncthreads();
         constexpr int CHUNKS = COLS / VEC;
         for (int p = threadIdx.x; p < BM * CHUNKS; p += THREADS)
             store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), m0 + p / CHUNKS, n0 + p % CHUNKS * VEC);
     }
-}
-
-// The parts' sums joined and scaled: a thread has four channels of a row.
-template <class T> __global__ __launch_bounds__(256) void k_linear8_join(Linear8Args a)
-{
-    const int fours = (a.channels + 3) / 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t m = i / fours;
-    const int n = (int)(i % fours) * 4;
-    if (m >= a.rows) return;
-    i32x4 s = {};
-    for (int k = 0; k < a.splits; k += 4) { // four parts' reads under way together
-        i32x4 v[4];
-#pragma unroll
-        for (int u = 0; u < 4; u++) v[u] = load_vec<int, 4>(a.part + ((size_t)min(k + u, a.splits - 1) * a.rows + m) * a.channels, n, a.channels);
-#pragma unroll
-        for (int u = 0; u < 4; u++)
-            if (k + u < a.splits) s += v[u];
-    }
-    const float xs = a.x_scale[m];
-    Vec<T, 4> y;
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-        const int c = min(n + e, a.channels - 1);
-        const float b = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[c] : (float)((const T *)a.bias)[c];
-        y[e] = (T)fmaf((float)s[e] * xs, a.w_scale[c], b);
-    }
-    store_vec<T, 4>(y, (T *)a.o + m * a.o_row, n, a.channels);
 }

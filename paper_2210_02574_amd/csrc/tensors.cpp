@@ -439,14 +439,7 @@ PyObject *linear8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             orows = rows_of(a, out, "out", shape, dtype);
             apart(out, "out", {a.at[0], a.at[1], a.at[2], a.at[3], a.at[4]});
         }
-        // most calls take no workspace, and one that does says so before it enqueues anything
-        int32_t rc = he_linear8(a.ctx, &p, &xr, &wr, bias, &orows, nullptr, 0, a.stream);
-        if (rc == HE_EWORKSPACE) {
-            size_t need = 0;
-            if (const int32_t bad = he_linear8_workspace_bytes(a.ctx, &p, &need)) return status(bad);
-            const Tensor ws = scratch(x, need);
-            rc = he_linear8(a.ctx, &p, &xr, &wr, bias, &orows, address(ws), need, a.stream);
-        }
+        const int32_t rc = he_linear8(a.ctx, &p, &xr, &wr, bias, &orows, a.stream);
         if (rc != HE_OK) return status(rc);
         if (o.defined()) return wrap(o);
         written(tensor(a.at[6], "out"));
