@@ -795,12 +795,8 @@ class HE:
         return self._on_tensors("quantize8", "he_quantize8", x, gelu)
 
     def linear8(self, x8, scale, w8, w_scale, bias=None, dtype=None, out=None):
-        """x8 scale (w8 w_scale)^T + bias, of type dtype (bfloat16 by default): x8 [rows][width] with a scale for each row, w8 [channels][width] with one for each
+        """x8 scale (w8 w_scale)^T + bias, of type dtype (by default out's, else bfloat16): x8 [rows][width] with a scale for each row, w8 [channels][width] with one for each
         channel, bias [channels] float32 or of type dtype.  Sums are exact.  Rows of x8 and w8 begin at multiples of 16 bytes, as quantize8 and rms_norm8 make them."""
-        import torch
-
-        if dtype is None:
-            dtype = torch.bfloat16 if out is None else out.dtype
         return self._on_tensors("linear8", "he_linear8", x8, scale, w8, w_scale, bias, dtype, out)
 
     def pool_mean(self, x, offsets, out=None):

