@@ -1,8 +1,8 @@
 """From the states of a sentence's tokens to the embedding that is encrypted: the data owner's half of the paper's pipeline (Section 2.1,
 x -> F_emb(x), then encryption), with gradients, so that an encoder can be fitted in the clear before its embeddings are.
 
-The operators are the library's (HE.attention, HE.layer_norm, HE.pool_mean); the functions here make them differentiable, and SentenceEncoder puts them
-together.  Matrix products with weights are plain library products.  Sentences are packed back to back or padded, as HE's offsets say.
+The operators are the library's (HE.attention, HE.layer_norm, HE.rms_norm, HE.pool_mean); the functions here make them differentiable, and SentenceEncoder puts them
+together.  Matrix products with weights are plain library products there; SentenceEncoder8, for inference, has them in 8 bits (HE.rms_norm8, HE.quantize8, HE.linear8).  Sentences are packed back to back or padded, as HE's offsets say.
 Gradients are of the first order: a backward pass that is to be differentiated again is refused.
 """
 from __future__ import annotations
@@ -53,6 +53,31 @@ class _Norm(torch.autograd.Function):
 def layer_norm(he, x, weight, bias, residual=None, eps: float = 1e-5):
     """(y, s): layer norm of s = x + residual, and s itself (x without a residual).  Differentiable in x, residual, weight and bias."""
     y, s = _Norm.apply(he, x, weight, bias, residual, eps)
+    return y, x if s is None else s
+
+
+class _Rms(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, he, x, weight, residual, eps):
+        y, s, rstd = he.rms_norm(x, weight, residual=residual, eps=eps)
+        ctx.he, ctx.residual = he, residual is not None
+        ctx.save_for_backward(s, weight, rstd)
+        ctx.set_materialize_grads(False)
+        return (y, s) if ctx.residual else (y, None)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, ds):
+        s, weight, rstd = ctx.saved_tensors
+        if dy is None:  # only the sum was used
+            return None, ds, None, ds if ctx.residual else None, None
+        dx, dw = ctx.he.rms_norm_backward(dy.contiguous(), s, weight, rstd, ds=None if ds is None else ds.contiguous())
+        return None, dx, dw, dx if ctx.residual else None, None
+
+
+def rms_norm(he, x, weight, residual=None, eps: float = 1e-5):
+    """(y, s): root-mean-square norm of s = x + residual, and s itself (x without a residual).  Differentiable in x, residual and weight."""
+    y, s = _Rms.apply(he, x, weight, residual, eps)
     return y, x if s is None else s
 
 
@@ -126,29 +151,37 @@ def pool_mean(he, x, offsets):
 
 
 class SentenceEncoder:
-    """Post-norm transformer layers over packed sentences, and the embedding of each sentence.
+    """Transformer layers over packed sentences, and the embedding of each sentence.
 
     layers: per layer a dict of weights: qkv [(heads + 2 kv_heads) dim][width] and qkv_bias, out [width][heads dim] and out_bias, up and up_bias,
-    down and down_bias (the products of the feed-forward part, with a Gaussian error unit between), norm1, norm1_bias, norm2, norm2_bias.
+    down and down_bias (the products of the feed-forward part, with a Gaussian error unit between), and its norms' weights.
+    norm: "layer", a layer norm behind each residual sum (norm1, norm1_bias, norm2, norm2_bias), or "rms", a root-mean-square norm ahead of each half of a layer (norm1,
+    norm2) and one behind the last layer (last: its weight [width]).
     pool: "mean" of a sentence's rows, or its "first" row; the last layer then computes that row of each sentence alone.
     cap, slopes: as HE.attention takes them, the same in every layer; no slopes with pool "first"."""
 
-    NAMES = ("qkv", "qkv_bias", "out", "out_bias", "up", "up_bias", "down", "down_bias", "norm1", "norm1_bias", "norm2", "norm2_bias")
+    PRODUCTS = ("qkv", "out", "up", "down")
+    NORMS = {"layer": ("norm1", "norm1_bias", "norm2", "norm2_bias"), "rms": ("norm1", "norm2")}
+    NAMES = ("qkv", "qkv_bias", "out", "out_bias", "up", "up_bias", "down", "down_bias") + NORMS["layer"]
 
     def __init__(self, he, layers: Sequence[Dict[str, torch.Tensor]], heads: int, kv_heads: int = 0, pool: str = "mean", cap: float = 0.0,
-                 slopes=None, eps: float = 1e-5):
+                 slopes=None, eps: float = 1e-5, norm: str = "layer", last=None):
         if pool not in ("mean", "first"):
             raise ValueError(f"pool: {pool!r}, want 'mean' or 'first'")
+        if norm not in self.NORMS:
+            raise ValueError(f"norm: {norm!r}, want 'layer' or 'rms'")
+        if (last is None) == (norm == "rms"):
+            raise ValueError("last: the weight of the norm behind the last layer, with norm='rms' alone")
         if slopes is not None and slopes.requires_grad:
             raise ValueError("slopes are constants: they have no gradient")
         if slopes is not None and pool == "first":
             raise ValueError("pool='first' with a distance bias: a lone query stands at its sentence's last position, not its first")
         for i, w in enumerate(layers):
-            missing = [n for n in self.NAMES if n not in w]
+            missing = [n for n in self.NAMES[:8] + self.NORMS[norm] if n not in w]
             if missing:
                 raise ValueError(f"layer {i} lacks {', '.join(missing)}")
         self.he, self.layers, self.heads, self.kv_heads = he, list(layers), heads, kv_heads or heads
-        self.pool, self.cap, self.slopes, self.eps = pool, cap, slopes, eps
+        self.pool, self.cap, self.slopes, self.eps, self.norm, self.last = pool, cap, slopes, eps, norm, last
 
     @classmethod
     def random_layer(cls, width: int, heads: int, inner: int, seed: int, dtype, device, kv_heads: int = 0, std: float = 0.02):
@@ -163,23 +196,59 @@ class SentenceEncoder:
             w[n], w[n + "_bias"] = torch.ones(width, dtype=dtype, device=device), torch.zeros(width, dtype=dtype, device=device)
         return w
 
+    def in_8_bits(self) -> "SentenceEncoder8":
+        """This encoder with its products in 8 bits, for inference; later changes of its weights do not reach the result."""
+        return SentenceEncoder8(self)
+
+    # What a product reads, of rows, of their Gaussian error units, and of the norm of the sum f + x (x alone without f), which comes back as well.
+    def _rows(self, x):
+        return x
+
+    def _units(self, x):
+        return F.gelu(x)
+
+    def _rms(self, f, x, weight):
+        return rms_norm(self.he, x, weight, eps=self.eps) if f is None else rms_norm(self.he, f, weight, residual=x, eps=self.eps)
+
+    def _take(self, a, begin):
+        return a[begin]
+
+    def _product(self, w, name, a, lo=None, hi=None):
+        """Rows of a times weights w[name], or their channels lo .. hi."""
+        return F.linear(a, w[name][lo:hi], w[name + "_bias"][lo:hi])
+
+    def _head(self, w, f, x):
+        """What a layer's first product reads, and the layer's input."""
+        return (self._rows(x), x) if self.norm == "layer" else self._rms(f, x, w["norm1"])
+
     def _rest(self, w, o, x):
-        """The layer behind its attention: o [rows][heads][dim], x the layer's input on those rows."""
-        x, _ = layer_norm(self.he, F.linear(o.flatten(1), w["out"], w["out_bias"]), w["norm1"], w["norm1_bias"], residual=x, eps=self.eps)
-        f = F.linear(F.gelu(F.linear(x, w["up"], w["up_bias"])), w["down"], w["down_bias"])
-        return layer_norm(self.he, f, w["norm2"], w["norm2_bias"], residual=x, eps=self.eps)[0]
+        """The layer behind its attention: o [rows][heads][dim], x the layer's input on those rows.  (f, x): the layer's result is x, or x + f where f is not None."""
+        f = self._product(w, "out", self._rows(o.flatten(1)))
+        if self.norm == "rms":
+            a, x = self._rms(f, x, w["norm2"])
+            return self._product(w, "down", self._units(self._product(w, "up", a))), x
+        x, _ = layer_norm(self.he, f, w["norm1"], w["norm1_bias"], residual=x, eps=self.eps)
+        f = self._product(w, "down", self._units(self._product(w, "up", self._rows(x))))
+        return None, layer_norm(self.he, f, w["norm2"], w["norm2_bias"], residual=x, eps=self.eps)[0]
+
+    def _end(self, f, x):
+        """The states behind the last layer."""
+        if self.norm == "layer":
+            return x
+        return rms_norm(self.he, x, self.last, eps=self.eps)[0] if f is None else rms_norm(self.he, f, self.last, residual=x, eps=self.eps)[0]
 
     def __call__(self, states, offsets):
         """states [rows][width], offsets as HE's operators take them -> embeddings [sentences][width] in 32 bits."""
-        x, kv = states, self.kv_heads
+        f, x, kv = None, states, self.kv_heads
         if not x.shape[0]:
             return pool_mean(self.he, x, offsets)  # sentences without rows
         for i, w in enumerate(self.layers):
-            dim = w["out"].shape[1] // self.heads
+            a, x = self._head(w, f, x)
             if self.pool == "first" and i == len(self.layers) - 1:
-                return self._last_first(w, x, offsets, dim)
-            qkv = F.linear(x, w["qkv"], w["qkv_bias"]).unflatten(1, (self.heads + 2 * kv, dim))
-            x = self._rest(w, _SelfAttention.apply(self.he, qkv, kv, offsets, self.cap, self.slopes), x)
+                return self._last_first(w, a, x, offsets)
+            qkv = self._product(w, "qkv", a).unflatten(1, (self.heads + 2 * kv, -1))
+            f, x = self._rest(w, _SelfAttention.apply(self.he, qkv, kv, offsets, self.cap, self.slopes), x)
+        x = self._end(f, x)
         if self.pool == "mean":
             return pool_mean(self.he, x, offsets)
         begin, some = self._first(x, offsets)
@@ -191,15 +260,55 @@ class SentenceEncoder:
         begin, end = offsets if isinstance(offsets, (tuple, list)) else (offsets[:-1], offsets[1:])
         return begin.clamp(0, max(x.shape[0] - 1, 0)).long(), end > begin
 
-    def _last_first(self, w, x, offsets, dim):
+    def _last_first(self, w, a, x, offsets):
         """The last layer on the first row of each sentence: one query to a sentence's keys."""
         begin, some = self._first(x, offsets)
-        rows, cut = x[begin], self.heads * dim
-        q = F.linear(rows, w["qkv"][:cut], w["qkv_bias"][:cut]).unflatten(1, (self.heads, dim))
-        kvs = F.linear(x, w["qkv"][cut:], w["qkv_bias"][cut:]).unflatten(1, (2 * self.kv_heads, dim))
+        rows = x[begin]
+        dim = w["qkv_bias"].shape[0] // (self.heads + 2 * self.kv_heads)
+        cut = self.heads * dim
+        q = self._product(w, "qkv", rows if a is x else self._take(a, begin), None, cut).unflatten(1, (self.heads, dim))
+        kvs = self._product(w, "qkv", a, cut).unflatten(1, (2 * self.kv_heads, dim))
         one = torch.arange(len(begin) + 1, dtype=torch.int32, device=x.device)
         o = attention(self.he, q, kvs[:, :self.kv_heads], kvs[:, self.kv_heads:], one, offsets_k=offsets, cap=self.cap)
-        return torch.where(some[:, None], self._rest(w, o, rows), 0.0).float()
+        return torch.where(some[:, None], self._end(*self._rest(w, o, rows)), 0.0).float()
+
+
+class SentenceEncoder8(SentenceEncoder):
+    """An encoder whose products with weights are in 8 bits, with a scale for each row and channel: weights are laid out once, rows where they come out of a norm, attention
+    or the Gaussian error units.  Norms, attention and residual sums stay as they are.  No gradients pass through 8-bit rows."""
+
+    def __init__(self, encoder: SentenceEncoder):
+        he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach())
+        layers = [{n: eight(w[n]) if n in self.PRODUCTS else w[n].detach() for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]
+        last = None if encoder.last is None else encoder.last.detach()
+        super().__init__(he, layers, encoder.heads, encoder.kv_heads, encoder.pool, encoder.cap, encoder.slopes, encoder.eps, encoder.norm, last)
+        self.dtype = encoder.layers[0]["qkv"].dtype if layers else None  # of the states between the products
+
+    def in_8_bits(self):
+        return self
+
+    def _rows(self, x):
+        return self.he.quantize8(x)
+
+    def _units(self, x):
+        return self.he.quantize8(x, gelu=True)
+
+    def _rms(self, f, x, weight):
+        x8, scale, s = self.he.rms_norm8(x, weight, eps=self.eps) if f is None else self.he.rms_norm8(f, weight, residual=x, eps=self.eps)
+        return (x8, scale), s
+
+    def _take(self, a, begin):
+        x8, scale = a  # with what stands behind each row: rows begin at multiples of 64 bytes
+        return x8.as_strided((x8.shape[0], x8.stride(0)), (x8.stride(0), 1))[begin][:, :x8.shape[1]], scale[begin]
+
+    def _product(self, w, name, a, lo=None, hi=None):
+        w8, scale = w[name]
+        return self.he.linear8(*a, w8[lo:hi], scale[lo:hi], bias=w[name + "_bias"][lo:hi], dtype=self.dtype)
+
+    def __call__(self, states, offsets):
+        if states.requires_grad and torch.is_grad_enabled():
+            raise ValueError("states: an encoder in 8 bits has no gradients")
+        return super().__call__(states, offsets)
 
 
 def pack_embeddings(e, n_slots: int) -> List[np.ndarray]:

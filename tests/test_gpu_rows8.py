@@ -32,6 +32,10 @@ def integers(seed, rows, width, pad=0):
     return torch.randint(-128, 128, (rows, (width + 15) // 16 * 16 + pad), generator=g, dtype=torch.int8).cuda()[:, :width]
 
 
+def offsets_of(lengths):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lengths)]).tolist(), dtype=torch.int32, device="cuda")
+
+
 # ---- root-mean-square norm --------------------------------------------------------------------------------------------------
 
 
@@ -223,3 +227,325 @@ def test_product_of_views(he):
         assert torch.equal(he.linear8(big[:2 * (rows // 2):2, 256:512], scale[::2].contiguous(), w8, ws, dtype=F32), want[::2])
         with pytest.raises(pkg.HeError, match="EINVAL"):  # rows in one place, as everywhere
             he.linear8(big[:1, 256:512].expand(rows, -1), scale, w8, ws, dtype=F32)
+
+
+@pytest.mark.parametrize("rows,width,channels", [(600000, 8192, 40), (600001, 16, 4096), (70000, 32, 33000)])
+def test_product_far_into_long_buffers(he, rows, width, channels):
+    """Rows of x8, and of results, that begin behind 2^32 bytes and 2^31 elements."""
+    x8 = torch.randint(-127, 128, (rows, width), dtype=torch.int8, device="cuda")
+    scale, w8, ws = torch.rand(rows, device="cuda") / width, integers(2, channels, width), rand(3, channels).abs()
+    o = he.linear8(x8, scale, w8, ws)
+    for at in (0, rows // 2, rows - 300):
+        want = ref.linear8(x8[at:at + 300], scale[at:at + 300], w8, ws, None, BF16)
+        assert ((o[at:at + 300].double() - want[0]).abs() <= want[1]).all(), at
+
+
+def test_more_rows_than_a_launch_holds(he):
+    """2^32 threads are too many, and 32 of them are a row's here.  Every row has the same numbers in another order of its two halves."""
+    rows, row, w = (1 << 27) + 37, rand(1, 8, dtype=BF16), torch.ones(8, device="cuda")
+    x = row.expand(rows, 8).contiguous()
+    x[1::2] = row.roll(4)
+    y, _, rstd = he.rms_norm(x, w)
+    small = he.rms_norm(x[:2], w)
+    for k in range(2):
+        assert (y[k::2] == small[0][k]).all() and (rstd[k::2] == small[2][k]).all()
+    del y, rstd
+    x8, scale = he.quantize8(x)
+    small = he.quantize8(x[:2])
+    for k in range(2):
+        assert (x8[k::2] == small[0][k]).all() and (scale[k::2] == small[1][k]).all()
+
+
+def test_rms_norm_weight_gradient_of_many_rows_repeats(he):
+    x, dy = rand(1, 70001, 64, dtype=F16), rand(2, 70001, 64, dtype=F16)
+    w = rand(3, 64)
+    _, s, rstd = he.rms_norm(x, w)
+    a, b = he.rms_norm_backward(dy, s, w, rstd), he.rms_norm_backward(dy, s, w, rstd)
+    want = ref.rms_norm(x, w, dy=dy)
+    for name, u, v in zip(("dx", "dw"), a, b):
+        assert torch.equal(u, v)
+        eref.check(u, want[name], name)
+
+
+# ---- arguments -----------------------------------------------------------------------------------------------------------------------
+
+
+def test_refusals_on_the_device(he):
+    x, w = rand(1, 8, 64, dtype=BF16), rand(2, 64)
+    x8, s = he.quantize8(x)
+    w8, ws = he.quantize8(rand(3, 5, 64))
+    flat = torch.zeros(400, dtype=torch.int8, device="cuda")
+    for f in (lambda: he.rms_norm(x, w[:63]), lambda: he.rms_norm(x, w, residual=x[:4]), lambda: he.rms_norm(x, w, residual=x.float()), lambda: he.rms_norm(x.double(), w),
+              lambda: he.rms_norm(x, w, out=x.float()), lambda: he.rms_norm8(x, w.cpu()), lambda: he.rms_norm_backward(x, x, w, rand(1, 7)), lambda: he.quantize8(x[0]),
+              lambda: he.quantize8(x.t()), lambda: he.quantize8(x.cpu()), lambda: he.quantize8(x8), lambda: he.linear8(x, s, w8, ws), lambda: he.linear8(x8, s[:7], w8, ws),
+              lambda: he.linear8(x8, s, w8, ws[:4]), lambda: he.linear8(x8, s, w8[:, :48], ws), lambda: he.linear8(x8, s, w8, ws, bias=rand(1, 4)),
+              lambda: he.linear8(x8, s, w8, ws, dtype=torch.float64), lambda: he.linear8(x8, s, w8, ws, dtype=5), lambda: he.linear8(x8, s, w8, ws, out=torch.zeros(8, 4, device="cuda")),
+              lambda: he.linear8(x8, s, w8, ws, dtype=F32, out=torch.zeros(8, 5, device="cuda", dtype=BF16)), lambda: he.linear8(x8.cpu(), s, w8, ws),
+              lambda: he.linear8(x8[:, 1:17], s, w8[:, :16], ws), lambda: he.linear8(flat[:144].view(8, 18)[:, :16], s, w8[:, :16], ws),
+              lambda: he.linear8(flat[:136].view(8, 17), s, w8[:, :17], ws),  # rows at no multiples of 16 bytes, and a last piece that the buffer does not hold
+              lambda: he.linear8(torch.zeros(7 * 32 + 20, dtype=torch.int8, device="cuda").as_strided((8, 20), (32, 1)), s, w8[:, :20], ws)):
+        with pytest.raises(ValueError):
+            f()
+    wide = torch.zeros(2, 16385, device="cuda")
+    for f in (lambda: he.rms_norm(x, w, eps=-1.0), lambda: he.rms_norm(x, rand(2, 64, dtype=F16)), lambda: he.rms_norm8(wide, wide[0]), lambda: he.quantize8(wide),
+              lambda: he.quantize8(wide[:, :0]), lambda: he.linear8(x8, s, w8[:0], ws[:0]), lambda: he.linear8(x8, s, w8, ws, bias=rand(1, 5, dtype=F16)),
+              lambda: he.linear8(torch.zeros(2, 65552, dtype=torch.int8, device="cuda"), s[:2], torch.zeros(2, 65552, dtype=torch.int8, device="cuda"), s[:2]),
+              lambda: he.linear8(torch.zeros(2, 1 << 23, dtype=torch.int8, device="cuda")[:, :64], s[:2], w8, ws)):
+        with pytest.raises(pkg.HeError, match="EINVAL"):
+            f()
+
+
+def test_buffers_to_write_to(he):
+    """They get another version, are refused where autograd tracks them or where they overlap what the call reads, and taken beside it."""
+    buf = rand(1, 2048)
+    x, w = buf[:512].view(8, 64), rand(2, 64)
+    x8, s = he.quantize8(x)
+    w8, ws = he.quantize8(rand(3, 64, 64))
+    calls = (lambda out: he.rms_norm(x, w, out=out), lambda out: he.linear8(x8, s, w8, ws, out=out))
+    for f in calls:
+        out, t = torch.ones(8, 64, device="cuda"), torch.ones(8, 64, device="cuda", requires_grad=True)
+        y = (t * out).sum()
+        f(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+        with pytest.raises(ValueError, match="require gradients"):
+            f(torch.ones(8, 64, device="cuda", requires_grad=True))
+    for f in (lambda: he.rms_norm(x, w, out=x), lambda: he.rms_norm(x, buf[1024:1088], out=buf[1000:1512].view(8, 64)),
+              lambda: he.linear8(x8, buf[600:608], w8, ws, out=buf[512:1024].view(8, 64)), lambda: he.linear8(x8, s, w8, ws, bias=buf[:64], out=x)):
+        with pytest.raises(ValueError, match="overlap"):
+            f()
+    both = torch.cat([x, torch.zeros_like(x)], 1)
+    assert torch.equal(he.rms_norm(both[:, :64], w, out=both[:, 64:])[0], he.rms_norm(x, w)[0]) and torch.equal(both[:, :64], x)
+
+
+# ---- streams, graphs, together ---------------------------------------------------------------------------------------------------------
+
+
+def _everything(he, x, r, w, dy, w8, ws, b):
+    y, s, rstd = he.rms_norm(x, w, residual=r)
+    y8, scale, _ = he.rms_norm8(x, w, residual=r)
+    u8, u_scale = he.quantize8(y, gelu=True)
+    return (y, s, rstd, y8.clone(), scale, u8.clone(), u_scale, he.linear8(y8, scale, w8, ws, bias=b), he.linear8(y8[:40], scale[:40], w8, ws, bias=b),
+            he.linear8(u8, u_scale, w8[:100], ws[:100], dtype=F32), *he.rms_norm_backward(dy, s, w, rstd, ds=r))
+
+
+def _inputs(he, seed, rows=3000, width=328, channels=4100):
+    w8, ws = he.quantize8(rand(seed, channels, width))
+    return [rand(seed + 1, rows, width, dtype=BF16), rand(seed + 2, rows, width, dtype=BF16), rand(seed + 3, width), rand(seed + 4, rows, width, dtype=BF16), w8, ws,
+            rand(seed + 5, channels)]
+
+
+def test_repeats_bit_for_bit_on_two_streams_at_once(he):
+    ins = [_inputs(he, 10), _inputs(he, 20)]
+    want = [[t.clone() for t in _everything(he, *i)] for i in ins]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for rep in range(3):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k] = _everything(he, *ins[k])
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(got[k], want[k])), (rep, k)
+
+
+def test_two_captured_graphs(he):
+    """Two graphs captured on one stream and replayed on two at once; inputs change between replays."""
+    ins, fresh = [_inputs(he, 30), _inputs(he, 40)], [_inputs(he, 50), _inputs(he, 60)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in ins:
+            _everything(he, *i)
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], [None, None]
+    for k in range(2):
+        with torch.cuda.graph(graphs[k], stream=side):
+            outs[k] = _everything(he, *ins[k])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(4):
+        if rep == 2:
+            for k in range(2):
+                for a, b in zip(ins[k], fresh[k]):
+                    a.copy_(b)
+        want = [[t.clone() for t in _everything(he, *i)] for i in ins]  # eager work between the replays
+        torch.cuda.synchronize()
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                graphs[k].replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k])), (rep, k)
+
+
+def test_rms_norm_gradients_against_differences(he):
+    """Along random directions: central differences with step h are off by h^2 and by 2^-24 |f| / h."""
+    from paper_2210_02574_amd.embedding import rms_norm
+
+    x, c, e = [rand(1, 39, 128), rand(2, 39, 128), rand(3, 128)], rand(4, 39, 128).double(), rand(5, 39, 128).double()
+
+    def f(x, r, w):
+        y, s = rms_norm(he, x, w, residual=r)
+        return (y.double() * c + s.double() * e).sum()
+
+    leaves = [t.requires_grad_(True) for t in x]
+    grads = torch.autograd.grad(f(*leaves), leaves)
+    h = 2.0**-7
+    for i in range(3):
+        d = rand(10 + i, *x[i].shape)
+        d = d / d.norm()
+        with torch.no_grad():
+            a = [t + h * d if j == i else t for j, t in enumerate(x)]
+            b = [t - h * d if j == i else t for j, t in enumerate(x)]
+            diff = float(f(*a) - f(*b)) / (2 * h)
+        want = float((grads[i] * d).sum())
+        assert abs(diff - want) < 2.0**-11 * (1 + float(grads[i].norm())), (i, diff, want)
+
+
+def test_rms_norm_passes_gradients_of_either_result_alone(he):
+    from paper_2210_02574_amd.embedding import rms_norm
+
+    x, r, w = (t.requires_grad_(True) for t in (rand(1, 6, 64), rand(2, 6, 64), rand(3, 64)))
+    _, s = rms_norm(he, x, w, residual=r)
+    s.sum().backward()
+    assert (x.grad == 1).all() and (r.grad == 1).all() and w.grad is None
+    y, same = rms_norm(he, x, w)
+    assert same is x
+    g, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
+
+
+def _plain_encoder(layers, last, x, off, heads, pool):
+    """A pre-norm encoder in 64 bits by torch's differentiable elementary operations."""
+    x = x.double()
+    norm = lambda t, w: t * (t.pow(2).mean(1, keepdim=True) + 1e-5).rsqrt() * w  # noqa: E731
+    o = off.tolist()
+    for w in layers:
+        w = {k: v.double() for k, v in w.items()}
+        times = lambda t, n: t @ w[n].T + w[n + "_bias"]  # noqa: E731, B023
+        d = x.shape[1] // heads
+        qkv = times(norm(x, w["norm1"]), "qkv").view(-1, 3 * heads, d)
+        rows = []
+        for b, e in zip(o[:-1], o[1:]):
+            q, k, v = (qkv[b:e, i * heads:(i + 1) * heads].transpose(0, 1) for i in range(3))
+            rows.append((torch.softmax(q @ k.transpose(1, 2) * d**-0.5, -1) @ v).transpose(0, 1).flatten(1))
+        x = x + times(torch.cat(rows), "out")
+        x = x + times(torch.nn.functional.gelu(times(norm(x, w["norm2"]), "up")), "down")
+    x = norm(x, last.double())
+    take = (lambda b, e: x[b:e].mean(0)) if pool == "mean" else lambda b, e: x[b]
+    return torch.stack([take(b, e) if e > b else x[:1].sum(0) * 0 for b, e in zip(o[:-1], o[1:])])
+
+
+@pytest.mark.parametrize("pool", ["mean", "first"])
+def test_encoder_with_root_mean_square_norms_and_its_gradients(he, pool):
+    """All operators together in 32 bits.  Errors of single operations are near 2^-24 of their operands, a few hundred of them follow one another
+    over two layers, norms multiply by at most rstd ~ 1: 2^-14 of the largest element is granted."""
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    layers = [SentenceEncoder.random_layer(64, 2, 96, 5 + i, F32, "cuda", std=0.1) for i in range(2)]
+    layers = [{k: v for k, v in w.items() if k not in ("norm1_bias", "norm2_bias")} for w in layers]
+    states, off, de, last = rand(1, 60, 64), offsets_of([20, 0, 1, 39]), rand(2, 4, 64), 1 + rand(3, 64, scale=0.1)
+    leaves = [states, last] + [v for w in layers for v in w.values()]
+    for t in leaves:
+        t.requires_grad_(True)
+    e = SentenceEncoder(he, layers, 2, pool=pool, norm="rms", last=last)(states, off)
+    got = torch.autograd.grad(e, leaves, de)
+    plain = _plain_encoder(layers, last, states, off, 2, pool)
+    want = torch.autograd.grad(plain, leaves, de.double())
+    assert e.dtype == F32 and (e - plain).abs().max() <= 2.0**-14 * plain.abs().max()
+    for g, w in zip(got, want):
+        assert (g - w).abs().max() <= 2.0**-14 * max(1.0, float(w.abs().max())), g.shape
+
+
+@pytest.mark.parametrize("pool", ["mean", "first"])
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+@pytest.mark.parametrize("width,inner", [(64, 96), (80, 100)])
+def test_encoder_in_8_bits(he, norm, pool, width, inner):
+    """Against the calls of the operators one by one, equal, and against the encoder that it comes from.  A row of a hundred values has its largest at about 2.6 times their mean
+    size, so a step of 1/127 of it is off by 0.006 of that size in the mean (a step over root 12); a product has two such factors, a layer four products that add up or follow
+    one another: 0.006 root 2 root 8 = 0.024 over two layers, of which the norms at the end keep what stands across the sum; three times that is granted."""
+    from paper_2210_02574_amd.embedding import SentenceEncoder, SentenceEncoder8
+
+    layers = [SentenceEncoder.random_layer(width, 2, inner, 5 + i, F32, "cuda", std=0.1) for i in range(2)]
+    last = 1 + rand(3, width, scale=0.1) if norm == "rms" else None
+    states, off = rand(1, 60, width), offsets_of([20, 0, 1, 39])
+    enc = SentenceEncoder(he, layers, 2, pool=pool, norm=norm, last=last)
+    enc8 = enc.in_8_bits()
+    assert isinstance(enc8, SentenceEncoder8) and enc8.in_8_bits() is enc8
+    e, e8 = enc(states, off), enc8(states, off)
+    assert e8.dtype == F32 and not e8[1].any()
+    some = [0, 2, 3]
+    assert (e8 - e)[some].norm() <= 0.072 * e[some].norm()
+
+    times = lambda a, w, n: he.linear8(*a, *he.quantize8(w[n]), bias=w[n + "_bias"], dtype=F32)  # noqa: E731
+    x, f = states, None
+    for w in layers:
+        if norm == "rms":
+            x8, s, x = he.rms_norm8(x, w["norm1"]) if f is None else he.rms_norm8(f, w["norm1"], residual=x)
+            a = x8, s
+        else:
+            a = he.quantize8(x)
+        qkv = times(a, w, "qkv").view(60, 6, -1)
+        o, _ = he.attention(qkv[:, :2], qkv[:, 2:4], qkv[:, 4:], off)
+        f = times(he.quantize8(o.flatten(1)), w, "out")
+        if norm == "rms":
+            x8, s, x = he.rms_norm8(f, w["norm2"], residual=x)
+            a = x8, s
+        else:
+            x = he.layer_norm(f, w["norm1"], w["norm1_bias"], residual=x)[0]
+            a = he.quantize8(x)
+        f = times(he.quantize8(times(a, w, "up"), gelu=True), w, "down")
+        if norm == "layer":
+            x = he.layer_norm(f, w["norm2"], w["norm2_bias"], residual=x)[0]
+    if norm == "rms":
+        x = he.rms_norm(f, last, residual=x)[0]
+    if pool == "mean":
+        assert torch.equal(e8, he.pool_mean(x, off))
+    else:  # the same rows in another product, and an attention of lone queries
+        assert (e8[some] - x[[0, 20, 21]]).abs().max() <= 0.02 * x.abs().max()
+    assert enc8(states[:0], offsets_of([0, 0])).shape == (2, width)
+    with pytest.raises(ValueError, match="no gradients"):
+        enc8(states.clone().requires_grad_(True), off)
+
+
+def test_encoder_in_8_bits_in_a_graph(he):
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    layers = [SentenceEncoder.random_layer(768, 12, 1000, 5 + i, BF16, "cuda") for i in range(2)]
+    enc = SentenceEncoder(he, layers, 12, norm="rms", last=torch.ones(768, dtype=BF16, device="cuda")).in_8_bits()
+    states, off = rand(1, 700, 768, dtype=BF16), offsets_of([20, 0, 1, 39, 500, 140])
+    enc(states, off)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = enc(states, off)
+    for rep in range(3):
+        states.copy_(rand(10 + rep, 700, 768, dtype=BF16))
+        off.copy_(offsets_of([20 + rep, 0, 1, 39 - rep, 400, 240]))
+        want = enc(states, off).clone()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), rep
+
+
+def test_sentences_in_8_bits_to_encrypted_logits(he):
+    """Token states -> 8-bit encoder -> packed, encrypted -> encrypted classifier -> logits, against the same in the clear."""
+    from paper_2210_02574_amd.classifier import EncryptedInference, logits_from_slots
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    layers = [SentenceEncoder.random_layer(768, 12, 1024, 7 + i, BF16, "cuda") for i in range(2)]
+    enc = SentenceEncoder(he, layers, 12).in_8_bits()
+    lengths = [17, 1, 64]
+    states, off = rand(9, sum(lengths), 768, dtype=BF16), offsets_of(lengths)
+    W = wl.weights(11)
+    level, scale = 3, 2.0**30
+    inf = EncryptedInference(he, level)
+    sk = he.keygen_secret(12)
+    keys = inf.make_keys(sk, 13)
+    cts = inf.encrypt_sentences(sk, enc, states, off, scale, 14)
+    e = enc(states, off).double().cpu().numpy()
+    pts = inf.encode_weights(W)
+    got = np.concatenate([logits_from_slots(he.decrypt(sk, he.to_host(inf.run(ct, pts, keys)), scale)) for ct in cts])
+    assert np.abs(got[:3] - e @ W.T).max() < 2.0**-8  # scale 2^30 on the smallest ring
