@@ -49,31 +49,31 @@ template <int TPR> __device__ __forceinline__ void row_sum_max(float &v, unsigne
     }
 }
 
-// x Phi(x).  With z = |x|: Phi(-z) = exp(-z^2 / 2) t p(t), t = 1 / (1 + c z); p is a fit of degree 8 to the function that this leaves, within 2e-8 of it, so that the lower tail is
-// as exact, relatively, as the exponential: 1 + erf would lose it.
+// x Phi(x) = max(x, 0) - z Phi(-z) with z = |x|, and Phi(-z) = t 2^(q(t) - z^2 log2(e) / 2), t = 1 / (1 + c z): q is a fit of degree 8 to the function that this leaves, within
+// 1.1e-7 of it, so that the lower tail is as exact, relatively, as the exponential: 1 + erf would lose it.
 __device__ __forceinline__ float gelu(float x)
 {
-    const float z = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(z, 0.21f, 1.f));
-    float p = -0.07129527628421783f;
-    p = fmaf(p, t, 0.28180667757987976f);
-    p = fmaf(p, t, -0.32649728655815125f);
-    p = fmaf(p, t, 0.34499093890190125f);
-    p = fmaf(p, t, -0.09077534824609756f);
-    p = fmaf(p, t, 0.12347319722175598f);
-    p = fmaf(p, t, 0.06956949084997177f);
-    p = fmaf(p, t, 0.08501247316598892f);
-    p = fmaf(p, t, 0.08371514827013016f);
-    const float tail = p * t * __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); // log2(e) / 2
-    return x * (x > 0.f ? 1.f - tail : tail);
+    const float z = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(z, 0.28f, 1.f));
+    float q = -0.31165364384651184f;
+    q = fmaf(q, t, 1.4158542156219482f);
+    q = fmaf(q, t, -2.3475422859191895f);
+    q = fmaf(q, t, 1.6794201135635376f);
+    q = fmaf(q, t, -0.780142068862915f);
+    q = fmaf(q, t, 0.49303320050239563f);
+    q = fmaf(q, t, 0.5668017268180847f);
+    q = fmaf(q, t, 1.4466335773468018f);
+    q = fmaf(q, t, -3.162405014038086f);
+    q = fmaf(x * x, -0.72134752044448170f, q);
+    return fmaf(-z, t * __builtin_amdgcn_exp2f(q), fmaxf(x, 0.f));
 }
 
-// The row's numbers for its integers, from the bits of max |f| (largest as an integer: a NaN is above an infinity is above all others).  Values and maximum are
-// taken times a power of two that brings the maximum into [1/2, 1): 127 / t then neither overflows nor loses bits.
+// The row's numbers for its integers, from the bits of max |f| (largest as an integer: a NaN is above an infinity is above all others).
 struct Eight {
-    float top, inv; // the maximum in [1/2, 1), and 127 / top
-    int exp;        // the power of two
-    float t;        // the maximum
-    bool bad;       // not finite
+    float t, c; // the maximum, and 127 / t
+    float top;  // the maximum times a power of two that brings it into [1/2, 1), and that power
+    int exp;
+    bool bad;   // not finite
+    bool plain; // far from the ends of the range: c neither overflows nor loses bits
     __device__ __forceinline__ explicit Eight(unsigned bits)
     {
         bad = bits >= 0x7f800000u;
@@ -81,35 +81,36 @@ struct Eight {
         const float one = bad || !bits ? 1.f : t;
         exp = -__builtin_amdgcn_frexp_expf(one);
         top = __builtin_amdgcn_frexp_mantf(one);
-        inv = 127.f / top;
+        c = __builtin_amdgcn_ldexpf(127.f / top, exp);
+        plain = exp > -100 && exp < 100;
     }
     __device__ __forceinline__ float scale(float rstd) const { return bad ? __builtin_nanf("") : t == 0.f ? 0.f : t * rstd / 127.f; }
-    // f / t * 127 to the nearest integer, in the low byte of the result: the sum with 1.5 2^23 rounds to whole numbers, ties to the even one.
+    // 127 f / t to the nearest integer, in the low byte of the result: the sum with 1.5 2^23 rounds to whole numbers, ties to the even one.
     static constexpr float MAGIC = 12582912.f;
-    __device__ __forceinline__ unsigned near(float f, float &far) const
-    {
-        const float p = __builtin_amdgcn_ldexpf(f, exp), m = fmaf(p, inv, MAGIC);
-        far = fmaxf(far, fabsf(fmaf(p, inv, MAGIC - m)));
-        return __float_as_uint(m);
-    }
-    // The same where the quotient, off by up to 2^-17 as inv is rounded, may lie on the other side of a border, or on it: the rest 127 f - n t decides, with
-    // no rounding that could change its sign for 16-bit rows and weights.
+    __device__ __forceinline__ unsigned near(float f) const { return __float_as_uint(fmaf(f, c, MAGIC)); }
+    // How far the quotient is from that integer.
+    __device__ __forceinline__ float far(float f) const { return fabsf(fmaf(f, c, MAGIC - fmaf(f, c, MAGIC))); }
+    // The same integer at the ends of the range, and where the quotient, off by up to 2^-17 as c is rounded, may lie on the other side of a border, or on it: the rest 127 f - n t
+    // decides, with no rounding that could change its sign for 16-bit rows and weights.
     __device__ __forceinline__ unsigned exact(float f) const
     {
-        const float p = __builtin_amdgcn_ldexpf(f, exp), m = fmaf(p, inv, MAGIC), n = m - MAGIC;
+        const float p = __builtin_amdgcn_ldexpf(f, exp), m = fmaf(p, 127.f / top, MAGIC), n = m - MAGIC;
         const float h = 127.f * p, rest = 2.f * (fmaf(-n, top, h) + fmaf(127.f, p, -h));
         const unsigned i = __float_as_uint(m), odd = i & 1;
         return i + (rest > top || (rest == top && odd) ? 1u : 0u) - (rest < -top || (rest == -top && odd) ? 1u : 0u);
     }
 };
-// VEC values of a row in 8 bits.
-template <int VEC> __device__ __forceinline__ Vec<int8_t, VEC> eight_vec(const float (&f)[VEC], const Eight &q)
+// VEC values of a row in 8 bits.  EXACT: the nearest integers; else, of values that are themselves off by a few 2^-22, the nearest to quotients off by 2^-17.
+template <int VEC, bool EXACT> __device__ __forceinline__ Vec<int8_t, VEC> eight_vec(const float (&f)[VEC], const Eight &q)
 {
     unsigned b[VEC];
     float far = 0.f;
 #pragma unroll
-    for (int e = 0; e < VEC; e++) b[e] = q.near(f[e], far);
-    if (!(far < 0.4999f))
+    for (int e = 0; e < VEC; e++) {
+        b[e] = q.near(f[e]);
+        if constexpr (EXACT) far = fmaxf(far, q.far(f[e]));
+    }
+    if (!q.plain || !(far < 0.49999f))
 #pragma unroll
         for (int e = 0; e < VEC; e++) b[e] = q.exact(f[e]);
     unsigned w[VEC / 4];
@@ -169,7 +170,7 @@ template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __
         const float rstd = rsqrtf(sq * inv_w + a.eps);
         if (t == 0) a.out[row] = q.scale(rstd);
 #pragma unroll
-        for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC>(v[c], q), (int8_t *)a.y + r * a.y_row);
+        for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC, true>(v[c], q), (int8_t *)a.y + r * a.y_row);
     } else {
         const float rstd = rsqrtf(row_sum<TPR>(sq, red) * inv_w + a.eps);
         if (!live) return;
@@ -333,5 +334,5 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize8(Rows8Args a
     const Eight q(top);
     if (t == 0) a.scale[row] = q.scale(1.f);
 #pragma unroll
-    for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC>(v[c], q), a.y + r * a.y_row);
+    for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC, !GELU>(v[c], q), a.y + r * a.y_row);
 }
