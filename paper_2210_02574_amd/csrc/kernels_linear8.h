@@ -176,6 +176,10 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     if constexpr (G == 1) { // 32 rows at a time, by each wave in a part of its own
         int8_t *const own = lds + wave * 32 * PITCH;
         constexpr int CHUNKS = COLS / VEC, PER = CHUNKS / 2;
+        const auto exchange = [] { // between the lanes of a wave
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
 #pragma unroll
         for (int i = 0; i < MB; i++) {
             const int m = 32 * (MB * wm + i);
@@ -188,11 +192,11 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
                     const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
                     *(Vec<T, 4> *)(own + row * PITCH + col * SIZE) = scaled(s, xs, COLS * wn + col);
                 }
-            __builtin_amdgcn_wave_barrier();
+            exchange();
             Vec<T, VEC> y[PER];
 #pragma unroll
             for (int p = 0; p < PER; p++) y[p] = *(const Vec<T, VEC> *)(own + (p * 64 + lane) / CHUNKS * PITCH + 16 * (lane % CHUNKS));
-            __builtin_amdgcn_wave_barrier();
+            exchange();
 #pragma unroll
             for (int p = 0; p < PER; p++) store(y[p], m0 + m + (p * 64 + lane) / CHUNKS, n0 + COLS * wn + lane % CHUNKS * VEC);
         }
