@@ -154,8 +154,11 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         }
     }
 
-    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as whole pieces of rows, with no lines kept: the next kernel begins
-    // with another L2, and what is written early need not be when this one ends.
+    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as whole pieces of rows.  Where those are whole lines, or halves, none is
+    // kept: the next kernel begins with another L2, and what is written early need not be when this one ends (16384 x 768 x 768 in bf16 15.3 us, 17.5 with lines kept).  Parts of lines
+    // have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
+    constexpr int SEGMENT = COLS * SIZE < 128 ? COLS * SIZE : 128;
+    const bool whole_lines = (((int64_t)a.o | a.o_row * SIZE) & (SEGMENT - 1)) == 0;
     const int row = lane % 32, h = lane / 32;
     const auto scaled = [&](const i32x4 s, float xs, int col) {
         const f32x4 ws = *(const f32x4 *)(sw + col), b = *(const f32x4 *)(sb + col);
@@ -167,9 +170,11 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     const auto store = [&](const Vec<T, VEC> y, int m, int n) {
         if (m >= a.rows) return;
         T *const to = (T *)a.o + m * a.o_row;
-        if (n + VEC <= a.channels)
+        if (n + VEC <= a.channels && whole_lines) {
+            asm volatile(""); // (or the two stores become one that keeps its lines)
             __builtin_nontemporal_store(y, (typename UnalignedVec<T, VEC>::type *)(to + n));
-        else
+            asm volatile("");
+        } else
             store_vec<T, VEC>(y, to, n, a.channels);
     };
     __syncthreads();
