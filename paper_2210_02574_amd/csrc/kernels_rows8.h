@@ -21,6 +21,7 @@ struct RmsGradArgs {
     void *ds;
     const float *rstd;
     float *part; // [gridDim.x][width]: every work-group's share of dw
+    void *dw;    // for a lone work-group, which has all of it
     int64_t dy_row, s_row, add_row, ds_row;
     int rows, width;
 };
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm8(RmsArgs a)
     rms_norm_rows<T, TW, VEC, TPR, NC, WIDTH, true>(a);
 }
 
-// Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows.  No atomics: a run repeats bit for bit.
+// Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows, unless there is but one.  No atomics: a run repeats bit for bit.
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGradArgs a)
 {
@@ -275,7 +276,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGrad
                 if constexpr (RPW > 1)
 #pragma unroll
                     for (int i = 0; i < RPW - 1; i++) u += join[(i * VEC + e) * TPR + t];
-                part[k.at + e] = u;
+                if (gridDim.x == 1)
+                    ((TW *)a.dw)[k.at + e] = (TW)u;
+                else
+                    part[k.at + e] = u;
             }
     }
 }

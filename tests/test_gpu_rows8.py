@@ -509,6 +509,52 @@ def test_encoder_in_8_bits(he, norm, pool, width, inner):
         enc8(states.clone().requires_grad_(True), off)
 
 
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+def test_encoder_in_8_bits_keeps_sentences_and_padding_apart(he, norm):
+    """A padded batch whose padding holds NaN and infinities, against the same sentences packed: every operator works on rows or sequences alone; attention's tiles lie elsewhere,
+    which is a rounding of 2^-24 here, and a neighbouring integer now and then."""
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    layers = [SentenceEncoder.random_layer(64, 2, 96, 5 + i, F32, "cuda", std=0.1) for i in range(2)]
+    enc = SentenceEncoder(he, layers, 2, norm=norm, last=rand(3, 64) if norm == "rms" else None).in_8_bits()
+    lengths, packed = [20, 0, 1, 39], rand(1, 60, 64)
+    padded, at = torch.full((4 * 40, 64), float("nan"), device="cuda"), 0
+    padded[30] = float("inf")
+    for i, n in enumerate(lengths):
+        padded[40 * i:40 * i + n] = packed[at:at + n]
+        at += n
+    begin = torch.arange(0, 160, 40, dtype=torch.int32, device="cuda")
+    a, b = enc(packed, offsets_of(lengths)), enc(padded, (begin, begin + torch.tensor(lengths, dtype=torch.int32, device="cuda")))
+    assert torch.isfinite(b).all() and (a - b).abs().max() <= 0.02 * a.abs().max()
+    packed[5, 7] = float("nan")  # of the first sentence
+    c = enc(packed, offsets_of(lengths))
+    assert torch.isnan(c[0]).all() and torch.equal(a[1:], c[1:])
+
+
+def test_two_threads_at_once(he):
+    import threading
+
+    ins = [_inputs(he, 70, 400, 200, 300), _inputs(he, 80, 20, 1000, 90)]
+    want = [[t.clone() for t in _everything(he, *i)] for i in ins]
+    torch.cuda.synchronize()
+    bad, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def work(k):
+        with torch.cuda.stream(streams[k]):
+            for _ in range(50):
+                got = _everything(he, *ins[k])
+            streams[k].synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(got, want[k])):
+                bad.append(k)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
 def test_encoder_in_8_bits_in_a_graph(he):
     from paper_2210_02574_amd.embedding import SentenceEncoder
 
