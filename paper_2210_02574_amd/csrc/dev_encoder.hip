@@ -457,23 +457,25 @@ struct Product8Plan {
     int tile, groups; // rows and channels of a work-group, groups of waves that share its sums
     int64_t tiles;
 };
-// Rules go by the number of tiles.  Times in us with results in bf16, rows x width x channels: tiles of 256, 128, 64, of 64 with four groups, of 32 with four and with eight:
+// Rules go by the number of tiles.  Times in us with results in bf16, rows x width x channels: tiles of 256, 128, 64, of 64 with four groups;
 //   16384 x 4096 x 4096 236, 281, 400, 582; 4096 x 4096 x 4096 63, 73, 112; 2048 x 4096 x 4096 50, 37, 54; 768 x 4096 x 4096 44, 24, 21; 16384 x 2048 x 768 30, 32, 43;
 //   16384 x 768 x 768 15.8, 15.3, 21; 4096 x 768 x 2304 15, 14, 17; 4096 x 768 x 768 14, 6.9, 7.0; 1000 x 768 x 768 13, 5.9, 4.8, 4.9;
-//   1000 x 4096 x 1024 42, 23, 13, 10, 14, 20; 300 x 2048 x 2048 24, 9.9, 7.6, 6.7, 8.4, 10; 512 x 4096 x 4096 43, 22, 17, 20, 29, 41;
-//   200 x 8192 x 2000 -, 30, 22, 15, 12, 16; 500 x 768 x 768 -, 5.9, 4.6, 5.0, 4.4, 6.0; 64 x 4096 x 4096 41, 16, 12, 9.0, 7.3, 7.1;
-//   100 x 8192 x 1024 75, 28, 20, 14, 9.2, 8.0; 32 x 2048 x 768 23, 9.4, 7.2, 6.2, 4.5, 4.2; 23 x 768 x 768 12, 5.6, 4.5, 4.8, 3.7, 3.6.
+//   1000 x 4096 x 1024 42, 23, 13, 10; 512 x 4096 x 4096 43, 22, 17, 20.
+// Of 64, of 64 with four groups, of 32 with four, of 16 with four and with eight:
+//   1000 x 768 x 768 4.9, 5.1, 6.1; 300 x 2048 x 2048 7.9, 6.9, 7.7, 9.4; 500 x 768 x 768 4.7, 5.0, 4.2, 5.3; 200 x 8192 x 2000 22, 15, 12, 19; 64 x 4096 x 4096 12, 9.0, 6.2, 7.8;
+//   8 x 8192 x 8192 33, 18, 11.8, 11.6; 16 x 1024 x 8192 5.2, 5.2, 3.7, 3.3; 100 x 8192 x 1024 20, 14, 7.0, 7.0, 7.3; 20 x 3000 x 3000 9.8, 7.7, 4.5, 4.2, 4.4;
+//   32 x 8192 x 1024 20, 14, 6.7, 5.0, 4.6; 5 x 4861 x 1900 13, 9.8, 5.4, 4.1, 3.9; 23 x 768 x 768 4.6, 4.8, 3.5, 3.0, 3.1; 1 x 768 x 768 4.4, 4.7, 3.6, 2.9, 3.0.
 // 256: from three quarters of a round of the 256 CUs on, unless a short sum meets a last round with few tiles (16384 x 768 x 2304, 2.25 rounds: 49, 41) or edges
-// leave an eighth more of the area empty than in tiles of 128 (65536 x 2048 x 64: 34, 23, 22).  128: from a tile for each CU on.  32: as long as all tiles are resident at once,
-// two of them to a CU with four groups, one with eight.
+// leave an eighth more of the area empty than in tiles of 128 (65536 x 2048 x 64: 34, 23, 22).  128: from a tile for each CU on.  32 and 16: as long as two tiles to a CU
+// are all there are.  Eight groups: a tile to a CU, and sums that are long enough for all.
 Product8Plan product8_plan(const he_product8 *p)
 {
     const auto tiles = [&](int tile) { return ((p->rows + tile - 1) / tile) * ((p->channels + tile - 1) / tile); };
-    const int64_t t256 = tiles(256), t128 = tiles(128), t64 = tiles(64), t32 = tiles(32);
+    const int64_t t256 = tiles(256), t128 = tiles(128), t64 = tiles(64), t32 = tiles(32), t16 = tiles(16);
     const bool ragged = p->width < 1024 && t256 > 256 && 10 * ((t256 + 255) / 256 * 256) > 13 * t256;
     if (t256 >= 192 && !ragged && 32 * t256 <= 9 * t128) return {256, 1, t256};
     if (t128 >= 256 && 32 * t128 <= 9 * t64) return {128, 1, t128};
-    if (t32 <= 256) return {32, 8, t32};
+    if (t16 <= 512) return {16, t16 <= 256 && p->width >= 2048 ? 8 : 4, t16};
     if (t32 <= 512) return {32, 4, t32};
     return {64, t64 <= 256 && p->width >= 1024 ? 4 : 1, t64};
 }

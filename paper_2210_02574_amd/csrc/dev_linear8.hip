@@ -16,6 +16,11 @@ template <int MB, int NB, int WM, int WN, int G, int OCC> static void tiles(he_c
     a.tiles_m = (a.rows + BM - 1) / BM, a.tiles_n = (a.channels + BN - 1) / BN;
     KLAUNCH_T(c, st, KID_LINEAR8, bytes, (k_linear8<T, MB, NB, WM, WN, G, OCC>), (unsigned)(a.tiles_m * a.tiles_n), 64 * WM * WN * G, a);
 }
+template <int BLK, int G> static void few(he_ctx *c, hipStream_t st, double bytes, Linear8Args a)
+{
+    a.tiles_m = (a.rows + BLK - 1) / BLK, a.tiles_n = (a.channels + BLK - 1) / BLK;
+    KLAUNCH_T(c, st, KID_LINEAR8_FEW, bytes, (k_linear8_few<T, BLK, G>), (unsigned)(a.tiles_m * a.tiles_n), 64 * G, a);
+}
 static void product(he_ctx *c, hipStream_t st, double bytes, int tile, int groups, const Linear8Args &a)
 {
     if (tile == 256)
@@ -26,10 +31,12 @@ static void product(he_ctx *c, hipStream_t st, double bytes, int tile, int group
         tiles<1, 1, 2, 2, 1, 4>(c, st, bytes, a);
     else if (tile == 64)
         tiles<1, 1, 2, 2, 4, 4>(c, st, bytes, a);
+    else if (tile == 32)
+        few<32, 4>(c, st, bytes, a);
     else if (groups == 4)
-        tiles<1, 1, 1, 1, 4, 2>(c, st, bytes, a);
+        few<16, 4>(c, st, bytes, a);
     else
-        tiles<1, 1, 1, 1, 8, 2>(c, st, bytes, a);
+        few<16, 8>(c, st, bytes, a);
 }
 
 #define NAME_(t) linear8_launch_##t

@@ -5,6 +5,7 @@
 // Weights are operand A, rows of x operand B: a lane then holds four neighbouring channels of one row, which it can write together.
 #pragma once
 #include "enc_common.h"
+#include <type_traits>
 
 typedef Vec<int, 4> i32x4;
 typedef Vec<int, 16> i32x16;
@@ -31,12 +32,22 @@ __device__ __forceinline__ void fetch_lds(__amdgpu_buffer_rsrc_t from, unsigned 
 // Chunk c of 16 bytes of row r lies at c ^ (r / 2 mod 8) of the row's 128 bytes in LDS: the 16 rows that a 16-byte read takes at a time then lie in 16 different places.
 __device__ __forceinline__ int linear8_twist(int row) { return row >> 1 & 7; }
 
+// The tile of a work-group.  Each of the eight dies takes a run of tiles that follow one another, in bands of eight tiles of rows, so that they share operands in its L2.
+__device__ __forceinline__ void linear8_tile(const Linear8Args &a, int &m, int &n)
+{
+    const int tiles = a.tiles_m * a.tiles_n, per = tiles / 8, extra = tiles % 8, die = blockIdx.x % 8;
+    const int id = die * per + min(die, extra) + blockIdx.x / 8;
+    constexpr int BAND = 8;
+    const int band = id / (BAND * a.tiles_n), first = band * BAND, high = min(BAND, a.tiles_m - first), in = id - band * BAND * a.tiles_n;
+    m = first + in % high, n = in / high;
+}
+
 // Tiles of 32 MB WM rows by 32 NB WN channels, WM x WN waves with MB x NB blocks of 32 x 32 each; G such groups of waves share the sum, each taking every G-th
 // stage.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
 // stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
 template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
 {
-    static_assert(G == 1 || (G % 4 == 0 && MB == 1 && NB == 1), "");
+    static_assert(G == 1 || (G == 4 && MB == 1 && NB == 1), "");
     constexpr int W = WM * WN, THREADS = 64 * W * G, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * LINEAR8_K;
     constexpr int SIZE = (int)sizeof(T), VEC = 16 / SIZE;
     constexpr int COLS = G == 1 ? 32 * NB : BN, PITCH = COLS * SIZE + 16; // of a row of results in LDS, bytes
@@ -45,12 +56,9 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     __shared__ __attribute__((aligned(16))) float sx[BM], sw[BN], sb[BN];
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % W, group = all / W, wm = wave % WM, wn = wave / WM;
 
-    // Each of the eight dies takes a run of tiles that follow one another, in bands of eight tiles of rows, so that they share operands in its L2.
-    const int tiles = a.tiles_m * a.tiles_n, per = tiles / 8, extra = tiles % 8, die = blockIdx.x % 8;
-    const int id = die * per + min(die, extra) + blockIdx.x / 8;
-    constexpr int BAND = 8;
-    const int band = id / (BAND * a.tiles_n), first = band * BAND, high = min(BAND, a.tiles_m - first), in = id - band * BAND * a.tiles_n;
-    const int m0 = (first + in % high) * BM, n0 = in / high * BN;
+    int tile_m, tile_n;
+    linear8_tile(a, tile_m, tile_n);
+    const int m0 = tile_m * BM, n0 = tile_n * BN;
 
     const int steps = (a.width + LINEAR8_K - 1) / LINEAR8_K, rounds = (steps + G - 1) / G, tail = a.width % LINEAR8_K;
     const int whole = (a.width + 15) / 16 * 16; // bytes of a row that may be read
@@ -205,21 +213,111 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
 #pragma unroll
             for (int p = 0; p < PER; p++) store(y[p], m0 + m + (p * 64 + lane) / CHUNKS, n0 + COLS * wn + lane % CHUNKS * VEC);
         }
-    } else { // each of the first four groups joins a quarter of all groups' sums of each block
+    } else { // each of the four groups joins a quarter of all groups' sums of each block
         i32x4 *const join = (i32x4 *)lds + wave * G * 256; // [group][quarter][lane]
 #pragma unroll
         for (int g = 0; g < 4; g++) join[(group * 4 + g) * 64 + lane] = i32x4{acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2], acc[0][0][4 * g + 3]};
         __syncthreads();
         i32x4 s = {};
-        if (group < 4)
 #pragma unroll
-            for (int g = 0; g < G; g++) s += join[(g * 4 + group) * 64 + lane];
+        for (int g = 0; g < G; g++) s += join[(g * 4 + group) * 64 + lane];
         int8_t *const out = lds + G * W * 4096;
         const int m = 32 * wm + row, col = 32 * wn + 8 * group + 4 * h;
-        if (group < 4) *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
+        *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
         __syncthreads();
         constexpr int CHUNKS = COLS / VEC;
         for (int p = threadIdx.x; p < BM * CHUNKS; p += THREADS)
             store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), m0 + p / CHUNKS, n0 + p % CHUNKS * VEC);
     }
+}
+
+// Few tiles: BLK rows by BLK channels, 16 or 32, and G waves that share the sum, each with two stages of its own, which it alone waits for: no barrier until the waves' sums are joined.
+// What bounds it is how much the card has under way and, of short sums, a launch and two trips to memory.
+template <class T, int BLK, int G> __global__ __launch_bounds__(64 * G) void k_linear8_few(Linear8Args a)
+{
+    constexpr int ROWS = BLK * LINEAR8_K, STAGE = 2 * ROWS, LOADS = BLK / 8;       // bytes of a stage's rows of x, of all of it; loads that bring the former
+    constexpr int KK = BLK == 32 ? 4 : 2, PARTS = 64 / BLK, QUARTERS = BLK * BLK / 256; // matrix instructions to a stage; lanes to a row; results of a lane, by fours
+    __shared__ __attribute__((aligned(1024))) int8_t lds[G * 2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int tile_m, tile_n;
+    linear8_tile(a, tile_m, tile_n);
+    const int m0 = tile_m * BLK, n0 = tile_n * BLK;
+    const int steps = (a.width + LINEAR8_K - 1) / LINEAR8_K, tail = a.width % LINEAR8_K, whole = (a.width + 15) / 16 * 16;
+    const int8_t *const xb = a.x + m0 * a.x_row, *const wb = a.w + n0 * a.w_row;
+    const int bytes_m = (min(BLK, a.rows - m0) - 1) * (int)a.x_row + whole, bytes_n = (min(BLK, a.channels - n0) - 1) * (int)a.w_row + whole;
+    unsigned at_m[LOADS], at_n[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+        const int row = 8 * i + lane / 8, c = 16 * (lane % 8 ^ linear8_twist(row));
+        at_m[i] = (unsigned)row * (unsigned)a.x_row + c;
+        at_n[i] = (unsigned)row * (unsigned)a.w_row + c;
+    }
+    int8_t *const mine = lds + wave * 2 * STAGE;
+    const auto fetch = [&](int step, int8_t *stage) { // step < steps
+        const int k = step * LINEAR8_K;
+        const __amdgpu_buffer_rsrc_t rm = __builtin_amdgcn_make_buffer_rsrc((void *)(xb + k), 0, bytes_m - k, 0x00027000);
+        const __amdgpu_buffer_rsrc_t rn = __builtin_amdgcn_make_buffer_rsrc((void *)(wb + k), 0, bytes_n - k, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            fetch_lds(rm, at_m[i], stage + i * 1024);
+            fetch_lds(rn, at_n[i], stage + ROWS + i * 1024);
+        }
+    };
+    typedef typename std::conditional<BLK == 32, i32x16, i32x4>::type Sums;
+    Sums acc = {};
+    const int row = lane % BLK, part = lane / BLK;
+    if (wave < steps) fetch(wave, mine);
+    if (wave + G < steps) fetch(wave + G, mine + STAGE);
+    for (int t = 0, step = wave; step < steps; t ^= 1, step += G) {
+        int8_t *const stage = mine + t * STAGE;
+        if (step + G < steps) // the next stage's loads may be under way
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        i32x4 fx[KK], fw[KK];
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            const int at = row * LINEAR8_K + 16 * ((PARTS * kk + part) ^ linear8_twist(row));
+            fx[kk] = *(const i32x4 *)(stage + at);
+            fw[kk] = *(const i32x4 *)(stage + ROWS + at);
+        }
+        if (step + 1 == steps && tail) // numbers of weights behind the end of the sum
+#pragma unroll
+            for (int kk = 0; kk < KK; kk++) {
+                const int left = tail - 16 * (PARTS * kk + part);
+#pragma unroll
+                for (int e = 0; e < 4; e++) fw[kk][e] &= left >= 4 * e + 4 ? -1 : left <= 4 * e ? 0 : (int)((1u << 8 * (left - 4 * e)) - 1);
+            }
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            if constexpr (BLK == 32)
+                acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk], fx[kk], acc, 0, 0, 0);
+            else
+                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[kk], fx[kk], acc, 0, 0, 0);
+        }
+        if (step + 2 * G < steps) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // this one has been read
+            fetch(step + 2 * G, stage);
+        }
+    }
+    __syncthreads();
+    i32x4 *const join = (i32x4 *)lds; // [wave][quarter][lane]
+#pragma unroll
+    for (int p = 0; p < QUARTERS; p++) join[(wave * QUARTERS + p) * 64 + lane] = i32x4{acc[4 * p], acc[4 * p + 1], acc[4 * p + 2], acc[4 * p + 3]};
+    __syncthreads();
+    if (wave >= QUARTERS) return;
+    i32x4 s = {};
+#pragma unroll
+    for (int g = 0; g < G; g++) s += join[(g * QUARTERS + wave) * 64 + lane];
+    const int m = m0 + row, n = n0 + 8 * wave + 4 * part; // four channels of a row
+    if (m >= a.rows) return;
+    const float xs = a.x_scale[m];
+    Vec<T, 4> y;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const int c = min(n + e, a.channels - 1);
+        const float b = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[c] : (float)((const T *)a.bias)[c];
+        y[e] = (T)fmaf((float)s[e] * xs, a.w_scale[c], b);
+    }
+    store_vec<T, 4>(y, (T *)a.o + m * a.o_row, n, a.channels);
 }

@@ -16,7 +16,7 @@ enum KernelId {
     KID_INV_BLOCKS, KID_INV_COLS, KID_LIMBWISE, KID_CMULT, KID_COPY, KID_INNER_SPECIAL, KID_INNER_FINISHED, KID_INNER_FIN,
     KID_FWD12, KID_FWD12_MODUP, KID_FWD12_RESCALE, KID_INV12, KID_INNER12, KID_FIN12, // N = 2^12
     KID_ATTN, KID_ATTN_FEW, KID_ATTN_JOIN, KID_ATTN_GRAD_SIZE, KID_ATTN_GRAD_Q, KID_ATTN_GRAD_KV, KID_ATTN_GRAD_JOIN, KID_NORM, KID_NORM_GRAD, KID_NORM_WEIGHT_GRAD, KID_POOL, KID_POOL_JOIN, KID_POOL_GRAD, // token states
-    KID_RMS, KID_RMS8, KID_RMS_GRAD, KID_RMS_WEIGHT_GRAD, KID_QUANTIZE8, KID_LINEAR8,
+    KID_RMS, KID_RMS8, KID_RMS_GRAD, KID_RMS_WEIGHT_GRAD, KID_QUANTIZE8, KID_LINEAR8, KID_LINEAR8_FEW,
     KID_COUNT
 };
 
