@@ -2,8 +2,10 @@
 x -> F_emb(x), then encryption), with gradients, so that an encoder can be fitted in the clear before its embeddings are.
 
 The operators are the library's (HE.attention, HE.layer_norm, HE.rms_norm, HE.pool_mean); the functions here make them differentiable, and SentenceEncoder puts them
-together.  Matrix products with weights are plain library products there; SentenceEncoder8, for inference, has them in 8 bits (HE.rms_norm8, HE.quantize8, HE.linear8).  Sentences are packed back to back or padded, as HE's offsets say.
-Gradients are of the first order: a backward pass that is to be differentiated again is refused.
+together.  Matrix products with weights are plain library products there; SentenceEncoder8, for inference, has them in 8 bits (HE.rms_norm8, HE.quantize8,
+HE.linear8).  Sentences are packed back to back or padded, as HE's offsets say.
+Gradients are of the first order: a backward pass that is to be differentiated again is refused.  One that is captured in a HIP graph needs leaves that no living eager
+graph has: torch would have the capture wait for that graph's stream.
 """
 from __future__ import annotations
 
@@ -215,7 +217,12 @@ class SentenceEncoder:
 
     def _product(self, w, name, a, lo=None, hi=None):
         """Rows of a times weights w[name], or their channels lo .. hi."""
-        return F.linear(a, w[name][lo:hi], w[name + "_bias"][lo:hi])
+        part = self._all if lo is None and hi is None else lambda t: t[lo:hi]
+        return F.linear(a, part(w[name]), part(w[name + "_bias"]))
+
+    @staticmethod
+    def _all(t):  # (a slice of all would be a copy of the gradient)
+        return t
 
     def _head(self, w, f, x):
         """What a layer's first product reads, and the layer's input."""
@@ -302,8 +309,9 @@ class SentenceEncoder8(SentenceEncoder):
         return x8.as_strided((x8.shape[0], x8.stride(0)), (x8.stride(0), 1))[begin][:, :x8.shape[1]], scale[begin]
 
     def _product(self, w, name, a, lo=None, hi=None):
+        part = self._all if lo is None and hi is None else lambda t: t[lo:hi]
         w8, scale = w[name]
-        return self.he.linear8(*a, w8[lo:hi], scale[lo:hi], bias=w[name + "_bias"][lo:hi], dtype=self.dtype)
+        return self.he.linear8(*a, part(w8), part(scale), bias=part(w[name + "_bias"]), dtype=self.dtype)
 
     def __call__(self, states, offsets):
         if states.requires_grad and torch.is_grad_enabled():

@@ -164,3 +164,17 @@ def test_reference_of_8_bits():
     x8, w8 = torch.tensor([[1, -2]], dtype=torch.int8), torch.tensor([[3, 4], [5, -6], [0, 0]], dtype=torch.int8)
     o, _ = ref.linear8(x8, torch.tensor([0.5]), w8, torch.tensor([1.0, 2.0, 3.0]), torch.tensor([0.0, 1.0, 2.0]), torch.float32)
     assert o.tolist() == [[-2.5, 18.0, 2.0]]
+
+
+def test_an_encoders_products_take_whole_weights_as_they_are():
+    """A slice of all channels would cost a copy of their gradient."""
+    from paper_2210_02574_amd.embedding import SentenceEncoder
+
+    w = SentenceEncoder.random_layer(16, 2, 8, 1, torch.float32, "cpu")
+    for t in w.values():
+        t.requires_grad_(True)
+    enc = SentenceEncoder(None, [w], 2)
+    parts = lambda y: sorted(f.name() for f, _ in y.grad_fn.next_functions if f)  # noqa: E731
+    x = torch.ones(3, 16)
+    assert not any("Slice" in n for n in parts(enc._product(w, "qkv", x)))
+    assert any("Slice" in n for n in parts(enc._product(w, "qkv", x, 16)))
