@@ -340,7 +340,7 @@ int32_t rms_args(RmsArgs &a, const he_norm *n, const he_rows *x, const he_rows *
 int rms_parts(const he_norm *n)
 {
     const int vec = 16 / (int)type_size(n->type), rows = n->width <= vec * 128 ? 8 : n->width <= vec * 256 ? 4 : 1; // of a work-group at a time
-    return n->rows <= 2 * rows ? 1 : (int)std::min<int64_t>(512, rows == 1 ? n->rows : (n->rows + 3) / 4);
+    return n->rows <= 2 * rows ? 1 : (int)std::min<int64_t>(512, (n->rows + rows - 1) / rows);
 }
 size_t rms_bytes(const he_norm *n) { return n->rows && rms_parts(n) > 1 ? (size_t)rms_parts(n) * n->width * sizeof(float) : 0; }
 bool eps_ok(const he_norm *n) { return n->eps >= 0.0 && std::isfinite((float)n->eps); }
