@@ -45,6 +45,10 @@ __device__ __forceinline__ void linear8_tile(const Linear8Args &a, int &m, int &
 // Tiles of 32 MB WM rows by 32 NB WN channels, WM x WN waves with MB x NB blocks of 32 x 32 each; G such groups of waves share the sum, each taking every G-th
 // stage.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
 // stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
+// Large products are bound by the power limit: 16384 x 4096 x 4096 231 us (2380 TOPS, matrix instructions in 0.64 of the cycles), 180 us where all numbers are zero.  Short sums are
+// bound by LDS, by a tile's first loads and by its results, which tiles of 128 cover with a second work-group on the CU: 16384 x 768 x 2304 in bf16 41 us (18 of them the
+// rate of memory), 16384 x 2048 x 768 31 us.  What gained nothing: three or four stages, of 64 or 128 numbers; work-groups that go on to another tile, its first loads under way;
+// blocks of 4 x 4 to a wave, or of 2 x 2 in tiles of 128, which read less of LDS with fewer waves; operands from memory to registers; wave priorities.
 template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
 {
     static_assert(G == 1 || (G == 4 && MB == 1 && NB == 1), "");
@@ -232,7 +236,8 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
 }
 
 // Few tiles: BLK rows by BLK channels, 16 or 32, and G waves that share the sum, each with two stages of its own, which it alone waits for: no barrier until the waves' sums are joined.
-// What bounds it is how much the card has under way and, of short sums, a launch and two trips to memory.
+// What bounds it is how much the card has under way and, of short sums, a launch and two trips to memory: 32 x 8192 x 1024 4.5 us (7.8 where
+// barriers keep eight waves together on tiles of 32), 23 x 768 x 768 3.0 us (3.6).
 template <class T, int BLK, int G> __global__ __launch_bounds__(64 * G) void k_linear8_few(Linear8Args a)
 {
     constexpr int ROWS = BLK * LINEAR8_K, STAGE = 2 * ROWS, LOADS = BLK / 8;       // bytes of a stage's rows of x, of all of it; loads that bring the former

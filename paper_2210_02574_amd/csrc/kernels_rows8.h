@@ -125,6 +125,8 @@ template <int VEC, bool EXACT> __device__ __forceinline__ Vec<int8_t, VEC> eight
     return v;
 }
 
+// Bound by memory, reads being faster than a copy: 65536 x 768 in bf16 with a residual 73 us (5.5 TB/s), 4999 x 1021 in 32 bits 8.2 us (5.0 TB/s); in 8 bits 16384 x 768 in
+// bf16 with a residual 15.6 us (5.6 TB/s), 23 rows 3.5 us, two trips to memory.
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __device__ __forceinline__ void rms_norm_rows(const RmsArgs &a)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
@@ -200,6 +202,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm8(RmsArgs a)
 }
 
 // Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows, unless there is but one.  No atomics: a run repeats bit for bit.
+// Bound by memory: 16384 x 768 in bf16 with ds' 17 us (5.9 TB/s), 4999 x 1021 in 32 bits 13.9 us (4.4 TB/s).
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGradArgs a)
 {
@@ -284,7 +287,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGrad
     }
 }
 
-// dw from the partial rows: 16 columns per work-group, 16 threads to a column.
+// dw from the partial rows: 16 columns per work-group, 16 threads to a column.  Bound by the trips to memory that follow the other kernel's end: 512 x 768 3.8 to 4.6 us, and as
+// much with 64 threads to a column.
 template <class TW> __global__ __launch_bounds__(256) void k_rms_weight_grad(const float *__restrict__ part, int parts, int width, TW *dw)
 {
     __shared__ float red[256];
@@ -310,6 +314,8 @@ struct Rows8Args {
     int64_t x_row, y_row;
     int rows, width, first;
 };
+// Gaussian error units are bound by vector instructions, some 30 to a number: 16384 x 2048 in bf16 26 us (3.9 TB/s); rows as they are by memory, or by two trips to it: 3001 x 1000
+// in fp16 5.8 us.
 template <class T, int VEC, int TPR, int NC, int WIDTH, bool GELU>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize8(Rows8Args a)
 {
