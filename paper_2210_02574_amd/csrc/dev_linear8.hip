@@ -25,6 +25,8 @@ static void product(he_ctx *c, hipStream_t st, double bytes, int tile, int group
 {
     if (tile == 256)
         tiles<4, 2, 2, 4, 1, 2>(c, st, bytes, a);
+    else if (tile == 192)
+        tiles<2, 3, 4, 2, 1, 2>(c, st, bytes, a);
     else if (tile == 128)
         tiles<2, 1, 2, 4, 1, 4>(c, st, bytes, a);
     else if (tile == 64 && groups == 1)

@@ -62,7 +62,7 @@ void rows8_launch_1(Rows8Launch &t);
 void rows8_launch_2(Rows8Launch &t);
 
 struct Linear8Launch {
-    // tile: rows and channels of a work-group; groups: of waves that share a sum.  256, 128 and 64 with one, 64 and 32 with four, 16 with four or eight
+    // tile: channels of a work-group and rows, but 256 rows with 192 channels; groups: of waves that share a sum.  256, 192, 128 and 64 with one, 64 and 32 with four, 16 with four or eight
     void (*product)(he_ctx *c, hipStream_t st, double bytes, int tile, int groups, const Linear8Args &a);
 };
 void linear8_launch_0(Linear8Launch &t);

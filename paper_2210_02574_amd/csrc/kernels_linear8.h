@@ -28,6 +28,13 @@ __device__ __forceinline__ void fetch_lds(__amdgpu_buffer_rsrc_t from, unsigned 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, at, 0, 0, 0);
 }
 
+// 16 bytes of each lane to `at` of a buffer, written to memory at once
+__device__ __forceinline__ void store_through(i32x4 v, __amdgpu_buffer_rsrc_t to, int at)
+{
+    typedef int Words __attribute__((ext_vector_type(4)));
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(Words, v), to, at, 0, 1 << 4); // scope: the device
+}
+
 #define LINEAR8_K 128 // numbers of a row that a stage holds
 // Chunk c of 16 bytes of row r lies at c ^ (r / 2 mod 8) of the row's 128 bytes in LDS: the 16 rows that a 16-byte read takes at a time then lie in 16 different places.
 __device__ __forceinline__ int linear8_twist(int row) { return row >> 1 & 7; }
@@ -54,8 +61,8 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     static_assert(G == 1 || (G == 4 && MB == 1 && NB == 1), "");
     constexpr int W = WM * WN, THREADS = 64 * W * G, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * LINEAR8_K;
     constexpr int SIZE = (int)sizeof(T), VEC = 16 / SIZE;
-    constexpr int COLS = G == 1 ? 32 * NB : BN, PITCH = COLS * SIZE + 16; // of a row of results in LDS, bytes
-    constexpr int OUT = G == 1 ? W * 32 * PITCH : G * W * 4096 + BM * PITCH, LDS = G * 2 * STAGE > OUT ? G * 2 * STAGE : OUT;
+    constexpr int PITCH = BN * SIZE + 16; // of a row of results in LDS, bytes
+    constexpr int OUT = G == 1 ? 32 * WM * PITCH : G * W * 4096 + BM * PITCH, LDS = G * 2 * STAGE > OUT ? G * 2 * STAGE : OUT;
     __shared__ __attribute__((aligned(1024))) int8_t lds[LDS];
     __shared__ __attribute__((aligned(16))) float sx[BM], sw[BN], sb[BN];
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % W, group = all / W, wm = wave % WM, wn = wave / WM;
@@ -166,11 +173,12 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         }
     }
 
-    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as whole pieces of rows.  Where those are whole lines, or halves, none is
-    // kept: the next kernel begins with another L2, and what is written early need not be when this one ends (16384 x 768 x 768 in bf16 15.3 us, 17.5 with lines kept).  Parts of lines
-    // have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
-    constexpr int SEGMENT = COLS * SIZE < 128 ? COLS * SIZE : 128;
-    const bool whole_lines = (((int64_t)a.o | a.o_row * SIZE) & (SEGMENT - 1)) == 0;
+    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as the tile's rows, whole.  Where those are whole lines they are written
+    // through L2 as they come: the next kernel begins with another L2, and what is written early need not be when this one ends (16384 x 768 x 2304 in bf16, tiles of 192 38 us, 42 with
+    // lines kept; 40 past the caches, and with halves of lines 45 to 70).  Parts of lines have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
+    const int64_t pitch = a.o_row * SIZE;
+    const bool through = (((int64_t)a.o | pitch) & 127) == 0 && pitch < (1 << 23); // (offsets inside a tile have 32 bits)
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((int8_t *)a.o + m0 * pitch, 0, through ? min(BM, a.rows - m0) * (int)pitch : 0, 0x00027000);
     const int row = lane % 32, h = lane / 32;
     const auto scaled = [&](const i32x4 s, float xs, int col) {
         const f32x4 ws = *(const f32x4 *)(sw + col), b = *(const f32x4 *)(sb + col);
@@ -179,43 +187,42 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         for (int e = 0; e < 4; e++) y[e] = (T)fmaf((float)s[e] * xs, ws[e], b[e]);
         return y;
     };
-    const auto store = [&](const Vec<T, VEC> y, int m, int n) {
-        if (m >= a.rows) return;
-        T *const to = (T *)a.o + m * a.o_row;
-        if (n + VEC <= a.channels && whole_lines) {
-            asm volatile(""); // (or the two stores become one that keeps its lines)
-            __builtin_nontemporal_store(y, (typename UnalignedVec<T, VEC>::type *)(to + n));
-            asm volatile("");
-        } else
-            store_vec<T, VEC>(y, to, n, a.channels);
+    const auto store = [&](const Vec<T, VEC> y, int m, int n) { // row m of the tile
+        if (m0 + m >= a.rows) return;
+        if (n + VEC <= a.channels && through)
+            store_through(__builtin_bit_cast(i32x4, y), ro, m * (int)pitch + n * SIZE);
+        else
+            store_vec<T, VEC>(y, (T *)((int8_t *)a.o + (m0 + m) * pitch), n, a.channels);
     };
     __syncthreads();
-    if constexpr (G == 1) { // 32 rows at a time, by each wave in a part of its own
-        int8_t *const own = lds + wave * 32 * PITCH;
-        constexpr int CHUNKS = COLS / VEC, PER = CHUNKS / 2;
-        const auto exchange = [] { // between the lanes of a wave
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        };
+    constexpr int CHUNKS = BN / VEC;
+    if constexpr (G == 1) { // 32 rows of each wave at a time
+        constexpr int PER = 32 * WM * CHUNKS / THREADS;
+        static_assert(PER * THREADS == 32 * WM * CHUNKS, "");
 #pragma unroll
         for (int i = 0; i < MB; i++) {
-            const int m = 32 * (MB * wm + i);
-            const float xs = sx[m + row];
+            if (i) __syncthreads();
+            const float xs = sx[32 * (MB * wm + i) + row];
 #pragma unroll
             for (int j = 0; j < NB; j++)
 #pragma unroll
                 for (int g = 0; g < 4; g++) {
-                    const int col = 32 * j + 8 * g + 4 * h;
+                    const int col = 32 * (NB * wn + j) + 8 * g + 4 * h;
                     const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    *(Vec<T, 4> *)(own + row * PITCH + col * SIZE) = scaled(s, xs, COLS * wn + col);
+                    *(Vec<T, 4> *)(lds + (32 * wm + row) * PITCH + col * SIZE) = scaled(s, xs, col);
                 }
-            exchange();
+            __syncthreads();
             Vec<T, VEC> y[PER];
 #pragma unroll
-            for (int p = 0; p < PER; p++) y[p] = *(const Vec<T, VEC> *)(own + (p * 64 + lane) / CHUNKS * PITCH + 16 * (lane % CHUNKS));
-            exchange();
+            for (int p = 0; p < PER; p++) {
+                const int at = p * THREADS + threadIdx.x;
+                y[p] = *(const Vec<T, VEC> *)(lds + at / CHUNKS * PITCH + 16 * (at % CHUNKS));
+            }
 #pragma unroll
-            for (int p = 0; p < PER; p++) store(y[p], m0 + m + (p * 64 + lane) / CHUNKS, n0 + COLS * wn + lane % CHUNKS * VEC);
+            for (int p = 0; p < PER; p++) {
+                const int at = p * THREADS + threadIdx.x, r = at / CHUNKS;
+                store(y[p], 32 * (MB * (r / 32) + i) + r % 32, n0 + at % CHUNKS * VEC);
+            }
         }
     } else { // each of the four groups joins a quarter of all groups' sums of each block
         i32x4 *const join = (i32x4 *)lds + wave * G * 256; // [group][quarter][lane]
@@ -229,9 +236,8 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         const int m = 32 * wm + row, col = 32 * wn + 8 * group + 4 * h;
         *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
         __syncthreads();
-        constexpr int CHUNKS = COLS / VEC;
         for (int p = threadIdx.x; p < BM * CHUNKS; p += THREADS)
-            store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), m0 + p / CHUNKS, n0 + p % CHUNKS * VEC);
+            store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), p / CHUNKS, n0 + p % CHUNKS * VEC);
     }
 }
 

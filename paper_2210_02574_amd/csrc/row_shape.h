@@ -1,5 +1,6 @@
 // How the rows of a width are laid over threads; T is the translation unit's element type.
 #pragma once
+#include "enc_launch.h"
 static constexpr int VEC = 16 / sizeof(T);
 static constexpr unsigned GRID_THREADS = 1u << 31; // of one launch: the hardware counts them in 32 bits
 
@@ -17,6 +18,7 @@ template <class F> static void row_shape(int width, F f)
     SHAPE(32, 1) SHAPE(32, 2) SHAPE(32, 3) SHAPE(32, 4)
     SHAPE(64, 3) SHAPE(64, 4)
     SHAPE(256, 2) SHAPE(256, 3) SHAPE(256, 4)
-    SHAPE(1024, 2) SHAPE(1024, 4)
+    SHAPE(1024, 2)
+    if constexpr (VEC * 1024 * 2 < NORM_MAX_WIDTH) { SHAPE(1024, 4) }
 #undef SHAPE
 }

@@ -193,7 +193,8 @@ def test_quantize_of_strided_and_unaligned_rows(he):
     (1, 1, 1), (1, 16, 16), (2, 15, 17), (15, 64, 3), (16, 65, 16), (17, 127, 33), (23, 768, 768), (31, 1021, 50), (32, 128, 257), (33, 100, 64), (48, 300, 31),
     (64, 2048, 65), (65, 64, 64), (65, 1, 1), (65, 129, 200), (100, 768, 100), (127, 1000, 129), (128, 130, 128), (129, 16, 63), (200, 257, 1021), (300, 113, 300),
     (1000, 384, 777), (1, 8192, 20), (40, 65536, 17), (70, 65535, 66), (700, 300, 700), (600, 1400, 800), (1100, 700, 1000), (2050, 200, 1500), (3100, 144, 4000), (3333, 1040, 4001), (1024, 129, 12400),
-    (1000, 1101, 777), (1, 2048, 1), (17, 5001, 100), (16, 33, 4000), (40, 7777, 31), (500, 2000, 1000), (33, 4097, 700)])
+    (1000, 1101, 777), (1, 2048, 1), (17, 5001, 100), (16, 33, 4000), (40, 7777, 31), (500, 2000, 1000), (33, 4097, 700),
+    (2900, 130, 3301), (700, 1040, 12001), (8000, 1030, 2896)])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_product(he, rows, width, channels, dtype):
     x8, w8 = integers(1, rows, width, 32), integers(2, channels, width)
