@@ -8,12 +8,42 @@
 #pragma once
 #include "kernels_norm.h"
 
+// How results are written that fill whole lines, each by one wave.  KEEP: as lines that stay in L2 until the kernel's end.  THROUGH: to the last-level cache as they come, where all of
+// them fit in the L2s, and would leave them only at the end.  PAST: to memory, where what the call moves does not fit in the last-level cache.
+enum { KEEP, THROUGH, PAST };
+template <class T, int VEC, int WIDTH> __device__ __forceinline__ void write_vec(const Cols<VEC, WIDTH> &k, const Vec<T, VEC> v, void *to, int64_t row, int how)
+{
+    if constexpr (WIDTH == WIDTH_EVEN) {
+        if (how == THROUGH) {
+            typedef int Words __attribute__((ext_vector_type(sizeof(v) / 4)));
+            const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(to, 0, 0x7fffffff, 0x00027000);
+            const int at = (int)(row + k.at) * (int)sizeof(T);
+            if (!k.in) return;
+            if constexpr (sizeof(v) == 16)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(Words, v), all, at, 0, 1 << 4); // scope: the device
+            else if constexpr (sizeof(v) == 8)
+                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(Words, v), all, at, 0, 1 << 4);
+            else
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, v), all, at, 0, 1 << 4);
+            return;
+        }
+        if (how == PAST) {
+            asm volatile(""); // (or this store and the other become one that keeps its lines)
+            if (k.in) __builtin_nontemporal_store(v, (Vec<T, VEC> *)((T *)to + row + k.at));
+            asm volatile("");
+            return;
+        }
+    }
+    k.store(v, (T *)to + row);
+}
+
 struct RmsArgs {
     const void *x, *r, *w;
     void *y, *s;  // y: the rows' type, or 8-bit integers
     float *out;   // [rows]: rstd, or the scales
     int64_t x_row, r_row, y_row, s_row; // row strides, in elements
     int rows, width, first; // rows, of them the first one of this launch
+    int how;                // y and s are written
     float eps;
 };
 struct RmsGradArgs {
@@ -23,7 +53,7 @@ struct RmsGradArgs {
     float *part; // [gridDim.x][width]: every work-group's share of dw
     void *dw;    // for a lone work-group, which has all of it
     int64_t dy_row, s_row, add_row, ds_row;
-    int rows, width;
+    int rows, width, how;
 };
 
 // The sum of v and the largest m over the TPR threads of a row, the same in each; red: two words per wave.
@@ -153,7 +183,7 @@ template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __
         if (a.r) {
 #pragma unroll
             for (int e = 0; e < VEC; e++) x[c][e] = (T)((float)x[c][e] + (float)res[c][e]);
-            if (live) k.store(x[c], (T *)a.s + r * a.s_row);
+            if (live) write_vec<T>(k, x[c], a.s, r * a.s_row, a.how);
         }
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
@@ -173,7 +203,7 @@ template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __
         const float rstd = rsqrtf(sq * inv_w + a.eps);
         if (t == 0) a.out[row] = q.scale(rstd);
 #pragma unroll
-        for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC, true>(v[c], q), (int8_t *)a.y + r * a.y_row);
+        for (int c = 0; c < NC; c++) write_vec<int8_t>(Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width), eight_vec<VEC, true>(v[c], q), a.y, r * a.y_row, a.how);
     } else {
         const float rstd = rsqrtf(row_sum<TPR>(sq, red) * inv_w + a.eps);
         if (!live) return;
@@ -185,7 +215,7 @@ template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __
             Vec<T, VEC> y;
 #pragma unroll
             for (int e = 0; e < VEC; e++) y[e] = (T)(v[c][e] * rstd * (float)w[e]);
-            k.store(y, (T *)a.y + r * a.y_row);
+            write_vec<T>(k, y, a.y, r * a.y_row, a.how);
         }
     }
 }
@@ -257,7 +287,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGrad
                 if (a.add) u += (float)add[c][e];
                 o[e] = (T)u;
             }
-            k.store(o, (T *)a.ds + row * a.ds_row);
+            write_vec<T>(k, o, a.ds, row * a.ds_row, a.how);
         }
     }
     float *part = a.part + (size_t)blockIdx.x * a.width;
@@ -312,7 +342,7 @@ struct Rows8Args {
     int8_t *y;
     float *scale;
     int64_t x_row, y_row;
-    int rows, width, first;
+    int rows, width, first, how;
 };
 // Gaussian error units are bound by vector instructions, some 30 to a number: 16384 x 2048 in bf16 26 us (3.9 TB/s); rows as they are by memory, or by two trips to it: 3001 x 1000
 // in fp16 5.8 us.
@@ -344,5 +374,5 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize8(Rows8Args a
     const Eight q(top);
     if (t == 0) a.scale[row] = q.scale(1.f);
 #pragma unroll
-    for (int c = 0; c < NC; c++) Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width).store(eight_vec<VEC, !GELU>(v[c], q), a.y + r * a.y_row);
+    for (int c = 0; c < NC; c++) write_vec<int8_t>(Cols<VEC, WIDTH>((c * TPR + t) * VEC, a.width), eight_vec<VEC, !GELU>(v[c], q), a.y, r * a.y_row, a.how);
 }

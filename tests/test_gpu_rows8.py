@@ -242,6 +242,35 @@ def test_product_far_into_long_buffers(he, rows, width, channels):
         assert ((o[at:at + 300].double() - want[0]).abs() <= want[1]).all(), at
 
 
+@pytest.mark.parametrize("dtype,width", [(BF16, 768), (F16, 64), (F32, 128), (BF16, 100), (F32, 1021)])
+def test_results_are_the_same_however_they_are_written(he, dtype, width):
+    """Rows do not hang on one another: a call that moves more than the last-level cache holds, rows of it alone, and rows that begin inside lines, bit for bit."""
+    rows = 300 * 2**20 // (width * torch.finfo(dtype).bits // 8) // 3
+    x, r, w = rand(1, rows, width, dtype=dtype), rand(2, rows, width, dtype=dtype), rand(3, width, dtype=dtype)
+    y, s, rstd = he.rms_norm(x, w, residual=r)
+    alone, _, rstd1 = he.rms_norm(x, w)
+    y8, scale, s8 = he.rms_norm8(x, w, residual=r)
+    q8, q = he.quantize8(x)
+    dx, _ = he.rms_norm_backward(r, s, w, rstd, ds=x)
+    assert torch.equal(s, x + r) and torch.equal(s8, s)
+    for at in (0, rows // 3, rows - 1000):
+        i = slice(at, at + 1000)
+        small = he.rms_norm(x[i], w, residual=r[i])
+        assert torch.equal(small[0], y[i]) and torch.equal(small[2], rstd[i])
+        buf = torch.full((1002, width + 64 * 4), 7.0, dtype=dtype, device="cuda")
+        for out in (buf[1:-1, 64:64 + width], buf[1:-1, 1:1 + width]):
+            out.fill_(0)
+            assert he.rms_norm(x[i], w, out=out)[0] is out and torch.equal(out, alone[i])
+            out.fill_(7)
+        assert (buf == 7).all()
+        small8 = he.rms_norm8(x[i], w, residual=r[i])
+        assert torch.equal(small8[0], y8[i]) and torch.equal(small8[1], scale[i])
+        small8 = he.quantize8(x[i])
+        assert torch.equal(small8[0], q8[i]) and torch.equal(small8[1], q[i])
+        assert torch.equal(he.rms_norm_backward(r[i], s[i], w, rstd[i], ds=x[i])[0], dx[i])
+    assert torch.equal(rstd1[:9], he.rms_norm(x[:9], w)[2])
+
+
 def test_more_rows_than_a_launch_holds(he):
     """2^32 threads are too many, and 32 of them are a row's here.  Every row has the same numbers in another order of its two halves."""
     rows, row, w = (1 << 27) + 37, rand(1, 8, dtype=BF16), torch.ones(8, device="cuda")
