@@ -28,11 +28,11 @@ __device__ __forceinline__ void fetch_lds(__amdgpu_buffer_rsrc_t from, unsigned 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, at, 0, 0, 0);
 }
 
-// 16 bytes of each lane to `at` of a buffer, written to memory at once
+// 16 bytes of each lane to `at` of a buffer, written to memory at once and past the last-level cache
 __device__ __forceinline__ void store_through(i32x4 v, __amdgpu_buffer_rsrc_t to, int at)
 {
     typedef int Words __attribute__((ext_vector_type(4)));
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(Words, v), to, at, 0, 1 << 4); // scope: the device
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(Words, v), to, at, 0, 2 | 1 << 4); // non-temporal; scope: the device
 }
 
 #define LINEAR8_K 128 // numbers of a row that a stage holds
@@ -53,9 +53,9 @@ __device__ __forceinline__ void linear8_tile(const Linear8Args &a, int &m, int &
 // stage.  A stage is 128 bytes of every row of both, written to LDS by the loads themselves.  A group has two: the loads of one are under way for the whole of the other.  Per
 // stage one barrier, ahead of its last products: behind it the next stage's first operands are read while those run.
 // Large products are bound by the power limit: 16384 x 4096 x 4096 231 us (2380 TOPS, matrix instructions in 0.64 of the cycles), 180 us where all numbers are zero.  Short sums are
-// bound by LDS, by a tile's first loads and by its results, which tiles of 128 cover with a second work-group on the CU: 16384 x 768 x 2304 in bf16 41 us (18 of them the
-// rate of memory), 16384 x 2048 x 768 31 us.  What gained nothing: three or four stages, of 64 or 128 numbers; work-groups that go on to another tile, its first loads under way;
-// blocks of 4 x 4 to a wave, or of 2 x 2 in tiles of 128, which read less of LDS with fewer waves; operands from memory to registers; wave priorities.
+// bound by LDS, by a tile's first loads and by its results, which tiles of 128 cover with a second work-group on the CU: 16384 x 768 x 2304 in bf16 41 us, with tiles of 192 40
+// (18 of them the rate of memory), 16384 x 2048 x 768 27 us.  What gained nothing: three or four stages, of 64 or 128 numbers; work-groups that go on to another tile, its first loads
+// under way; blocks of 4 x 4 to a wave, or of 2 x 2 in tiles of 128, which read less of LDS with fewer waves; operands from memory to registers; wave priorities.
 template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __launch_bounds__(64 * WM * WN * G, OCC) void k_linear8(Linear8Args a)
 {
     static_assert(G == 1 || (G == 4 && MB == 1 && NB == 1), "");
@@ -174,8 +174,9 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     }
 
     // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as the tile's rows, whole.  Where those are whole lines they are written
-    // through L2 as they come: the next kernel begins with another L2, and what is written early need not be when this one ends (16384 x 768 x 2304 in bf16, tiles of 192 38 us, 42 with
-    // lines kept; 40 past the caches, and with halves of lines 45 to 70).  Parts of lines have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
+    // to memory as they come: the next kernel begins with another L2, and what is written early need not be when this one ends; and operands stay in the last-level cache
+    // (16384 x 768 x 2304 in bf16 behind the norm, three sets of inputs in turn, 58 us, 71 with lines kept there; 16384 x 4096 x 4096 231, 256; four layers of an encoder on 32 sentences
+    // of 512 1.06 ms, 1.09).  Parts of lines have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
     const int64_t pitch = a.o_row * SIZE;
     const bool through = (((int64_t)a.o | pitch) & 127) == 0 && pitch < (1 << 23); // (offsets inside a tile have 32 bits)
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((int8_t *)a.o + m0 * pitch, 0, through ? min(BM, a.rows - m0) * (int)pitch : 0, 0x00027000);

@@ -155,8 +155,8 @@ template <int VEC, bool EXACT> __device__ __forceinline__ Vec<int8_t, VEC> eight
     return v;
 }
 
-// Bound by memory, reads being faster than a copy: 65536 x 768 in bf16 with a residual 73 us (5.5 TB/s), 4999 x 1021 in 32 bits 8.2 us (5.0 TB/s); in 8 bits 16384 x 768 in
-// bf16 with a residual 15.6 us (5.6 TB/s), 23 rows 3.5 us, two trips to memory.
+// Bound by memory, reads being faster than a copy: 65536 x 768 in bf16 with a residual 58 us (6.9 TB/s, a part of it from the last-level cache; three sets of inputs in turn 71 us,
+// 5.7 TB/s), 4999 x 1021 in 32 bits 8.2 us (5.0 TB/s); in 8 bits 16384 x 768 in bf16 with a residual 15.6 us (5.6 TB/s), 23 rows 3.5 us, two trips to memory.
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __device__ __forceinline__ void rms_norm_rows(const RmsArgs &a)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm8(RmsArgs a)
 }
 
 // Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows, unless there is but one.  No atomics: a run repeats bit for bit.
-// Bound by memory: 16384 x 768 in bf16 with ds' 17 us (5.9 TB/s), 4999 x 1021 in 32 bits 13.9 us (4.4 TB/s).
+// Bound by memory: 16384 x 768 in bf16 with ds' 17 us (5.9 TB/s), 65536 x 768 with the sum of dw 65 us (6.2 TB/s), 4999 x 1021 in 32 bits 13.9 us (4.4 TB/s).
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGradArgs a)
 {
