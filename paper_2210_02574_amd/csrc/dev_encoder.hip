@@ -491,7 +491,7 @@ struct Product8Plan {
 //   16384 x 768 x 2304 40, 44, 41 and with results in 32 bits 47, 53, 48.
 // 192: where they need no more rounds of the 256 CUs than tiles of 256, from two thirds of a round on, and tiles of 128 are more than two to a CU; more than one round only of long
 // sums, or where the last one is full too and results have 16 bits.  256: from three quarters of a round on.  Neither where sums are not long and the last round has few tiles (16384 x 768 x 2304, 2.25 rounds), or where edges leave an eighth
-// more of the area empty than in tiles of 128 (65536 x 2048 x 64: 256 34, 128 23, 64 22).  128: from 0.8 tiles to a CU on (5284 x 768 x 768 7.4, 64 8.0; 3001 x 1000 x 1021 9.0, 8.1).
+// more of the area empty than in tiles of 128 (65536 x 2048 x 64: 256 34, 128 23, 64 22), nor 256 for the shortest sums (16818 x 23 x 3078 38, 33).  128: from 0.8 tiles to a CU on (5284 x 768 x 768 7.4, 64 8.0; 3001 x 1000 x 1021 9.0, 8.1).
 // 32 and 16: as long as two tiles to a CU are all there are.  Eight groups: a tile to a CU, and sums that are long enough for all.
 Product8Plan product8_plan(const he_product8 *p)
 {
@@ -501,7 +501,7 @@ Product8Plan product8_plan(const he_product8 *p)
     const auto full = [&](int64_t t) { return t <= 256 || p->width >= 2048 || 10 * rounds(t) * 256 <= 13 * t; };
     const bool brim = p->width >= 512 && p->type != HE_F32 && 39 * rounds(t192) * 256 <= 40 * t192;
     if (t192 >= 176 && t128 > 512 && (t192 <= 256 || p->width >= 1024 || brim) && full(t192) && rounds(t192) == rounds(t256) && 8 * t192 <= 3 * t128) return {192, 1, t192};
-    if (t256 >= 192 && full(t256) && 32 * t256 <= 9 * t128) return {256, 1, t256};
+    if (t256 >= 192 && p->width > 256 && full(t256) && 32 * t256 <= 9 * t128) return {256, 1, t256};
     if (t128 >= 205 && 32 * t128 <= 9 * t64) return {128, 1, t128};
     if (t16 <= 512) return {16, t16 <= 256 && p->width >= 2048 ? 8 : 4, t16};
     if (t32 <= 512) return {32, 4, t32};

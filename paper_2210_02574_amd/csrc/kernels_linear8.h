@@ -61,8 +61,9 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     static_assert(G == 1 || (G == 4 && MB == 1 && NB == 1), "");
     constexpr int W = WM * WN, THREADS = 64 * W * G, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * LINEAR8_K;
     constexpr int SIZE = (int)sizeof(T), VEC = 16 / SIZE;
-    constexpr int PITCH = BN * SIZE + 16; // of a row of results in LDS, bytes
-    constexpr int OUT = G == 1 ? 32 * WM * PITCH : G * W * 4096 + BM * PITCH, LDS = G * 2 * STAGE > OUT ? G * 2 * STAGE : OUT;
+    constexpr bool ALONE = G == 1 && 32 * NB * SIZE % 128 == 0; // a wave's results are whole lines, which it writes by itself
+    constexpr int COLS = ALONE ? 32 * NB : BN, PITCH = COLS * SIZE + 16; // of a row of results in LDS, bytes
+    constexpr int OUT = ALONE ? 32 * W * PITCH : G == 1 ? 32 * WM * PITCH : G * W * 4096 + BM * PITCH, LDS = G * 2 * STAGE > OUT ? G * 2 * STAGE : OUT;
     __shared__ __attribute__((aligned(1024))) int8_t lds[LDS];
     __shared__ __attribute__((aligned(16))) float sx[BM], sw[BN], sb[BN];
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % W, group = all / W, wm = wave % WM, wn = wave / WM;
@@ -173,7 +174,8 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         }
     }
 
-    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as the tile's rows, whole.  Where those are whole lines they are written
+    // Results: a lane has channels 8 g + 4 (l / 32) .. of row l mod 32 of a block.  They leave through LDS as whole pieces of rows, a wave's or the
+    // tile's.  Where those are whole lines they are written
     // to memory as they come: the next kernel begins with another L2, and what is written early need not be when this one ends; and operands stay in the last-level cache
     // (16384 x 768 x 2304 in bf16 behind the norm, three sets of inputs in turn, 58 us, 71 with lines kept there; 16384 x 4096 x 4096 231, 256; four layers of an encoder on 32 sentences
     // of 512 1.06 ms, 1.09).  Parts of lines have to meet in L2 (16384 x 64 x 3000: 30 us, 54 without).
@@ -196,13 +198,22 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
             store_vec<T, VEC>(y, (T *)((int8_t *)a.o + (m0 + m) * pitch), n, a.channels);
     };
     __syncthreads();
-    constexpr int CHUNKS = BN / VEC;
+    constexpr int CHUNKS = COLS / VEC;
     if constexpr (G == 1) { // 32 rows of each wave at a time
-        constexpr int PER = 32 * WM * CHUNKS / THREADS;
-        static_assert(PER * THREADS == 32 * WM * CHUNKS, "");
+        constexpr int SHARE = ALONE ? 64 : THREADS, PER = (ALONE ? 32 : 32 * WM) * CHUNKS / SHARE;
+        static_assert(PER * SHARE == (ALONE ? 32 : 32 * WM) * CHUNKS, "");
+        int8_t *const own = lds + (ALONE ? wave * 32 * PITCH : 0);
+        const int me = ALONE ? lane : threadIdx.x, first_row = ALONE ? 0 : 32 * wm, first_col = ALONE ? COLS * wn : 0;
+        const auto exchange = [] {
+            if constexpr (ALONE) { // between the lanes of a wave
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            } else
+                __syncthreads();
+        };
 #pragma unroll
         for (int i = 0; i < MB; i++) {
-            if (i) __syncthreads();
+            if (i) exchange();
             const float xs = sx[32 * (MB * wm + i) + row];
 #pragma unroll
             for (int j = 0; j < NB; j++)
@@ -210,19 +221,19 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
                 for (int g = 0; g < 4; g++) {
                     const int col = 32 * (NB * wn + j) + 8 * g + 4 * h;
                     const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    *(Vec<T, 4> *)(lds + (32 * wm + row) * PITCH + col * SIZE) = scaled(s, xs, col);
+                    *(Vec<T, 4> *)(own + (first_row + row) * PITCH + (col - first_col) * SIZE) = scaled(s, xs, col);
                 }
-            __syncthreads();
+            exchange();
             Vec<T, VEC> y[PER];
 #pragma unroll
             for (int p = 0; p < PER; p++) {
-                const int at = p * THREADS + threadIdx.x;
-                y[p] = *(const Vec<T, VEC> *)(lds + at / CHUNKS * PITCH + 16 * (at % CHUNKS));
+                const int at = p * SHARE + me;
+                y[p] = *(const Vec<T, VEC> *)(own + at / CHUNKS * PITCH + 16 * (at % CHUNKS));
             }
 #pragma unroll
             for (int p = 0; p < PER; p++) {
-                const int at = p * THREADS + threadIdx.x, r = at / CHUNKS;
-                store(y[p], 32 * (MB * (r / 32) + i) + r % 32, n0 + at % CHUNKS * VEC);
+                const int at = p * SHARE + me, r = at / CHUNKS;
+                store(y[p], ALONE ? 32 * (MB * wm + i) + r : 32 * (MB * (r / 32) + i) + r % 32, n0 + first_col + at % CHUNKS * VEC);
             }
         }
     } else { // each of the four groups joins a quarter of all groups' sums of each block
