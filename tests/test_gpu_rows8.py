@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
 WIDTHS = [(1, 1), (3, 7), (33, 16), (5, 250), (9, 256), (17, 257), (64, 768), (23, 1000), (7, 1021), (2050, 96), (6, 2048), (5, 2056), (3, 4096), (2, 5000), (3, 8192),
-          (2, 10001), (2, 16384)]
+          (2, 10001), (2, 16384), (32, 100), (33, 100), (31, 513), (17, 768)]
 
 
 @pytest.fixture(scope="module")
