@@ -340,7 +340,8 @@ int32_t rms_args(RmsArgs &a, const he_norm *n, const he_rows *x, const he_rows *
 // 6.2, 9.5, captured 6.1, 5.0); else two for each of the 256 CUs and no more than rows need.
 int rms_parts(const he_norm *n)
 {
-    const int vec = 16 / (int)type_size(n->type), rows = n->width <= vec * 128 ? 8 : n->width <= vec * 256 ? 4 : 1; // of a work-group at a time
+    const int vec = 16 / (int)type_size(n->type);
+    const int rows = n->width <= vec * 8 ? 32 : n->width <= vec * 16 ? 16 : n->width <= vec * 128 ? 8 : n->width <= vec * 256 ? 4 : 1; // of a work-group at a time
     return n->rows <= (n->width <= vec * 64 ? 4 : 2) * rows ? 1 : (int)std::min<int64_t>(512, (n->rows + rows - 1) / rows);
 }
 size_t rms_bytes(const he_norm *n) { return n->rows && rms_parts(n) > 1 ? (size_t)rms_parts(n) * n->width * sizeof(float) : 0; }

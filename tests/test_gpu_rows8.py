@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
 WIDTHS = [(1, 1), (3, 7), (33, 16), (5, 250), (9, 256), (17, 257), (64, 768), (23, 1000), (7, 1021), (2050, 96), (6, 2048), (5, 2056), (3, 4096), (2, 5000), (3, 8192),
-          (2, 10001), (2, 16384), (32, 100), (33, 100), (31, 513), (17, 768)]
+          (2, 10001), (2, 16384), (32, 100), (33, 100), (31, 513), (17, 768), (70, 40), (65, 64), (37, 65), (140, 31), (99, 128)]
 
 
 @pytest.fixture(scope="module")
@@ -272,8 +272,8 @@ def test_results_are_the_same_however_they_are_written(he, dtype, width):
 
 
 def test_more_rows_than_a_launch_holds(he):
-    """2^32 threads are too many, and 32 of them are a row's here.  Every row has the same numbers in another order of its two halves."""
-    rows, row, w = (1 << 27) + 37, rand(1, 8, dtype=BF16), torch.ones(8, device="cuda")
+    """2^32 threads are too many, and eight of them are a row's here.  Every row has the same numbers in another order of its two halves."""
+    rows, row, w = (1 << 28) + 37, rand(1, 8, dtype=BF16), torch.ones(8, device="cuda")
     x = row.expand(rows, 8).contiguous()
     x[1::2] = row.roll(4)
     y, _, rstd = he.rms_norm(x, w)
