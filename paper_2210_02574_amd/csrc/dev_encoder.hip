@@ -337,12 +337,14 @@ int32_t rms_args(RmsArgs &a, const he_norm *n, const he_rows *x, const he_rows *
 }
 // Work-groups of its backward pass: a lone one where it has no more than two rounds of rows, four of narrow ones, which saves a launch (bf16, a call with one and with two, and in a
 // captured graph: 8 x 768 5.0, 8.7; 17 x 768, three rounds, 7.1, 9.0, captured 6.9, 6.4; 20 x 400 5.7, 9.6, captured 5.5, 5.5; 24 x 100 5.3, 9.6, captured 4.2, 4.9; 48 x 100, six rounds,
-// 6.2, 9.5, captured 6.1, 5.0); else two for each of the 256 CUs and no more than rows need.
+// 6.2, 9.5, captured 6.1, 5.0); else one for each of the 256 CUs and no more than rows need, two where these would take more than three rounds (two and one: 2000 x 1901 17.4, 14.8;
+// 700 x 8192 18.2, 16.7; 3000 x 1901, 750 work-groups' rows, 17.3, 17.8; 4154 x 1901 19.5, 22.6; 4008 x 1048 12.3, 13.3).
 int rms_parts(const he_norm *n)
 {
     const int vec = 16 / (int)type_size(n->type);
     const int rows = n->width <= vec * 8 ? 32 : n->width <= vec * 16 ? 16 : n->width <= vec * 128 ? 8 : n->width <= vec * 256 ? 4 : 1; // of a work-group at a time
-    return n->rows <= (n->width <= vec * 64 ? 4 : 2) * rows ? 1 : (int)std::min<int64_t>(512, (n->rows + rows - 1) / rows);
+    const int64_t need = (n->rows + rows - 1) / rows;
+    return need <= (n->width <= vec * 64 ? 4 : 2) ? 1 : (int)std::min<int64_t>(need <= 768 ? 256 : 512, need);
 }
 size_t rms_bytes(const he_norm *n) { return n->rows && rms_parts(n) > 1 ? (size_t)rms_parts(n) * n->width * sizeof(float) : 0; }
 // Whether rows of `width` bytes, `stride` bytes apart, are whole lines.
