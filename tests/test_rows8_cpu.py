@@ -64,17 +64,17 @@ def test_rms_norm_refusals(he):
 
 
 def test_rms_norm_grad_refusals(he):
-    def grad(n=norm_(2, 0, 50, 64, 0.0), dy=(P, 64), s=(P, 64), w=P, rstd=P, add=None, ds=(P, 64), dw=P, ws=P, size=1 << 40):
+    def grad(n=norm_(2, 0, 500, 64, 0.0), dy=(P, 64), s=(P, 64), w=P, rstd=P, add=None, ds=(P, 64), dw=P, ws=P, size=1 << 40):
         return he.lib.he_rms_norm_grad(he.ctx, n, _pack(rows_, dy), _pack(rows_, s), w, rstd, _pack(rows_, add), _pack(rows_, ds), dw, ws, size, None)
 
-    need = ctypes.c_size_t()
+    need = ctypes.c_size_t()  # (500 rows: 50 of this width are one work-group's, which needs no workspace)
     assert grad() == ENODEV and grad(add=(P, 64)) == ENODEV
     for n in [None] + BAD_NORMS:
         assert grad(n) == EINVAL and he.lib.he_rms_norm_workspace_bytes(he.ctx, n, ctypes.byref(need)) == EINVAL
     for kw in ({"dy": None}, {"dy": (P, 63)}, {"s": None}, {"s": (P + 1, 64)}, {"w": None}, {"w": P + 2}, {"rstd": None}, {"rstd": P + 2}, {"add": (P, 63)}, {"ds": None}, {"ds": (P, 63)},
                {"dw": None}, {"dw": P + 2}, {"ws": P + 2}):
         assert grad(**kw) == EINVAL, kw
-    assert he.lib.he_rms_norm_workspace_bytes(he.ctx, norm_(2, 0, 50, 64, 0.0), ctypes.byref(need)) == 0 and need.value >= 64 * 4
+    assert he.lib.he_rms_norm_workspace_bytes(he.ctx, norm_(2, 0, 500, 64, 0.0), ctypes.byref(need)) == 0 and need.value >= 64 * 4
     assert grad(ws=None) == EWORKSPACE and grad(size=need.value - 1) == EWORKSPACE and grad(size=need.value) == ENODEV
     assert he.lib.he_rms_norm_workspace_bytes(he.ctx, norm_(2, 0, 5, 64, 0.0), ctypes.byref(need)) == 0 and need.value == 0
     assert grad(norm_(2, 0, 5, 64, 0.0), ws=None, size=0) == ENODEV  # few rows
