@@ -43,7 +43,7 @@ struct RmsArgs {
     float *out;   // [rows]: rstd, or the scales
     int64_t x_row, r_row, y_row, s_row; // row strides, in elements
     int rows, width, first; // rows, of them the first one of this launch
-    int how;                // y and s are written
+    int how;                // y is written; s past the caches too, or kept
     float eps;
 };
 struct RmsGradArgs {
@@ -183,7 +183,7 @@ template <class T, class TW, int VEC, int TPR, int NC, int WIDTH, bool EIGHT> __
         if (a.r) {
 #pragma unroll
             for (int e = 0; e < VEC; e++) x[c][e] = (T)((float)x[c][e] + (float)res[c][e]);
-            if (live) write_vec<T>(k, x[c], a.s, r * a.s_row, a.how);
+            if (live) write_vec<T>(k, x[c], a.s, r * a.s_row, a.how == PAST ? PAST : KEEP);
         }
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGrad
                 if (a.add) u += (float)add[c][e];
                 o[e] = (T)u;
             }
-            write_vec<T>(k, o, a.ds, row * a.ds_row, a.how);
+            write_vec<T>(k, o, a.ds, row * a.ds_row, a.how == PAST ? PAST : KEEP);
         }
     }
     float *part = a.part + (size_t)blockIdx.x * a.width;
