@@ -281,14 +281,14 @@ class SentenceEncoder:
 
 
 class SentenceEncoder8(SentenceEncoder):
-    """An encoder whose products with weights are in 8 bits, with a scale for each row and channel: weights are laid out once, rows where they come out of a norm, attention
+    """An encoder whose products with weights are in 8 bits, with a scale for each row and channel: weights are laid out once, all others copied, rows where they come out of a norm, attention
     or the Gaussian error units.  Norms, attention and residual sums stay as they are.  No gradients pass through 8-bit rows."""
 
     def __init__(self, encoder: SentenceEncoder):
         he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach())
-        layers = [{n: eight(w[n]) if n in self.PRODUCTS else w[n].detach() for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]
-        last = None if encoder.last is None else encoder.last.detach()
-        super().__init__(he, layers, encoder.heads, encoder.kv_heads, encoder.pool, encoder.cap, encoder.slopes, encoder.eps, encoder.norm, last)
+        copy = lambda t: None if t is None else t.detach().clone()  # noqa: E731 (a step of an optimizer writes to the source's tensors)
+        layers = [{n: eight(w[n]) if n in self.PRODUCTS else copy(w[n]) for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]
+        super().__init__(he, layers, encoder.heads, encoder.kv_heads, encoder.pool, encoder.cap, copy(encoder.slopes), encoder.eps, encoder.norm, copy(encoder.last))
         self.dtype = encoder.layers[0]["qkv"].dtype if layers else None  # of the states between the products
 
     def in_8_bits(self):

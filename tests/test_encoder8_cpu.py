@@ -1,0 +1,38 @@
+"""What an encoder in 8 bits takes from the encoder that it comes from, without a GPU: a context's stand-in lays weights out in plain torch."""
+import pytest
+import torch
+
+from paper_2210_02574_amd.embedding import SentenceEncoder
+
+
+class Weights:
+    """Rows in 8 bits as HE.quantize8 makes them, on the CPU."""
+
+    def quantize8(self, x, gelu=False):
+        top = x.float().abs().amax(1)
+        return torch.round(127 * x.float() / top[:, None]).to(torch.int8), top / 127
+
+
+def _encoder(norm, dtype=torch.float32, slopes=None):
+    layers = [SentenceEncoder.random_layer(16, 2, 24, 3 + i, dtype, "cpu") for i in range(2)]
+    return SentenceEncoder(Weights(), layers, 2, norm=norm, last=torch.ones(16, dtype=dtype) if norm == "rms" else None, slopes=slopes)
+
+
+def _tensors(encoder):
+    out = [t for w in encoder.layers for v in w.values() for t in (v if isinstance(v, tuple) else (v,))]
+    return out + [t for t in (encoder.last, encoder.slopes) if t is not None]
+
+
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+def test_an_encoder_in_8_bits_shares_nothing_with_its_source(norm):
+    enc = _encoder(norm, slopes=torch.tensor([0.5, 0.25]))
+    for t in _tensors(enc)[:-1]:
+        t.requires_grad_(True)
+    enc8 = enc.in_8_bits()
+    before = [t.clone() for t in _tensors(enc8)]
+    theirs = {t.data_ptr() for t in _tensors(enc)}
+    assert not any(t.requires_grad or t.data_ptr() in theirs for t in _tensors(enc8))
+    with torch.no_grad():
+        for t in _tensors(enc):
+            t.mul_(3).add_(1)
+    assert all(torch.equal(a, b) for a, b in zip(_tensors(enc8), before))
