@@ -285,7 +285,7 @@ class SentenceEncoder8(SentenceEncoder):
     or the Gaussian error units.  Norms, attention and residual sums stay as they are.  No gradients pass through 8-bit rows."""
 
     def __init__(self, encoder: SentenceEncoder):
-        he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach())
+        he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach().contiguous())  # (weights may be views of any strides)
         copy = lambda t: None if t is None else t.detach().clone()  # noqa: E731 (a step of an optimizer writes to the source's tensors)
         layers = [{n: eight(w[n]) if n in self.PRODUCTS else copy(w[n]) for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]
         super().__init__(he, layers, encoder.heads, encoder.kv_heads, encoder.pool, encoder.cap, copy(encoder.slopes), encoder.eps, encoder.norm, copy(encoder.last))

@@ -36,3 +36,22 @@ def test_an_encoder_in_8_bits_shares_nothing_with_its_source(norm):
         for t in _tensors(enc):
             t.mul_(3).add_(1)
     assert all(torch.equal(a, b) for a, b in zip(_tensors(enc8), before))
+
+
+class DenseWeights(Weights):
+    def quantize8(self, x, gelu=False):
+        if x.stride(1) != 1:
+            raise ValueError("x: want rows that are dense along the width")
+        return super().quantize8(x, gelu)
+
+
+def test_weights_of_any_strides():
+    """Views that an encoder's plain products take: transposed, and one row for all channels."""
+    enc = _encoder("layer")
+    enc.he = DenseWeights()
+    want = enc.in_8_bits().layers[0]["up"]
+    enc.layers[0]["up"] = enc.layers[0]["up"].t().contiguous().t()
+    enc.layers[1]["out"] = enc.layers[1]["out"][:1].expand(16, -1)
+    enc8 = enc.in_8_bits()
+    assert all(torch.equal(a, b) for a, b in zip(enc8.layers[0]["up"], want))
+    assert (enc8.layers[1]["out"][0] == enc8.layers[1]["out"][0][:1]).all()

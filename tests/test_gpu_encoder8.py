@@ -40,3 +40,14 @@ def test_later_changes_of_the_source_do_not_reach_an_encoder_in_8_bits(he, norm,
         t.add_(rand(20 + i, *t.shape, scale=0.05).abs())
     assert torch.equal(enc8(states, off), before)
     assert not torch.equal(enc.in_8_bits()(states, off)[0], before[0])
+
+
+def test_weights_of_any_strides(he):
+    """Transposed views as plain products take them: the same encoder in 8 bits as with dense weights."""
+    w = SentenceEncoder.random_layer(64, 2, 96, 5, torch.bfloat16, "cuda", std=0.1)
+    states, off = rand(1, 60, 64, dtype=torch.bfloat16), offsets_of([20, 0, 1, 39])
+    want = SentenceEncoder(he, [w], 2).in_8_bits()(states, off)
+    views = {n: t.t().contiguous().t() if t.dim() == 2 else torch.stack([t, t], 1)[:, 0] for n, t in w.items() if "norm" not in n}
+    enc = SentenceEncoder(he, [{**w, **views}], 2)
+    enc(states, off)
+    assert torch.equal(enc.in_8_bits()(states, off), want)
