@@ -785,13 +785,13 @@ class HE:
         return self._on_tensors("rms_norm_backward", "he_rms_norm_grad", dy, s, weight, rstd, ds)
 
     # Rows in 8 bits: int8 integers, each standing for itself times its row's scale (float32), with max |row| at +-127.  A row with an infinity or a NaN has the
-    # scale NaN, so that all that is made of it is NaN.  No gradients pass through them.
+    # scale NaN, so that all that is made of it is NaN.  No gradients pass through them.  rms_norm8 and quantize8 make rows of at most 16384; linear8 takes rows of up to 65536.
     def rms_norm8(self, x, weight, residual=None, eps: float = 1e-5):
         """rms_norm with y in 8 bits: (y8 [rows][width], scale [rows], s)."""
         return self._on_tensors("rms_norm8", "he_rms_norm8", x, weight, residual, eps)
 
     def quantize8(self, x, gelu: bool = False):
-        """Rows x [rows][width], or Gaussian error units of them, in 8 bits: (x8 [rows][width], scale [rows]).  Weights of a product too: a row is a channel."""
+        """Rows x [rows][width], or Gaussian error units of them, in 8 bits: (x8 [rows][width], scale [rows]), width at most 16384.  Weights of a product too: a row is a channel."""
         return self._on_tensors("quantize8", "he_quantize8", x, gelu)
 
     def linear8(self, x8, scale, w8, w_scale, bias=None, dtype=None, out=None):

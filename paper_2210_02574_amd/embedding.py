@@ -282,9 +282,16 @@ class SentenceEncoder:
 
 class SentenceEncoder8(SentenceEncoder):
     """An encoder whose products with weights are in 8 bits, with a scale for each row and channel: weights are laid out once, all others copied, rows where they come out of a norm, attention
-    or the Gaussian error units.  Norms, attention and residual sums stay as they are.  No gradients pass through 8-bit rows."""
+    or the Gaussian error units.  Norms, attention and residual sums stay as they are.  No gradients pass through 8-bit rows.
+    The rows of a product's weights are at most MAX_WIDTH wide."""
+
+    MAX_WIDTH = 16384  # of rows that HE.quantize8 and HE.rms_norm8 make
 
     def __init__(self, encoder: SentenceEncoder):
+        for i, w in enumerate(encoder.layers):
+            for n in self.PRODUCTS:
+                if w[n].shape[1] > self.MAX_WIDTH:
+                    raise ValueError(f"layer {i}: {n} has rows of {w[n].shape[1]}, rows in 8 bits are at most {self.MAX_WIDTH} wide")
         he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach().contiguous())  # (weights may be views of any strides)
         copy = lambda t: None if t is None else t.detach().clone()  # noqa: E731 (a step of an optimizer writes to the source's tensors)
         layers = [{n: eight(w[n]) if n in self.PRODUCTS else copy(w[n]) for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]

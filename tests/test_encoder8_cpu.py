@@ -55,3 +55,18 @@ def test_weights_of_any_strides():
     enc8 = enc.in_8_bits()
     assert all(torch.equal(a, b) for a, b in zip(enc8.layers[0]["up"], want))
     assert (enc8.layers[1]["out"][0] == enc8.layers[1]["out"][0][:1]).all()
+
+
+def _layer(width, inner):
+    """A layer of one column to a head and one key head; what is not a product's weight does not matter here."""
+    w = {n: torch.ones(1) for n in SentenceEncoder.NAMES}
+    return {**w, "qkv": torch.ones(4, width), "out": torch.ones(width, 2), "up": torch.ones(inner, width), "down": torch.ones(width, inner)}
+
+
+@pytest.mark.parametrize("width,inner,text", [(16, 16385, "layer 1: down has rows of 16385"), (16386, 24, "layer 1: qkv has rows of 16386")])
+def test_rows_wider_than_8_bit_rows_are_refused_by_name(width, inner, text):
+    """An encoder of plain products takes any width; rows in 8 bits are made up to 16384."""
+    enc = SentenceEncoder(Weights(), [_layer(16, 16384), _layer(width, inner)], 2, kv_heads=1)
+    with pytest.raises(ValueError, match=text + ".*16384"):
+        enc.in_8_bits()
+    SentenceEncoder(Weights(), [_layer(16, 16384), _layer(16384, 24)], 2, kv_heads=1).in_8_bits()
