@@ -384,7 +384,8 @@ int32_t he_quantize8(he_ctx *ctx, int32_t type, int64_t rows, int32_t width, int
 int32_t he_rms_norm8(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows8 *y,
                      const he_rows *sum, void *stream);
 /* Product of 8-bit rows and 8-bit weights: o[m][n] = (sum over k of x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n], of type `type`.  The sums are exact; a result
- * takes three roundings to 32 bits (the sum's, its product with x_scale, that with w_scale together with the bias's addition) and one to its type.  width (of k)
+ * takes three roundings to 32 bits (the sum's, its product with one scale, that with the other together with the bias's addition) and one to its type; it is not finite
+ * only where it leaves the range itself, or a scale or the bias is not.  width (of k)
  * at most 65536, strides below 2^23 bytes; HE_EINVAL also: more than 2^31 - 65536 rows, 2^24 channels or 2^22 work-groups (tiles of up to 256 rows and channels).
  * bias_type: HE_F32 or `type`; d_bias NULL: no bias. */
 typedef struct {

@@ -39,6 +39,15 @@ __device__ __forceinline__ void store_through(i32x4 v, __amdgpu_buffer_rsrc_t to
 // Chunk c of 16 bytes of row r lies at c ^ (r / 2 mod 8) of the row's 128 bytes in LDS: the 16 rows that a 16-byte read takes at a time then lie in 16 different places.
 __device__ __forceinline__ int linear8_twist(int row) { return row >> 1 & 7; }
 
+// A result: s x_scale w_scale + b.  From 2^64 on x_scale (FAR: where there may be such rows) comes last: a sum times it may leave 32 bits where the result does not,
+// while one times w_scale then leaves them only where the result does.  Sums are below 2^31.
+__device__ __forceinline__ bool linear8_far(float xs) { return fabsf(xs) >= 0x1p64f; }
+template <bool FAR> __device__ __forceinline__ float linear8_scaled(int s, float xs, float ws, float b)
+{
+    const bool last = FAR && linear8_far(xs);
+    return fmaf((float)s * (last ? ws : xs), last ? xs : ws, b);
+}
+
 // The tile of a work-group.  Each of the eight dies takes a run of tiles that follow one another, in bands of eight tiles of rows, so that they share operands in its L2.
 __device__ __forceinline__ void linear8_tile(const Linear8Args &a, int &m, int &n)
 {
@@ -183,11 +192,11 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     const bool through = (((int64_t)a.o | pitch) & 127) == 0 && pitch < (1 << 23); // (offsets inside a tile have 32 bits)
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((int8_t *)a.o + m0 * pitch, 0, through ? min(BM, a.rows - m0) * (int)pitch : 0, 0x00027000);
     const int row = lane % 32, h = lane / 32;
-    const auto scaled = [&](const i32x4 s, float xs, int col) {
+    const auto scaled = [&](const i32x4 s, float xs, int col, auto far) {
         const f32x4 ws = *(const f32x4 *)(sw + col), b = *(const f32x4 *)(sb + col);
         Vec<T, 4> y;
 #pragma unroll
-        for (int e = 0; e < 4; e++) y[e] = (T)fmaf((float)s[e] * xs, ws[e], b[e]);
+        for (int e = 0; e < 4; e++) y[e] = (T)linear8_scaled<far>(s[e], xs, ws[e], b[e]);
         return y;
     };
     const auto store = [&](const Vec<T, VEC> y, int m, int n) { // row m of the tile
@@ -215,14 +224,20 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         for (int i = 0; i < MB; i++) {
             if (i) exchange();
             const float xs = sx[32 * (MB * wm + i) + row];
+            const auto put = [&](auto far) {
 #pragma unroll
-            for (int j = 0; j < NB; j++)
+                for (int j = 0; j < NB; j++)
 #pragma unroll
-                for (int g = 0; g < 4; g++) {
-                    const int col = 32 * (NB * wn + j) + 8 * g + 4 * h;
-                    const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    *(Vec<T, 4> *)(own + (first_row + row) * PITCH + (col - first_col) * SIZE) = scaled(s, xs, col);
-                }
+                    for (int g = 0; g < 4; g++) {
+                        const int col = 32 * (NB * wn + j) + 8 * g + 4 * h;
+                        const i32x4 s = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                        *(Vec<T, 4> *)(own + (first_row + row) * PITCH + (col - first_col) * SIZE) = scaled(s, xs, col, far);
+                    }
+            };
+            if (__builtin_expect(__ballot(linear8_far(xs)) != 0, 0)) // (rather than a choice for each result)
+                put(std::true_type{});
+            else
+                put(std::false_type{});
             exchange();
             Vec<T, VEC> y[PER];
 #pragma unroll
@@ -246,7 +261,7 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
         for (int g = 0; g < G; g++) s += join[(g * 4 + group) * 64 + lane];
         int8_t *const out = lds + G * W * 4096;
         const int m = 32 * wm + row, col = 32 * wn + 8 * group + 4 * h;
-        *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col);
+        *(Vec<T, 4> *)(out + m * PITCH + col * SIZE) = scaled(s, sx[m], col, std::true_type{});
         __syncthreads();
         for (int p = threadIdx.x; p < BM * CHUNKS; p += THREADS)
             store(*(const Vec<T, VEC> *)(out + p / CHUNKS * PITCH + 16 * (p % CHUNKS)), p / CHUNKS, n0 + p % CHUNKS * VEC);
@@ -340,7 +355,7 @@ template <class T, int BLK, int G> __global__ __launch_bounds__(64 * G) void k_l
     for (int e = 0; e < 4; e++) {
         const int c = min(n + e, a.channels - 1);
         const float b = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[c] : (float)((const T *)a.bias)[c];
-        y[e] = (T)fmaf((float)s[e] * xs, a.w_scale[c], b);
+        y[e] = (T)linear8_scaled<true>(s[e], xs, a.w_scale[c], b);
     }
     store_vec<T, 4>(y, (T *)a.o + m * a.o_row, n, a.channels);
 }

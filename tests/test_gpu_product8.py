@@ -1,0 +1,54 @@
+"""Products of 8-bit rows and weights on the GPU, in every variant, against 64 bits with the bounds of rows8_reference."""
+import pytest
+import torch
+
+import paper_2210_02574_amd as pkg
+import rows8_reference as ref
+import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+# rows, width, channels: tiles of 16 with four and eight groups of waves, of 32, of 64 with one and four groups, of 128, of 256 by 192, of 256
+SHAPES = [(23, 768, 768), (17, 2100, 100), (500, 768, 768), (1000, 300, 1000), (1000, 1040, 1000), (5284, 200, 768), (16380, 144, 768), (4090, 300, 4096)]
+
+
+@pytest.fixture(scope="module")
+def he():
+    assert torch.cuda.is_available(), "this test needs the MI355X"
+    return pkg.HE.from_params(wl.C1B, device=0)
+
+
+def rand(seed, *shape, dtype=F32, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn(*shape, generator=g)).to(dtype).cuda()
+
+
+def integers(seed, rows, width, pad=0):
+    """8-bit rows of any integers, with others behind them up to a multiple of 16."""
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-128, 128, (rows, (width + 15) // 16 * 16 + pad), generator=g, dtype=torch.int8).cuda()[:, :width]
+
+
+@pytest.mark.parametrize("rows,width,channels", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scales_at_the_ends_of_the_range(he, rows, width, channels, dtype):
+    """Sums of up to 2^20 times the scale of a row of large values leave 32 bits, results do not: x_scale up to 2^120, w_scale about 2^-110; and the other way round.  Rows beside
+    them are ordinary, one is zero, and one's results leave the range."""
+    x8, w8, bias = integers(1, rows, width), integers(2, channels, width), rand(3, channels)
+    x8[1] = 0
+    w8[5] = 0
+    e = torch.arange(rows) % 5
+    scale = (1 + rand(4, rows).abs()) * torch.tensor([2.0**120, 1.0, 2.0**63, 2.0**64, 2.0**100])[e].cuda()
+    w_scale = (1 + rand(5, channels).abs()) * 2.0**-110
+    scale[1] = 2.0**126
+    for xs, ws in ((scale, w_scale), (scale * 2.0**-110, w_scale * 2.0**110), (scale * 2.0**-120, w_scale * 2.0**120)):
+        for b in (None, bias):
+            want, bound = ref.linear8(x8, xs, w8, ws, b, dtype)
+            assert want.abs().max() < 2.0**127
+            o = he.linear8(x8, xs, w8, ws, bias=b, dtype=dtype).double()
+            assert ((o - want).abs() <= bound).all()
+    xs = torch.full_like(scale, 2.0**120)
+    o = he.linear8(x8, xs, w8, torch.full_like(w_scale, 2.0**20), bias=bias, dtype=F32)
+    sums = x8.double() @ w8.double().t()
+    assert torch.equal(o.double(), torch.where(sums == 0, bias.double(), sums * float("inf")))
