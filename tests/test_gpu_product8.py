@@ -5,6 +5,7 @@ import torch
 import paper_2210_02574_amd as pkg
 import rows8_reference as ref
 import workloads as wl
+from product8_shapes import PITCH, VARIANTS
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,24 @@ def test_scales_at_the_ends_of_the_range(he, rows, width, channels, dtype):
     o = he.linear8(x8, xs, w8, torch.full_like(w_scale, 2.0**20), bias=bias, dtype=F32)
     sums = x8.double() @ w8.double().t()
     assert torch.equal(o.double(), torch.where(sums == 0, bias.double(), sums * float("inf")))
+
+
+@pytest.mark.parametrize("rows,width,channels", list(VARIANTS))
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_results_that_fill_whole_lines(he, rows, width, channels, dtype):
+    """Rows of results that begin at multiples of 128 bytes, the last tile of rows ragged: alone, and in a wider buffer with channels that no vector divides, where a row's last piece is
+    written element by element behind whole ones.  What stands around the results stays."""
+    x8, w8 = integers(1, rows, width, 32), integers(2, channels, width)
+    scale, w_scale = (1 + rand(3, rows).abs()) / (74 * 74 * width**0.5), 1 + rand(4, channels).abs()  # results of about one
+    bias = rand(5, channels, dtype=dtype)
+    want, bound = ref.linear8(x8, scale, w8, w_scale, bias, dtype)
+    o = he.linear8(x8, scale, w8, w_scale, bias=bias, dtype=dtype)
+    assert channels % PITCH == 0 and o.data_ptr() % 128 == 0
+    assert ((o.double() - want).abs() <= bound).all()
+    for fewer, pitch in ((0, channels + PITCH), (3, channels), (11, channels + 2 * PITCH)):
+        n = channels - fewer
+        buf = torch.full((rows + 2, pitch), 7.0, dtype=dtype, device="cuda")
+        r = he.linear8(x8, scale, w8[:n], w_scale[:n], bias=bias[:n], dtype=dtype, out=buf[1:-1, :n])
+        assert r.data_ptr() % 128 == 0
+        assert torch.equal(r, o[:, :n])
+        assert (buf[0] == 7).all() and (buf[-1] == 7).all() and (buf[:, n:] == 7).all()

@@ -1,0 +1,58 @@
+"""Which tiles a product of 8-bit rows and weights takes: the library's own rule, compiled for the host."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from product8_shapes import VARIANTS
+
+SOURCE = """
+#include "linear8_plan.h"
+extern "C" void plan(long long rows, int width, int channels, int wide, long long *out)
+{
+    const Product8Plan p = product8_plan(rows, width, channels, wide != 0);
+    out[0] = p.tile, out[1] = p.groups, out[2] = p.tiles;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    import paper_2210_02574_amd as pkg
+
+    d = tmp_path_factory.mktemp("plan")
+    src, lib = str(d / "plan.cpp"), str(d / "plan.so")
+    with open(src, "w") as f:
+        f.write(SOURCE)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(os.path.dirname(pkg.__file__), "csrc"), src, "-o", lib])
+    f = ctypes.CDLL(lib).plan
+    f.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_longlong)]
+
+    def call(rows, width, channels, wide):
+        out = (ctypes.c_longlong * 3)()
+        f(rows, width, channels, wide, out)
+        return tuple(out)
+
+    return call
+
+
+@pytest.mark.parametrize("shape", list(VARIANTS))
+def test_the_shapes_of_the_tests_are_of_the_variants_that_they_stand_for(plan, shape):
+    for wide in (0, 1):
+        tile, groups, tiles = plan(*shape, wide)
+        assert (tile, groups) == VARIANTS[shape][wide]
+        rows, channels = (256, 192) if tile == 192 else (tile, tile)
+        assert tiles == -(-shape[0] // rows) * -(-shape[2] // channels)
+
+
+def test_all_variants_are_reached_and_no_others(plan):
+    import random
+
+    r, seen = random.Random(1), set()
+    for _ in range(20000):
+        rows, width, channels = (int(2 ** r.uniform(0, top)) for top in (31, 16, 24))
+        tile, groups, tiles = plan(rows, width, channels, r.randrange(2))
+        seen.add((tile, groups))
+        assert tiles >= 1
+    assert seen == {v for pair in VARIANTS.values() for v in pair}
