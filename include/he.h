@@ -376,8 +376,8 @@ typedef struct {
 } he_rows8;
 /* Rows in 8 bits: t = max |f|, integers rint(127 f / t) (ties to the even one), scale = t / 127, in the order of these operations; for a row of zeros both are 0.  A row with
  * an infinity or a NaN: scale NaN, integers 0, so that nothing made of it is finite.
- *   he_quantize8: f = x; or the Gaussian error unit x Phi(x) of it with gelu != 0, within 2^-20 (1 + x^2 / 8) of itself, and integers nearest to a quotient that is 2^-17 off.
- *     width at most 16384.
+ *   he_quantize8: f = x; or the Gaussian error unit x Phi(x) of it with gelu != 0, within 2^-20 (1 + x^2 / 8) of itself for x >= -13 (units below are
+ *     smaller than 2^-123, lose bits and vanish), and integers nearest to a quotient that is 2^-17 off.  width at most 16384.
  *   he_rms_norm8: f = s w of he_rms_norm, not rounded to the type; the scale is (t rstd) / 127.  The integers hang on s w alone.
  * Integers are exact for rows and weights of 16 bits and one type; a product s w beyond 32 bits is rounded to those first. */
 int32_t he_quantize8(he_ctx *ctx, int32_t type, int64_t rows, int32_t width, int32_t gelu, const he_rows *x, const he_rows8 *y, void *stream);

@@ -81,7 +81,8 @@ template <int TPR> __device__ __forceinline__ void row_sum_max(float &v, unsigne
 }
 
 // x Phi(x) = max(x, 0) - z Phi(-z) with z = |x|, and Phi(-z) = t 2^(q(t) - z^2 log2(e) / 2), t = 1 / (1 + c z): q is a fit of degree 8 to the function that this leaves, within
-// 1.1e-7 of it, so that the lower tail is as exact, relatively, as the exponential: 1 + erf would lose it.
+// 2e-7 of it for z <= 14 (1.35e-7 of Phi), so that the lower tail is as exact, relatively, as the exponential: 1 + erf would lose it.  Half of the 2^-20 (1 + x^2 / 8) that is
+// granted is used from -13 on; below, 2^(..) becomes subnormal, which the instruction makes zero.
 __device__ __forceinline__ float gelu(float x)
 {
     const float z = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(z, 0.28f, 1.f));
