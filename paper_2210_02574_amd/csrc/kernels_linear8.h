@@ -47,6 +47,15 @@ template <bool FAR> __device__ __forceinline__ float linear8_scaled(int s, float
     const bool last = FAR && linear8_far(xs);
     return fmaf((float)s * (last ? ws : xs), last ? xs : ws, b);
 }
+// Four of them in their type.  Each is rounded to 32 bits first: in some places of some variants one instruction would round to fp16 alone, and a row's results hang on the rows beside it.
+template <class T> __device__ __forceinline__ Vec<T, 4> linear8_typed(f32x4 y)
+{
+    if constexpr (std::is_same<T, f16>::value) asm("" : "+v"(y));
+    Vec<T, 4> o;
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = (T)y[e];
+    return o;
+}
 
 // The tile of a work-group.  Each of the eight dies takes a run of tiles that follow one another, in bands of eight tiles of rows, so that they share operands in its L2.
 __device__ __forceinline__ void linear8_tile(const Linear8Args &a, int &m, int &n)
@@ -194,10 +203,10 @@ template <class T, int MB, int NB, int WM, int WN, int G, int OCC> __global__ __
     const int row = lane % 32, h = lane / 32;
     const auto scaled = [&](const i32x4 s, float xs, int col, auto far) {
         const f32x4 ws = *(const f32x4 *)(sw + col), b = *(const f32x4 *)(sb + col);
-        Vec<T, 4> y;
+        f32x4 y;
 #pragma unroll
-        for (int e = 0; e < 4; e++) y[e] = (T)linear8_scaled<far>(s[e], xs, ws[e], b[e]);
-        return y;
+        for (int e = 0; e < 4; e++) y[e] = linear8_scaled<far>(s[e], xs, ws[e], b[e]);
+        return linear8_typed<T>(y);
     };
     const auto store = [&](const Vec<T, VEC> y, int m, int n) { // row m of the tile
         if (m0 + m >= a.rows) return;
@@ -350,12 +359,12 @@ template <class T, int BLK, int G> __global__ __launch_bounds__(64 * G) void k_l
     const int m = m0 + row, n = n0 + 8 * wave + 4 * part; // four channels of a row
     if (m >= a.rows) return;
     const float xs = a.x_scale[m];
-    Vec<T, 4> y;
+    f32x4 y;
 #pragma unroll
     for (int e = 0; e < 4; e++) {
         const int c = min(n + e, a.channels - 1);
         const float b = !a.bias ? 0.f : a.bias32 ? ((const float *)a.bias)[c] : (float)((const T *)a.bias)[c];
-        y[e] = (T)linear8_scaled<true>(s[e], xs, a.w_scale[c], b);
+        y[e] = linear8_scaled<true>(s[e], xs, a.w_scale[c], b);
     }
-    store_vec<T, 4>(y, (T *)a.o + m * a.o_row, n, a.channels);
+    store_vec<T, 4>(linear8_typed<T>(y), (T *)a.o + m * a.o_row, n, a.channels);
 }

@@ -74,3 +74,17 @@ def test_results_that_fill_whole_lines(he, rows, width, channels, dtype):
         assert r.data_ptr() % 128 == 0
         assert torch.equal(r, o[:, :n])
         assert (buf[0] == 7).all() and (buf[-1] == 7).all() and (buf[:, n:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_rows_and_channels_do_not_hang_on_those_beside_them(he, dtype):
+    """The same rows and channels in calls of every variant, bit for bit: sums are exact, and each result is rounded to 32 bits before its type."""
+    rows, width, channels = 16380, 1040, 4096
+    x8, w8 = integers(1, rows, width), integers(2, channels, width)
+    scale, w_scale, bias = (1 + rand(3, rows).abs()) / (74 * 74 * width**0.5), 1 + rand(4, channels).abs(), rand(5, channels, dtype=dtype)
+    call = lambda m, n: he.linear8(x8[:m], scale[:m], w8[:n], w_scale[:n], bias=bias[:n], dtype=dtype)  # noqa: E731
+    whole = call(rows, channels)
+    for m, n in ((rows, 768), (rows, 765), (4001, 4032), (5284, 700), (1000, 1024), (1000, 2000), (500, 768), (23, 765), (1, 100)):
+        assert torch.equal(call(m, n), whole[:m, :n]), (m, n)
+    eight = he.linear8(x8[:20, :400], scale[:20], w8[:50, :400], w_scale[:50], bias=bias[:50], dtype=dtype)
+    assert torch.equal(he.linear8(x8[:3000, :400], scale[:3000], w8[:3000, :400], w_scale[:3000], bias=bias[:3000], dtype=dtype)[:20, :50], eight)
