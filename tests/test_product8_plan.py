@@ -46,6 +46,12 @@ def test_the_shapes_of_the_tests_are_of_the_variants_that_they_stand_for(plan, s
         assert tiles == -(-shape[0] // rows) * -(-shape[2] // channels)
 
 
+def test_short_sums_whose_results_begin_inside_lines_keep_tiles_of_128(plan):
+    for rows, width, channels in ((16384, 768, 2304), (32768, 768, 768), (8192, 768, 4608), (48000, 600, 768)):
+        assert [plan(rows, width, n, wide)[0] for n in (channels, channels - 4) for wide in (0, 1)] == [192, 128, 128, 128]
+    assert plan(16384, 2048, 764, 0)[0] == 192  # of long sums they do not hang on it
+
+
 def test_all_variants_are_reached_and_no_others(plan):
     import random
 
