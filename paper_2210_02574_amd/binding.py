@@ -786,6 +786,7 @@ class HE:
 
     # Rows in 8 bits: int8 integers, each standing for itself times its row's scale (float32), with max |row| at +-127.  A row with an infinity or a NaN has the
     # scale NaN, so that all that is made of it is NaN.  No gradients pass through them.  rms_norm8 and quantize8 make rows of at most 16384; linear8 takes rows of up to 65536.
+    # Integers and scales are two views of one allocation, whose two types torch.save refuses: it takes them with a clone of the scales.
     def rms_norm8(self, x, weight, residual=None, eps: float = 1e-5):
         """rms_norm with y in 8 bits: (y8 [rows][width], scale [rows], s)."""
         return self._on_tensors("rms_norm8", "he_rms_norm8", x, weight, residual, eps)

@@ -292,7 +292,12 @@ class SentenceEncoder8(SentenceEncoder):
             for n in self.PRODUCTS:
                 if w[n].shape[1] > self.MAX_WIDTH:
                     raise ValueError(f"layer {i}: {n} has rows of {w[n].shape[1]}, rows in 8 bits are at most {self.MAX_WIDTH} wide")
-        he, eight = encoder.he, lambda t: encoder.he.quantize8(t.detach().contiguous())  # (weights may be views of any strides)
+        he = encoder.he
+
+        def eight(t):
+            rows, scale = he.quantize8(t.detach().contiguous())  # (weights may be views of any strides)
+            return rows, scale.clone()  # (apart from the integers' storage: torch.save takes no two types of one)
+
         copy = lambda t: None if t is None else t.detach().clone()  # noqa: E731 (a step of an optimizer writes to the source's tensors)
         layers = [{n: eight(w[n]) if n in self.PRODUCTS else copy(w[n]) for n in self.NAMES[:8] + self.NORMS[encoder.norm]} for w in encoder.layers]
         super().__init__(he, layers, encoder.heads, encoder.kv_heads, encoder.pool, encoder.cap, copy(encoder.slopes), encoder.eps, encoder.norm, copy(encoder.last))

@@ -51,3 +51,19 @@ def test_weights_of_any_strides(he):
     enc = SentenceEncoder(he, [{**w, **views}], 2)
     enc(states, off)
     assert torch.equal(enc.in_8_bits()(states, off), want)
+
+
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+def test_weights_of_an_encoder_in_8_bits_can_be_saved(he, norm, tmp_path):
+    """torch.save takes no two types of tensors in one storage, as the integers and scales of HE.quantize8 are."""
+    layers = [SentenceEncoder.random_layer(64, 2, 96, 5 + i, torch.bfloat16, "cuda", std=0.1) for i in range(2)]
+    enc8 = SentenceEncoder(he, layers, 2, norm=norm, last=rand(3, 64, dtype=torch.bfloat16) if norm == "rms" else None).in_8_bits()
+    states, off = rand(1, 60, 64, dtype=torch.bfloat16), offsets_of([20, 0, 1, 39])
+    want = enc8(states, off)
+    torch.save({"layers": enc8.layers, "last": enc8.last}, tmp_path / "weights")
+    saved = torch.load(tmp_path / "weights", weights_only=True)
+    enc8.layers, enc8.last = saved["layers"], saved["last"]
+    assert torch.equal(enc8(states, off), want)
+    x8, scale = he.quantize8(states)
+    torch.save((x8, scale.clone()), tmp_path / "rows")
+    assert all(torch.equal(a, b) for a, b in zip(torch.load(tmp_path / "rows", weights_only=True), (x8, scale)))
