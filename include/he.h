@@ -359,7 +359,8 @@ int32_t he_layer_norm_grad(he_ctx *ctx, const he_norm *n, const he_rows *dy, con
                            void *stream);
 
 /* Root-mean-square norm over the last dimension: s as in he_layer_norm; rstd = (mean(s^2) + eps)^-1/2; y = s rstd w.  Limits as there; the squares
- * are summed in 32 bits (a sum beyond them: y = 0; with eps = 0, a row whose squares all vanish in them: y is not finite). */
+ * are summed in 32 bits (a sum beyond them: y = 0; squares below 2^-126 lose bits, which shows where eps is no larger; with eps = 0, a row whose squares all vanish:
+ * y is not finite). */
 int32_t he_rms_norm(he_ctx *ctx, const he_norm *n, const he_rows *x, const he_rows *residual, const void *d_w, const he_rows *y,
                     const he_rows *sum, float *d_rstd, void *stream);
 /* With g = dy w: ds = rstd (g - s rstd^2 mean(g s)) + add, dw = sum over rows of dy s rstd; otherwise as he_layer_norm_grad. */

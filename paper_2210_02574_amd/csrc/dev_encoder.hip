@@ -336,10 +336,12 @@ int32_t rms_args(RmsArgs &a, const he_norm *n, const he_rows *x, const he_rows *
     a.rows = (int)n->rows, a.width = n->width, a.eps = (float)n->eps;
     return HE_OK;
 }
-// Work-groups of its backward pass: a lone one where it has no more than two rounds of rows, four of narrow ones, which saves a launch (bf16, a call with one and with two, and in a
-// captured graph: 8 x 768 5.0, 8.7; 17 x 768, three rounds, 7.1, 9.0, captured 6.9, 6.4; 20 x 400 5.7, 9.6, captured 5.5, 5.5; 24 x 100 5.3, 9.6, captured 4.2, 4.9; 48 x 100, six rounds,
-// 6.2, 9.5, captured 6.1, 5.0); else one for each of the 256 CUs and no more than rows need, two where these would take more than three rounds (two and one: 2000 x 1901 17.4, 14.8;
-// 700 x 8192 18.2, 16.7; 3000 x 1901, 750 work-groups' rows, 17.3, 17.8; 4154 x 1901 19.5, 22.6; 4008 x 1048 12.3, 13.3).
+// Work-groups of its backward pass: a lone one where it has no more than two rounds of rows, four of narrow ones, which saves a launch (bf16, us with one and with one to a round: in a
+// captured graph 118 x 64, four rounds of 32 rows, 5.5, 5.7; five 6.1, 5.6; 59 x 100, four of 16, 5.3, 5.5; five 5.9, 5.4; 22 x 400, three of 8, 5.3, 5.4; four 6.2, 5.5; 14 x 768, two,
+// 5.5, 6.1; three 6.7, 6.2; 2 x 8192 5.8, 6.2; 3 7.6, 6.2; a call by itself takes 5.2 to 6.3 in all of these up to the limit, with two launches 8.6 to 9.1); else one for each of the 256
+// CUs and no more than rows need, two where these would take more than three rounds (bf16 with ds', captured, one and two to a CU: 768 x 8192 17.3, 18.1 and 520 x 8192 17.8, 20.0; 800 x 8192
+// 19.2, 18.5; 6142 x 768, 768 work-groups' rows, 12.5, 12.2; 6398 x 768 13.9, 12.9; 3071 x 1901 18.5, 17.8; 3199 x 1901 21.1, 19.3; 24566 x 64 7.9, 8.3; 31990 x 64 9.1, 8.7; fp32
+// 768 x 4096 13.3, 14.3; 2799 x 1021 13.7, 13.7; 3199 x 1021 15.7, 14.8).
 int rms_parts(const he_norm *n)
 {
     const int vec = 16 / (int)type_size(n->type);

@@ -232,7 +232,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm8(RmsArgs a)
     rms_norm_rows<T, TW, VEC, TPR, NC, WIDTH, true>(a);
 }
 
-// Work-groups, rows and shares of dw as in k_layer_norm_grad; k_rms_weight_grad sums the partial rows, unless there is but one.  No atomics: a run repeats bit for bit.
+// A work-group takes every gridDim.x-th group of RPW rows, holds its share of dw in registers and writes it as a partial row; k_rms_weight_grad sums those, unless there is but one.
+// How many work-groups there are: rms_parts.  No atomics: a run repeats bit for bit.
 // Bound by memory: 16384 x 768 in bf16 with ds' 17 us (5.9 TB/s), 65536 x 768 with the sum of dw 65 us (6.2 TB/s), 4999 x 1021 in 32 bits 13.9 us (4.4 TB/s).
 template <class T, class TW, int VEC, int TPR, int NC, int WIDTH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_rms_norm_grad(RmsGradArgs a)
